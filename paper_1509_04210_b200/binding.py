@@ -1,4 +1,4 @@
-"""Thin ctypes binding of ``include/rudra_ps.h``: argument marshalling only.
+"""Thin ctypes binding of ``include/rudra_ps.h`` (and the signatures of ``include/rudra_learner.h``): argument marshalling only.
 
 Every step of the path runs in the native library; this module never computes on weights or
 gradients.  The library is loaded on first use.  If it is missing it is built with nvcc; if
@@ -94,6 +94,21 @@ def lib():
         "rudra_ps_enable_views": (C.c_int, [vp, u32]),
         "rudra_ps_pull_view": (i64, [vp, u32, vp]),
         "rudra_ps_view_of": (i64, [vp, u32, vp]),
+        # include/rudra_learner.h
+        "rudra_mx4_codes_bytes": (u64, [u64, u64]),
+        "rudra_mx4_scales_bytes": (u64, [u64, u64]),
+        "rudra_mx4_quantize": (C.c_int, [vp, C.c_int, u64, u64, u64, C.c_int, vp, vp, vp]),
+        "rudra_mx4_dequantize": (C.c_int, [vp, vp, u64, u64, vp, C.c_int, u64, vp]),
+        "rudra_ps_pull_mx4": (i64, [vp, u64, u64, u64, C.c_int, vp, vp]),
+        "rudra_mx4_matmul": (C.c_int, [vp, vp, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp]),
+        "rudra_mx4_linear_workspace": (u64, [u64, u64]),
+        "rudra_mx4_linear": (C.c_int, [vp, C.c_int, u64, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp, u64, vp]),
+        "rudra_act8_codes_bytes": (u64, [u64, u64]),
+        "rudra_act8_scales_bytes": (u64, [u64, u64]),
+        "rudra_act8_forward": (C.c_int, [C.c_int, vp, vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, vp, vp, vp]),
+        "rudra_act8_backward": (C.c_int, [C.c_int, vp, C.c_int, u64, u64, u64, vp, vp, vp, vp, vp, vp, u64, vp]),
+        "rudra_act8_weight_grad_workspace": (u64, [vp, C.c_int, u64, u64, u64]),
+        "rudra_act8_weight_grad": (C.c_int, [vp, C.c_int, u64, u64, u64, vp, vp, u64, vp, C.c_int, u64, vp, u64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -243,6 +258,11 @@ class ParameterServer:
 
     def pull(self, dst_dev):
         return _check(lib().rudra_ps_pull(self._h, _ptr(dst_dev)))
+
+    def pull_mx4(self, offset, rows, cols, transpose, codes_dev, scales_dev):
+        """The rows x cols matrix at weight ``offset``, quantized to MX4 (``learner.pull_mx4`` allocates)."""
+        return _check(lib().rudra_ps_pull_mx4(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
+                                              _ptr(scales_dev)))
 
     def pull_host(self, dst_host):
         return _check(lib().rudra_ps_pull_host(self._h, _ptr(dst_host)))

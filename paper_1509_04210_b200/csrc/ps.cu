@@ -14,12 +14,17 @@
 
 #include <cuda_runtime.h>
 
-#include "../../include/rudra_ps.h"
+#include "../../include/rudra_learner.h"
+#include "host.h"
 #include "kernels.cuh"
+#include "learner.cuh"
 
+namespace rudra {
 namespace {
 
 thread_local char g_error[512] = "";
+
+}  // namespace
 
 int fail(int code, const char* fmt, ...) {
   va_list ap;
@@ -33,25 +38,16 @@ int cuda_fail(cudaError_t e, const char* what) {
   return fail(RUDRA_E_CUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
 }
 
-// Runs the body of an exported function; a C++ exception (in practice std::bad_alloc from a host
-// container) becomes an error code instead of crossing the C boundary.
-template <typename F>
-auto guarded(F&& body) -> decltype(body()) {
-  using R = decltype(body());
-  try {
-    return body();
-  } catch (const std::bad_alloc&) {
-    return (R)fail(RUDRA_E_NOMEM, "out of host memory");
-  } catch (...) {
-    return (R)fail(RUDRA_E_NOMEM, "unexpected C++ exception");
-  }
-}
+}  // namespace rudra
+
+namespace {
+
+using rudra::aligned;
+using rudra::cuda_fail;
+using rudra::fail;
+using rudra::guarded;
 
 constexpr uint32_t kMagic = 0x52554452u;   // "RUDR"
-constexpr uintptr_t kAlignMask = 31;       // 256-bit vector accesses
-
-bool aligned(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & kAlignMask) == 0; }
-
 // One gradient the queue stands for.  A learner's own gradient is a message of one entry.  The
 // average a leaf of the server tree relays for k gradients (Section 3.3) is a message of k entries,
 // one per timestamp it carries: the first holds the vector (the leaf's average), the others none.
@@ -518,7 +514,7 @@ int do_step(rudra_ps* ps, float* const* dsts, uint32_t k) {
 
 extern "C" {
 
-const char* rudra_last_error(void) { return g_error; }
+const char* rudra_last_error(void) { return rudra::g_error; }
 
 rudra_ps* rudra_ps_create(uint64_t nparams, uint32_t lambda, uint32_t n, float alpha0, float momentum,
                           float weight_decay) {
@@ -1024,6 +1020,24 @@ int64_t rudra_ps_pull_many(rudra_ps* ps, float* const* dsts_dev, uint32_t k) {
 }
 
 int64_t rudra_ps_pull(rudra_ps* ps, float* dst_dev) { return rudra_ps_pull_many(ps, &dst_dev, 1); }
+
+int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                          void* scales_dev) {
+  return guarded([&]() -> int64_t {
+    if (!valid(ps)) return fail(RUDRA_E_INVAL, "bad handle");
+    if (rows > RUDRA_MAX_DIM || cols > RUDRA_MAX_DIM) return fail(RUDRA_E_INVAL, "more than RUDRA_MAX_DIM rows or columns");
+    if (offset > ps->N || (cols && rows > (ps->N - offset) / cols)) return fail(RUDRA_E_INVAL, "weights %llu + %llu x %llu reach past the end of the vector", (unsigned long long)offset, (unsigned long long)rows, (unsigned long long)cols);
+    if (rows == 0 || cols == 0) return (int64_t)ps->ts;
+    if (!aligned(codes_dev) || !aligned(scales_dev)) return fail(RUDRA_E_INVAL, "codes or scales are null or not 32-byte aligned");
+    DeviceScope dev(ps->device);
+    rudra::MatrixIn src = {ps->theta + offset, rudra::kF32, rows, cols, cols};
+    cudaError_t e = rudra::launch_mx4_quantize(src, transpose != 0, codes_dev, scales_dev, ps->stream);
+    if (e != cudaSuccess) return cuda_fail(e, "quantization kernel launch");
+    ps->counters[2] += 1;
+    ps->counters[3] += 1;
+    return (int64_t)ps->ts;
+  });
+}
 
 int64_t rudra_ps_pull_host(rudra_ps* ps, float* dst_host) {
   return guarded([&]() -> int64_t {

@@ -1,0 +1,124 @@
+"""Sizes, constants and refusals of the learner-side operators: host code only, no GPU needed."""
+import os
+import re
+
+import numpy as np
+import pytest
+
+import learner_reference as ref
+from paper_1509_04210_b200 import binding as rb
+from paper_1509_04210_b200 import learner
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 4096   # an address that is aligned and never followed: every call below is refused first
+
+
+def test_constants_match_the_header():
+    text = open(os.path.join(ROOT, "include", "rudra_learner.h")).read()
+    defs = {k: int(v) for k, v in re.findall(r"#define\s+(RUDRA_[A-Z0-9_]+)\s+(\d+)", text)}
+    assert (defs["RUDRA_F32"], defs["RUDRA_BF16"]) == (learner.F32, learner.BF16) == (rb.GRAD_F32, rb.GRAD_BF16)
+    assert {k: defs["RUDRA_ACT_" + k.upper()] for k in learner.ACTS} == learner.ACTS
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 0), (1, 1), (1, 32), (128, 33), (129, 128), (4096, 9216), (5, 4097), (2**31 - 128, 2**20)])
+def test_sizes(rows, cols):
+    L = rb.lib()
+    nb = -(-cols // 32)
+    assert L.rudra_mx4_codes_bytes(rows, cols) == rows * nb * 16
+    assert L.rudra_mx4_scales_bytes(rows, cols) == -(-rows // 128) * -(-nb // 4) * 512
+    assert L.rudra_act8_codes_bytes(rows, cols) == rows * nb * 32
+    assert L.rudra_act8_scales_bytes(rows, cols) == rows * nb
+    assert L.rudra_mx4_linear_workspace(rows, cols) >= rows * nb * 16 + -(-rows // 128) * -(-nb // 4) * 512
+
+
+def test_scale_places_are_distinct_and_fill_the_array():
+    rows, nb = 300, 9
+    kt = -(-nb // 4)
+    r, b = np.meshgrid(np.arange(384), np.arange(4 * kt), indexing="ij")
+    at = ref.mx4_scale_at(r, b, kt)
+    assert sorted(at.ravel()) == list(range(rb.lib().rudra_mx4_scales_bytes(rows, nb * 32)))
+
+
+def _refused(code, text):
+    assert code == rb.E_INVAL and text in rb.last_error(), (code, rb.last_error())
+
+
+def test_quantize_refusals():
+    q = rb.lib().rudra_mx4_quantize
+    _refused(q(P, 2, 4, 64, 64, 0, P, P, None), "dtype")
+    _refused(q(None, 0, 4, 64, 64, 0, P, P, None), "source")
+    _refused(q(P + 2, 0, 4, 64, 64, 0, P, P, None), "aligned to its elements")
+    _refused(q(P, 0, 4, 64, 63, 0, P, P, None), "apart")
+    _refused(q(P, 0, 2**31, 64, 64, 0, P, P, None), "RUDRA_MAX_DIM")
+    _refused(q(P, 0, 4, 64, 2**62, 0, P, P, None), "ld")
+    _refused(q(P, 0, 4, 64, 64, 0, P + 16, P, None), "32-byte")
+    _refused(q(P, 0, 4, 64, 64, 0, P, None, None), "32-byte")
+    assert q(None, 0, 0, 64, 64, 0, None, None, None) == 0 and q(None, 1, 7, 0, 0, 1, None, None, None) == 0
+    d = rb.lib().rudra_mx4_dequantize
+    _refused(d(P, P, 4, 64, P, 7, 64, None), "dtype")
+    _refused(d(P, P + 1, 4, 64, P, 0, 64, None), "32-byte")
+    _refused(d(P, P, 4, 64, None, 0, 64, None), "destination")
+    assert d(None, None, 0, 64, None, 0, 64, None) == 0
+
+
+def test_product_refusals():
+    m = rb.lib().rudra_mx4_matmul
+    _refused(m(None, P, 4, P, P, 8, 64, P, 0, 8, None), "first factor")
+    _refused(m(P, P, 4, P, P + 8, 8, 64, P, 0, 8, None), "second factor")
+    _refused(m(P, P, 4, P, P, 8, 64, P, 0, 7, None), "apart")
+    _refused(m(P, P, 4, P, P, 8, 64, P + 1, 1, 8, None), "product")
+    _refused(m(P, P, 4, P, P, 8, 2**40, P, 1, 8, None), "RUDRA_MAX_DIM")
+    assert m(None, None, 0, P, P, 8, 64, None, 0, 8, None) == 0
+    lin = rb.lib().rudra_mx4_linear
+    need = rb.lib().rudra_mx4_linear_workspace(4, 64)
+    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, P, need - 1, None), "workspace")
+    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, None, need, None), "workspace")
+    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, P + 8, need, None), "workspace")
+    _refused(lin(P, 9, 64, 4, P, P, 8, 64, P, 0, 8, P, need, None), "dtype")
+    _refused(lin(P, 0, 64, 4, None, P, 8, 64, P, 0, 8, P, need, None), "weights")
+
+
+def test_checkpoint_refusals():
+    f = rb.lib().rudra_act8_forward
+    _refused(f(5, P, None, 0, 4, 64, 64, P, 64, P, P, None, None, None), "activation")
+    _refused(f(-1, P, None, 0, 4, 64, 64, P, 64, P, P, None, None, None), "activation")
+    _refused(f(2, P, P, 0, 4, 64, 64, P, 64, P, P, None, None, None), "second input")
+    _refused(f(2, P, None, 0, 4, 64, 64, None, 64, P, P, None, None, None), "output")
+    _refused(f(0, P, None, 0, 4, 64, 64, P, 64, P, P, None, None, None), "no output")
+    _refused(f(4, P, P, 0, 4, 64, 64, P, 64, P, P, P, None, None), "second checkpoint")
+    _refused(f(4, P, None, 0, 4, 64, 64, P, 64, P, P, P, P, None), "second input")
+    b = rb.lib().rudra_act8_backward
+    _refused(b(2, None, 0, 4, 64, 64, P, P, None, None, P, None, 64, None), "gradient of the output")
+    _refused(b(0, P, 0, 4, 64, 64, P, P, None, None, P, None, 64, None), "no gradient")
+    _refused(b(4, P, 0, 4, 64, 64, P, P, P, P, P, None, 64, None), "second input")
+    _refused(b(2, P, 0, 4, 64, 64, P, P, None, None, P, P, 64, None), "second input")
+    assert b(2, None, 0, 0, 64, 64, None, None, None, None, None, None, 64, None) == 0
+
+
+def test_weight_gradient_refusals():
+    w = rb.lib().rudra_act8_weight_grad
+    need = rb.lib().rudra_act8_weight_grad_workspace
+    _refused(w(P, 1, 64, 10, 64, P, P, 32, None, 0, 32, None, 0, None), "weight gradient")
+    _refused(w(P, 1, 64, 10, 64, None, P, 32, P, 0, 32, None, 0, None), "checkpoint")
+    _refused(w(P, 1, 63, 10, 64, P, P, 32, P, 0, 32, None, 0, None), "apart")
+    _refused(w(P, 5, 64, 10, 64, P, P, 32, P, 0, 32, None, 0, None), "dtype")
+    assert need(P, 1, 10, 64, 64) == 0                                   # bf16 with aligned rows needs none
+    assert need(P, 9, 10, 64, 64) == 0 and need(P, 1, 2**32, 64, 64) == 0   # arguments the call refuses
+    assert w(None, 1, 64, 10, 0, P, P, 32, None, 0, 32, None, 0, None) == 0
+
+
+def test_pull_refusals_need_a_handle():
+    assert rb.lib().rudra_ps_pull_mx4(None, 0, 1, 1, 0, P, P) == rb.E_INVAL and "handle" in rb.last_error()
+
+
+def test_python_refuses_tensors_that_are_not_on_the_gpu():
+    import torch
+
+    with pytest.raises(ValueError):
+        learner.mx4_quantize(torch.zeros(4, 32))
+    with pytest.raises(ValueError):
+        learner.mx4_quantize(torch.zeros(4))
+    with pytest.raises(ValueError):
+        learner.act8_forward("none", torch.zeros(4, 32))
+    with pytest.raises(ValueError):
+        learner.mx4_dequantize(learner.MX4(torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 4, 32))
