@@ -1,0 +1,125 @@
+// sm_100a building blocks of the two products: barriers with bounded waits, TMA and bulk copies, tensor
+// memory, and the descriptors of tcgen05.mma.
+#pragma once
+#include <cstdint>
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_runtime.h>
+
+namespace rudra {
+namespace {
+
+// ------------------------------------------------------------------------------------ barriers
+
+__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// A wait that gives up after about two seconds.  The caller then stops issuing work and the block ends
+// through its ordinary exit; the flag it raises is read by rudra_learner_sync.
+constexpr long long kWaitCycles = 4000000000ll;
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
+  if (barrier_try(bar, parity)) return true;
+  const long long begin = clock64();
+  while (!barrier_try(bar, parity))
+    if (clock64() - begin > kWaitCycles) return false;
+  return true;
+}
+__device__ __forceinline__ void barrier_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+
+// -------------------------------------------------------------------------------------- copies
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
+  asm volatile("prefetch.tensormap [%0];" :: "l"(m) : "memory");
+}
+// One box; x in elements of the map's type and a multiple of 16 bytes.
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// `bytes` (a multiple of 16) from a 16-byte boundary.
+__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               :: "r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
+// ------------------------------------------------------------------------------- tensor memory
+
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {   // a whole warp; slot: shared address
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(slot), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {    // a whole warp
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(base), "r"(columns));
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Arrives on the barrier once every tcgen05 operation this thread issued has finished.
+__device__ __forceinline__ void tensor_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+// 16 columns of this warp's 32 lanes: register i is column i.
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                 "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(at));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// 128 rows of four scale bytes (512 bytes in shared memory) to four columns, repeated for the four lane groups.
+__device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
+}
+
+// --------------------------------------------------------------------------------- descriptors
+
+// A shared-memory matrix in rows of 128 bytes, swizzled, 8-row groups 1024 bytes apart.  Along the
+// rows: an operand whose reduction index is contiguous.
+__device__ __forceinline__ uint64_t swizzled_rows(uint32_t at) {
+  return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// 32 rows of 16 bytes, as tcgen05.cp takes them.
+__device__ __forceinline__ uint64_t scale_rows(uint32_t at) {
+  return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
+}
+
+// ---------------------------------------------------------------------------------------- host
+
+// cuTensorMapEncodeTiled, looked up in the driver once.
+inline PFN_cuTensorMapEncodeTiled map_encoder() {
+  static const PFN_cuTensorMapEncodeTiled fn = []() -> PFN_cuTensorMapEncodeTiled {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled>(p);
+  }();
+  return fn;
+}
+
+// A row-major matrix, read in 128-byte wide boxes of `box_rows` rows with the 128-byte swizzle; what
+// lies outside reads as zero.
+inline cudaError_t encode_rows(CUtensorMap* map, CUtensorMapDataType type, uint32_t element, const void* p, uint64_t cols, uint64_t rows,
+                               uint64_t pitch_bytes, uint32_t box_rows) {
+  const PFN_cuTensorMapEncodeTiled fn = map_encoder();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {128 / element, box_rows}, steps[2] = {1, 1};
+  return fn(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace rudra
