@@ -1,55 +1,383 @@
-// dw = dy^T xhat with xhat from an 8-bit checkpoint: one output per thread, 32 tokens at a time through
-// shared memory.
+// dw = dy^T xhat, the weight gradient of a linear layer, with xhat from its 8-bit checkpoint, on the bf16
+// tensor cores.
+//
+// A code times its block's power of two is a bf16 number exactly, so the checkpoint is expanded to
+// bf16 on its way into shared memory (eight warps, integer and bf16 instructions only) and never exists
+// wide in memory.  Both operands run along tokens, the reduction, so both sit in shared memory as they
+// sit in global memory, tokens as rows ("transposed" operands for the tensor core): dy arrives by TMA.
+// Inputs of the layer (k) are the 128 lanes of an accumulator, outputs (n) its columns, so a warp
+// writes 32 neighbouring weights whatever the alignment of dw.
+//
+// One block per SM walks over its tiles with two accumulators: while one is written out the other is
+// filled.  With few tiles the tokens are split over the blocks of a cluster, which add their parts in
+// rank order through distributed shared memory.
+//
+// dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an exact split),
+// and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.
 #include "blocks.cuh"
 #include "learner.cuh"
+#include "tensor.cuh"
 
 namespace rudra {
 namespace {
 
-__global__ void __launch_bounds__(256) weight_grad_kernel(MatrixIn dy, Act8 saved, MatrixOut dw) {
-  __shared__ float gs[32][17], xs[32][17];
-  const uint32_t tiles = (uint32_t)((dw.cols + 15) / 16);
-  const uint64_t n0 = (uint64_t)(blockIdx.x / tiles) * 16, k0 = (uint64_t)(blockIdx.x % tiles) * 16;
-  const uint64_t nb = (dw.cols + 31) / 32;
-  const uint32_t i = threadIdx.x / 16, j = threadIdx.x % 16;
-  float acc = 0.f;
-  for (uint64_t t0 = 0; t0 < dy.rows; t0 += 32) {
+constexpr uint32_t kLanes = 128, kColumns = 256, kTokens = 64;      // a tile, and a stage of it
+constexpr uint32_t kStages = 4, kStageX = kLanes * kTokens * 2, kStageDy = kColumns * kTokens * 2, kStage = kStageX + kStageDy;
+constexpr uint32_t kExpandWarps = 8, kThreads = 32 * (6 + kExpandWarps);   // 0 loads dy, 1 issues, 2-5 write out, 6-13 expand
+constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
+constexpr uint32_t kChunk = 64 * 2 * kTokens;                       // 64 values wide, kTokens rows of 128 bytes
+static_assert(kLanes * kColumns * 4 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
+
+struct Params {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  void* dw;
+  uint64_t lddw;
+  uint32_t tokens, n, k;
+  uint32_t blocks;          // of 32 values in a row of the checkpoint
+  uint32_t token_stages;    // ceil(tokens / kTokens)
+  uint32_t stages;          // of the whole reduction: token_stages for each of dy's planes
+  uint32_t lane_tiles, tiles;
+  uint32_t split;
+};
+
+__device__ uint32_t g_wait_failed;
+
+// kind::f16: bf16 x bf16 -> f32, both operands with the reduction across rows, 128 x 256.
+constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (kColumns / 8) << 17 | (kLanes / 16) << 24;
+
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(kInstruction), "r"(add) : "memory");
+}
+
+// Four int8 codes to two pairs of bf16 under a scale (a pair of equal bf16).  With u the byte, its low
+// seven bits set into 128 = 0x4300 give 128 + u % 128, and 0x4300 with bit 7 of u gives 128 or 256:
+// their difference is the signed code.
+__device__ __forceinline__ uint32_t scaled(uint32_t bytes, uint32_t scale) {   // bytes 0 and 2
+  const uint32_t low = (bytes & 0x007F007Fu) | 0x43004300u, base = (bytes & 0x00800080u) | 0x43004300u;
+  const __nv_bfloat162 d = __hsub2(reinterpret_cast<const __nv_bfloat162&>(low), reinterpret_cast<const __nv_bfloat162&>(base));
+  const __nv_bfloat162 r = __hmul2(d, reinterpret_cast<const __nv_bfloat162&>(scale));
+  return reinterpret_cast<const uint32_t&>(r);
+}
+__device__ __forceinline__ uint2 expand4(uint32_t w, uint32_t scale) {
+  return make_uint2(scaled(__byte_perm(w, 0, 0x4140), scale), scaled(__byte_perm(w, 0, 0x4342), scale));
+}
+__device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
+  const uint32_t h = s == 255u ? 0x7FC0u : s ? s << 7 : 0x0040u;
+  return h | h << 16;
+}
+
+struct Unit {   // 32 codes of one token, and their scale
+  uint32_t w[8];
+  uint32_t s;
+};
+__device__ __forceinline__ void fetch(Unit& u, const Params& p, uint32_t token, uint32_t block) {
+  if (token < p.tokens && block < p.blocks) {
+    const uint64_t at = (uint64_t)token * p.blocks + block;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]), "=r"(u.w[4]), "=r"(u.w[5]), "=r"(u.w[6]), "=r"(u.w[7])
+                 : "l"(p.codes + at * 32));
+    u.s = __ldg(p.scales + at);
+  } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint64_t t = t0 + h * 16 + i;
-      float g = 0.f, x = 0.f;
-      if (t < dy.rows) {
-        if (n0 + j < dy.cols)
-          g = dy.type == kBF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(dy.p)[t * dy.ld + n0 + j])
-                               : static_cast<const float*>(dy.p)[t * dy.ld + n0 + j];
-        if (k0 + j < dw.cols)
-          x = (float)static_cast<const int8_t*>(saved.codes)[t * nb * 32 + k0 + j] *
-              scale_value(static_cast<const uint8_t*>(saved.scales)[t * nb + (k0 + j) / 32]);
-      }
-      gs[h * 16 + i][j] = g;
-      xs[h * 16 + i][j] = x;
+    for (int i = 0; i < 8; ++i) u.w[i] = 0;
+    u.s = 0;
+  }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float peer_float(uint32_t at, uint32_t rank) {
+  uint32_t remote;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+  return v;
+}
+template <typename G> __device__ __forceinline__ void put(const Params& p, uint32_t n, uint32_t k, float v) {
+  G* dw = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
+  if constexpr (sizeof(G) == 2) *dw = __float2bfloat16_rn(v);
+  else *dw = v;
+}
+
+template <typename G>
+__global__ void __launch_bounds__(kThreads) weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t stage0 = smem_address(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
+  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
+
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
+  const uint32_t tile0 = blockIdx.x / p.split, tile_step = gridDim.x / p.split;
+  const uint32_t first = (uint32_t)((uint64_t)p.stages * rank / p.split), last = (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
+
+  if (threadIdx.x == 0) {
+    prefetch_map(&dy_map);
+    for (uint32_t s = 0; s < kStages; ++s) {
+      barrier_init(full + 8 * s, 1 + kExpandWarps);
+      barrier_init(empty + 8 * s, 1);
     }
-    __syncthreads();
+    for (uint32_t b = 0; b < 2; ++b) {
+      barrier_init(ready + 8 * b, 1);
+      barrier_init(drained + 8 * b, 4);
+    }
+    barrier_init_fence();
+  }
+  if (warp == 1) tmem_alloc(smem_address(slot), 2 * kColumns);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = *slot;
+  bool ok = true;
+  float* part = reinterpret_cast<float*>(smem);   // [column][lane], once the stages are done with
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t c = 0;
+      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
+        const int n0 = (int)(tile / p.lane_tiles * kColumns);
+        for (uint32_t i = first; i < last; ++i, ++c) {
+          const uint32_t s = c % kStages, bar = full + 8 * s, at = stage0 + s * kStage + kStageX;
+          if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
+          barrier_expect(bar, kStageDy);
 #pragma unroll
-    for (int e = 0; e < 32; ++e) acc = fmaf(gs[e][i], xs[e][j], acc);
-    __syncthreads();
+          for (uint32_t q = 0; q < kColumns / 64; ++q) copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), bar);
+        }
+      }
+      // given up: what is on its way has landed once every copy issued has had its time
+      if (!ok)
+        for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t c = 0, done = 0;
+      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++done) {
+        const uint32_t buffer = done & 1, d = tmem + buffer * kColumns;
+        if (!(ok = barrier_wait(drained + 8 * buffer, (done / 2 & 1) ^ 1))) break;
+        tmem_fence_after();
+        for (uint32_t i = first; i < last; ++i, ++c) {
+          const uint32_t s = c % kStages, at = stage0 + s * kStage;
+          if (!(ok = barrier_wait(full + 8 * s, c / kStages & 1))) break;
+          tmem_fence_after();
+#pragma unroll
+          for (uint32_t j = 0; j < kTokens / 16; ++j)
+            multiply(d, swizzled_columns(at + j * 2048, kChunk), swizzled_columns(at + kStageX + j * 2048, kChunk), i != first || j);
+          tensor_commit(empty + 8 * s);
+        }
+        if (ok) tensor_commit(ready + 8 * buffer);
+      }
+    }
+  } else if (warp >= 6) {
+    // a thread expands one block of 32 values: token 8 * (warp - 6) + lane % 8 of the stage, block lane / 8
+    const uint32_t t = (warp - 6) * 8 + lane % 8, b = lane / 8;
+    const uint32_t to = (b / 2) * kChunk + t * 128, x = t % 8;
+    uint32_t tile = tile0, i = first, c = 0;
+    uint32_t ftile = tile0, fi = first;     // what is fetched, two stages ahead
+    auto next = [&](Unit& u) {
+      u.s = 0;
+      if (ftile >= p.tiles) return;
+      fetch(u, p, fi % p.token_stages * kTokens + t, ftile % p.lane_tiles * (kLanes / 32) + b);
+      if (++fi == last) {
+        fi = first;
+        ftile += tile_step;
+      }
+    };
+    Unit ahead[2];
+    if (first < last) {
+      next(ahead[0]);
+      next(ahead[1]);
+    }
+    while (first < last && tile < p.tiles) {
+      const Unit u = ahead[0];
+      ahead[0] = ahead[1];
+      next(ahead[1]);
+      const uint32_t s = c % kStages;
+      if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
+      const uint32_t scale = scale_pair(u.s), at = stage0 + s * kStage + to;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint2 lo = expand4(u.w[2 * j], scale), hi = expand4(u.w[2 * j + 1], scale);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at + ((b % 2 * 4 + j) ^ x) * 16), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) barrier_arrive(full + 8 * s);
+      ++c;
+      if (++i == last) {
+        i = first;
+        tile += tile_step;
+      }
+    }
+  } else {
+    const uint32_t group = warp % 4;      // the lanes of tensor memory a warp may read
+    uint32_t done = 0;
+    for (uint32_t tile = tile0; tile < p.tiles; tile += tile_step, ++done) {
+      const uint32_t buffer = done & 1, k = tile % p.lane_tiles * kLanes + group * 32 + lane, n0 = tile / p.lane_tiles * kColumns;
+      const uint32_t have = min(kColumns, p.n - n0);
+      if (first < last) {
+        if (!(ok = barrier_wait(ready + 8 * buffer, done / 2 & 1))) break;
+        tmem_fence_after();
+      }
+#pragma unroll 1
+      for (uint32_t c = 0; c < have; c += 16) {
+        uint32_t r[16];
+        tmem_load16(tmem + (group * 32 << 16) + buffer * kColumns + c, r);
+        tmem_load_wait();
+#pragma unroll
+        for (uint32_t j = 0; j < 16; ++j) {
+          const float v = first < last ? __uint_as_float(r[j]) : 0.f;
+          if (p.split > 1) part[(c + j) * kLanes + group * 32 + lane] = v;
+          else if (k < p.k && c + j < have) put<G>(p, n0 + c + j, k, v);
+        }
+      }
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(drained + 8 * buffer);
+    }
   }
-  const uint64_t n = n0 + i, k = k0 + j;
-  if (n < dw.rows && k < dw.cols) {
-    if (dw.type == kBF16) static_cast<__nv_bfloat16*>(dw.p)[n * dw.ld + k] = __float2bfloat16_rn(acc);
-    else static_cast<float*>(dw.p)[n * dw.ld + k] = acc;
+  if (!ok) g_wait_failed = 1;
+  __syncwarp();
+  if (p.split > 1) {   // one tile to a cluster
+    cluster_sync();
+    const uint32_t k0 = tile0 % p.lane_tiles * kLanes, n0 = tile0 / p.lane_tiles * kColumns, have = min(kColumns, p.n - n0);
+    for (uint32_t e = rank * kThreads + threadIdx.x; e < have * kLanes; e += p.split * kThreads) {
+      float v = 0.f;
+      for (uint32_t r = 0; r < p.split; ++r) v += peer_float(stage0 + e * 4, r);
+      if (k0 + e % kLanes < p.k) put<G>(p, n0 + e / kLanes, k0 + e % kLanes, v);
+    }
+    cluster_sync();
   }
+  tmem_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tmem_fence_after();
+    tmem_free(tmem, 2 * kColumns);
+  }
+}
+
+// ------------------------------------------------------------------------------ dy that TMA can read
+
+// Planes of bf16 with rows of `pitch` values (a multiple of 8) and `rows` of them (whole stages, the last
+// ones zero): dy itself, or the three parts of a float's significand.
+template <typename G>
+__global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, uint64_t ld, uint32_t tokens, uint32_t n, uint32_t pitch,
+                                                     uint64_t rows, bool wide, uint4* __restrict__ out) {
+  const uint32_t per_row = pitch / 8;
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t row = i / per_row;
+  if (row >= rows) return;
+  const uint32_t c = (uint32_t)(i - row * per_row) * 8;
+  const int have = row < tokens && c < n ? (int)min(8u, n - c) : 0;
+  float x[8];
+  load8(dy + (have ? row * ld + c : 0), wide && have == 8, have, x);
+  constexpr int kPlanes = sizeof(G) == 4 ? 3 : 1;
+#pragma unroll
+  for (int q = 0; q < kPlanes; ++q) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = __float_as_uint(x[e]), top = bits & 0xFFFF0000u;
+      // a number loses its upper eight bits to this plane; an infinity or NaN goes there whole
+      const bool number = (bits & 0x7F800000u) != 0x7F800000u;
+      const uint32_t mine = number ? top : top | ((bits & 0xFFFFu) ? 0x00400000u : 0u);
+      x[e] = number ? x[e] - __uint_as_float(top) : 0.f;
+      w[e / 2] = e % 2 ? w[e / 2] | mine : mine >> 16;
+    }
+    out[((uint64_t)q * rows + row) * per_row + c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+uint64_t plane_pitch(uint64_t n) { return (n + 7) / 8 * 8; }
+uint64_t plane_rows(uint64_t tokens) { return (tokens + kTokens - 1) / kTokens * kTokens; }
+bool readable(const MatrixIn& dy) {
+  return dy.type == kBF16 && reinterpret_cast<uintptr_t>(dy.p) % 16 == 0 && (dy.ld % 8 == 0 || dy.rows <= 1) && dy.ld < (1ull << 32);
+}
+
+template <typename G>
+cudaError_t launch(const CUtensorMap& map, const Params& p, unsigned grid, cudaStream_t stream) {
+  const cudaError_t e = cudaFuncSetAttribute(weight_grad_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = p.split;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, weight_grad_kernel<G>, map, p);
 }
 
 }  // namespace
 
-uint64_t act8_weight_grad_workspace(const MatrixIn&) { return 0; }
+uint64_t act8_weight_grad_workspace(const MatrixIn& dy) {
+  if (dy.rows == 0 || dy.cols == 0 || readable(dy)) return 0;
+  return (dy.type == kF32 ? 3 : 1) * plane_rows(dy.rows) * plane_pitch(dy.cols) * 2;
+}
 
-cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const MatrixOut& dw, void*, cudaStream_t stream) {
-  const uint64_t blocks = ((dw.rows + 15) / 16) * ((dw.cols + 15) / 16);
-  if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-  weight_grad_kernel<<<(unsigned)blocks, 256, 0, stream>>>(dy, saved, dw);
-  return cudaGetLastError();
+cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const MatrixOut& dw, void* workspace, cudaStream_t stream) {
+  const uint64_t size = dw.type == kBF16 ? 2 : 4;
+  if (dy.rows == 0) return cudaMemset2DAsync(dw.p, dw.ld * size, 0, dw.cols * size, dw.rows, stream);   // a sum over nothing
+  const bool direct = readable(dy);
+  const uint64_t planes = direct || dy.type == kBF16 ? 1 : 3;
+  const void* from = dy.p;
+  uint64_t pitch = dy.rows > 1 ? dy.ld : plane_pitch(dy.cols), rows = dy.rows;
+  if (!direct) {
+    from = workspace;
+    pitch = plane_pitch(dy.cols);
+    rows = plane_rows(dy.rows);
+    const uint64_t blocks = (rows * (pitch / 8) + 255) / 256;
+    if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    if (dy.type == kF32)
+      planes_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows, (uint32_t)dy.cols,
+                                                                 (uint32_t)pitch, rows, wide_rows<float>(dy.p, dy.ld), static_cast<uint4*>(workspace));
+    else
+      planes_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(dy.p), dy.ld, (uint32_t)dy.rows,
+                                                                         (uint32_t)dy.cols, (uint32_t)pitch, rows,
+                                                                         wide_rows<__nv_bfloat16>(dy.p, dy.ld), static_cast<uint4*>(workspace));
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  CUtensorMap map;
+  cudaError_t e = encode_rows(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, from, dy.cols, planes * rows, pitch * 2, kTokens);
+  if (e != cudaSuccess) return e;
+  Params p = {};
+  p.codes = static_cast<const uint8_t*>(saved.codes);
+  p.scales = static_cast<const uint8_t*>(saved.scales);
+  p.dw = dw.p;
+  p.lddw = dw.ld;
+  p.tokens = (uint32_t)dy.rows;
+  p.n = (uint32_t)dw.rows;
+  p.k = (uint32_t)dw.cols;
+  p.blocks = (p.k + 31) / 32;
+  p.token_stages = (p.tokens + kTokens - 1) / kTokens;
+  p.stages = p.token_stages * (uint32_t)planes;
+  p.lane_tiles = (p.k + kLanes - 1) / kLanes;
+  const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + kColumns - 1) / kColumns);
+  if (tiles > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+  p.tiles = (uint32_t)tiles;
+  int device = 0, sms = 0;
+  e = cudaGetDevice(&device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (e != cudaSuccess) return e;
+  p.split = 1;
+  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
+  const unsigned grid = p.split > 1 ? (unsigned)(tiles * p.split) : (unsigned)(tiles < (uint64_t)sms ? tiles : sms);
+  return dw.type == kBF16 ? launch<__nv_bfloat16>(map, p, grid, stream) : launch<float>(map, p, grid, stream);
 }
 
 }  // namespace rudra

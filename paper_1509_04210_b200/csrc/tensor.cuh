@@ -91,6 +91,11 @@ __device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
 __device__ __forceinline__ uint64_t swizzled_rows(uint32_t at) {
   return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
+// The same rows, across them: an operand whose reduction index counts rows.  A row is 64 values wide;
+// the next 64 lie `chunk` bytes on.
+__device__ __forceinline__ uint64_t swizzled_columns(uint32_t at, uint32_t chunk) {
+  return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)(chunk >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
 // 32 rows of 16 bytes, as tcgen05.cp takes them.
 __device__ __forceinline__ uint64_t scale_rows(uint32_t at) {
   return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
