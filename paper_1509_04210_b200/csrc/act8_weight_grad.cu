@@ -8,12 +8,19 @@
 // Inputs of the layer (k) are the 128 lanes of an accumulator, outputs (n) its columns, so a warp
 // writes 32 neighbouring weights whatever the alignment of dw.
 //
-// One block per SM walks over its tiles with two accumulators: while one is written out the other is
+// One block per SM walks over its tiles with two accumulators: while one is taken out the other is
 // filled.  With few tiles the tokens are split over the blocks of a cluster, which add their parts in
 // rank order through distributed shared memory.
 //
+// The tensor core truncates where it adds to an accumulator, which costs half a unit in the last place
+// every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken out every
+// kChain stages and the parts are added in registers, rounding to nearest; a bf16 result keeps 16 bits
+// fewer and is taken out once.
+//
 // dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an exact split),
 // and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.
+#include <algorithm>
+
 #include "blocks.cuh"
 #include "learner.cuh"
 #include "tensor.cuh"
@@ -23,7 +30,13 @@ namespace {
 
 constexpr uint32_t kLanes = 128, kColumns = 256, kTokens = 64;      // a tile, and a stage of it
 constexpr uint32_t kStages = 4, kStageX = kLanes * kTokens * 2, kStageDy = kColumns * kTokens * 2, kStage = kStageX + kStageDy;
-constexpr uint32_t kExpandWarps = 8, kThreads = 32 * (6 + kExpandWarps);   // 0 loads dy, 1 issues, 2-5 write out, 6-13 expand
+// Warpgroups: 0 manages (warp 0 loads dy, warp 1 issues), 1 and 2 take results out, 3 and 4 expand, each
+// every second stage.
+constexpr uint32_t kThreads = 640;
+constexpr uint32_t kChain = 4;       // stages in one accumulator where the result is f32
+// Registers of a thread by its group, of the 96 each that the block is launched with (640 x 96 in all).
+constexpr int kManageRegisters = 32, kTakeRegisters = 152, kExpandRegisters = 72;
+static_assert(128 * (kManageRegisters + 2 * kTakeRegisters + 2 * kExpandRegisters) <= 640 * 96, "more registers than the block has");
 constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
 constexpr uint32_t kChunk = 64 * 2 * kTokens;                       // 64 values wide, kTokens rows of 128 bytes
 static_assert(kLanes * kColumns * 4 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
@@ -38,6 +51,7 @@ struct Params {
   uint32_t token_stages;    // ceil(tokens / kTokens)
   uint32_t stages;          // of the whole reduction: token_stages for each of dy's planes
   uint32_t lane_tiles, tiles;
+  uint32_t chain;           // stages in one accumulator
   uint32_t split;
 };
 
@@ -102,14 +116,13 @@ __device__ __forceinline__ float peer_float(uint32_t at, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
   return v;
 }
-template <typename G> __device__ __forceinline__ void put(const Params& p, uint32_t n, uint32_t k, float v) {
-  G* dw = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
-  if constexpr (sizeof(G) == 2) *dw = __float2bfloat16_rn(v);
-  else *dw = v;
+template <typename G> __device__ __forceinline__ void put(G* to, float v) {
+  if constexpr (sizeof(G) == 2) *to = __float2bfloat16_rn(v);
+  else *to = v;
 }
 
 template <typename G>
-__global__ void __launch_bounds__(kThreads) weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ Params p) {
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage0 = smem_address(smem);
@@ -125,25 +138,25 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const __grid_cons
   if (threadIdx.x == 0) {
     prefetch_map(&dy_map);
     for (uint32_t s = 0; s < kStages; ++s) {
-      barrier_init(full + 8 * s, 1 + kExpandWarps);
+      barrier_init(full + 8 * s, 1 + 4);
       barrier_init(empty + 8 * s, 1);
     }
     for (uint32_t b = 0; b < 2; ++b) {
       barrier_init(ready + 8 * b, 1);
-      barrier_init(drained + 8 * b, 4);
+      barrier_init(drained + 8 * b, 8);
     }
     barrier_init_fence();
   }
-  if (warp == 1) tmem_alloc(smem_address(slot), 2 * kColumns);
+  if (warp == 2) tmem_alloc(smem_address(slot), 2 * kColumns);
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = *slot;
   bool ok = true;
-  float* part = reinterpret_cast<float*>(smem);   // [column][lane], once the stages are done with
 
-  if (warp == 0) {
-    if (lane == 0) {
+  if (warp < 4) {
+    give_registers<kManageRegisters>();
+    if (warp == 0 && lane == 0) {
       uint32_t c = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         const int n0 = (int)(tile / p.lane_tiles * kColumns);
@@ -158,92 +171,112 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const __grid_cons
       // given up: what is on its way has landed once every copy issued has had its time
       if (!ok)
         for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
-    }
-  } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t c = 0, done = 0;
-      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++done) {
-        const uint32_t buffer = done & 1, d = tmem + buffer * kColumns;
-        if (!(ok = barrier_wait(drained + 8 * buffer, (done / 2 & 1) ^ 1))) break;
-        tmem_fence_after();
-        for (uint32_t i = first; i < last; ++i, ++c) {
-          const uint32_t s = c % kStages, at = stage0 + s * kStage;
-          if (!(ok = barrier_wait(full + 8 * s, c / kStages & 1))) break;
+    } else if (warp == 1 && lane == 0) {
+      uint32_t c = 0, q = 0;     // stages and accumulators so far
+      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
+        for (uint32_t i = first; ok && i < last; ++q) {
+          const uint32_t buffer = q & 1, d = tmem + buffer * kColumns, end = min(last, i + p.chain);
+          if (!(ok = barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1))) break;
           tmem_fence_after();
+          for (uint32_t begin = i; i < end; ++i, ++c) {
+            const uint32_t s = c % kStages, at = stage0 + s * kStage;
+            if (!(ok = barrier_wait(full + 8 * s, c / kStages & 1))) break;
+            tmem_fence_after();
 #pragma unroll
-          for (uint32_t j = 0; j < kTokens / 16; ++j)
-            multiply(d, swizzled_columns(at + j * 2048, kChunk), swizzled_columns(at + kStageX + j * 2048, kChunk), i != first || j);
-          tensor_commit(empty + 8 * s);
+            for (uint32_t j = 0; j < kTokens / 16; ++j)
+              multiply(d, swizzled_columns(at + j * 2048, kChunk), swizzled_columns(at + kStageX + j * 2048, kChunk), i != begin || j);
+            tensor_commit(empty + 8 * s);
+          }
+          if (ok) tensor_commit(ready + 8 * buffer);
         }
-        if (ok) tensor_commit(ready + 8 * buffer);
       }
     }
-  } else if (warp >= 6) {
-    // a thread expands one block of 32 values: token 8 * (warp - 6) + lane % 8 of the stage, block lane / 8
-    const uint32_t t = (warp - 6) * 8 + lane % 8, b = lane / 8;
-    const uint32_t to = (b / 2) * kChunk + t * 128, x = t % 8;
-    uint32_t tile = tile0, i = first, c = 0;
-    uint32_t ftile = tile0, fi = first;     // what is fetched, two stages ahead
-    auto next = [&](Unit& u) {
-      u.s = 0;
-      if (ftile >= p.tiles) return;
-      fetch(u, p, fi % p.token_stages * kTokens + t, ftile % p.lane_tiles * (kLanes / 32) + b);
-      if (++fi == last) {
-        fi = first;
-        ftile += tile_step;
-      }
-    };
-    Unit ahead[2];
-    if (first < last) {
-      next(ahead[0]);
-      next(ahead[1]);
-    }
-    while (first < last && tile < p.tiles) {
-      const Unit u = ahead[0];
-      ahead[0] = ahead[1];
-      next(ahead[1]);
-      const uint32_t s = c % kStages;
-      if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
-      const uint32_t scale = scale_pair(u.s), at = stage0 + s * kStage + to;
+  } else if (warp < 12) {
+    take_registers<kTakeRegisters>();
+    const uint32_t group = warp % 4, half = (warp - 4) / 4 * 128;   // the lanes a warp may read; its columns
+    const uint32_t at = tmem + (group * 32 << 16) + half;
+    float* part = reinterpret_cast<float*>(smem) + half * kLanes + group * 32 + lane;   // [column][lane], once the stages are done with
+    uint32_t q = 0;
+    for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
+      const uint32_t k = tile % p.lane_tiles * kLanes + group * 32 + lane, n = tile / p.lane_tiles * kColumns + half;
+      const uint32_t have = n < p.n ? min(128u, p.n - n) : 0;
+      float acc[128];
+      for (uint32_t i = first; i < last; i += p.chain, ++q) {
+        const uint32_t buffer = q & 1;
+        if (!(ok = barrier_wait(ready + 8 * buffer, q / 2 & 1))) break;
+        tmem_fence_after();
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint2 lo = expand4(u.w[2 * j], scale), hi = expand4(u.w[2 * j + 1], scale);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at + ((b % 2 * 4 + j) ^ x) * 16), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+        for (uint32_t c = 0; c < 128; c += 8) {
+          uint32_t r[8];
+          tmem_load8(at + buffer * kColumns + c, r);
+          tmem_load_wait();
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j) acc[c + j] = i == first ? __uint_as_float(r[j]) : acc[c + j] + __uint_as_float(r[j]);
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) barrier_arrive(drained + 8 * buffer);
+      }
+      if (p.split > 1) {
+#pragma unroll
+        for (uint32_t c = 0; c < 128; ++c) part[c * kLanes] = acc[c];
+      } else if (k < p.k) {
+        G* to = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
+        if (have == 128) {
+#pragma unroll
+          for (uint32_t c = 0; c < 128; ++c, to += p.lddw) put(to, acc[c]);
+        } else {
+#pragma unroll
+          for (uint32_t c = 0; c < 128; ++c, to += p.lddw)
+            if (c < have) put(to, acc[c]);
+        }
+      }
+    }
+  } else {
+    give_registers<kExpandRegisters>();
+    // a thread expands two blocks of 32 values: tokens t and t + 32 of a stage, block b
+    const uint32_t mine = (warp - 12) / 4, t = warp % 4 * 8 + lane % 8, b = lane / 8;
+    const uint32_t to = stage0 + (b / 2) * kChunk + t * 128, x = t % 8, u0 = b % 2 * 4, length = last - first;
+    uint32_t tile = tile0, i = first;       // the next to be fetched
+    auto step = [&](uint32_t by) {
+      for (i += by; i >= last && tile < p.tiles; i -= length) tile += tile_step;
+    };
+    auto next = [&](Unit (&u)[2]) {
+      if (tile < p.tiles) {
+        const uint32_t token = i % p.token_stages * kTokens + t, block = tile % p.lane_tiles * (kLanes / 32) + b;
+        fetch(u[0], p, token, block);
+        fetch(u[1], p, token + 32, block);
+      }
+      step(2);
+    };
+    auto expand = [&](const Unit (&u)[2], uint32_t c) {
+      const uint32_t s = c % kStages;
+      if (!barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1)) return false;
+#pragma unroll
+      for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t scale = scale_pair(u[h].s), at = to + s * kStage + h * 32 * 128;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+          const uint2 lo = expand4(u[h].w[2 * j], scale), hi = expand4(u[h].w[2 * j + 1], scale);
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at + ((u0 + j) ^ x) * 16), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) barrier_arrive(full + 8 * s);
-      ++c;
-      if (++i == last) {
-        i = first;
-        tile += tile_step;
-      }
-    }
-  } else {
-    const uint32_t group = warp % 4;      // the lanes of tensor memory a warp may read
-    uint32_t done = 0;
-    for (uint32_t tile = tile0; tile < p.tiles; tile += tile_step, ++done) {
-      const uint32_t buffer = done & 1, k = tile % p.lane_tiles * kLanes + group * 32 + lane, n0 = tile / p.lane_tiles * kColumns;
-      const uint32_t have = min(kColumns, p.n - n0);
-      if (first < last) {
-        if (!(ok = barrier_wait(ready + 8 * buffer, done / 2 & 1))) break;
-        tmem_fence_after();
-      }
-#pragma unroll 1
-      for (uint32_t c = 0; c < have; c += 16) {
-        uint32_t r[16];
-        tmem_load16(tmem + (group * 32 << 16) + buffer * kColumns + c, r);
-        tmem_load_wait();
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) {
-          const float v = first < last ? __uint_as_float(r[j]) : 0.f;
-          if (p.split > 1) part[(c + j) * kLanes + group * 32 + lane] = v;
-          else if (k < p.k && c + j < have) put<G>(p, n0 + c + j, k, v);
-        }
-      }
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) barrier_arrive(drained + 8 * buffer);
+      return true;
+    };
+    const uint32_t total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
+    Unit even[2], odd[2];
+    step(mine);
+    next(even);
+    next(odd);
+    for (uint32_t c = mine; c < total; c += 4) {     // `even` and `odd` of this group's stages
+      if (!(ok = expand(even, c))) break;
+      next(even);
+      if (c + 2 >= total) break;
+      if (!(ok = expand(odd, c + 2))) break;
+      next(odd);
     }
   }
   if (!ok) g_wait_failed = 1;
@@ -254,13 +287,13 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const __grid_cons
     for (uint32_t e = rank * kThreads + threadIdx.x; e < have * kLanes; e += p.split * kThreads) {
       float v = 0.f;
       for (uint32_t r = 0; r < p.split; ++r) v += peer_float(stage0 + e * 4, r);
-      if (k0 + e % kLanes < p.k) put<G>(p, n0 + e / kLanes, k0 + e % kLanes, v);
+      if (k0 + e % kLanes < p.k) put(static_cast<G*>(p.dw) + (uint64_t)(n0 + e / kLanes) * p.lddw + k0 + e % kLanes, v);
     }
     cluster_sync();
   }
   tmem_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == 2) {
     tmem_fence_after();
     tmem_free(tmem, 2 * kColumns);
   }
@@ -305,9 +338,15 @@ bool readable(const MatrixIn& dy) {
 }
 
 template <typename G>
-cudaError_t launch(const CUtensorMap& map, const Params& p, unsigned grid, cudaStream_t stream) {
-  const cudaError_t e = cudaFuncSetAttribute(weight_grad_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+cudaError_t launch(const CUtensorMap& map, Params& p, cudaStream_t stream) {
+  static Device device;
+  int sms;
+  const cudaError_t e = device.prepare(reinterpret_cast<const void*>(weight_grad_kernel<G>), kSmem, &sms);
   if (e != cudaSuccess) return e;
+  p.chain = sizeof(G) == 4 ? kChain : p.stages;
+  p.split = 1;
+  while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
+  const unsigned grid = p.split > 1 ? p.tiles * p.split : std::min<unsigned>(p.tiles, (unsigned)sms);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kThreads);
@@ -370,14 +409,7 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + kColumns - 1) / kColumns);
   if (tiles > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
   p.tiles = (uint32_t)tiles;
-  int device = 0, sms = 0;
-  e = cudaGetDevice(&device);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-  if (e != cudaSuccess) return e;
-  p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
-  const unsigned grid = p.split > 1 ? (unsigned)(tiles * p.split) : (unsigned)(tiles < (uint64_t)sms ? tiles : sms);
-  return dw.type == kBF16 ? launch<__nv_bfloat16>(map, p, grid, stream) : launch<float>(map, p, grid, stream);
+  return dw.type == kBF16 ? launch<__nv_bfloat16>(map, p, stream) : launch<float>(map, p, stream);
 }
 
 }  // namespace rudra

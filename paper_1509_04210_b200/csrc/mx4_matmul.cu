@@ -210,6 +210,10 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
 template <typename G, int COLS>
 cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   using S = Shape<COLS>;
+  static Device device;
+  int sms;
+  cudaError_t e = device.prepare(reinterpret_cast<const void*>(matmul_kernel<G, COLS>), S::kSmem, &sms);
+  if (e != cudaSuccess) return e;
   Params p = {};
   const uint64_t nb = (a.cols + 31) / 32;
   p.lane_scales = static_cast<const uint8_t*>(b.scales);
@@ -224,12 +228,10 @@ cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t 
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
   const uint32_t stages = (p.kt + 1) / 2;
   p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= 148 && stages >= p.split * 2) p.split *= 2;
+  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && stages >= p.split * 2) p.split *= 2;
   CUtensorMap lane_map, column_map;
-  cudaError_t e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
+  e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
   if (e == cudaSuccess) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
-  if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(matmul_kernel<G, COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.split));

@@ -1,6 +1,7 @@
 // sm_100a building blocks of the two products: barriers with bounded waits, TMA and bulk copies, tensor
 // memory, and the descriptors of tcgen05.mma.
 #pragma once
+#include <atomic>
 #include <cstdint>
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -40,6 +41,10 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
 }
 __device__ __forceinline__ void barrier_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
+// A warpgroup's registers per thread, out of those the block was launched with.
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
+
 // -------------------------------------------------------------------------------------- copies
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
@@ -78,6 +83,10 @@ __device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
                  "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(at));
 }
+__device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at));
+}
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // 128 rows of four scale bytes (512 bytes in shared memory) to four columns, repeated for the four lane groups.
 __device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
@@ -113,6 +122,31 @@ inline PFN_cuTensorMapEncodeTiled map_encoder() {
   }();
   return fn;
 }
+
+// What a launch asks of the current device, asked once per device: its multiprocessors, and `kernel`'s
+// leave to use `bytes` of shared memory.  One static instance per kernel.
+class Device {
+ public:
+  cudaError_t prepare(const void* kernel, uint32_t bytes, int* sms) {
+    int d = 0;
+    cudaError_t e = cudaGetDevice(&d);
+    if (e != cudaSuccess) return e;
+    if (d < 0 || d >= kMost) return cudaErrorInvalidDevice;
+    int have = sms_[d].load(std::memory_order_acquire);
+    if (have == 0) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+      if (e == cudaSuccess) e = cudaDeviceGetAttribute(&have, cudaDevAttrMultiProcessorCount, d);
+      if (e != cudaSuccess) return e;
+      sms_[d].store(have, std::memory_order_release);
+    }
+    *sms = have;
+    return cudaSuccess;
+  }
+
+ private:
+  static constexpr int kMost = 64;
+  std::atomic<int> sms_[kMost] = {};
+};
 
 // A row-major matrix, read in 128-byte wide boxes of `box_rows` rows with the 128-byte swizzle; what
 // lies outside reads as zero.
