@@ -2,6 +2,8 @@
 // pass) and backward (slope from the checkpoint).  Element-wise but for a block's shared scale, so bound
 // by HBM: per value and input 2G + 33/32 bytes each way (G = 2 bf16, 4 f32).  Sigmoids are formed from the
 // fast exponential and reciprocal, each within about 2 ulp in 32 bits.
+#include <algorithm>
+
 #include "blocks.cuh"
 #include "learner.cuh"
 
@@ -41,108 +43,117 @@ template <Act A> __device__ __forceinline__ float slope(float x, float& f) {
 }
 
 struct Saved {
-  uint2* codes;
+  uint4* codes;
   uint8_t* scales;
 };
 
-__device__ __forceinline__ void save(const Saved& to, uint64_t unit, const float (&x)[8], bool in) {
-  const uint32_t s = scale_byte(block_max_bits(max_bits(x)), 6);
-  const uint2 w = int8_codes(x, inverse_scale(s));
+template <typename G> __device__ __forceinline__ void save(const Saved& to, uint32_t unit, const Values<G>& x, bool in) {
+  const uint32_t s = scale_byte(block_max_bits(x.max_bits()), 6);
+  const uint4 w = int8_codes(x, s);
   if (!in) return;
   to.codes[unit] = w;
-  if (unit % 4 == 0) to.scales[unit / 4] = (uint8_t)s;
+  if (unit % 2 == 0) to.scales[unit / 2] = (uint8_t)s;
 }
 
-__device__ __forceinline__ void restore(const Saved& from, uint64_t unit, float (&x)[8]) {
-  int8_values(__ldg(from.codes + unit), scale_value(__ldg(from.scales + unit / 4)), x);
-}
+struct Restored {
+  uint4 w;
+  uint32_t s;
+  __device__ __forceinline__ void load(const Saved& from, uint32_t unit) {
+    w = __ldcs(from.codes + unit);
+    s = __ldg(from.scales + unit / 2);
+  }
+  __device__ __forceinline__ void values(float (&x)[kValues]) const { int8_values(w, scale_value(s), x); }
+};
 
-// A unit is 8 values; checkpoint rows are whole blocks of four units, so unit numbers run through the
-// checkpoint without gaps and four neighbouring lanes always share a block.
+// Checkpoint rows are whole blocks of two units (of a thread's values), so unit numbers run through the
+// checkpoint without gaps and neighbouring lanes share a block.
 template <typename G, Act A>
 __global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__ x, const G* __restrict__ up, uint64_t ldx,
-                                                           uint32_t cols, uint64_t units, bool wide_in, bool wide_out,
+                                                           uint32_t cols, Divisor per_row, uint32_t units, bool wide_in, bool wide_out,
                                                            G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
-  const uint32_t per_row = (cols + 31) / 32 * 4;
-  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-  const uint64_t row = i / per_row;
-  const uint32_t c = (uint32_t)(i - row * per_row) * 8;
+  const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   const bool in = i < units;
-  const int have = in && c < cols ? (int)min(8u, cols - c) : 0;
+  const int have = in && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
   const uint64_t at = have ? row * ldx + c : 0;
-  float a[8], b[8];
-  load8(x + at, wide_in && have == 8, have, a);
-  if (A == kSwiglu) load8(up + at, wide_in && have == 8, have, b);
+  Values<G> a, b;
+  a.load(x + at, wide_in && have == kValues, have);
+  if (A == kSwiglu) b.load(up + at, wide_in && have == kValues, have);
   save(saved, i, a, in);
   if (A == kSwiglu) save(saved_up, i, b, in);
   if constexpr (A != kNone) {
     if (!have) return;
+    float v[kValues];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = A == kSwiglu ? value<A>(a[e]) * b[e] : value<A>(a[e]);
-    store8(y + row * ldy + c, wide_out && have == 8, have, a);
+    for (int e = 0; e < kValues; ++e) v[e] = A == kSwiglu ? value<A>(a.get(e)) * b.get(e) : value<A>(a.get(e));
+    store_values(y + row * ldy + c, wide_out && have == kValues, have, v);
   }
 }
 
 template <typename G, Act A>
-__global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_t lddy, uint32_t cols, uint64_t units, bool wide_in,
-                                                            bool wide_out, Saved saved, Saved saved_up, G* dx, G* dup, uint64_t lddx) {
-  const uint32_t per_row = (cols + 31) / 32 * 4;
-  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= units) return;
-  const uint64_t row = i / per_row;
-  const uint32_t c = (uint32_t)(i - row * per_row) * 8;
-  if (c >= cols) return;
-  const int have = (int)min(8u, cols - c);
-  float g[8], x[8], u[8];
-  if (A != kNone) load8(dy + row * lddy + c, wide_in && have == 8, have, g);
-  restore(saved, i, x);
-  if (A == kSwiglu) restore(saved_up, i, u);
+__global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_t lddy, uint32_t cols, Divisor per_row, uint32_t units,
+                                                            bool wide_in, bool wide_out, Saved saved, Saved saved_up, G* dx, G* dup,
+                                                            uint64_t lddx) {
+  const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
+  if (i >= units || c >= cols) return;
+  const int have = (int)min((uint32_t)kValues, cols - c);
+  Values<G> g;
+  Restored rx, ru;
+  if (A != kNone) g.load(dy + row * lddy + c, wide_in && have == kValues, have);
+  rx.load(saved, i);
+  if (A == kSwiglu) ru.load(saved_up, i);
+  float x[kValues], u[kValues];
+  rx.values(x);
+  if (A == kSwiglu) ru.values(u);
   if constexpr (A != kNone) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < kValues; ++e) {
       float f;
       const float d = slope<A>(x[e], f);
-      x[e] = A == kSwiglu ? g[e] * u[e] * d : g[e] * d;
-      if (A == kSwiglu) u[e] = g[e] * f;
+      x[e] = A == kSwiglu ? g.get(e) * u[e] * d : g.get(e) * d;
+      if (A == kSwiglu) u[e] = g.get(e) * f;
     }
   }
-  store8(dx + row * lddx + c, wide_out && have == 8, have, x);
-  if (A == kSwiglu) store8(dup + row * lddx + c, wide_out && have == 8, have, u);
+  store_values(dx + row * lddx + c, wide_out && have == kValues, have, x);
+  if (A == kSwiglu) store_values(dup + row * lddx + c, wide_out && have == kValues, have, u);
 }
 
-cudaError_t shape(uint64_t rows, uint64_t cols, uint64_t* units, unsigned* blocks) {
-  *units = rows * ((cols + 31) / 32 * 4);
-  const uint64_t b = (*units + kThreads - 1) / kThreads;
-  if (b > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-  *blocks = (unsigned)b;
-  return cudaSuccess;
-}
+// Rows of a launch: as many as keep the number of its units below 2^31.
+struct Part {
+  uint64_t per_row, most;
+  Part(uint64_t cols) : per_row((cols + 31) / 32 * 2), most(std::max<uint64_t>(1, 0x70000000ull / per_row)) {}
+};
 
-Saved saved_of(const Act8& a) { return Saved{static_cast<uint2*>(a.codes), static_cast<uint8_t*>(a.scales)}; }
+Saved saved_of(const Act8& a) { return Saved{static_cast<uint4*>(a.codes), static_cast<uint8_t*>(a.scales)}; }
+
+Saved after(const Saved& s, uint64_t units) { return s.codes ? Saved{s.codes + units, s.scales + units / 2} : s; }
 
 template <typename G, Act A>
 cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const Act8& saved, const Act8& saved_up, cudaStream_t stream) {
-  uint64_t units;
-  unsigned blocks;
-  const cudaError_t e = shape(x.rows, x.cols, &units, &blocks);
-  if (e != cudaSuccess) return e;
+  const Part part(x.cols);
   const bool wide_in = wide_rows<G>(x.p, x.ld) && (A != kSwiglu || wide_rows<G>(up, x.ld));
-  forward_kernel<G, A><<<blocks, kThreads, 0, stream>>>(static_cast<const G*>(x.p), static_cast<const G*>(up), x.ld, (uint32_t)x.cols,
-                                                        units, wide_in, wide_rows<G>(y.p, y.ld), static_cast<G*>(y.p), y.ld,
-                                                        saved_of(saved), saved_of(saved_up));
+  for (uint64_t r = 0; r < x.rows; r += part.most) {
+    const uint64_t units = std::min(part.most, x.rows - r) * part.per_row;
+    if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    forward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
+        static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
+        Divisor((uint32_t)part.per_row), (uint32_t)units, wide_in, wide_rows<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
+        after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row));
+  }
   return cudaGetLastError();
 }
 
 template <typename G, Act A>
 cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up, const MatrixOut& dx, void* dup, cudaStream_t stream) {
-  uint64_t units;
-  unsigned blocks;
-  const cudaError_t e = shape(dx.rows, dx.cols, &units, &blocks);
-  if (e != cudaSuccess) return e;
+  const Part part(dx.cols);
   const bool wide_out = wide_rows<G>(dx.p, dx.ld) && (A != kSwiglu || wide_rows<G>(dup, dx.ld));
-  backward_kernel<G, A><<<blocks, kThreads, 0, stream>>>(static_cast<const G*>(dy.p), dy.ld, (uint32_t)dx.cols, units, wide_rows<G>(dy.p, dy.ld),
-                                                         wide_out, saved_of(saved), saved_of(saved_up), static_cast<G*>(dx.p),
-                                                         static_cast<G*>(dup), dx.ld);
+  for (uint64_t r = 0; r < dx.rows; r += part.most) {
+    const uint64_t units = std::min(part.most, dx.rows - r) * part.per_row;
+    if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    backward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
+        static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
+        wide_rows<G>(dy.p, dy.ld), wide_out, after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row),
+        static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
+  }
   return cudaGetLastError();
 }
 

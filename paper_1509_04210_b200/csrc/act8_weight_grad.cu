@@ -249,34 +249,36 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       }
       step(2);
     };
-    auto expand = [&](const Unit (&u)[2], uint32_t c) {
-      const uint32_t s = c % kStages;
-      if (!barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1)) return false;
+    const uint32_t total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
+    Unit u[2];
+    step(mine);
+    next(u);
+    for (uint32_t c = mine; c < total; c += 2) {
+      // expanded in registers, and the next codes on their way, before the stage is free
+      uint32_t w[2][16];
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h) {
-        const uint32_t scale = scale_pair(u[h].s), at = to + s * kStage + h * 32 * 128;
+        const uint32_t scale = scale_pair(u[h].s);
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-          const uint2 lo = expand4(u[h].w[2 * j], scale), hi = expand4(u[h].w[2 * j + 1], scale);
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at + ((u0 + j) ^ x) * 16), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+        for (uint32_t j = 0; j < 8; ++j) {
+          const uint2 e = expand4(u[h].w[j], scale);
+          w[h][2 * j] = e.x;
+          w[h][2 * j + 1] = e.y;
         }
       }
+      next(u);
+      const uint32_t s = c % kStages;
+      if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
+#pragma unroll
+      for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
+                       :: "r"(to + s * kStage + h * 32 * 128 + ((u0 + j) ^ x) * 16), "r"(w[h][4 * j]), "r"(w[h][4 * j + 1]), "r"(w[h][4 * j + 2]),
+                          "r"(w[h][4 * j + 3]) : "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) barrier_arrive(full + 8 * s);
-      return true;
-    };
-    const uint32_t total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
-    Unit even[2], odd[2];
-    step(mine);
-    next(even);
-    next(odd);
-    for (uint32_t c = mine; c < total; c += 4) {     // `even` and `odd` of this group's stages
-      if (!(ok = expand(even, c))) break;
-      next(even);
-      if (c + 2 >= total) break;
-      if (!(ok = expand(odd, c + 2))) break;
-      next(odd);
     }
   }
   if (!ok) g_wait_failed = 1;
@@ -301,37 +303,43 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------ dy that TMA can read
 
-// Planes of bf16 with rows of `pitch` values (a multiple of 8) and `rows` of them (whole stages, the last
+// Planes of bf16 with rows of `pitch` values (whole threads) and `rows` of them (whole stages, the last
 // ones zero): dy itself, or the three parts of a float's significand.
 template <typename G>
 __global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, uint64_t ld, uint32_t tokens, uint32_t n, uint32_t pitch,
                                                      uint64_t rows, bool wide, uint4* __restrict__ out) {
-  const uint32_t per_row = pitch / 8;
+  const uint32_t per_row = pitch / kValues;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t row = i / per_row;
   if (row >= rows) return;
-  const uint32_t c = (uint32_t)(i - row * per_row) * 8;
-  const int have = row < tokens && c < n ? (int)min(8u, n - c) : 0;
-  float x[8];
-  load8(dy + (have ? row * ld + c : 0), wide && have == 8, have, x);
-  constexpr int kPlanes = sizeof(G) == 4 ? 3 : 1;
+  const uint32_t c = (uint32_t)(i - row * per_row) * kValues;
+  const int have = row < tokens && c < n ? (int)min((uint32_t)kValues, n - c) : 0;
+  Values<G> v;
+  v.load(dy + (have ? row * ld + c : 0), wide && have == kValues, have);
+  if constexpr (sizeof(G) == 2) {
 #pragma unroll
-  for (int q = 0; q < kPlanes; ++q) {
-    uint32_t w[4];
+    for (int h = 0; h < 2; ++h) out[row * per_row * 2 + c / 8 + h] = make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]);
+  } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t bits = __float_as_uint(x[e]), top = bits & 0xFFFF0000u;
-      // a number loses its upper eight bits to this plane; an infinity or NaN goes there whole
-      const bool number = (bits & 0x7F800000u) != 0x7F800000u;
-      const uint32_t mine = number ? top : top | ((bits & 0xFFFFu) ? 0x00400000u : 0u);
-      x[e] = number ? x[e] - __uint_as_float(top) : 0.f;
-      w[e / 2] = e % 2 ? w[e / 2] | mine : mine >> 16;
+    for (int q = 0; q < 3; ++q) {
+      uint32_t w[kValues / 2];
+#pragma unroll
+      for (int e = 0; e < kValues; ++e) {
+        const uint32_t bits = v.w[e], top = bits & 0xFFFF0000u;
+        // a number loses its upper eight bits to this plane; an infinity or NaN goes there whole
+        const bool number = (bits & 0x7F800000u) != 0x7F800000u;
+        const uint32_t mine = number ? top : top | ((bits & 0xFFFFu) ? 0x00400000u : 0u);
+        v.w[e] = number ? __float_as_uint(__uint_as_float(bits) - __uint_as_float(top)) : 0u;
+        w[e / 2] = e % 2 ? w[e / 2] | mine : mine >> 16;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        out[((uint64_t)q * rows + row) * per_row * 2 + c / 8 + h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
     }
-    out[((uint64_t)q * rows + row) * per_row + c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
-uint64_t plane_pitch(uint64_t n) { return (n + 7) / 8 * 8; }
+uint64_t plane_pitch(uint64_t n) { return (n + kValues - 1) / kValues * kValues; }
 uint64_t plane_rows(uint64_t tokens) { return (tokens + kTokens - 1) / kTokens * kTokens; }
 bool readable(const MatrixIn& dy) {
   return dy.type == kBF16 && reinterpret_cast<uintptr_t>(dy.p) % 16 == 0 && (dy.ld % 8 == 0 || dy.rows <= 1) && dy.ld < (1ull << 32);
@@ -379,7 +387,7 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     from = workspace;
     pitch = plane_pitch(dy.cols);
     rows = plane_rows(dy.rows);
-    const uint64_t blocks = (rows * (pitch / 8) + 255) / 256;
+    const uint64_t blocks = (rows * (pitch / kValues) + 255) / 256;
     if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     if (dy.type == kF32)
       planes_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows, (uint32_t)dy.cols,

@@ -1,5 +1,5 @@
 // Blocks of 32 values with a shared power-of-two scale, as MX4 and ACT8 hold them: a thread works on
-// 8 consecutive values of a row, four neighbouring lanes on one block.
+// 16 consecutive values of a row, two neighbouring lanes on one block.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -10,32 +10,53 @@
 namespace rudra {
 namespace {
 
-// 8 values from p; `wide`: p sits on a boundary of the whole access and all 8 exist, else `have` do.
-template <typename G> __device__ __forceinline__ void load8(const G* p, bool wide, int have, float (&x)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float* p, bool wide, int have, float (&x)[8]) {
-  if (wide) {
-    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
-                 : "l"(p));
-  } else {
+constexpr int kValues = 16;   // of a row per thread
+
+// The values from p; `wide`: p sits on a boundary of the accesses (16 bytes bf16, 32 f32) and all of
+// them exist, else `have` do.
+template <typename G> struct Values {
+  static constexpr int kWords = kValues * sizeof(G) / 4;
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ void load(const G* p, bool wide, int have) {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < have ? p[i] : 0.f;
-  }
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, bool wide, int have, float (&x)[8]) {
-  if (wide) {
-    const uint4 r = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+      for (int i = 0; i < kWords; i += 8) {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p) + i;
+        if (sizeof(G) == 4) {
+          asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                       : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
+                       : "l"(q));
+        } else {
+          asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(q));
+          asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"(q + 4));
+        }
+      }
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      for (int i = 0; i < kWords; ++i) {
+        if (sizeof(G) == 4) w[i] = i < have ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+        else w[i] = (2 * i < have ? h[2 * i] : 0u) | (2 * i + 1 < have ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < have ? __bfloat162float(p[i]) : 0.f;
   }
-}
+  __device__ __forceinline__ float get(int i) const {
+    if (sizeof(G) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);   // bf16 is the upper half of a float
+  }
+  // Largest magnitude as the bits of a float: they order like the magnitudes, an infinity above every
+  // number and NaN above both.
+  __device__ __forceinline__ uint32_t max_bits() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if (sizeof(G) == 4) m = max(m, w[i] & 0x7FFFFFFFu);
+      else m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+    }
+    return sizeof(G) == 4 ? m : max(m << 16, m & 0xFFFF0000u);
+  }
+};
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
@@ -43,45 +64,51 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-template <typename G> __device__ __forceinline__ void store8(G* p, bool wide, int have, const float (&x)[8]);
-template <> __device__ __forceinline__ void store8<float>(float* p, bool wide, int have, const float (&x)[8]) {
-  if (wide) {
-    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 :: "l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
-                 : "memory");
-  } else {
+template <typename G> __device__ __forceinline__ void store_values(G* p, bool wide, int have, const float (&x)[kValues]) {
+  if constexpr (sizeof(G) == 4) {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < have) p[i] = x[i];
-  }
-}
-template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, bool wide, int have, const float (&x)[8]) {
-  if (wide) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+      for (int i = 0; i < kValues; i += 8)
+        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     :: "l"(p + i), "f"(x[i]), "f"(x[i + 1]), "f"(x[i + 2]), "f"(x[i + 3]), "f"(x[i + 4]), "f"(x[i + 5]), "f"(x[i + 6]), "f"(x[i + 7])
+                     : "memory");
+      return;
+    }
   } else {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < have) p[i] = __float2bfloat16_rn(x[i]);
+      for (int i = 0; i < kValues; i += 8)
+        *reinterpret_cast<uint4*>(p + i) = make_uint4(pack_bf16(x[i], x[i + 1]), pack_bf16(x[i + 2], x[i + 3]), pack_bf16(x[i + 4], x[i + 5]), pack_bf16(x[i + 6], x[i + 7]));
+      return;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < kValues; ++i)
+    if (i < have) {
+      if constexpr (sizeof(G) == 4) p[i] = x[i];
+      else p[i] = __float2bfloat16_rn(x[i]);
+    }
 }
 
-// Whether every 8-value unit of a matrix's rows sits on a boundary of its access (16 bytes bf16, 32 f32).
+// Whether every thread's values in a matrix's rows sit on a boundary of its accesses.
 template <typename G> inline bool wide_rows(const void* p, uint64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % (8 * sizeof(G)) == 0 && ld % 8 == 0;
 }
 
-// Largest magnitude as the bits of a float: they order like the magnitudes, an infinity above every
-// number and NaN above both.
-__device__ __forceinline__ uint32_t max_bits(const float (&x)[8]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-  return m;
+__device__ __forceinline__ uint32_t block_max_bits(uint32_t m) {   // over the two lanes of a block
+  return max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
 }
-__device__ __forceinline__ uint32_t block_max_bits(uint32_t m) {   // over the four lanes of a block
-  m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-  return max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-}
+
+// Division of numbers below 2^31 by a fixed one below 2^31: the quotient is the high half of a product.
+struct Divisor {
+  uint32_t d, mul, shift;
+  Divisor() = default;
+  explicit Divisor(uint32_t by) : d(by), shift(0) {
+    while ((1ull << shift) < by) ++shift;   // 2^(shift - 1) < by <= 2^shift: the rounded-up multiplier errs below one part in 2^31
+    mul = (uint32_t)(((1ull << (31 + shift)) + by - 1) / by);
+  }
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> (31 + shift)); }
+};
 
 // Scale byte s of a block for a format whose values reach 2^below * 2^(s - 127): 255 marks a block that
 // holds an infinity or NaN.
@@ -96,8 +123,8 @@ __device__ __forceinline__ float scale_value(uint32_t s) {
   return __uint_as_float(s == 255u ? 0x7FC00000u : s ? s << 23 : 0x00400000u);
 }
 
-// 8 values to E2M1 codes, the first in the low bits: nearest, ties to even, saturating.
-__device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float inv) {
+// E2M1 codes of the thread's values, the first in the low bits: nearest, ties to even, saturating.
+__device__ __forceinline__ uint32_t e2m1_codes8(const float (&x)[8]) {
   uint32_t r;
   asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
@@ -105,44 +132,64 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float inv) {
       "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
       "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
-      : "=r"(r)
-      : "f"(x[0] * inv), "f"(x[1] * inv), "f"(x[2] * inv), "f"(x[3] * inv), "f"(x[4] * inv), "f"(x[5] * inv),
-        "f"(x[6] * inv), "f"(x[7] * inv));
-  return inv == 0.f ? 0u : r;
+      : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return r;
+}
+template <typename V> __device__ __forceinline__ uint2 e2m1_codes(const V& v, uint32_t s) {
+  const float inv = inverse_scale(s);
+  float x[8];
+  uint2 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = v.get(i) * inv;
+  r.x = e2m1_codes8(x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = v.get(8 + i) * inv;
+  r.y = e2m1_codes8(x);
+  return s == 255u ? make_uint2(0u, 0u) : r;
 }
 
-// 8 E2M1 codes to the values they stand for under a scale.
-__device__ __forceinline__ void e2m1_values(uint32_t codes, float scale, float (&x)[8]) {
-  uint32_t h[4];
-  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-      "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-      : "r"(codes));
+// The values E2M1 codes stand for under a scale.
+__device__ __forceinline__ void e2m1_values(uint2 codes, float scale, float (&x)[kValues]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-    x[2 * i] = f.x * scale;
-    x[2 * i + 1] = f.y * scale;
+  for (int q = 0; q < 2; ++q) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(q ? codes.y : codes.x));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+      x[8 * q + 2 * i] = f.x * scale;
+      x[8 * q + 2 * i + 1] = f.y * scale;
+    }
   }
 }
 
-// 8 values to int8 codes in two words: nearest, ties to even, at most 127 in magnitude.
-__device__ __forceinline__ uint2 int8_codes(const float (&x)[8], float inv) {
-  uint32_t w[2] = {0u, 0u};
+// int8 codes of the thread's values: nearest, ties to even, at most 127 in magnitude.  Adding 1.5 * 2^23
+// rounds to a whole number whose two's complement is the sum's low byte.
+template <typename V> __device__ __forceinline__ uint4 int8_codes(const V& v, uint32_t s) {
+  constexpr float kWhole = 12582912.f;
+  const float inv = inverse_scale(s);
+  uint32_t r[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = max(-127, min(127, __float2int_rn(x[i] * inv)));
-    w[i / 4] |= (uint32_t)(c & 255) << (8 * (i % 4));
+  for (int q = 0; q < 4; ++q) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fminf(fmaxf(fmaf(v.get(4 * q + i), inv, kWhole), kWhole - 127.f), kWhole + 127.f));
+    r[q] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   }
-  return inv == 0.f ? make_uint2(0u, 0u) : make_uint2(w[0], w[1]);
+  return s == 255u ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(r[0], r[1], r[2], r[3]);
 }
-__device__ __forceinline__ void int8_values(uint2 w, float scale, float (&x)[8]) {
+// The values int8 codes stand for: a code plus 128, set into 2^23, is a float less 2^23 + 128.
+__device__ __forceinline__ void int8_values(uint4 codes, float scale, float (&x)[kValues]) {
+  const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = (float)(int8_t)(w.x >> (8 * i)) * scale;
-    x[4 + i] = (float)(int8_t)(w.y >> (8 * i)) * scale;
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t u = c[q] ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[4 * q + i] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + i)) - 8388736.f) * scale;
   }
 }
 

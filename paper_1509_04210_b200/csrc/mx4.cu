@@ -3,6 +3,8 @@
 // A block's scale is a power of two read off the exponent field of its largest magnitude, so scaling
 // is exact and the only rounding is the one to E2M1, done by the conversion instruction.  One read and
 // 17/32 byte written per value: bound by HBM for large matrices, by launch latency for small ones.
+#include <algorithm>
+
 #include "blocks.cuh"
 #include "learner.cuh"
 
@@ -11,37 +13,34 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Rows as they stand.  16 lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
+// Rows as they stand.  Eight lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
 template <typename G>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __restrict__ src, uint64_t ld, uint32_t cols,
-                                                                 uint32_t kt, uint64_t items, bool wide,
-                                                                 uint32_t* __restrict__ codes, uint32_t* __restrict__ scales) {
-  constexpr int U = 2;
-  const uint32_t lane = threadIdx.x % 16;
-  const uint32_t nb = (cols + 31) / 32;
-  float x[U][8];
-  uint64_t row[U];
-  uint32_t k[U], c[U];
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __restrict__ src, uint64_t ld, uint32_t cols, Divisor kt,
+                                                                 uint32_t items, bool wide, uint2* __restrict__ codes,
+                                                                 uint32_t* __restrict__ scales) {
+  constexpr uint32_t U = 2, kItems = kThreads / 8;
+  const uint32_t lane = threadIdx.x % 8, nb = (cols + 31) / 32;
+  Values<G> x[U];
+  uint32_t row[U], k[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint64_t item = (uint64_t)blockIdx.x * (U * kThreads / 16) + u * (kThreads / 16) + threadIdx.x / 16;
-    const bool in = item < items;
-    row[u] = in ? (uint32_t)item / kt : ~0ull;   // items < 2^32
-    k[u] = (uint32_t)item % kt;
-    c[u] = k[u] * 128 + lane * 8;
-    const int have = in && c[u] < cols ? (int)min(8u, cols - c[u]) : 0;
-    load8(src + (have ? row[u] * ld + c[u] : 0), wide && have == 8, have, x[u]);
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t item = blockIdx.x * (U * kItems) + u * kItems + threadIdx.x / 8;
+    row[u] = kt.quotient(item);
+    k[u] = item - row[u] * kt.d;
+    const uint32_t c = k[u] * 128 + lane * kValues;
+    const int have = item < items && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
+    x[u].load(src + (have ? row[u] * ld + c : 0), wide && have == kValues, have);
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t s = scale_byte(block_max_bits(max_bits(x[u])), 2);
-    const uint32_t w = e2m1_codes(x[u], inverse_scale(s));
-    uint32_t four = s << (8 * (lane / 4));
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t s = scale_byte(block_max_bits(x[u].max_bits()), 2);
+    const uint2 w = e2m1_codes(x[u], s);
+    uint32_t four = s << (8 * (lane / 2));
+    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 2);
     four |= __shfl_xor_sync(0xFFFFFFFFu, four, 4);
-    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 8);
-    if (row[u] == ~0ull) continue;
-    if (c[u] / 32 < nb) codes[row[u] * nb * 4 + c[u] / 8] = w;
-    if (lane == 0) scales[mx4_scale_at(row[u], k[u] * 4, kt) / 4] = four;
+    if (blockIdx.x * (U * kItems) + u * kItems + threadIdx.x / 8 >= items) continue;
+    if (k[u] * 4 + lane / 2 < nb) codes[(uint64_t)row[u] * nb * 2 + k[u] * 8 + lane] = w;
+    if (lane == 0) scales[mx4_scale_at(row[u], k[u] * 4, kt.d) / 4] = four;
   }
 }
 
@@ -84,13 +83,12 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    float(&v)[4][8] = reinterpret_cast<float(&)[4][8]>(x[j]);
-    uint32_t m = 0;
+    Values<float> v[2];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) m = max(m, max_bits(v[q]));
-    const uint32_t s = scale_byte(m, 2);
-    const float inv = inverse_scale(s);
-    tile[lane * 2 + j][warp] = make_uint4(e2m1_codes(v[0], inv), e2m1_codes(v[1], inv), e2m1_codes(v[2], inv), e2m1_codes(v[3], inv));
+    for (int i = 0; i < 32; ++i) v[i / kValues].w[i % kValues] = __float_as_uint(x[j][i]);
+    const uint32_t s = scale_byte(max(v[0].max_bits(), v[1].max_bits()), 2);
+    const uint2 lo = e2m1_codes(v[0], s), hi = e2m1_codes(v[1], s);
+    tile[lane * 2 + j][warp] = make_uint4(lo.x, lo.y, hi.x, hi.y);
     sbytes[lane * 2 + j][warp] = (uint8_t)s;
   }
   __syncthreads();
@@ -105,44 +103,55 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
 }
 
 template <typename G>
-__global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                              uint32_t cols, uint32_t kt, uint64_t units, bool wide,
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                              uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, bool wide,
                                                               G* __restrict__ dst, uint64_t ld) {
-  const uint32_t per_row = (cols + 7) / 8, nb = (cols + 31) / 32;
-  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= units) return;
-  const uint64_t row = i / per_row;
-  const uint32_t unit = (uint32_t)(i - row * per_row), c = unit * 8;
-  const int have = (int)min(8u, cols - c);
-  float x[8];
-  e2m1_values(codes[row * nb * 4 + unit], scale_value(scales[mx4_scale_at(row, c / 32, kt)]), x);
-  store8(dst + row * ld + c, wide && have == 8, have, x);
+  constexpr uint32_t U = 2;
+  const uint32_t nb = (cols + 31) / 32;
+  uint2 w[U];
+  uint8_t s[U];
+  uint32_t row[U], c[U];
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t i = (blockIdx.x * U + u) * kThreads + threadIdx.x;
+    row[u] = per_row.quotient(i);
+    c[u] = (i - row[u] * per_row.d) * kValues;
+    if (i < units) {
+      w[u] = __ldcs(codes + (uint64_t)row[u] * nb * 2 + c[u] / kValues);
+      s[u] = __ldg(scales + mx4_scale_at(row[u], c[u] / 32, kt));
+    }
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    if ((blockIdx.x * U + u) * kThreads + threadIdx.x >= units) continue;
+    const int have = (int)min((uint32_t)kValues, cols - c[u]);
+    float x[kValues];
+    e2m1_values(w[u], scale_value(s[u]), x);
+    store_values(dst + row[u] * ld + c[u], wide && have == kValues, have, x);
+  }
 }
 
-cudaError_t grid_of(uint64_t work, uint64_t per_block, unsigned* blocks) {
-  const uint64_t b = (work + per_block - 1) / per_block;
-  if (b > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-  *blocks = (unsigned)b;
-  return cudaSuccess;
-}
+unsigned grid_of(uint64_t work, uint64_t per_block) { return (unsigned)((work + per_block - 1) / per_block); }
 
 template <typename G>
 cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scales, cudaStream_t stream) {
   const G* src = static_cast<const G*>(m.p);
-  unsigned blocks;
   if (!transpose) {
-    const uint64_t kt = (m.cols + 127) / 128, items = m.rows * kt;
-    if (items > 0xFFFFFFFFull) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = grid_of(items, 2 * kThreads / 16, &blocks);
-    if (e != cudaSuccess) return e;
-    quantize_rows_kernel<G><<<blocks, kThreads, 0, stream>>>(src, m.ld, (uint32_t)m.cols, (uint32_t)kt, items, wide_rows<G>(src, m.ld),
-                                                             static_cast<uint32_t*>(codes), static_cast<uint32_t*>(scales));
+    // as many rows to a launch as keep the count of its work below 2^31
+    const uint64_t kt = (m.cols + 127) / 128, most = std::max<uint64_t>(1, 0x70000000ull / kt / 128) * 128;
+    for (uint64_t r = 0; r < m.rows; r += most) {
+      const uint64_t rows = std::min(most, m.rows - r);
+      if (rows * kt > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+      quantize_rows_kernel<G><<<grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, stream>>>(
+          src + r * m.ld, m.ld, (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), wide_rows<G>(src, m.ld),
+          static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2, static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
+    }
   } else {
     const uint64_t tiles = (m.cols + 63) / 64;
-    const cudaError_t e = grid_of(tiles * ((m.rows + 127) / 128), 1, &blocks);
-    if (e != cudaSuccess) return e;
+    const uint64_t blocks = tiles * ((m.rows + 127) / 128);
+    if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const bool pairs = reinterpret_cast<uintptr_t>(src) % (2 * sizeof(G)) == 0 && m.ld % 2 == 0;
-    quantize_transposed_kernel<G><<<blocks, 128, 0, stream>>>(src, m.ld, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)tiles, pairs,
+    quantize_transposed_kernel<G><<<(unsigned)blocks, 128, 0, stream>>>(src, m.ld, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)tiles, pairs,
                                                               static_cast<uint4*>(codes), static_cast<uint32_t*>(scales));
   }
   return cudaGetLastError();
@@ -150,12 +159,15 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
 
 template <typename G>
 cudaError_t dequantize(const Mx4& m, const MatrixOut& d, cudaStream_t stream) {
-  const uint64_t units = m.rows * ((m.cols + 7) / 8), kt = (m.cols + 127) / 128;
-  unsigned blocks;
-  const cudaError_t e = grid_of(units, kThreads, &blocks);
-  if (e != cudaSuccess) return e;
-  dequantize_kernel<G><<<blocks, kThreads, 0, stream>>>(static_cast<const uint32_t*>(m.codes), static_cast<const uint8_t*>(m.scales),
-                                                        (uint32_t)m.cols, (uint32_t)kt, units, wide_rows<G>(d.p, d.ld), static_cast<G*>(d.p), d.ld);
+  const uint64_t per_row = (m.cols + kValues - 1) / kValues, nb = (m.cols + 31) / 32, kt = (m.cols + 127) / 128;
+  const uint64_t most = std::max<uint64_t>(1, 0x70000000ull / per_row / 128) * 128;
+  for (uint64_t r = 0; r < m.rows; r += most) {
+    const uint64_t units = std::min(most, m.rows - r) * per_row;
+    if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    dequantize_kernel<G><<<grid_of(units, 2 * kThreads), kThreads, 0, stream>>>(
+        static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
+        Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, wide_rows<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
+  }
   return cudaGetLastError();
 }
 
