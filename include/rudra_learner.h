@@ -77,8 +77,8 @@ int rudra_mx4_matmul(const void* a_codes_dev, const void* a_scales_dev, uint64_t
                      void* cuda_stream);
 
 /* The same with a = x (m x k of x_dtype) brought to MX4 inside the call: a linear layer without
- * bias.  workspace_dev: rudra_mx4_linear_workspace(m, k) bytes on a 32-byte boundary, free for other
- * use once the call's work has run. */
+ * bias.  workspace_dev: rudra_mx4_linear_workspace(m, k) bytes (zero for few rows) on a 32-byte boundary,
+ * free for other use once the call's work has run. */
 uint64_t rudra_mx4_linear_workspace(uint64_t m, uint64_t k);
 int rudra_mx4_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, const void* w_codes_dev,
                      const void* w_scales_dev, uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy,

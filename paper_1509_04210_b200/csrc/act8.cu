@@ -69,15 +69,15 @@ struct Restored {
 // checkpoint without gaps and neighbouring lanes share a block.
 template <typename G, Act A>
 __global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__ x, const G* __restrict__ up, uint64_t ldx,
-                                                           uint32_t cols, Divisor per_row, uint32_t units, bool wide_in, bool wide_out,
+                                                           uint32_t cols, Divisor per_row, uint32_t units, Access access_in, Access access_out,
                                                            G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   const bool in = i < units;
   const int have = in && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
   const uint64_t at = have ? row * ldx + c : 0;
   Values<G> a, b;
-  a.load(x + at, wide_in && have == kValues, have);
-  if (A == kSwiglu) b.load(up + at, wide_in && have == kValues, have);
+  a.load(x + at, access_in, have);
+  if (A == kSwiglu) b.load(up + at, access_in, have);
   save(saved, i, a, in);
   if (A == kSwiglu) save(saved_up, i, b, in);
   if constexpr (A != kNone) {
@@ -85,20 +85,20 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__
     float v[kValues];
 #pragma unroll
     for (int e = 0; e < kValues; ++e) v[e] = A == kSwiglu ? value<A>(a.get(e)) * b.get(e) : value<A>(a.get(e));
-    store_values(y + row * ldy + c, wide_out && have == kValues, have, v);
+    store_values(y + row * ldy + c, access_out, have, v);
   }
 }
 
 template <typename G, Act A>
 __global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_t lddy, uint32_t cols, Divisor per_row, uint32_t units,
-                                                            bool wide_in, bool wide_out, Saved saved, Saved saved_up, G* dx, G* dup,
+                                                            Access access_in, Access access_out, Saved saved, Saved saved_up, G* dx, G* dup,
                                                             uint64_t lddx) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   if (i >= units || c >= cols) return;
   const int have = (int)min((uint32_t)kValues, cols - c);
   Values<G> g;
   Restored rx, ru;
-  if (A != kNone) g.load(dy + row * lddy + c, wide_in && have == kValues, have);
+  if (A != kNone) g.load(dy + row * lddy + c, access_in, have);
   rx.load(saved, i);
   if (A == kSwiglu) ru.load(saved_up, i);
   float x[kValues], u[kValues];
@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_
       if (A == kSwiglu) u[e] = g.get(e) * f;
     }
   }
-  store_values(dx + row * lddx + c, wide_out && have == kValues, have, x);
-  if (A == kSwiglu) store_values(dup + row * lddx + c, wide_out && have == kValues, have, u);
+  store_values(dx + row * lddx + c, access_out, have, x);
+  if (A == kSwiglu) store_values(dup + row * lddx + c, access_out, have, u);
 }
 
 // Rows of a launch: as many as keep the number of its units below 2^31.
@@ -130,13 +130,13 @@ Saved after(const Saved& s, uint64_t units) { return s.codes ? Saved{s.codes + u
 template <typename G, Act A>
 cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const Act8& saved, const Act8& saved_up, cudaStream_t stream) {
   const Part part(x.cols);
-  const bool wide_in = wide_rows<G>(x.p, x.ld) && (A != kSwiglu || wide_rows<G>(up, x.ld));
+  const Access in = A == kSwiglu ? both(access_of<G>(x.p, x.ld), access_of<G>(up, x.ld)) : access_of<G>(x.p, x.ld);
   for (uint64_t r = 0; r < x.rows; r += part.most) {
     const uint64_t units = std::min(part.most, x.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     forward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
         static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
-        Divisor((uint32_t)part.per_row), (uint32_t)units, wide_in, wide_rows<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
+        Divisor((uint32_t)part.per_row), (uint32_t)units, in, access_of<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
         after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row));
   }
   return cudaGetLastError();
@@ -145,13 +145,13 @@ cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const
 template <typename G, Act A>
 cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up, const MatrixOut& dx, void* dup, cudaStream_t stream) {
   const Part part(dx.cols);
-  const bool wide_out = wide_rows<G>(dx.p, dx.ld) && (A != kSwiglu || wide_rows<G>(dup, dx.ld));
+  const Access out = A == kSwiglu ? both(access_of<G>(dx.p, dx.ld), access_of<G>(dup, dx.ld)) : access_of<G>(dx.p, dx.ld);
   for (uint64_t r = 0; r < dx.rows; r += part.most) {
     const uint64_t units = std::min(part.most, dx.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     backward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
         static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
-        wide_rows<G>(dy.p, dy.ld), wide_out, after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row),
+        access_of<G>(dy.p, dy.ld), out, after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row),
         static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
   }
   return cudaGetLastError();

@@ -101,26 +101,6 @@ __device__ __forceinline__ void fetch(Unit& u, const Params& p, uint32_t token, 
   }
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float peer_float(uint32_t at, uint32_t rank) {
-  uint32_t remote;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-  return v;
-}
-template <typename G> __device__ __forceinline__ void put(G* to, float v) {
-  if constexpr (sizeof(G) == 2) *to = __float2bfloat16_rn(v);
-  else *to = v;
-}
-
 template <typename G>
 __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ Params p) {
   extern __shared__ uint8_t raw[];
@@ -284,14 +264,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   if (!ok) g_wait_failed = 1;
   __syncwarp();
   if (p.split > 1) {   // one tile to a cluster
-    cluster_sync();
-    const uint32_t k0 = tile0 % p.lane_tiles * kLanes, n0 = tile0 / p.lane_tiles * kColumns, have = min(kColumns, p.n - n0);
-    for (uint32_t e = rank * kThreads + threadIdx.x; e < have * kLanes; e += p.split * kThreads) {
-      float v = 0.f;
-      for (uint32_t r = 0; r < p.split; ++r) v += peer_float(stage0 + e * 4, r);
-      if (k0 + e % kLanes < p.k) put(static_cast<G*>(p.dw) + (uint64_t)(n0 + e / kLanes) * p.lddw + k0 + e % kLanes, v);
-    }
-    cluster_sync();
+    const uint32_t k0 = tile0 % p.lane_tiles * kLanes, n0 = tile0 / p.lane_tiles * kColumns;
+    join_parts(stage0, p.split, rank, min(kColumns, p.n - n0), min(kLanes, p.k - k0), static_cast<G*>(p.dw) + (uint64_t)n0 * p.lddw + k0, p.lddw);
   }
   tmem_fence_before();
   __syncthreads();
@@ -307,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 // ones zero): dy itself, or the three parts of a float's significand.
 template <typename G>
 __global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, uint64_t ld, uint32_t tokens, uint32_t n, uint32_t pitch,
-                                                     uint64_t rows, bool wide, uint4* __restrict__ out) {
+                                                     uint64_t rows, Access access, uint4* __restrict__ out) {
   const uint32_t per_row = pitch / kValues;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t row = i / per_row;
@@ -315,7 +289,7 @@ __global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, u
   const uint32_t c = (uint32_t)(i - row * per_row) * kValues;
   const int have = row < tokens && c < n ? (int)min((uint32_t)kValues, n - c) : 0;
   Values<G> v;
-  v.load(dy + (have ? row * ld + c : 0), wide && have == kValues, have);
+  v.load(dy + (have ? row * ld + c : 0), access, have);
   if constexpr (sizeof(G) == 2) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) out[row * per_row * 2 + c / 8 + h] = make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]);
@@ -391,11 +365,11 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     if (dy.type == kF32)
       planes_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows, (uint32_t)dy.cols,
-                                                                 (uint32_t)pitch, rows, wide_rows<float>(dy.p, dy.ld), static_cast<uint4*>(workspace));
+                                                                 (uint32_t)pitch, rows, access_of<float>(dy.p, dy.ld), static_cast<uint4*>(workspace));
     else
       planes_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(dy.p), dy.ld, (uint32_t)dy.rows,
                                                                          (uint32_t)dy.cols, (uint32_t)pitch, rows,
-                                                                         wide_rows<__nv_bfloat16>(dy.p, dy.ld), static_cast<uint4*>(workspace));
+                                                                         access_of<__nv_bfloat16>(dy.p, dy.ld), static_cast<uint4*>(workspace));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }

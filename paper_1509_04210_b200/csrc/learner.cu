@@ -43,10 +43,6 @@ int check_blocks(const char* what, const void* codes, const void* scales, uint64
 int done(cudaError_t e, const char* what) { return e == cudaSuccess ? 0 : cuda_fail(e, what); }
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 
-int matmul(const rudra::Mx4& a, const rudra::Mx4& b, const MatrixOut& y, void* cuda_stream) {
-  return done(rudra::launch_mx4_matmul(a, b, y, stream_of(cuda_stream)), "4-bit product kernel launch");
-}
-
 }  // namespace
 
 extern "C" {
@@ -83,13 +79,13 @@ int rudra_mx4_matmul(const void* a_codes_dev, const void* a_scales_dev, uint64_t
     if (const int e = check_blocks("second factor", b_codes_dev, b_scales_dev, n, k)) return e;
     if (const int e = check_matrix("product", y_dev, y_dtype, m, n, ldy)) return e;
     if (m == 0 || n == 0) return 0;
-    return matmul({a_codes_dev, a_scales_dev, m, k}, {b_codes_dev, b_scales_dev, n, k}, {y_dev, type_of(y_dtype), m, n, ldy}, cuda_stream);
+    return done(rudra::launch_mx4_matmul({a_codes_dev, a_scales_dev, m, k}, {b_codes_dev, b_scales_dev, n, k}, {y_dev, type_of(y_dtype), m, n, ldy},
+                                         stream_of(cuda_stream)),
+                "4-bit product kernel launch");
   });
 }
 
-uint64_t rudra_mx4_linear_workspace(uint64_t m, uint64_t k) {
-  return (rudra_mx4_codes_bytes(m, k) + 31) / 32 * 32 + rudra_mx4_scales_bytes(m, k);
-}
+uint64_t rudra_mx4_linear_workspace(uint64_t m, uint64_t k) { return rudra::mx4_linear_workspace(m, k); }
 
 int rudra_mx4_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, const void* w_codes_dev, const void* w_scales_dev,
                      uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy, void* workspace_dev, uint64_t workspace_bytes,
@@ -102,14 +98,9 @@ int rudra_mx4_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, c
     const uint64_t need = rudra_mx4_linear_workspace(m, k);
     if (need && (!aligned(workspace_dev) || workspace_bytes < need))
       return fail(RUDRA_E_INVAL, "workspace is null, not 32-byte aligned or smaller than %llu bytes", (unsigned long long)need);
-    uint8_t* codes = static_cast<uint8_t*>(workspace_dev);
-    uint8_t* scales = codes + (rudra_mx4_codes_bytes(m, k) + 31) / 32 * 32;
-    if (k) {
-      const int e = done(rudra::launch_mx4_quantize({x_dev, type_of(x_dtype), m, k, ldx}, false, codes, scales, stream_of(cuda_stream)),
-                         "quantization kernel launch");
-      if (e) return e;
-    }
-    return matmul({codes, scales, m, k}, {w_codes_dev, w_scales_dev, n, k}, {y_dev, type_of(y_dtype), m, n, ldy}, cuda_stream);
+    return done(rudra::launch_mx4_linear({x_dev, type_of(x_dtype), m, k, ldx}, {w_codes_dev, w_scales_dev, n, k},
+                                         {y_dev, type_of(y_dtype), m, n, ldy}, workspace_dev, stream_of(cuda_stream)),
+                "4-bit product kernel launch");
   });
 }
 

@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 // Rows as they stand.  Eight lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
 template <typename G>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __restrict__ src, uint64_t ld, uint32_t cols, Divisor kt,
-                                                                 uint32_t items, bool wide, uint2* __restrict__ codes,
+                                                                 uint32_t items, Access access, uint2* __restrict__ codes,
                                                                  uint32_t* __restrict__ scales) {
   constexpr uint32_t U = 2, kItems = kThreads / 8;
   const uint32_t lane = threadIdx.x % 8, nb = (cols + 31) / 32;
@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __rest
     k[u] = item - row[u] * kt.d;
     const uint32_t c = k[u] * 128 + lane * kValues;
     const int have = item < items && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-    x[u].load(src + (have ? row[u] * ld + c : 0), wide && have == kValues, have);
+    x[u].load(src + (have ? row[u] * ld + c : 0), access, have);
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
 
 template <typename G>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                              uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, bool wide,
+                                                              uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
                                                               G* __restrict__ dst, uint64_t ld) {
   constexpr uint32_t U = 2;
   const uint32_t nb = (cols + 31) / 32;
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
     const int have = (int)min((uint32_t)kValues, cols - c[u]);
     float x[kValues];
     e2m1_values(w[u], scale_value(s[u]), x);
-    store_values(dst + row[u] * ld + c[u], wide && have == kValues, have, x);
+    store_values(dst + row[u] * ld + c[u], access, have, x);
   }
 }
 
@@ -143,7 +143,7 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
       const uint64_t rows = std::min(most, m.rows - r);
       if (rows * kt > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
       quantize_rows_kernel<G><<<grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, stream>>>(
-          src + r * m.ld, m.ld, (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), wide_rows<G>(src, m.ld),
+          src + r * m.ld, m.ld, (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), access_of<G>(src, m.ld),
           static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2, static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
     }
   } else {
@@ -166,7 +166,7 @@ cudaError_t dequantize(const Mx4& m, const MatrixOut& d, cudaStream_t stream) {
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     dequantize_kernel<G><<<grid_of(units, 2 * kThreads), kThreads, 0, stream>>>(
         static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
-        Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, wide_rows<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
+        Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, access_of<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
   }
   return cudaGetLastError();
 }

@@ -4,12 +4,16 @@
 // kernel only moves codes and scale bytes: TMA brings 128-byte (256-value) pieces of rows into
 // swizzled shared memory, bulk copies bring the scale bytes, tcgen05.cp places those in tensor memory
 // next to the accumulators.  Rows of b (a layer's outputs) are the 128 lanes of an accumulator and rows
-// of a (tokens) its columns, so one shape serves a single token (16 columns) as well as large
-// batches (256), and neighbouring lanes write neighbouring outputs.
+// of a (tokens) its columns, so one shape serves a single token (16 columns) as well as a batch, and
+// neighbouring lanes write neighbouring outputs.
 //
-// Few tiles: the reduction is split over the blocks of a cluster, which add their parts in rank order
-// through distributed shared memory; the sum does not depend on the run.
+// Few tiles: the reduction is split over the blocks of a cluster.  Their parts
+// are added in rank order through distributed shared memory, so the sum does not depend on the run.
+//
+// Up to 32 tokens the kernel can take x itself: every block brings its slice of the few rows to MX4 on
+// the way into shared memory, which costs less than another launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "blocks.cuh"
 #include "learner.cuh"
@@ -18,30 +22,32 @@
 namespace rudra {
 namespace {
 
-constexpr int kThreads = 192;        // warp 0 loads, warp 1 issues, warps 2-5 take the results
 constexpr uint32_t kStageBytes = 128;   // of a row per stage: 256 values
 
-template <int COLS> struct Shape {
-  static constexpr uint32_t kRowAtoms = COLS > 128 ? COLS / 128 : 1;     // 512-byte scale atoms per 128 values
+// Warp 0 loads, warp 1 issues, warps 2-5 take the results; where x is brought to MX4 here, warps 2-9 do that.
+template <int COLS, bool QUANTIZE> struct Shape {
+  static constexpr uint32_t kQuantizers = QUANTIZE ? 8 : 0;
+  static constexpr uint32_t kThreads = QUANTIZE ? 320 : 192;
   static constexpr uint32_t kLanes = 128 * kStageBytes;
   static constexpr uint32_t kColumns = COLS * kStageBytes;
-  static constexpr uint32_t kScales = 1024 * (1 + kRowAtoms);
+  static constexpr uint32_t kScales = 1024 * 2;                          // two 512-byte scale atoms of each operand
   static constexpr uint32_t kStage = kLanes + kColumns + kScales;
-  static constexpr uint32_t kStages = COLS == 256 ? 4 : COLS == 128 ? 5 : 8;
-  static constexpr uint32_t kScaleColumns = 8 * (1 + kRowAtoms);         // tensor memory per stage
-  static constexpr uint32_t kUsed = COLS + kStages * kScaleColumns;
-  static constexpr uint32_t kTmem = kUsed > 256 ? 512 : 256;
+  static constexpr uint32_t kStages = COLS == 128 ? 6 : COLS == 64 ? 8 : COLS == 32 ? 9 : 10;
+  static constexpr uint32_t kScaleColumns = 16;                          // tensor memory per stage
+  static constexpr uint32_t kTmem = 256;
   static constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
-  static_assert(kUsed <= 512 && kSmem <= 227 * 1024, "does not fit an SM");
-  static_assert(kStages * kStage >= COLS * 512, "the parts of a split sum are kept where the stages were");
+  static_assert(COLS + kStages * kScaleColumns <= kTmem && kSmem <= 227 * 1024, "does not fit an SM");
 };
 
 struct Params {
   const uint8_t* lane_scales;     // of b
   const uint8_t* column_scales;   // of a
+  const void* x;                  // or a as it came
+  uint64_t ldx;
+  Access access;
   void* y;
   uint64_t ldy;
-  uint32_t m, n;                  // rows of a, rows of b
+  uint32_t m, n, k;               // rows of a, rows of b, their length
   uint32_t kt;                    // 128-value scale atoms along a row
   uint32_t lane_tiles;
   uint32_t split;                 // blocks of a cluster that share a tile
@@ -60,36 +66,16 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
                :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add) : "memory");
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float peer_float(uint32_t at, uint32_t rank) {
-  uint32_t remote;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-  return v;
-}
-
-template <typename G> __device__ __forceinline__ void put(const Params& p, uint32_t m, uint32_t n, float v) {
-  G* y = static_cast<G*>(p.y) + (uint64_t)m * p.ldy + n;
-  if constexpr (sizeof(G) == 2) *y = __float2bfloat16_rn(v);
-  else *y = v;
-}
-
-template <typename G, int COLS>
-__global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant__ CUtensorMap lane_map,
-                                                          const __grid_constant__ CUtensorMap column_map,
-                                                          const __grid_constant__ Params p) {
-  using S = Shape<COLS>;
+// X: type of x where it is brought to MX4 here, else void.
+template <typename G, int COLS, typename X>
+__global__ void __launch_bounds__(Shape<COLS, !std::is_void<X>::value>::kThreads)
+matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map, const __grid_constant__ Params p) {
+  constexpr bool kQuantize = !std::is_void<X>::value;
+  using S = Shape<COLS, kQuantize>;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage0 = smem_address(smem);
+  float* part = reinterpret_cast<float*>(smem);      // [column][lane], once the stages are done with
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
   const uint32_t full = smem_address(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
   uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * S::kStages + 1);
@@ -103,9 +89,9 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
 
   if (threadIdx.x == 0) {
     prefetch_map(&lane_map);
-    prefetch_map(&column_map);
+    if (!kQuantize) prefetch_map(&column_map);
     for (uint32_t s = 0; s < S::kStages; ++s) {
-      barrier_init(full + 8 * s, 1);
+      barrier_init(full + 8 * s, kQuantize ? 2 : 1);
       barrier_init(empty + 8 * s, 1);
     }
     barrier_init(done, 1);
@@ -120,20 +106,19 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
 
   if (warp == 0) {
     if (lane == 0) {
-      const uint32_t atoms_of_columns = min(S::kRowAtoms, (p.m - m0 + 127) / 128);
       uint32_t issued = 0;
       for (uint32_t i = first; i < last; ++i, ++issued) {
         const uint32_t s = issued % S::kStages, round = issued / S::kStages;
         if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1))) break;
-        const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s;
+        const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s, scales = at + S::kLanes + S::kColumns;
         const uint32_t atoms = min(2u, p.kt - 2 * i);
-        barrier_expect(bar, S::kLanes + S::kColumns + atoms * 512 * (1 + atoms_of_columns));
+        barrier_expect(bar, S::kLanes + atoms * 512 + (kQuantize ? 0 : S::kColumns + atoms * 512));
         copy_box(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar);
-        copy_box(at + S::kLanes, &column_map, (int)(i * kStageBytes), (int)m0, bar);
-        const uint32_t scales = at + S::kLanes + S::kColumns;
         copy_bulk(scales, p.lane_scales + ((uint64_t)(n0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar);
-        for (uint32_t r = 0; r < atoms_of_columns; ++r)
-          copy_bulk(scales + 1024 * (1 + r), p.column_scales + ((uint64_t)(m0 / 128 + r) * p.kt + 2 * i) * 512, atoms * 512, bar);
+        if (!kQuantize) {
+          copy_box(at + S::kLanes, &column_map, (int)(i * kStageBytes), (int)m0, bar);
+          copy_bulk(scales + 1024, p.column_scales + ((uint64_t)(m0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar);
+        }
       }
       // given up: what is on its way lands before the block may end
       if (!ok)
@@ -150,10 +135,9 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
         const uint32_t ts = tmem + COLS + s * S::kScaleColumns;
         const uint32_t atoms = min(2u, p.kt - 2 * i);
         for (uint32_t k = 0; k < atoms; ++k) {
-          const uint32_t tl = ts + k * 4 * (1 + S::kRowAtoms), tc = tl + 4;
+          const uint32_t tl = ts + k * 8, tc = tl + 4;
           scales_to_tmem(tl, scale_rows(scales + 512 * k));
-#pragma unroll
-          for (uint32_t r = 0; r < S::kRowAtoms; ++r) scales_to_tmem(tc + 4 * r, scale_rows(scales + 1024 * (1 + r) + 512 * k));
+          scales_to_tmem(tc, scale_rows(scales + 1024 + 512 * k));
 #pragma unroll
           for (uint32_t h = 0; h < 2; ++h) {   // 64 values: two scale bytes of the four
             const uint32_t off = (2 * k + h) * 32;
@@ -165,40 +149,70 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
       }
       if (ok) tensor_commit(done);
     }
+  } else if (kQuantize) {
+    // a warp brings every eighth stage's values to MX4, where TMA and the bulk copies would have put them
+    using T = typename std::conditional<kQuantize, X, float>::type;
+    const T* x = static_cast<const T*>(p.x);
+    for (uint32_t i = first + (warp - 2); i < last; i += S::kQuantizers) {
+      const uint32_t c = i - first, s = c % S::kStages;
+      uint8_t* stage = smem + s * S::kStage + S::kLanes;
+      bool free = c < S::kStages;
+#pragma unroll 1
+      for (uint32_t r0 = 0; r0 < p.m; r0 += 8) {      // 16 lanes to a row: eight rows on their way at a time
+        Values<T> v[4];
+        const uint32_t k0 = i * 256 + lane % 16 * kValues;
+        const int have = k0 < p.k ? (int)min((uint32_t)kValues, p.k - k0) : 0;
+#pragma unroll
+        for (uint32_t h = 0; h < 4; ++h) {
+          const uint32_t r = r0 + 2 * h + lane / 16;
+          const int some = r < p.m ? have : 0;
+          v[h].load(x + (some ? r * p.ldx + k0 : 0), p.access, some);
+        }
+        if (!free && !(ok = free = barrier_wait(empty + 8 * s, (c / S::kStages & 1) ^ 1))) break;
+#pragma unroll
+        for (uint32_t h = 0; h < 4; ++h) {
+          if (r0 + 2 * h >= p.m) break;
+          const uint32_t r = r0 + 2 * h + lane / 16, u = lane % 16;
+          const uint32_t e = scale_byte(block_max_bits(v[h].max_bits()), 2);
+          const uint2 w = e2m1_codes(v[h], e);
+          if (r >= p.m) continue;
+          *reinterpret_cast<uint2*>(stage + r * 128 + ((u / 2) ^ (r % 8)) * 16 + u % 2 * 8) = w;
+          if (u % 2 == 0) stage[S::kColumns + 1024 + u / 8 * 512 + r * 16 + u / 2 % 4] = (uint8_t)e;   // r < 32
+        }
+      }
+      if (!ok) break;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) barrier_arrive(full + 8 * s);
+    }
   }
   __syncwarp();
 
   const uint32_t group = warp % 4;                       // the lanes of tensor memory a warp may read
   const uint32_t n = n0 + group * 32 + lane;
-  float* part = reinterpret_cast<float*>(smem);          // [column][lane]
-  if (warp >= 2) {
-    ok = barrier_wait(done, 0);
+  if (warp >= 2 && warp < 6) {
+    if (!barrier_wait(done, 0)) ok = false;
     tmem_fence_after();
 #pragma unroll 1
-    for (uint32_t c = 0; c < COLS; c += 16) {
+    for (uint32_t c = 0; c < COLS && m0 + c < p.m; c += 16) {
       uint32_t r[16];
       tmem_load16(tmem + (group * 32 << 16) + c, r);
       tmem_load_wait();
+      if (p.split > 1) {
 #pragma unroll
-      for (uint32_t j = 0; j < 16; ++j) {
-        const float v = __uint_as_float(r[j]);
-        if (p.split > 1) part[(c + j) * 128 + group * 32 + lane] = v;
-        else if (n < p.n && m0 + c + j < p.m) put<G>(p, m0 + c + j, n, v);
+        for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128 + group * 32 + lane] = __uint_as_float(r[j]);
+      } else if (n < p.n) {
+        G* y = static_cast<G*>(p.y) + (uint64_t)(m0 + c) * p.ldy + n;
+#pragma unroll
+        for (uint32_t j = 0; j < 16; ++j, y += p.ldy)
+          if (m0 + c + j < p.m) put(y, __uint_as_float(r[j]));
       }
     }
   }
   if (!ok) g_wait_failed = 1;
   __syncwarp();
-  if (p.split > 1) {
-    cluster_sync();
-    const uint32_t have = min((uint32_t)COLS, p.m - m0);
-    for (uint32_t e = rank * kThreads + threadIdx.x; e < have * 128; e += p.split * kThreads) {
-      float v = 0.f;
-      for (uint32_t r = 0; r < p.split; ++r) v += peer_float(stage0 + e * 4, r);
-      if (n0 + e % 128 < p.n) put<G>(p, m0 + e / 128, n0 + e % 128, v);
-    }
-    cluster_sync();
-  }
+  if (p.split > 1)
+    join_parts(stage0, p.split, rank, min((uint32_t)COLS, p.m - m0), min(128u, p.n - n0), static_cast<G*>(p.y) + (uint64_t)m0 * p.ldy + n0, p.ldy);
   tmem_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -207,21 +221,27 @@ __global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant_
   }
 }
 
-template <typename G, int COLS>
-cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
-  using S = Shape<COLS>;
+template <typename G, int COLS, typename X>
+cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
+  using S = Shape<COLS, !std::is_void<X>::value>;
   static Device device;
   int sms;
-  cudaError_t e = device.prepare(reinterpret_cast<const void*>(matmul_kernel<G, COLS>), S::kSmem, &sms);
+  cudaError_t e = device.prepare(reinterpret_cast<const void*>(matmul_kernel<G, COLS, X>), S::kSmem, &sms);
   if (e != cudaSuccess) return e;
   Params p = {};
-  const uint64_t nb = (a.cols + 31) / 32;
+  const uint64_t nb = (b.cols + 31) / 32;
   p.lane_scales = static_cast<const uint8_t*>(b.scales);
   p.column_scales = static_cast<const uint8_t*>(a.scales);
+  if (x) {
+    p.x = x->p;
+    p.ldx = x->ld;
+    p.access = sizeof(typename std::conditional<std::is_void<X>::value, float, X>::type) == 2 ? access_of<__nv_bfloat16>(x->p, x->ld) : access_of<float>(x->p, x->ld);
+  }
   p.y = y.p;
   p.ldy = y.ld;
   p.m = (uint32_t)y.rows;
   p.n = (uint32_t)y.cols;
+  p.k = (uint32_t)b.cols;
   p.kt = (uint32_t)((nb + 3) / 4);
   p.lane_tiles = (p.n + 127) / 128;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.m + COLS - 1) / COLS);
@@ -229,13 +249,13 @@ cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t 
   const uint32_t stages = (p.kt + 1) / 2;
   p.split = 1;
   while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && stages >= p.split * 2) p.split *= 2;
-  CUtensorMap lane_map, column_map;
+  CUtensorMap lane_map, column_map = {};
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
-  if (e == cudaSuccess) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
+  if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.split));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(S::kThreads);
   cfg.dynamicSmemBytes = S::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute cluster;
@@ -244,23 +264,48 @@ cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t 
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cfg.attrs = &cluster;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_kernel<G, COLS>, lane_map, column_map, p);
+  return cudaLaunchKernelEx(&cfg, matmul_kernel<G, COLS, X>, lane_map, column_map, p);
 }
 
 template <typename G> cudaError_t by_rows(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
-  if (y.rows <= 16) return launch<G, 16>(a, b, y, stream);
-  if (y.rows <= 32) return launch<G, 32>(a, b, y, stream);
-  if (y.rows <= 64) return launch<G, 64>(a, b, y, stream);
-  if (y.rows <= 128) return launch<G, 128>(a, b, y, stream);
-  return launch<G, 256>(a, b, y, stream);
+  if (y.rows <= 16) return launch<G, 16, void>(a, nullptr, b, y, stream);
+  if (y.rows <= 32) return launch<G, 32, void>(a, nullptr, b, y, stream);
+  if (y.rows <= 64) return launch<G, 64, void>(a, nullptr, b, y, stream);
+  return launch<G, 128, void>(a, nullptr, b, y, stream);
 }
+
+template <typename G, typename X> cudaError_t quantizing(const MatrixIn& x, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
+  return y.rows <= 16 ? launch<G, 16, X>({}, &x, b, y, stream) : launch<G, 32, X>({}, &x, b, y, stream);
+}
+
+cudaError_t nothing(const MatrixOut& y, cudaStream_t stream) {   // a sum over nothing
+  return cudaMemset2DAsync(y.p, y.ld * (y.type == kBF16 ? 2 : 4), 0, y.cols * (y.type == kBF16 ? 2 : 4), y.rows, stream);
+}
+
+constexpr uint64_t kQuantizedInside = 32;   // rows of x up to which the product brings them to MX4 itself
 
 }  // namespace
 
 cudaError_t launch_mx4_matmul(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
-  if (a.cols == 0)   // a sum over nothing
-    return cudaMemset2DAsync(y.p, y.ld * (y.type == kBF16 ? 2 : 4), 0, y.cols * (y.type == kBF16 ? 2 : 4), y.rows, stream);
+  if (a.cols == 0) return nothing(y, stream);
   return y.type == kBF16 ? by_rows<__nv_bfloat16>(a, b, y, stream) : by_rows<float>(a, b, y, stream);
+}
+
+uint64_t mx4_linear_workspace(uint64_t m, uint64_t k) {
+  if (m <= kQuantizedInside) return 0;
+  return m * ((k + 31) / 32) * 16 + 512 + (m + 127) / 128 * ((k + 127) / 128) * 512;
+}
+
+cudaError_t launch_mx4_linear(const MatrixIn& x, const Mx4& b, const MatrixOut& y, void* workspace, cudaStream_t stream) {
+  if (x.cols == 0) return nothing(y, stream);
+  if (x.rows <= kQuantizedInside) {
+    if (y.type == kBF16) return x.type == kBF16 ? quantizing<__nv_bfloat16, __nv_bfloat16>(x, b, y, stream) : quantizing<__nv_bfloat16, float>(x, b, y, stream);
+    return x.type == kBF16 ? quantizing<float, __nv_bfloat16>(x, b, y, stream) : quantizing<float, float>(x, b, y, stream);
+  }
+  uint8_t* codes = static_cast<uint8_t*>(workspace);
+  uint8_t* scales = codes + (x.rows * ((x.cols + 31) / 32) * 16 + 511) / 512 * 512;
+  const cudaError_t e = launch_mx4_quantize(x, false, codes, scales, stream);
+  return e != cudaSuccess ? e : launch_mx4_matmul({codes, scales, x.rows, x.cols}, b, y, stream);
 }
 
 }  // namespace rudra

@@ -4,6 +4,7 @@
 #include <atomic>
 #include <cstdint>
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
@@ -44,6 +45,25 @@ __device__ __forceinline__ void barrier_init_fence() { asm volatile("fence.mbarr
 // A warpgroup's registers per thread, out of those the block was launched with.
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
+
+// -------------------------------------------------------------------------------------- clusters
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Whole warps.  What a thread wrote before it arrives is seen by whoever has waited.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Four floats from another block's shared memory, at what is address `at` here.
+__device__ __forceinline__ float4 peer_load(uint32_t at, uint32_t rank) {
+  uint32_t remote;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+  return v;
+}
 
 // -------------------------------------------------------------------------------------- copies
 
@@ -91,6 +111,41 @@ __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::l
 // 128 rows of four scale bytes (512 bytes in shared memory) to four columns, repeated for the four lane groups.
 __device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
+}
+
+// ------------------------------------------------------------------------------------- results
+
+template <typename G> __device__ __forceinline__ void put(G* to, float v) {
+  if constexpr (sizeof(G) == 2) *to = __float2bfloat16_rn(v);
+  else *to = v;
+}
+
+// The end of a tile whose sum was split over the blocks of a cluster, each of which holds its part as
+// [column][128 lanes] at `part`: this block adds the parts of every split-th column in rank order and writes
+// them as rows of `out`.  `rows` columns and `lanes` lanes exist.  Every thread of every block calls it.
+template <typename G>
+__device__ __forceinline__ void join_parts(uint32_t part, uint32_t split, uint32_t rank, uint32_t rows, uint32_t lanes, G* out, uint64_t ld) {
+  cluster_arrive();
+  cluster_wait();
+  const uint32_t lane = threadIdx.x % 32 * 4, step = blockDim.x / 32 * split;
+  constexpr uint32_t kMost = 8;
+  for (uint32_t c = threadIdx.x / 32 * split + rank; c < rows; c += step) {
+    float4 v[kMost];
+#pragma unroll
+    for (uint32_t r = 0; r < kMost; ++r)
+      if (r < split) v[r] = peer_load(part + c * 512 + lane * 4, r);
+    float4 s = v[0];
+#pragma unroll
+    for (uint32_t r = 1; r < kMost; ++r)
+      if (r < split) s = make_float4(s.x + v[r].x, s.y + v[r].y, s.z + v[r].z, s.w + v[r].w);
+    G* to = out + c * ld + lane;
+    if (lane < lanes) put(to, s.x);
+    if (lane + 1 < lanes) put(to + 1, s.y);
+    if (lane + 2 < lanes) put(to + 2, s.z);
+    if (lane + 3 < lanes) put(to + 3, s.w);
+  }
+  cluster_arrive();      // the parts stay until all have read them
+  cluster_wait();
 }
 
 // --------------------------------------------------------------------------------- descriptors

@@ -193,9 +193,9 @@ def mx4_matmul(a, b, dtype=torch.bfloat16, out=None):
              ptr, kind, ld)
     else:
         need = L.rudra_mx4_linear_workspace(m, k)
-        work = torch.empty(need, dtype=torch.uint8, device=device)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
         _run(L.rudra_mx4_linear, device, (at, out.get_device()), aptr, adtype, lda, m, b.codes_ptr, b.scales_ptr, b.rows, k, ptr, kind,
-             ld, work.data_ptr(), need)
+             ld, work.data_ptr() if need else None, need)
     return out
 
 

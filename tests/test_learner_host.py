@@ -28,7 +28,8 @@ def test_sizes(rows, cols):
     assert L.rudra_mx4_scales_bytes(rows, cols) == -(-rows // 128) * -(-nb // 4) * 512
     assert L.rudra_act8_codes_bytes(rows, cols) == rows * nb * 32
     assert L.rudra_act8_scales_bytes(rows, cols) == rows * nb
-    assert L.rudra_mx4_linear_workspace(rows, cols) >= rows * nb * 16 + -(-rows // 128) * -(-nb // 4) * 512
+    need = L.rudra_mx4_linear_workspace(rows, cols)
+    assert need == 0 if rows <= 32 else need >= rows * nb * 16 + -(-rows // 128) * -(-nb // 4) * 512
 
 
 def test_scale_places_are_distinct_and_fill_the_array():
@@ -70,10 +71,10 @@ def test_product_refusals():
     _refused(m(P, P, 4, P, P, 8, 2**40, P, 1, 8, None), "RUDRA_MAX_DIM")
     assert m(None, None, 0, P, P, 8, 64, None, 0, 8, None) == 0
     lin = rb.lib().rudra_mx4_linear
-    need = rb.lib().rudra_mx4_linear_workspace(4, 64)
-    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, P, need - 1, None), "workspace")
-    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, None, need, None), "workspace")
-    _refused(lin(P, 0, 64, 4, P, P, 8, 64, P, 0, 8, P + 8, need, None), "workspace")
+    need = rb.lib().rudra_mx4_linear_workspace(40, 64)
+    _refused(lin(P, 0, 64, 40, P, P, 8, 64, P, 0, 8, P, need - 1, None), "workspace")
+    _refused(lin(P, 0, 64, 40, P, P, 8, 64, P, 0, 8, None, need, None), "workspace")
+    _refused(lin(P, 0, 64, 40, P, P, 8, 64, P, 0, 8, P + 8, need, None), "workspace")
     _refused(lin(P, 9, 64, 4, P, P, 8, 64, P, 0, 8, P, need, None), "dtype")
     _refused(lin(P, 0, 64, 4, None, P, 8, 64, P, 0, 8, P, need, None), "weights")
 
