@@ -10,7 +10,7 @@ _CSRC = os.path.join(_PKG, "csrc")
 _INCLUDE = os.path.join(os.path.dirname(_PKG), "include")
 LIB_PATH = os.path.join(_PKG, "librudra_ps.so")
 SOURCES = ["ps.cu", "update.cu", "snapshot.cu", "leaf.cu", "noalloc.cu", "sched.cpp",
-           "learner.cu", "mx4.cu", "mx4_matmul.cu", "act8.cu", "act8_weight_grad.cu"]
+           "learner.cu", "mx4.cu", "mx4_matmul.cu", "mx4_matmul_pair.cu", "act8.cu", "act8_weight_grad.cu"]
 # measurement utility of the benchmark, a library of its own: not part of the product interface
 PROBE_LIB_PATH = os.path.join(_PKG, "librudra_probe.so")
 PROBE_SOURCES = ["probe.cu"]

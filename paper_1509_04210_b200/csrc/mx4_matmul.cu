@@ -288,6 +288,7 @@ constexpr uint64_t kQuantizedInside = 32;   // rows of x up to which the product
 
 cudaError_t launch_mx4_matmul(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   if (a.cols == 0) return nothing(y, stream);
+  if (((a.rows + 255) / 256) * ((b.rows + 255) / 256) >= 74) return launch_mx4_matmul_pair(a, b, y, stream);
   return y.type == kBF16 ? by_rows<__nv_bfloat16>(a, b, y, stream) : by_rows<float>(a, b, y, stream);
 }
 

@@ -30,6 +30,17 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
+// The same for a barrier that other blocks of the cluster arrive on.
+__device__ __forceinline__ bool barrier_try_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Arrives on another block's barrier; `remote`: its address in the cluster.
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t remote) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(remote) : "memory");
+}
 // A wait that gives up after about two seconds.  The caller then stops issuing work and the block ends
 // through its ordinary exit; the flag it raises is read by rudra_learner_sync.
 constexpr long long kWaitCycles = 4000000000ll;
@@ -37,6 +48,13 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
   if (barrier_try(bar, parity)) return true;
   const long long begin = clock64();
   while (!barrier_try(bar, parity))
+    if (clock64() - begin > kWaitCycles) return false;
+  return true;
+}
+__device__ __forceinline__ bool barrier_wait_cluster(uint32_t bar, uint32_t parity) {
+  if (barrier_try_cluster(bar, parity)) return true;
+  const long long begin = clock64();
+  while (!barrier_try_cluster(bar, parity))
     if (clock64() - begin > kWaitCycles) return false;
   return true;
 }
@@ -56,12 +74,16 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 // Whole warps.  What a thread wrote before it arrives is seen by whoever has waited.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Where another block of the cluster has what is at `at` here.
+__device__ __forceinline__ uint32_t peer_address(uint32_t at, uint32_t rank) {
+  uint32_t remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
+  return remote;
+}
 // Four floats from another block's shared memory, at what is address `at` here.
 __device__ __forceinline__ float4 peer_load(uint32_t at, uint32_t rank) {
-  uint32_t remote;
   float4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(peer_address(at, rank)) : "memory");
   return v;
 }
 
@@ -81,6 +103,13 @@ __device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_
                :: "r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
 
+// For a pair of blocks that issue their tensor operations together (cta_group::2): a box into this block's shared
+// memory that counts on the barrier at cluster address `bar`, which may be the other's.
+__device__ __forceinline__ void copy_box_pair(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
 // ------------------------------------------------------------------------------- tensor memory
 
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {   // a whole warp; slot: shared address
@@ -90,11 +119,23 @@ __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {   
 __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {    // a whole warp
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(base), "r"(columns));
 }
+// The same by a warp of both blocks of a pair.
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t slot, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(slot), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t base, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(base), "r"(columns));
+}
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Arrives on the barrier once every tcgen05 operation this thread issued has finished.
 __device__ __forceinline__ void tensor_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+// The same on the barrier at this address in both blocks of a pair (ranks 0 and 1 of a cluster of two).
+__device__ __forceinline__ void tensor_commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
 // 16 columns of this warp's 32 lanes: register i is column i.
 __device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
@@ -111,6 +152,9 @@ __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::l
 // 128 rows of four scale bytes (512 bytes in shared memory) to four columns, repeated for the four lane groups.
 __device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void scales_to_tmem_pair(uint32_t at, uint64_t desc) {   // in both blocks of a pair, each from its own
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
 }
 
 // ------------------------------------------------------------------------------------- results

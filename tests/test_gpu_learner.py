@@ -140,7 +140,11 @@ def test_extreme_and_non_finite_blocks(dtype, transpose):
 
 def _product(a, b):
     """(a b^T, the same of magnitudes) in 64 bits."""
-    return a @ b.T, np.abs(a) @ np.abs(b).T
+    if a.shape[0] * b.shape[0] * a.shape[1] < 1e9:
+        return a @ b.T, np.abs(a) @ np.abs(b).T
+    torch = _torch()                                     # the same, sooner
+    a, b = torch.from_numpy(a).cuda(), torch.from_numpy(b).cuda()
+    return (a @ b.t()).cpu().numpy(), (a.abs() @ b.abs().t()).cpu().numpy()
 
 
 def _check_product(got, a, b, bf16):
@@ -151,7 +155,9 @@ def _check_product(got, a, b, bf16):
 # rows of x, outputs, inner length: single rows to several tiles, every kind of ragged edge
 PRODUCTS = [(1, 1, 1), (1, 8, 32), (1, 129, 33), (2, 64, 64), (3, 1000, 65), (8, 200, 257), (16, 128, 512), (17, 130, 500), (33, 31, 4096),
             (64, 384, 640), (65, 257, 96), (100, 1000, 512), (128, 128, 256), (129, 127, 1000), (200, 513, 288), (256, 256, 1024),
-            (300, 260, 2080), (513, 640, 384), (1, 4096, 9216), (5, 1000, 4096)]
+            (300, 260, 2080), (513, 640, 384), (1, 4096, 9216), (5, 1000, 4096),
+            # enough tiles for pairs of blocks: ragged in every direction, one stage and many
+            (2305, 2049, 33), (2310, 2050, 1000), (2560, 2304, 256), (4100, 1300, 130), (1281, 4000, 2200)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
