@@ -60,10 +60,10 @@ __device__ uint32_t g_wait_failed;
 // kind::f16: bf16 x bf16 -> f32, both operands with the reduction across rows, 128 x 256.
 constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (kColumns / 8) << 17 | (kLanes / 16) << 24;
 
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               :: "r"(d), "l"(a), "l"(b), "r"(kInstruction), "r"(add) : "memory");
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(kInstruction), "r"(add), "r"(elected) : "memory");
 }
 
 // Four int8 codes to two pairs of bf16 under a scale (a pair of equal bf16).  With u the byte, its low
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16;
   uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
 
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t warp = warp_index(), lane = threadIdx.x % 32;
   const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
   const uint32_t tile0 = blockIdx.x / p.split, tile_step = gridDim.x / p.split;
   const uint32_t first = (uint32_t)((uint64_t)p.stages * rank / p.split), last = (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
@@ -151,23 +151,25 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       // given up: what is on its way has landed once every copy issued has had its time
       if (!ok)
         for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
-    } else if (warp == 1 && lane == 0) {
-      uint32_t c = 0, q = 0;     // stages and accumulators so far
+    } else if (warp == 1) {
+      const uint32_t elected = elect();
+      uint32_t q = 0, s = 0, parity = 0;     // accumulators so far; stage
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         for (uint32_t i = first; ok && i < last; ++q) {
-          const uint32_t buffer = q & 1, d = tmem + buffer * kColumns, end = min(last, i + p.chain);
-          if (!(ok = barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1))) break;
+          const uint32_t buffer = q & 1, d = tmem + buffer * kColumns, begin = i, end = min(last, i + p.chain);
+          if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
           tmem_fence_after();
-          for (uint32_t begin = i; i < end; ++i, ++c) {
-            const uint32_t s = c % kStages, at = stage0 + s * kStage;
-            if (!(ok = barrier_wait(full + 8 * s, c / kStages & 1))) break;
+          for (; i < end; ++i) {
+            if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
             tmem_fence_after();
+            const uint32_t at = stage0 + s * kStage;
+            const uint64_t x = swizzled_columns(at, kChunk), dy = swizzled_columns(at + kStageX, kChunk);
 #pragma unroll
-            for (uint32_t j = 0; j < kTokens / 16; ++j)
-              multiply(d, swizzled_columns(at + j * 2048, kChunk), swizzled_columns(at + kStageX + j * 2048, kChunk), i != begin || j);
-            tensor_commit(empty + 8 * s);
+            for (uint32_t j = 0; j < kTokens / 16; ++j) multiply(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || j, elected);
+            tensor_commit(empty + 8 * s, elected);
+            if (++s == kStages) s = 0, parity ^= 1;
           }
-          if (ok) tensor_commit(ready + 8 * buffer);
+          if (ok) tensor_commit(ready + 8 * buffer, elected);
         }
       }
     }

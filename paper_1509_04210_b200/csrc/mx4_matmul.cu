@@ -60,10 +60,10 @@ template <int COLS> __device__ constexpr uint32_t instruction() {
   return 1u << 7 | 1u << 10 | (COLS / 8) << 17 | 1u << 23 | 1u << 27;
 }
 
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t sa, uint32_t sb, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-               :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add) : "memory");
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t sa, uint32_t sb, uint32_t add, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %6, 0;\n\tsetp.ne.u32 q, %7, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add), "r"(elected) : "memory");
 }
 
 // X: type of x where it is brought to MX4 here, else void.
@@ -80,7 +80,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
   const uint32_t full = smem_address(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
   uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * S::kStages + 1);
 
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t warp = warp_index(), lane = threadIdx.x % 32;
   const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
   const uint32_t tile = blockIdx.x / p.split;
   const uint32_t n0 = (tile % p.lane_tiles) * 128, m0 = (tile / p.lane_tiles) * COLS;
@@ -126,29 +126,30 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
           barrier_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      for (uint32_t i = first; i < last; ++i) {
-        const uint32_t c = i - first, s = c % S::kStages;
-        if (!(ok = barrier_wait(full + 8 * s, (c / S::kStages) & 1))) break;
-        tmem_fence_after();
-        const uint32_t at = stage0 + s * S::kStage, scales = at + S::kLanes + S::kColumns;
-        const uint32_t ts = tmem + COLS + s * S::kScaleColumns;
-        const uint32_t atoms = min(2u, p.kt - 2 * i);
-        for (uint32_t k = 0; k < atoms; ++k) {
-          const uint32_t tl = ts + k * 8, tc = tl + 4;
-          scales_to_tmem(tl, scale_rows(scales + 512 * k));
-          scales_to_tmem(tc, scale_rows(scales + 1024 + 512 * k));
+    const uint32_t elected = elect();
+    uint32_t s = 0, parity = 0;
+    for (uint32_t i = first; i < last; ++i) {
+      if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
+      tmem_fence_after();
+      const uint32_t at = stage0 + s * S::kStage, ts = tmem + COLS + s * S::kScaleColumns;
+      const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + S::kLanes), scales = scale_rows(at + S::kLanes + S::kColumns);
+      const uint32_t atoms = min(2u, p.kt - 2 * i);
+      // descriptors count in units of 16 bytes
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {   // 64 values: two scale bytes of the four
-            const uint32_t off = (2 * k + h) * 32;
-            multiply(tmem, swizzled_rows(at + off), swizzled_rows(at + S::kLanes + off), instruction<COLS>() | (2 * h) << 29 | (2 * h) << 4,
-                     tl, tc, c || k || h);
-          }
-        }
-        tensor_commit(empty + 8 * s);
+      for (uint32_t k = 0; k < 2; ++k) {
+        if (k == atoms) break;
+        const uint32_t tl = ts + k * 8, tc = tl + 4;
+        scales_to_tmem(tl, scales + 32 * k, elected);
+        scales_to_tmem(tc, scales + (64 + 32 * k), elected);
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h)   // 64 values: two scale bytes of the four
+          multiply(tmem, lanes + (2 * k + h) * 2, columns + (2 * k + h) * 2, instruction<COLS>() | (2 * h) << 29 | (2 * h) << 4, tl, tc,
+                   i != first || k || h, elected);
       }
-      if (ok) tensor_commit(done);
+      tensor_commit(empty + 8 * s, elected);
+      if (++s == S::kStages) s = 0, parity ^= 1;
     }
+    if (ok) tensor_commit(done, elected);
   } else if (kQuantize) {
     // a warp brings every eighth stage's values to MX4, where TMA and the bulk copies would have put them
     using T = typename std::conditional<kQuantize, X, float>::type;

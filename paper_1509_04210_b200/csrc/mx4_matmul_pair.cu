@@ -39,10 +39,10 @@ __device__ uint32_t g_wait_failed;
 // kind::mxf4: E2M1 x E2M1, E8M0 scales, 256 x 256.
 constexpr uint32_t kInstruction = 1u << 7 | 1u << 10 | (kTile / 8) << 17 | 1u << 23 | (kTile / 128) << 27;
 
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t sa, uint32_t sb, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-               "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-               :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add) : "memory");
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t sa, uint32_t sb, uint32_t add, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %6, 0;\n\tsetp.ne.u32 q, %7, 0;\n\t"
+               "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add), "r"(elected) : "memory");
 }
 
 template <typename G>
@@ -57,7 +57,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
   const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 8;
   uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2);
 
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
+  const uint32_t warp = warp_index(), lane = threadIdx.x % 32, rank = cluster_rank();
   const uint32_t tile0 = blockIdx.x / 2, tile_step = gridDim.x / 2, stages = (p.kt + 1) / 2;
 
   if (threadIdx.x == 0) {
@@ -105,32 +105,35 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
         for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait_cluster(full + 8 * (j % kStages), j / kStages & 1);
     }
   } else if (warp == 1) {
-    if (rank == 0 && lane == 0) {
-      uint32_t c = 0, q = 0;
+    if (rank == 0) {
+      const uint32_t elected = elect();
+      uint32_t q = 0, s = 0, parity = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++q) {
-        if (!(ok = barrier_wait_cluster(drained, (q & 1) ^ 1))) break;
+        if (!(ok = all_lanes(barrier_wait_cluster(drained, (q & 1) ^ 1)))) break;
         tmem_fence_after();
-        for (uint32_t i = 0; i < stages; ++i, ++c) {
-          const uint32_t s = c % kStages;
-          if (!(ok = barrier_wait_cluster(full + 8 * s, c / kStages & 1))) break;
+        for (uint32_t i = 0; i < stages; ++i) {
+          if (!(ok = all_lanes(barrier_wait_cluster(full + 8 * s, parity)))) break;
           tmem_fence_after();
-          const uint32_t at = stage0 + s * kStage, scales = at + 2 * kMatrix, ts = tmem + kTile + s * kScaleColumns;
+          const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + s * kScaleColumns;
+          const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + kMatrix), scales = scale_rows(at + 2 * kMatrix);
           const uint32_t atoms = min(2u, p.kt - 2 * i);
-          for (uint32_t k = 0; k < atoms; ++k) {
-            const uint32_t tl = ts + k * 12, tc = tl + 4;
-            scales_to_tmem_pair(tl, scale_rows(scales + 512 * k));
-            scales_to_tmem_pair(tc, scale_rows(scales + kScales + 512 * k));
-            scales_to_tmem_pair(tc + 4, scale_rows(scales + 2 * kScales + 512 * k));
+          // descriptors count in units of 16 bytes
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {   // 64 values: two scale bytes of the four
-              const uint32_t off = (2 * k + h) * 32;
-              multiply(tmem, swizzled_rows(at + off), swizzled_rows(at + kMatrix + off), kInstruction | (2 * h) << 29 | (2 * h) << 4, tl, tc,
-                       i || k || h);
-            }
+          for (uint32_t k = 0; k < 2; ++k) {
+            if (k == atoms) break;
+            const uint32_t tl = ts + k * 12, tc = tl + 4;
+            scales_to_tmem_pair(tl, scales + 32 * k, elected);
+            scales_to_tmem_pair(tc, scales + (kScales / 16 + 32 * k), elected);
+            scales_to_tmem_pair(tc + 4, scales + (2 * kScales / 16 + 32 * k), elected);
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h)   // 64 values: two scale bytes of the four
+              multiply(tmem, lanes + (2 * k + h) * 2, columns + (2 * k + h) * 2, kInstruction | (2 * h) << 29 | (2 * h) << 4, tl, tc, i || k || h,
+                       elected);
           }
-          tensor_commit_pair(empty + 8 * s);
+          tensor_commit_pair(empty + 8 * s, elected);
+          if (++s == kStages) s = 0, parity ^= 1;
         }
-        if (ok) tensor_commit_pair(ready);
+        if (ok) tensor_commit_pair(ready, elected);
       }
     }
   } else if (warp >= 4) {

@@ -110,6 +110,18 @@ __device__ __forceinline__ void copy_box_pair(uint32_t to, const CUtensorMap* m,
                :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
+// One lane of a converged warp.  The warps that issue tensor operations run whole, with this lane's predicate on
+// the operation alone: descriptors and addresses then live in uniform registers, where the operations
+// take them from.  (Issued from a branch of one lane, a stage of the 256 x 256 tile took 1150 cycles.)
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
+// The same to every lane of a warp: the compiler knows that what comes out is uniform.
+__device__ __forceinline__ uint32_t warp_index() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0); }
+__device__ __forceinline__ bool all_lanes(bool ok) { return __all_sync(0xFFFFFFFFu, ok); }
+
 // ------------------------------------------------------------------------------- tensor memory
 
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {   // a whole warp; slot: shared address
@@ -130,12 +142,14 @@ __device__ __forceinline__ void tmem_free_pair(uint32_t base, uint32_t columns) 
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Arrives on the barrier once every tcgen05 operation this thread issued has finished.
-__device__ __forceinline__ void tensor_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+__device__ __forceinline__ void tensor_commit(uint32_t bar, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+               :: "r"(bar), "r"(elected) : "memory");
 }
 // The same on the barrier at this address in both blocks of a pair (ranks 0 and 1 of a cluster of two).
-__device__ __forceinline__ void tensor_commit_pair(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
+__device__ __forceinline__ void tensor_commit_pair(uint32_t bar, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
+               :: "r"(bar), "r"(elected), "h"((uint16_t)3) : "memory");
 }
 // 16 columns of this warp's 32 lanes: register i is column i.
 __device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
@@ -150,11 +164,11 @@ __device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&r)[8]) {
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // 128 rows of four scale bytes (512 bytes in shared memory) to four columns, repeated for the four lane groups.
-__device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
+__device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" :: "r"(at), "l"(desc), "r"(elected) : "memory");
 }
-__device__ __forceinline__ void scales_to_tmem_pair(uint32_t at, uint64_t desc) {   // in both blocks of a pair, each from its own
-  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(at), "l"(desc) : "memory");
+__device__ __forceinline__ void scales_to_tmem_pair(uint32_t at, uint64_t desc, uint32_t elected) {   // in both blocks of a pair, each from its own
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" :: "r"(at), "l"(desc), "r"(elected) : "memory");
 }
 
 // ------------------------------------------------------------------------------------- results
