@@ -92,7 +92,8 @@ int rudra_mx4_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, c
  * by at most 1/127 of the block's largest magnitude, and exact in bf16.
  *
  * codes: int8, rows of 32 * ceil(channels / 32) bytes, codes past channels zero; scales: rows of
- * ceil(channels / 32) bytes.  Both arrays start on 32-byte boundaries.
+ * 16 * ceil(channels / 512) bytes, one for each block and the rest unused.  Both arrays start on
+ * 32-byte boundaries.
  */
 uint64_t rudra_act8_codes_bytes(uint64_t tokens, uint64_t channels);
 uint64_t rudra_act8_scales_bytes(uint64_t tokens, uint64_t channels);

@@ -45,22 +45,23 @@ template <Act A> __device__ __forceinline__ float slope(float x, float& f) {
 struct Saved {
   uint4* codes;
   uint8_t* scales;
+  uint32_t pitch;     // of the scale bytes
 };
 
-template <typename G> __device__ __forceinline__ void save(const Saved& to, uint32_t unit, const Values<G>& x, bool in) {
+template <typename G> __device__ __forceinline__ void save(const Saved& to, uint32_t unit, uint32_t row, uint32_t block, const Values<G>& x, bool in) {
   const uint32_t s = scale_byte(block_max_bits(x.max_bits()), 6);
   const uint4 w = int8_codes(x, s);
   if (!in) return;
   to.codes[unit] = w;
-  if (unit % 2 == 0) to.scales[unit / 2] = (uint8_t)s;
+  if (unit % 2 == 0) to.scales[(uint64_t)row * to.pitch + block] = (uint8_t)s;
 }
 
 struct Restored {
   uint4 w;
   uint32_t s;
-  __device__ __forceinline__ void load(const Saved& from, uint32_t unit) {
+  __device__ __forceinline__ void load(const Saved& from, uint32_t unit, uint32_t row, uint32_t block) {
     w = __ldcs(from.codes + unit);
-    s = __ldg(from.scales + unit / 2);
+    s = __ldg(from.scales + (uint64_t)row * from.pitch + block);
   }
   __device__ __forceinline__ void values(float (&x)[kValues]) const { int8_values(w, scale_value(s), x); }
 };
@@ -78,8 +79,8 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__
   Values<G> a, b;
   a.load(x + at, access_in, have);
   if (A == kSwiglu) b.load(up + at, access_in, have);
-  save(saved, i, a, in);
-  if (A == kSwiglu) save(saved_up, i, b, in);
+  save(saved, i, row, c / 32, a, in);
+  if (A == kSwiglu) save(saved_up, i, row, c / 32, b, in);
   if constexpr (A != kNone) {
     if (!have) return;
     float v[kValues];
@@ -99,8 +100,8 @@ __global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_
   Values<G> g;
   Restored rx, ru;
   if (A != kNone) g.load(dy + row * lddy + c, access_in, have);
-  rx.load(saved, i);
-  if (A == kSwiglu) ru.load(saved_up, i);
+  rx.load(saved, i, row, c / 32);
+  if (A == kSwiglu) ru.load(saved_up, i, row, c / 32);
   float x[kValues], u[kValues];
   rx.values(x);
   if (A == kSwiglu) ru.values(u);
@@ -123,9 +124,12 @@ struct Part {
   Part(uint64_t cols) : per_row((cols + 31) / 32 * 2), most(std::max<uint64_t>(1, 0x70000000ull / per_row)) {}
 };
 
-Saved saved_of(const Act8& a) { return Saved{static_cast<uint4*>(a.codes), static_cast<uint8_t*>(a.scales)}; }
-
-Saved after(const Saved& s, uint64_t units) { return s.codes ? Saved{s.codes + units, s.scales + units / 2} : s; }
+// A checkpoint of `cols` channels from row `r` on.
+Saved from_row(const Act8& a, uint64_t cols, uint64_t r) {
+  const uint64_t pitch = act8_scale_pitch(cols);
+  if (!a.codes) return Saved{nullptr, nullptr, 0};
+  return Saved{static_cast<uint4*>(a.codes) + r * ((cols + 31) / 32 * 2), static_cast<uint8_t*>(a.scales) + r * pitch, (uint32_t)pitch};
+}
 
 template <typename G, Act A>
 cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const Act8& saved, const Act8& saved_up, cudaStream_t stream) {
@@ -137,7 +141,7 @@ cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const
     forward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
         static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
         Divisor((uint32_t)part.per_row), (uint32_t)units, in, access_of<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
-        after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row));
+        from_row(saved, x.cols, r), from_row(saved_up, x.cols, r));
   }
   return cudaGetLastError();
 }
@@ -151,7 +155,7 @@ cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     backward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
         static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
-        access_of<G>(dy.p, dy.ld), out, after(saved_of(saved), r * part.per_row), after(saved_of(saved_up), r * part.per_row),
+        access_of<G>(dy.p, dy.ld), out, from_row(saved, dx.cols, r), from_row(saved_up, dx.cols, r),
         static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
   }
   return cudaGetLastError();

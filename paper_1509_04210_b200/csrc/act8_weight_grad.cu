@@ -2,23 +2,27 @@
 // tensor cores.
 //
 // A code times its block's power of two is a bf16 number exactly, so the checkpoint is expanded to
-// bf16 on its way into shared memory (eight warps, integer and bf16 instructions only) and never exists
+// bf16 between two places in shared memory (eight warps, integer and bf16 instructions only) and never exists
 // wide in memory.  Both operands run along tokens, the reduction, so both sit in shared memory as they
-// sit in global memory, tokens as rows ("transposed" operands for the tensor core): dy arrives by TMA.
-// Inputs of the layer (k) are the 128 lanes of an accumulator, outputs (n) its columns, so a warp
-// writes 32 neighbouring weights whatever the alignment of dw.
+// sit in global memory, tokens as rows ("transposed" operands for the tensor core).  Inputs of the layer
+// (k) are the 128 lanes of an accumulator, outputs (n) its columns, so a warp writes 32 neighbouring
+// weights whatever the alignment of dw.
 //
-// One block per SM walks over its tiles with two accumulators: while one is taken out the other is
-// filled.  With few tiles the tokens are split over the blocks of a cluster, which add their parts in
-// rank order through distributed shared memory.
+// What bounds a large product is shared memory: codes in and out, xhat in, dy in, and both operands read by
+// the tensor core.  Two SMs therefore share a tile of 256 x 256 (each expands 128 inputs and loads
+// 128 outputs' gradients), where there are enough tiles; else a block takes 128 x 128 by itself, and with few
+// of those the tokens are split over the blocks of a cluster, which add their parts in rank order.
+// Codes come by TMA eight warps ahead of their use: the same bytes by ordinary loads cost 100 of 315 us
+// at 8192 x 4096 x 4096, because loads queue behind the tensor core's reads of shared memory.
 //
-// The tensor core truncates where it adds to an accumulator, which costs half a unit in the last place
-// every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken out every
-// kChain stages and the parts are added in registers, rounding to nearest; a bf16 result keeps 16 bits
-// fewer and is taken out once.
+// A block (or pair) walks over its tiles with two accumulators: while one is taken out the other is
+// filled.  The tensor core truncates where it adds to an accumulator, which costs half a unit in the
+// last place every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken
+// out every kChain stages and the parts are added in registers, rounding to nearest (8192 tokens: an error
+// of 1e-7 instead of 1e-5); a bf16 result keeps 16 bits fewer and is taken out once.
 //
-// dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an exact split),
-// and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.
+// dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an
+// exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.
 #include <algorithm>
 
 #include "blocks.cuh"
@@ -28,42 +32,61 @@
 namespace rudra {
 namespace {
 
-constexpr uint32_t kLanes = 128, kColumns = 256, kTokens = 64;      // a tile, and a stage of it
-constexpr uint32_t kStages = 4, kStageX = kLanes * kTokens * 2, kStageDy = kColumns * kTokens * 2, kStage = kStageX + kStageDy;
-// Warpgroups: 0 manages (warp 0 loads dy, warp 1 issues), 1 and 2 take results out, 3 and 4 expand, each
-// every second stage.
+constexpr uint32_t kBlockK = 128, kBlockN = 128, kTokens = 64;      // what a block holds of a stage: inputs, outputs, tokens
+constexpr uint32_t kChunk = 64 * 2 * kTokens;                       // 64 values wide, kTokens rows of 128 bytes
+constexpr uint32_t kStageX = 2 * kChunk, kStage = 4 * kChunk, kStages = 5;
+constexpr uint32_t kCodes = kBlockK * kTokens, kScales = 16 * kTokens, kSlots = 7;   // of the checkpoint; stages of it on their way
+constexpr uint32_t kSmem = 1024 + kStages * kStage + kSlots * (kCodes + kScales) + 256;
+static_assert(kSmem <= 227 * 1024, "does not fit an SM");
+static_assert(kBlockN * 512 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
+// Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out,
+// 3 and 4 expand, each every second stage.
 constexpr uint32_t kThreads = 640;
 constexpr uint32_t kChain = 4;       // stages in one accumulator where the result is f32
 // Registers of a thread by its group, of the 96 each that the block is launched with (640 x 96 in all).
 constexpr int kManageRegisters = 32, kTakeRegisters = 152, kExpandRegisters = 72;
 static_assert(128 * (kManageRegisters + 2 * kTakeRegisters + 2 * kExpandRegisters) <= 640 * 96, "more registers than the block has");
-constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
-constexpr uint32_t kChunk = 64 * 2 * kTokens;                       // 64 values wide, kTokens rows of 128 bytes
-static_assert(kLanes * kColumns * 4 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
+
+// PAIR: two blocks, one tile.
+template <bool PAIR> struct Tile {
+  static constexpr uint32_t kK = PAIR ? 2 * kBlockK : kBlockK, kN = PAIR ? 2 * kBlockN : kBlockN;
+  // kind::f16: bf16 x bf16 -> f32, both operands with the reduction across rows
+  static constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (kN / 8) << 17 | (kK / 16) << 24;
+};
 
 struct Params {
-  const uint8_t* codes;
-  const uint8_t* scales;
   void* dw;
   uint64_t lddw;
-  uint32_t tokens, n, k;
-  uint32_t blocks;          // of 32 values in a row of the checkpoint
+  uint32_t n, k;
   uint32_t token_stages;    // ceil(tokens / kTokens)
   uint32_t stages;          // of the whole reduction: token_stages for each of dy's planes
   uint32_t lane_tiles, tiles;
   uint32_t chain;           // stages in one accumulator
-  uint32_t split;
+  uint32_t split;           // blocks of a cluster that share a tile's tokens
 };
 
 __device__ uint32_t g_wait_failed;
 
-// kind::f16: bf16 x bf16 -> f32, both operands with the reduction across rows, 128 x 256.
-constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (kColumns / 8) << 17 | (kLanes / 16) << 24;
-
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add, uint32_t elected) {
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
-               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               :: "r"(d), "l"(a), "l"(b), "r"(kInstruction), "r"(add), "r"(elected) : "memory");
+template <bool PAIR> __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add, uint32_t elected) {
+  if (PAIR)
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(Tile<PAIR>::kInstruction), "r"(add), "r"(elected) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(Tile<PAIR>::kInstruction), "r"(add), "r"(elected) : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar, uint32_t elected) {
+  if (PAIR) tensor_commit_pair(bar, elected);
+  else tensor_commit(bar, elected);
+}
+template <bool PAIR> __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+  return PAIR ? barrier_wait_cluster(bar, parity) : barrier_wait(bar, parity);
+}
+template <bool PAIR> __device__ __forceinline__ void arrive(uint32_t bar) {   // at the first block's barrier
+  if (PAIR) barrier_arrive_cluster(bar);
+  else barrier_arrive(bar);
 }
 
 // Four int8 codes to two pairs of bf16 under a scale (a pair of equal bf16).  With u the byte, its low
@@ -75,182 +98,198 @@ __device__ __forceinline__ uint32_t scaled(uint32_t bytes, uint32_t scale) {   /
   const __nv_bfloat162 r = __hmul2(d, reinterpret_cast<const __nv_bfloat162&>(scale));
   return reinterpret_cast<const uint32_t&>(r);
 }
-__device__ __forceinline__ uint2 expand4(uint32_t w, uint32_t scale) {
-  return make_uint2(scaled(__byte_perm(w, 0, 0x4140), scale), scaled(__byte_perm(w, 0, 0x4342), scale));
-}
 __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
   const uint32_t h = s == 255u ? 0x7FC0u : s ? s << 7 : 0x0040u;
   return h | h << 16;
 }
 
-struct Unit {   // 32 codes of one token, and their scale
-  uint32_t w[8];
-  uint32_t s;
-};
-__device__ __forceinline__ void fetch(Unit& u, const Params& p, uint32_t token, uint32_t block) {
-  if (token < p.tokens && block < p.blocks) {
-    const uint64_t at = (uint64_t)token * p.blocks + block;
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]), "=r"(u.w[4]), "=r"(u.w[5]), "=r"(u.w[6]), "=r"(u.w[7])
-                 : "l"(p.codes + at * 32));
-    u.s = __ldg(p.scales + at);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) u.w[i] = 0;
-    u.s = 0;
-  }
-}
-
-template <typename G>
-__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ Params p) {
+template <typename G, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
+                   const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
+  using T = Tile<PAIR>;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t stage0 = smem_address(smem);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
-  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
+  const uint32_t stage0 = smem_address(smem), codes0 = stage0 + kStages * kStage, scales0 = codes0 + kSlots * kCodes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage + kSlots * (kCodes + kScales));
+  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
+                 coded = drained + 16, taken = coded + 8 * kSlots;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4 + 2 * kSlots);
 
   const uint32_t warp = warp_index(), lane = threadIdx.x % 32;
-  const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
-  const uint32_t tile0 = blockIdx.x / p.split, tile_step = gridDim.x / p.split;
-  const uint32_t first = (uint32_t)((uint64_t)p.stages * rank / p.split), last = (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
+  const uint32_t rank = PAIR || p.split > 1 ? cluster_rank() : 0;
+  const uint32_t together = PAIR ? 2 : p.split, tile0 = blockIdx.x / together, tile_step = gridDim.x / together;
+  const uint32_t first = PAIR ? 0 : (uint32_t)((uint64_t)p.stages * rank / p.split);
+  const uint32_t last = PAIR ? p.stages : (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
 
   if (threadIdx.x == 0) {
     prefetch_map(&dy_map);
+    prefetch_map(&codes_map);
+    prefetch_map(&scales_map);
     for (uint32_t s = 0; s < kStages; ++s) {
-      barrier_init(full + 8 * s, 1 + 4);
+      barrier_init(full + 8 * s, 1 + (PAIR ? 8 : 4));      // dy, and the four warps of a group of each block
       barrier_init(empty + 8 * s, 1);
     }
     for (uint32_t b = 0; b < 2; ++b) {
       barrier_init(ready + 8 * b, 1);
-      barrier_init(drained + 8 * b, 8);
+      barrier_init(drained + 8 * b, PAIR ? 16 : 8);
+    }
+    for (uint32_t s = 0; s < kSlots; ++s) {
+      barrier_init(coded + 8 * s, 1);
+      barrier_init(taken + 8 * s, 4);
     }
     barrier_init_fence();
   }
-  if (warp == 2) tmem_alloc(smem_address(slot), 2 * kColumns);
+  if (warp == 2) {
+    if (PAIR) tmem_alloc_pair(smem_address(slot), 2 * T::kN);
+    else tmem_alloc(smem_address(slot), 2 * T::kN);
+  }
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
+  if (PAIR) {
+    cluster_arrive();
+    cluster_wait();
+  }
   const uint32_t tmem = *slot;
   bool ok = true;
 
   if (warp < 4) {
     give_registers<kManageRegisters>();
-    if (warp == 0 && lane == 0) {
-      uint32_t c = 0;
+    if (warp == 0) {
+      const uint32_t elected = elect(), first_full = PAIR ? peer_address(full, 0) : full;
+      uint32_t s = 0, parity = 1, issued = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
-        const int n0 = (int)(tile / p.lane_tiles * kColumns);
-        for (uint32_t i = first; i < last; ++i, ++c) {
-          const uint32_t s = c % kStages, bar = full + 8 * s, at = stage0 + s * kStage + kStageX;
-          if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
-          barrier_expect(bar, kStageDy);
+        const int n0 = (int)(tile / p.lane_tiles * T::kN + (PAIR ? rank * kBlockN : 0));
+        for (uint32_t i = first; i < last; ++i, ++issued) {
+          const uint32_t at = stage0 + s * kStage + kStageX;
+          if (!(ok = all_lanes(wait<PAIR>(empty + 8 * s, parity)))) break;
+          if (!PAIR || rank == 0) barrier_expect(full + 8 * s, (PAIR ? 2 : 1) * (kStage - kStageX), elected);
 #pragma unroll
-          for (uint32_t q = 0; q < kColumns / 64; ++q) copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), bar);
+          for (uint32_t q = 0; q < kBlockN / 64; ++q) {
+            if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), first_full + 8 * s, elected);
+            else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), full + 8 * s, elected);
+          }
+          if (++s == kStages) s = 0, parity ^= 1;
         }
       }
       // given up: what is on its way has landed once every copy issued has had its time
+      if (!ok && rank == 0)
+        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) wait<PAIR>(full + 8 * (j % kStages), j / kStages & 1);
+    } else if (warp == 3) {
+      const uint32_t elected = elect();
+      uint32_t s = 0, parity = 1, issued = 0;
+      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
+        const int k0 = (int)(tile % p.lane_tiles * T::kK + (PAIR ? rank * kBlockK : 0));
+        for (uint32_t i = first, t = first % p.token_stages; i < last; ++i, ++issued) {
+          if (!(ok = all_lanes(barrier_wait(taken + 8 * s, parity)))) break;
+          barrier_expect(coded + 8 * s, kCodes + kScales, elected);
+          copy_box(codes0 + s * kCodes, &codes_map, k0, (int)(t * kTokens), coded + 8 * s, elected);
+          copy_box(scales0 + s * kScales, &scales_map, k0 / 512 * 16, (int)(t * kTokens), coded + 8 * s, elected);
+          if (++t == p.token_stages) t = 0;          // dy's next plane meets the same tokens
+          if (++s == kSlots) s = 0, parity ^= 1;
+        }
+      }
       if (!ok)
-        for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
-    } else if (warp == 1) {
+        for (uint32_t j = issued > kSlots ? issued - kSlots : 0; j < issued; ++j) barrier_wait(coded + 8 * (j % kSlots), j / kSlots & 1);
+    } else if (warp == 1 && (!PAIR || rank == 0)) {
       const uint32_t elected = elect();
       uint32_t q = 0, s = 0, parity = 0;     // accumulators so far; stage
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         for (uint32_t i = first; ok && i < last; ++q) {
-          const uint32_t buffer = q & 1, d = tmem + buffer * kColumns, begin = i, end = min(last, i + p.chain);
-          if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
+          const uint32_t buffer = q & 1, d = tmem + buffer * T::kN, begin = i, end = min(last, i + p.chain);
+          if (!(ok = all_lanes(wait<PAIR>(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
           tmem_fence_after();
           for (; i < end; ++i) {
-            if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
+            if (!(ok = all_lanes(wait<PAIR>(full + 8 * s, parity)))) break;
             tmem_fence_after();
             const uint32_t at = stage0 + s * kStage;
             const uint64_t x = swizzled_columns(at, kChunk), dy = swizzled_columns(at + kStageX, kChunk);
 #pragma unroll
-            for (uint32_t j = 0; j < kTokens / 16; ++j) multiply(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || j, elected);
-            tensor_commit(empty + 8 * s, elected);
+            for (uint32_t j = 0; j < kTokens / 16; ++j) multiply<PAIR>(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || j, elected);
+            commit<PAIR>(empty + 8 * s, elected);
             if (++s == kStages) s = 0, parity ^= 1;
           }
-          if (ok) tensor_commit(ready + 8 * buffer, elected);
+          if (ok) commit<PAIR>(ready + 8 * buffer, elected);
         }
       }
     }
   } else if (warp < 12) {
     take_registers<kTakeRegisters>();
-    const uint32_t group = warp % 4, half = (warp - 4) / 4 * 128;   // the lanes a warp may read; its columns
+    constexpr uint32_t kMine = T::kN / 2;
+    const uint32_t group = warp % 4, half = (warp - 4) / 4 * kMine;   // the lanes a warp may read; its columns
     const uint32_t at = tmem + (group * 32 << 16) + half;
-    float* part = reinterpret_cast<float*>(smem) + half * kLanes + group * 32 + lane;   // [column][lane], once the stages are done with
+    const uint32_t first_drained = PAIR ? peer_address(drained, 0) : drained;
+    float* part = reinterpret_cast<float*>(smem) + half * 128 + group * 32 + lane;   // [column][lane], once the stages are done with
     uint32_t q = 0;
     for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
-      const uint32_t k = tile % p.lane_tiles * kLanes + group * 32 + lane, n = tile / p.lane_tiles * kColumns + half;
-      const uint32_t have = n < p.n ? min(128u, p.n - n) : 0;
-      float acc[128];
+      const uint32_t k = tile % p.lane_tiles * T::kK + (PAIR ? rank * kBlockK : 0) + group * 32 + lane, n = tile / p.lane_tiles * T::kN + half;
+      const uint32_t have = n < p.n ? min(kMine, p.n - n) : 0;
+      float acc[kMine];
       for (uint32_t i = first; i < last; i += p.chain, ++q) {
         const uint32_t buffer = q & 1;
-        if (!(ok = barrier_wait(ready + 8 * buffer, q / 2 & 1))) break;
+        if (!(ok = wait<PAIR>(ready + 8 * buffer, q / 2 & 1))) break;
         tmem_fence_after();
 #pragma unroll
-        for (uint32_t c = 0; c < 128; c += 8) {
+        for (uint32_t c = 0; c < kMine; c += 8) {
           uint32_t r[8];
-          tmem_load8(at + buffer * kColumns + c, r);
+          tmem_load8(at + buffer * T::kN + c, r);
           tmem_load_wait();
 #pragma unroll
           for (uint32_t j = 0; j < 8; ++j) acc[c + j] = i == first ? __uint_as_float(r[j]) : acc[c + j] + __uint_as_float(r[j]);
         }
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) barrier_arrive(drained + 8 * buffer);
+        if (lane == 0) arrive<PAIR>(first_drained + 8 * buffer);
       }
-      if (p.split > 1) {
+      if (!PAIR && p.split > 1) {
 #pragma unroll
-        for (uint32_t c = 0; c < 128; ++c) part[c * kLanes] = acc[c];
+        for (uint32_t c = 0; c < kMine; ++c) part[c * 128] = acc[c];
       } else if (k < p.k) {
         G* to = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
-        if (have == 128) {
+        if (have == kMine) {
 #pragma unroll
-          for (uint32_t c = 0; c < 128; ++c, to += p.lddw) put(to, acc[c]);
+          for (uint32_t c = 0; c < kMine; ++c, to += p.lddw) put(to, acc[c]);
         } else {
 #pragma unroll
-          for (uint32_t c = 0; c < 128; ++c, to += p.lddw)
+          for (uint32_t c = 0; c < kMine; ++c, to += p.lddw)
             if (c < have) put(to, acc[c]);
         }
       }
     }
   } else {
     give_registers<kExpandRegisters>();
-    // a thread expands two blocks of 32 values: tokens t and t + 32 of a stage, block b
-    const uint32_t mine = (warp - 12) / 4, t = warp % 4 * 8 + lane % 8, b = lane / 8;
-    const uint32_t to = stage0 + (b / 2) * kChunk + t * 128, x = t % 8, u0 = b % 2 * 4, length = last - first;
-    uint32_t tile = tile0, i = first;       // the next to be fetched
-    auto step = [&](uint32_t by) {
-      for (i += by; i >= last && tile < p.tiles; i -= length) tile += tile_step;
-    };
-    auto next = [&](Unit (&u)[2]) {
-      if (tile < p.tiles) {
-        const uint32_t token = i % p.token_stages * kTokens + t, block = tile % p.lane_tiles * (kLanes / 32) + b;
-        fetch(u[0], p, token, block);
-        fetch(u[1], p, token + 32, block);
-      }
-      step(2);
-    };
-    const uint32_t total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
-    Unit u[2];
-    step(mine);
-    next(u);
+    // a thread expands two blocks of 32 values: tokens t and t + 32 of a stage, block b of the four
+    const uint32_t mine = (warp - 12) / 4, t = warp % 4 * 8 + lane % 8, b = lane / 8, x = t % 8;
+    const uint32_t from = codes0 + t * 128 + ((2 * b) ^ x) * 16, other = ((2 * b) ^ x) % 2 ? 0u - 16 : 16;   // a block's two 16-byte pieces
+    const uint32_t to = stage0 + (b / 2) * kChunk + t * 128, u0 = b % 2 * 4;
+    const uint32_t first_full = PAIR ? peer_address(full, 0) : full;
+    const uint32_t length = last - first, total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
+    uint32_t s = mine, sparity = 0, v = mine, vparity = 0;     // stage and slot, and which turn of theirs
+    uint32_t tile = tile0, i = mine;
     for (uint32_t c = mine; c < total; c += 2) {
-      // expanded in registers, and the next codes on their way, before the stage is free
+      for (; i >= length; i -= length) tile += tile_step;
+      const uint32_t scale_at = scales0 + t * 16 + (tile % p.lane_tiles * (T::kK / 32) + (PAIR ? rank * 4 : 0) + b) % 16;
+      i += 2;
+      if (!(ok = barrier_wait(coded + 8 * v, vparity))) break;
       uint32_t w[2][16];
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h) {
-        const uint32_t scale = scale_pair(u[h].s);
+        uint32_t q[8], e;
+        const uint32_t at = from + v * kCodes + h * 32 * 128;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(at));
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7]) : "r"(at + other));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(scale_at + v * kScales + h * 32 * 16));
+        const uint32_t scale = scale_pair(e);
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j) {
-          const uint2 e = expand4(u[h].w[j], scale);
-          w[h][2 * j] = e.x;
-          w[h][2 * j + 1] = e.y;
+          w[h][2 * j] = scaled(__byte_perm(q[j], 0, 0x4140), scale);
+          w[h][2 * j + 1] = scaled(__byte_perm(q[j], 0, 0x4342), scale);
         }
       }
-      next(u);
-      const uint32_t s = c % kStages;
-      if (!(ok = barrier_wait(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
+      __syncwarp();
+      if (lane == 0) barrier_arrive(taken + 8 * v);
+      if (!(ok = wait<PAIR>(empty + 8 * s, sparity ^ 1))) break;
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
@@ -260,20 +299,27 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                           "r"(w[h][4 * j + 3]) : "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) barrier_arrive(full + 8 * s);
+      if (lane == 0) arrive<PAIR>(first_full + 8 * s);
+      if ((s += 2) >= kStages) s -= kStages, sparity ^= 1;
+      if ((v += 2) >= kSlots) v -= kSlots, vparity ^= 1;
     }
   }
   if (!ok) g_wait_failed = 1;
   __syncwarp();
-  if (p.split > 1) {   // one tile to a cluster
-    const uint32_t k0 = tile0 % p.lane_tiles * kLanes, n0 = tile0 / p.lane_tiles * kColumns;
-    join_parts(stage0, p.split, rank, min(kColumns, p.n - n0), min(kLanes, p.k - k0), static_cast<G*>(p.dw) + (uint64_t)n0 * p.lddw + k0, p.lddw);
+  if (!PAIR && p.split > 1) {   // one tile to a cluster
+    const uint32_t k0 = tile0 % p.lane_tiles * kBlockK, n0 = tile0 / p.lane_tiles * kBlockN;
+    join_parts(stage0, p.split, rank, min(kBlockN, p.n - n0), min(kBlockK, p.k - k0), static_cast<G*>(p.dw) + (uint64_t)n0 * p.lddw + k0, p.lddw);
   }
   tmem_fence_before();
   __syncthreads();
+  if (PAIR) {      // neither block ends while the other may still use its memory
+    cluster_arrive();
+    cluster_wait();
+  }
   if (warp == 2) {
     tmem_fence_after();
-    tmem_free(tmem, 2 * kColumns);
+    if (PAIR) tmem_free_pair(tmem, 2 * T::kN);
+    else tmem_free(tmem, 2 * T::kN);
   }
 }
 
@@ -321,28 +367,34 @@ bool readable(const MatrixIn& dy) {
   return dy.type == kBF16 && reinterpret_cast<uintptr_t>(dy.p) % 16 == 0 && (dy.ld % 8 == 0 || dy.rows <= 1) && dy.ld < (1ull << 32);
 }
 
-template <typename G>
-cudaError_t launch(const CUtensorMap& map, Params& p, cudaStream_t stream) {
+template <typename G, bool PAIR>
+cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
+  using T = Tile<PAIR>;
   static Device device;
   int sms;
-  const cudaError_t e = device.prepare(reinterpret_cast<const void*>(weight_grad_kernel<G>), kSmem, &sms);
+  const cudaError_t e = device.prepare(reinterpret_cast<const void*>(weight_grad_kernel<G, PAIR>), kSmem, &sms);
   if (e != cudaSuccess) return e;
   p.chain = sizeof(G) == 4 ? kChain : p.stages;
+  p.lane_tiles = (p.k + T::kK - 1) / T::kK;
+  const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
+  if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
+  p.tiles = (uint32_t)tiles;
   p.split = 1;
-  while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
-  const unsigned grid = p.split > 1 ? p.tiles * p.split : std::min<unsigned>(p.tiles, (unsigned)sms);
+  if (!PAIR)
+    while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
+  const uint32_t together = PAIR ? 2 : p.split;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = dim3(p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)sms / together) * together);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute cluster;
   cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = p.split;
+  cluster.val.clusterDim.x = together;
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cfg.attrs = &cluster;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, weight_grad_kernel<G>, map, p);
+  return cudaLaunchKernelEx(&cfg, weight_grad_kernel<G, PAIR>, dy, codes, scales, p);
 }
 
 }  // namespace
@@ -375,25 +427,23 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  CUtensorMap map;
-  cudaError_t e = encode_rows(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, from, dy.cols, planes * rows, pitch * 2, kTokens);
+  const uint64_t nb = (dw.cols + 31) / 32, scale_pitch = act8_scale_pitch(dw.cols);
+  CUtensorMap dy_map, codes_map, scales_map;
+  cudaError_t e = encode_rows(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, from, dy.cols, planes * rows, pitch * 2, kTokens);
+  if (e == cudaSuccess) e = encode_rows(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, saved.codes, nb * 32, dy.rows, nb * 32, kTokens);
+  if (e == cudaSuccess) e = encode_plain(&scales_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, saved.scales, scale_pitch, dy.rows, scale_pitch, 16, kTokens);
   if (e != cudaSuccess) return e;
   Params p = {};
-  p.codes = static_cast<const uint8_t*>(saved.codes);
-  p.scales = static_cast<const uint8_t*>(saved.scales);
   p.dw = dw.p;
   p.lddw = dw.ld;
-  p.tokens = (uint32_t)dy.rows;
   p.n = (uint32_t)dw.rows;
   p.k = (uint32_t)dw.cols;
-  p.blocks = (p.k + 31) / 32;
-  p.token_stages = (p.tokens + kTokens - 1) / kTokens;
+  p.token_stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
   p.stages = p.token_stages * (uint32_t)planes;
-  p.lane_tiles = (p.k + kLanes - 1) / kLanes;
-  const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + kColumns - 1) / kColumns);
-  if (tiles > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-  p.tiles = (uint32_t)tiles;
-  return dw.type == kBF16 ? launch<__nv_bfloat16>(map, p, stream) : launch<float>(map, p, stream);
+  const bool pair = ((dw.rows + 255) / 256) * ((dw.cols + 255) / 256) >= 74;
+  if (dw.type == kBF16)
+    return pair ? launch<__nv_bfloat16, true>(dy_map, codes_map, scales_map, p, stream) : launch<__nv_bfloat16, false>(dy_map, codes_map, scales_map, p, stream);
+  return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);
 }
 
 }  // namespace rudra

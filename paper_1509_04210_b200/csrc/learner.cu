@@ -105,7 +105,7 @@ int rudra_mx4_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, c
 }
 
 uint64_t rudra_act8_codes_bytes(uint64_t tokens, uint64_t channels) { return tokens * blocks_of(channels) * 32; }
-uint64_t rudra_act8_scales_bytes(uint64_t tokens, uint64_t channels) { return tokens * blocks_of(channels); }
+uint64_t rudra_act8_scales_bytes(uint64_t tokens, uint64_t channels) { return tokens * rudra::act8_scale_pitch(channels); }
 
 int rudra_act8_forward(int act, const void* x_dev, const void* up_dev, int dtype, uint64_t tokens, uint64_t channels, uint64_t ldx,
                        void* y_dev, uint64_t ldy, void* codes_dev, void* scales_dev, void* up_codes_dev, void* up_scales_dev,

@@ -26,11 +26,13 @@ struct Mx4 {
   const void* scales;
   uint64_t rows, cols;
 };
-// A checkpoint: rows of 32 * ceil(cols / 32) int8 codes, rows of ceil(cols / 32) scale bytes.
+// A checkpoint: rows of 32 * ceil(cols / 32) int8 codes, rows of act8_scale_pitch(cols) scale bytes.
 struct Act8 {
   void* codes;
   void* scales;
 };
+// Whole 16-byte pieces, which TMA can read.
+inline uint64_t act8_scale_pitch(uint64_t cols) { return (cols + 511) / 512 * 16; }
 
 enum Act : int { kNone = 0, kRelu = 1, kSilu = 2, kGelu = 3, kSwiglu = 4 };   // RUDRA_ACT_*
 

@@ -105,26 +105,25 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
   bool ok = true;
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t issued = 0;
-      for (uint32_t i = first; i < last; ++i, ++issued) {
-        const uint32_t s = issued % S::kStages, round = issued / S::kStages;
-        if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1))) break;
-        const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s, scales = at + S::kLanes + S::kColumns;
-        const uint32_t atoms = min(2u, p.kt - 2 * i);
-        barrier_expect(bar, S::kLanes + atoms * 512 + (kQuantize ? 0 : S::kColumns + atoms * 512));
-        copy_box(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar);
-        copy_bulk(scales, p.lane_scales + ((uint64_t)(n0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar);
-        if (!kQuantize) {
-          copy_box(at + S::kLanes, &column_map, (int)(i * kStageBytes), (int)m0, bar);
-          copy_bulk(scales + 1024, p.column_scales + ((uint64_t)(m0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar);
-        }
+    const uint32_t elected = elect();
+    uint32_t s = 0, parity = 1, issued = 0;
+    for (uint32_t i = first; i < last; ++i, ++issued) {
+      if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
+      const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s, scales = at + S::kLanes + S::kColumns;
+      const uint32_t atoms = min(2u, p.kt - 2 * i);
+      barrier_expect(bar, S::kLanes + atoms * 512 + (kQuantize ? 0 : S::kColumns + atoms * 512), elected);
+      copy_box(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
+      copy_bulk(scales, p.lane_scales + ((uint64_t)(n0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar, elected);
+      if (!kQuantize) {
+        copy_box(at + S::kLanes, &column_map, (int)(i * kStageBytes), (int)m0, bar, elected);
+        copy_bulk(scales + 1024, p.column_scales + ((uint64_t)(m0 / 128) * p.kt + 2 * i) * 512, atoms * 512, bar, elected);
       }
-      // given up: what is on its way lands before the block may end
-      if (!ok)
-        for (uint32_t k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
-          barrier_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1);
+      if (++s == S::kStages) s = 0, parity ^= 1;
     }
+    // given up: what is on its way lands before the block may end
+    if (!ok)
+      for (uint32_t k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
+        barrier_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1);
   } else if (warp == 1) {
     const uint32_t elected = elect();
     uint32_t s = 0, parity = 0;

@@ -83,27 +83,28 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
   bool ok = true;
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint32_t first_full = peer_address(full, 0);
-      uint32_t c = 0;
-      for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
-        const uint32_t n0 = tile % p.lane_tiles * kTile + rank * kRows, m0 = tile / p.lane_tiles * kTile;
-        for (uint32_t i = 0; i < stages; ++i, ++c) {
-          const uint32_t s = c % kStages, at = stage0 + s * kStage, bar = first_full + 8 * s;
-          if (!(ok = barrier_wait_cluster(empty + 8 * s, (c / kStages & 1) ^ 1))) break;
-          if (rank == 0) barrier_expect(full + 8 * s, 2 * kStage);
-          copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar);
-          copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar);
-          // atoms past a row's last one are read from elsewhere, or as zero, and not used
-          copy_box_pair(at + 2 * kMatrix, &lane_scales, 0, (int)(n0 / 128 * p.kt + 2 * i), bar);
-          copy_box_pair(at + 2 * kMatrix + kScales, &column_scales, 0, (int)(m0 / 128 * p.kt + 2 * i), bar);
-          copy_box_pair(at + 2 * kMatrix + 2 * kScales, &column_scales, 0, (int)((m0 / 128 + 1) * p.kt + 2 * i), bar);
-        }
+    const uint32_t elected = elect(), first_full = peer_address(full, 0);
+    uint32_t s = 0, parity = 1, issued = 0;
+    for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
+      const uint32_t n0 = tile % p.lane_tiles * kTile + rank * kRows, m0 = tile / p.lane_tiles * kTile;
+      const uint32_t lane_atom = n0 / 128 * p.kt, column_atom = m0 / 128 * p.kt;
+      for (uint32_t i = 0; i < stages; ++i) {
+        const uint32_t at = stage0 + s * kStage, bar = first_full + 8 * s;
+        if (!(ok = all_lanes(barrier_wait_cluster(empty + 8 * s, parity)))) break;
+        if (rank == 0) barrier_expect(full + 8 * s, 2 * kStage, elected);
+        copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
+        copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
+        // atoms past a row's last one are read from elsewhere, or as zero, and not used
+        copy_box_pair(at + 2 * kMatrix, &lane_scales, 0, (int)(lane_atom + 2 * i), bar, elected);
+        copy_box_pair(at + 2 * kMatrix + kScales, &column_scales, 0, (int)(column_atom + 2 * i), bar, elected);
+        copy_box_pair(at + 2 * kMatrix + 2 * kScales, &column_scales, 0, (int)(column_atom + p.kt + 2 * i), bar, elected);
+        ++issued;
+        if (++s == kStages) s = 0, parity ^= 1;
       }
-      // given up: what is on its way lands before the blocks may end
-      if (!ok && rank == 0)
-        for (uint32_t j = c > kStages ? c - kStages : 0; j < c; ++j) barrier_wait_cluster(full + 8 * (j % kStages), j / kStages & 1);
     }
+    // given up: what is on its way lands before the blocks may end
+    if (!ok && rank == 0)
+      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait_cluster(full + 8 * (j % kStages), j / kStages & 1);
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t elected = elect();
@@ -177,17 +178,6 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
   }
 }
 
-// An MX4 matrix's scale bytes, 512 to a row, read two rows at a time.
-cudaError_t encode_scales(CUtensorMap* map, const void* p, uint64_t atoms) {
-  const PFN_cuTensorMapEncodeTiled fn = map_encoder();
-  if (!fn) return cudaErrorNotSupported;
-  const cuuint64_t dims[2] = {128, atoms}, strides[1] = {512};
-  const cuuint32_t box[2] = {128, 2}, steps[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess
-                                                                                                                              : cudaErrorInvalidValue;
-}
-
 template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   static Device device;
   int sms;
@@ -200,8 +190,9 @@ template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const Matri
   CUtensorMap lane_map, column_map, lane_scales, column_scales;
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, kRows);
   if (e == cudaSuccess) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, kRows);
-  if (e == cudaSuccess) e = encode_scales(&lane_scales, b.scales, b_atoms);
-  if (e == cudaSuccess) e = encode_scales(&column_scales, a.scales, a_atoms);
+  // scale bytes by whole atoms of 512, two at a time
+  if (e == cudaSuccess) e = encode_plain(&lane_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, b.scales, 128, b_atoms, 512, 128, 2);
+  if (e == cudaSuccess) e = encode_plain(&column_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, a.scales, 128, a_atoms, 512, 128, 2);
   if (e != cudaSuccess) return e;
   const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)sms / 2);

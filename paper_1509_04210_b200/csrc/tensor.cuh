@@ -11,6 +11,20 @@
 namespace rudra {
 namespace {
 
+// ---------------------------------------------------------------------------------------- warps
+
+// One lane of a converged warp.  The warps that issue copies and tensor operations run whole, with this lane's
+// predicate on the operation alone: descriptors and addresses then live in uniform registers, where the operations
+// take them from.  (Issued from a branch of one lane, a stage of the 256 x 256 tile took 1150 cycles.)
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
+// The same to every lane of a warp: the compiler knows that what comes out is uniform.
+__device__ __forceinline__ uint32_t warp_index() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0); }
+__device__ __forceinline__ bool all_lanes(bool ok) { return __all_sync(0xFFFFFFFFu, ok); }
+
 // ------------------------------------------------------------------------------------ barriers
 
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -18,8 +32,8 @@ __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
 }
-__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" :: "r"(bar), "r"(bytes), "r"(elected) : "memory");
 }
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
@@ -93,34 +107,25 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" :: "l"(m) : "memory");
 }
 // One box; x in elements of the map's type and a multiple of 16 bytes.
-__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar) : "memory");
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+               "@q cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar), "r"(elected) : "memory");
 }
 // `bytes` (a multiple of 16) from a 16-byte boundary.
-__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               :: "r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint32_t bar, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %4, 0;\n\t"
+               "@q cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+               :: "r"(to), "l"(from), "r"(bytes), "r"(bar), "r"(elected) : "memory");
 }
 
 // For a pair of blocks that issue their tensor operations together (cta_group::2): a box into this block's shared
 // memory that counts on the barrier at cluster address `bar`, which may be the other's.
-__device__ __forceinline__ void copy_box_pair(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar) : "memory");
+__device__ __forceinline__ void copy_box_pair(uint32_t to, const CUtensorMap* m, int x, int y, uint32_t bar, uint32_t elected) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+               "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+               :: "r"(to), "l"(m), "r"(x), "r"(y), "r"(bar), "r"(elected) : "memory");
 }
-
-// One lane of a converged warp.  The warps that issue tensor operations run whole, with this lane's predicate on
-// the operation alone: descriptors and addresses then live in uniform registers, where the operations
-// take them from.  (Issued from a branch of one lane, a stage of the 256 x 256 tile took 1150 cycles.)
-__device__ __forceinline__ uint32_t elect() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-  return p;
-}
-// The same to every lane of a warp: the compiler knows that what comes out is uniform.
-__device__ __forceinline__ uint32_t warp_index() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0); }
-__device__ __forceinline__ bool all_lanes(bool ok) { return __all_sync(0xFFFFFFFFu, ok); }
 
 // ------------------------------------------------------------------------------- tensor memory
 
@@ -261,8 +266,18 @@ class Device {
   std::atomic<int> sms_[kMost] = {};
 };
 
-// A row-major matrix, read in 128-byte wide boxes of `box_rows` rows with the 128-byte swizzle; what
-// lies outside reads as zero.
+// A row-major matrix, read in boxes as it lies; what lies outside reads as zero.
+inline cudaError_t encode_plain(CUtensorMap* map, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
+                                uint32_t box_cols, uint32_t box_rows) {
+  const PFN_cuTensorMapEncodeTiled fn = map_encoder();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {box_cols, box_rows}, steps[2] = {1, 1};
+  return fn(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// The same in 128-byte wide boxes with the 128-byte swizzle.
 inline cudaError_t encode_rows(CUtensorMap* map, CUtensorMapDataType type, uint32_t element, const void* p, uint64_t cols, uint64_t rows,
                                uint64_t pitch_bytes, uint32_t box_rows) {
   const PFN_cuTensorMapEncodeTiled fn = map_encoder();

@@ -94,7 +94,7 @@ class Act8(_Blocks):
     @staticmethod
     def _sizes(rows, cols):
         nb = (cols + 31) // 32
-        return rows * nb * 32, rows * nb
+        return rows * nb * 32, rows * ((nb + 15) // 16 * 16)
 
     @property
     def codes(self):
@@ -105,7 +105,7 @@ class Act8(_Blocks):
     @property
     def scales(self):
         if self._scales is None:
-            self._scales = self._buf[self._split:].view(self.rows, (self.cols + 31) // 32)
+            self._scales = self._buf[self._split:].view(self.rows, (self.cols + 511) // 512 * 16)
         return self._scales
 
 

@@ -133,7 +133,7 @@ def test_extreme_and_non_finite_blocks(dtype, transpose):
     if not transpose:
         saved = L.act8_save(v)
         codes, s = ref.act8(held)
-        np.testing.assert_array_equal(saved.scales.cpu().numpy(), s)
+        np.testing.assert_array_equal(saved.scales.cpu().numpy()[:, :s.shape[1]], s)
         np.testing.assert_array_equal(saved.codes.cpu().numpy(), codes)
         np.testing.assert_array_equal(_np(L.act8_values(saved, _torch().float32)), ref.act8_values(held))
 
@@ -255,7 +255,7 @@ def test_activation_and_checkpoint(act, rows, cols, dtype, pad, shift):
         got = s.codes.cpu().numpy()
         np.testing.assert_array_equal(got[:, :cols], codes)
         assert not got[:, cols:].any()
-        np.testing.assert_array_equal(s.scales.cpu().numpy(), scale)
+        np.testing.assert_array_equal(s.scales.cpu().numpy()[:, :scale.shape[1]], scale)
         np.testing.assert_array_equal(_np(L.act8_values(s, torch.bfloat16)), ref.act8_values(h))
     xq, uq = ref.act8_values(xh), ref.act8_values(uh)
     d = ref.slope(act, xq)
@@ -327,7 +327,9 @@ def test_empty_activations(shape):
 
 # tokens, outputs, inputs
 GRADS = [(1, 1, 1), (1, 40, 33), (2, 8, 31), (7, 130, 64), (31, 64, 100), (64, 128, 256), (65, 127, 257), (100, 1000, 96), (128, 129, 512),
-         (300, 260, 1000), (509, 72, 640), (1000, 384, 130), (2048, 136, 264), (4100, 33, 40)]
+         (300, 260, 1000), (509, 72, 640), (1000, 384, 130), (2048, 136, 264), (4100, 33, 40),
+         # enough tiles for pairs of blocks
+         (1, 2304, 2305), (65, 2050, 2400), (321, 1290, 4000), (600, 4097, 1281)]
 
 
 @pytest.mark.parametrize("t,n,k", GRADS)
@@ -341,7 +343,7 @@ def test_weight_gradient_against_the_definition(t, n, k, dtype, pad, shift, out)
     kind = torch.float32 if out == "f32" else torch.bfloat16
     got = L.act8_weight_grad(dy, saved, kind)
     g, xq = dyh.astype(np.float64), ref.act8_values(xh)
-    want, size = g.T @ xq, np.abs(g).T @ np.abs(xq)
+    want, size = _product(np.ascontiguousarray(g.T), np.ascontiguousarray(xq.T))
     _close(_np(got), want, max(t, 8) * EPS * size + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0.0))
     # the same, written into a flat vector that is to be pushed, at an odd place, with canaries around it
     flat = torch.full((n * k + 20,), 7.0, dtype=kind, device="cuda")

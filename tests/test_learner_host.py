@@ -27,7 +27,7 @@ def test_sizes(rows, cols):
     assert L.rudra_mx4_codes_bytes(rows, cols) == rows * nb * 16
     assert L.rudra_mx4_scales_bytes(rows, cols) == -(-rows // 128) * -(-nb // 4) * 512
     assert L.rudra_act8_codes_bytes(rows, cols) == rows * nb * 32
-    assert L.rudra_act8_scales_bytes(rows, cols) == rows * nb
+    assert L.rudra_act8_scales_bytes(rows, cols) == rows * (-(-nb // 16) * 16)
     need = L.rudra_mx4_linear_workspace(rows, cols)
     assert need == 0 if rows <= 32 else need >= rows * nb * 16 + -(-rows // 128) * -(-nb // 4) * 512
 
