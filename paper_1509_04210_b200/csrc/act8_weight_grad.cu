@@ -81,9 +81,6 @@ template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar, uint32
   if (PAIR) tensor_commit_pair(bar, elected);
   else tensor_commit(bar, elected);
 }
-template <bool PAIR> __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
-  return PAIR ? barrier_wait_cluster(bar, parity) : barrier_wait(bar, parity);
-}
 template <bool PAIR> __device__ __forceinline__ void arrive(uint32_t bar) {   // at the first block's barrier
   if (PAIR) barrier_arrive_cluster(bar);
   else barrier_arrive(bar);
@@ -163,7 +160,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         const int n0 = (int)(tile / p.lane_tiles * T::kN + (PAIR ? rank * kBlockN : 0));
         for (uint32_t i = first; i < last; ++i, ++issued) {
           const uint32_t at = stage0 + s * kStage + kStageX;
-          if (!(ok = all_lanes(wait<PAIR>(empty + 8 * s, parity)))) break;
+          if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
           if (!PAIR || rank == 0) barrier_expect(full + 8 * s, (PAIR ? 2 : 1) * (kStage - kStageX), elected);
 #pragma unroll
           for (uint32_t q = 0; q < kBlockN / 64; ++q) {
@@ -175,7 +172,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       }
       // given up: what is on its way has landed once every copy issued has had its time
       if (!ok && rank == 0)
-        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) wait<PAIR>(full + 8 * (j % kStages), j / kStages & 1);
+        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
     } else if (warp == 3) {
       const uint32_t elected = elect();
       uint32_t s = 0, parity = 1, issued = 0;
@@ -198,10 +195,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         for (uint32_t i = first; ok && i < last; ++q) {
           const uint32_t buffer = q & 1, d = tmem + buffer * T::kN, begin = i, end = min(last, i + p.chain);
-          if (!(ok = all_lanes(wait<PAIR>(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
+          if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
           tmem_fence_after();
           for (; i < end; ++i) {
-            if (!(ok = all_lanes(wait<PAIR>(full + 8 * s, parity)))) break;
+            if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
             tmem_fence_after();
             const uint32_t at = stage0 + s * kStage;
             const uint64_t x = swizzled_columns(at, kChunk), dy = swizzled_columns(at + kStageX, kChunk);
@@ -228,7 +225,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       float acc[kMine];
       for (uint32_t i = first; i < last; i += p.chain, ++q) {
         const uint32_t buffer = q & 1;
-        if (!(ok = wait<PAIR>(ready + 8 * buffer, q / 2 & 1))) break;
+        if (!(ok = barrier_wait(ready + 8 * buffer, q / 2 & 1))) break;
         tmem_fence_after();
 #pragma unroll
         for (uint32_t c = 0; c < kMine; c += 8) {
@@ -289,7 +286,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       }
       __syncwarp();
       if (lane == 0) barrier_arrive(taken + 8 * v);
-      if (!(ok = wait<PAIR>(empty + 8 * s, sparity ^ 1))) break;
+      if (!(ok = barrier_wait(empty + 8 * s, sparity ^ 1))) break;
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll

@@ -90,7 +90,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
       const uint32_t lane_atom = n0 / 128 * p.kt, column_atom = m0 / 128 * p.kt;
       for (uint32_t i = 0; i < stages; ++i) {
         const uint32_t at = stage0 + s * kStage, bar = first_full + 8 * s;
-        if (!(ok = all_lanes(barrier_wait_cluster(empty + 8 * s, parity)))) break;
+        if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
         if (rank == 0) barrier_expect(full + 8 * s, 2 * kStage, elected);
         copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
         copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
@@ -104,16 +104,16 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
     }
     // given up: what is on its way lands before the blocks may end
     if (!ok && rank == 0)
-      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait_cluster(full + 8 * (j % kStages), j / kStages & 1);
+      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t elected = elect();
       uint32_t q = 0, s = 0, parity = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++q) {
-        if (!(ok = all_lanes(barrier_wait_cluster(drained, (q & 1) ^ 1)))) break;
+        if (!(ok = all_lanes(barrier_wait(drained, (q & 1) ^ 1)))) break;
         tmem_fence_after();
         for (uint32_t i = 0; i < stages; ++i) {
-          if (!(ok = all_lanes(barrier_wait_cluster(full + 8 * s, parity)))) break;
+          if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
           tmem_fence_after();
           const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + s * kScaleColumns;
           const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + kMatrix), scales = scale_rows(at + 2 * kMatrix);
@@ -144,7 +144,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
     for (uint32_t tile = tile0; tile < p.tiles; tile += tile_step, ++q) {
       const uint32_t n = tile % p.lane_tiles * kTile + rank * kRows + group * 32 + lane, m = tile / p.lane_tiles * kTile + half;
       const uint32_t have = m < p.m ? min(128u, p.m - m) : 0;
-      if (!(ok = barrier_wait_cluster(ready, q & 1))) break;
+      if (!(ok = barrier_wait(ready, q & 1))) break;
       tmem_fence_after();
       uint32_t r[8][16];
 #pragma unroll
