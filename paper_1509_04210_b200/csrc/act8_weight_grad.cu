@@ -39,13 +39,17 @@ constexpr uint32_t kCodes = kBlockK * kTokens, kScales = 16 * kTokens, kSlots = 
 constexpr uint32_t kSmem = 1024 + kStages * kStage + kSlots * (kCodes + kScales) + 256;
 static_assert(kSmem <= 227 * 1024, "does not fit an SM");
 static_assert(kBlockN * 512 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
-// Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out,
-// 3 and 4 expand, each every second stage.
-constexpr uint32_t kThreads = 640;
 constexpr uint32_t kChain = 4;       // stages in one accumulator where the result is f32
-// Registers of a thread by its group, of the 96 each that the block is launched with (640 x 96 in all).
-constexpr int kManageRegisters = 32, kTakeRegisters = 152, kExpandRegisters = 72;
-static_assert(128 * (kManageRegisters + 2 * kTakeRegisters + 2 * kExpandRegisters) <= 640 * 96, "more registers than the block has");
+
+// Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out, the
+// others expand, each every third or fourth stage; and the registers of a thread by its group, of those
+// that the block is launched with.  An f32 result is gathered in up to 128 registers of a thread.
+template <typename G> struct Groups {
+  static constexpr uint32_t kExpanders = sizeof(G) == 4 ? 3 : 4, kThreads = 128 * (3 + kExpanders);
+  static constexpr int kLaunch = sizeof(G) == 4 ? 80 : 72, kManage = sizeof(G) == 4 ? 40 : 56, kTake = sizeof(G) == 4 ? 144 : 72, kExpand = sizeof(G) == 4 ? 48 : 72;
+  static_assert(kManage + 2 * kTake + kExpanders * kExpand <= (3 + kExpanders) * kLaunch && kThreads * kLaunch <= 65536,
+                "more registers than the block has");
+};
 
 // PAIR: two blocks, one tile.
 template <bool PAIR> struct Tile {
@@ -101,10 +105,12 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 }
 
 template <typename G, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Groups<G>::kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
                    const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
   using T = Tile<PAIR>;
+  using R = Groups<G>;
+  constexpr uint32_t kExpanders = R::kExpanders;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage0 = smem_address(smem), codes0 = stage0 + kStages * kStage, scales0 = codes0 + kSlots * kCodes;
@@ -152,7 +158,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   bool ok = true;
 
   if (warp < 4) {
-    give_registers<kManageRegisters>();
+    give_registers<R::kManage>();
     if (warp == 0) {
       const uint32_t elected = elect(), first_full = PAIR ? peer_address(full, 0) : full;
       uint32_t s = 0, parity = 1, issued = 0;
@@ -212,7 +218,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       }
     }
   } else if (warp < 12) {
-    take_registers<kTakeRegisters>();
+    if (R::kTake > R::kLaunch) take_registers<R::kTake>();
     constexpr uint32_t kMine = T::kN / 2;
     const uint32_t group = warp % 4, half = (warp - 4) / 4 * kMine;   // the lanes a warp may read; its columns
     const uint32_t at = tmem + (group * 32 << 16) + half;
@@ -222,32 +228,57 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
       const uint32_t k = tile % p.lane_tiles * T::kK + (PAIR ? rank * kBlockK : 0) + group * 32 + lane, n = tile / p.lane_tiles * T::kN + half;
       const uint32_t have = n < p.n ? min(kMine, p.n - n) : 0;
-      float acc[kMine];
-      for (uint32_t i = first; i < last; i += p.chain, ++q) {
-        const uint32_t buffer = q & 1;
-        if (!(ok = barrier_wait(ready + 8 * buffer, q / 2 & 1))) break;
+      G* to = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
+      const bool mine = k < p.k;
+      if (last - first <= p.chain) {       // one accumulator: straight out
+        const uint32_t buffer = q++ & 1;
+        if (!(ok = barrier_wait(ready + 8 * buffer, (q - 1) / 2 & 1))) break;
         tmem_fence_after();
-#pragma unroll
-        for (uint32_t c = 0; c < kMine; c += 8) {
-          uint32_t r[8];
-          tmem_load8(at + buffer * T::kN + c, r);
+#pragma unroll 1
+        for (uint32_t c = 0; c < have; c += 16) {
+          uint32_t r[16];
+          tmem_load16(at + buffer * T::kN + c, r);
           tmem_load_wait();
+          if (!PAIR && p.split > 1) {
 #pragma unroll
-          for (uint32_t j = 0; j < 8; ++j) acc[c + j] = i == first ? __uint_as_float(r[j]) : acc[c + j] + __uint_as_float(r[j]);
+            for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128] = __uint_as_float(r[j]);
+          } else if (mine && c + 16 <= have) {
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j, to += p.lddw) put(to, __uint_as_float(r[j]));
+          } else if (mine) {
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j, to += p.lddw)
+              if (c + j < have) put(to, __uint_as_float(r[j]));
+          }
         }
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) arrive<PAIR>(first_drained + 8 * buffer);
-      }
-      if (!PAIR && p.split > 1) {
+      } else if constexpr (sizeof(G) == 4) {
+        float acc[kMine];
+        for (uint32_t i = first; i < last; i += p.chain, ++q) {
+          const uint32_t buffer = q & 1;
+          if (!(ok = barrier_wait(ready + 8 * buffer, q / 2 & 1))) break;
+          tmem_fence_after();
 #pragma unroll
-        for (uint32_t c = 0; c < kMine; ++c) part[c * 128] = acc[c];
-      } else if (k < p.k) {
-        G* to = static_cast<G*>(p.dw) + (uint64_t)n * p.lddw + k;
-        if (have == kMine) {
+          for (uint32_t c = 0; c < kMine; c += 8) {
+            uint32_t r[8];
+            tmem_load8(at + buffer * T::kN + c, r);
+            tmem_load_wait();
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) acc[c + j] = i == first ? __uint_as_float(r[j]) : acc[c + j] + __uint_as_float(r[j]);
+          }
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive<PAIR>(first_drained + 8 * buffer);
+        }
+        if (!PAIR && p.split > 1) {
+#pragma unroll
+          for (uint32_t c = 0; c < kMine; ++c) part[c * 128] = acc[c];
+        } else if (mine && have == kMine) {
 #pragma unroll
           for (uint32_t c = 0; c < kMine; ++c, to += p.lddw) put(to, acc[c]);
-        } else {
+        } else if (mine) {
 #pragma unroll
           for (uint32_t c = 0; c < kMine; ++c, to += p.lddw)
             if (c < have) put(to, acc[c]);
@@ -255,7 +286,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       }
     }
   } else {
-    give_registers<kExpandRegisters>();
+    if (R::kExpand < R::kLaunch) give_registers<R::kExpand>();
     // a thread expands two blocks of 32 values: tokens t and t + 32 of a stage, block b of the four
     const uint32_t mine = (warp - 12) / 4, t = warp % 4 * 8 + lane % 8, b = lane / 8, x = t % 8;
     const uint32_t from = codes0 + t * 128 + ((2 * b) ^ x) * 16, other = ((2 * b) ^ x) % 2 ? 0u - 16 : 16;   // a block's two 16-byte pieces
@@ -264,41 +295,34 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     const uint32_t length = last - first, total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
     uint32_t s = mine, sparity = 0, v = mine, vparity = 0;     // stage and slot, and which turn of theirs
     uint32_t tile = tile0, i = mine;
-    for (uint32_t c = mine; c < total; c += 2) {
+    for (uint32_t c = mine; c < total; c += kExpanders) {
       for (; i >= length; i -= length) tile += tile_step;
       const uint32_t scale_at = scales0 + t * 16 + (tile % p.lane_tiles * (T::kK / 32) + (PAIR ? rank * 4 : 0) + b) % 16;
-      i += 2;
-      if (!(ok = barrier_wait(coded + 8 * v, vparity))) break;
-      uint32_t w[2][16];
+      i += kExpanders;
+      if (!(ok = barrier_wait(coded + 8 * v, vparity) && barrier_wait(empty + 8 * s, sparity ^ 1))) break;
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t row = h * 32 * 128;
         uint32_t q[8], e;
-        const uint32_t at = from + v * kCodes + h * 32 * 128;
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(at));
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7]) : "r"(at + other));
         asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(scale_at + v * kScales + h * 32 * 16));
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(from + v * kCodes + row));
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7]) : "r"(from + v * kCodes + row + other));
         const uint32_t scale = scale_pair(e);
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-          w[h][2 * j] = scaled(__byte_perm(q[j], 0, 0x4140), scale);
-          w[h][2 * j + 1] = scaled(__byte_perm(q[j], 0, 0x4342), scale);
-        }
-      }
-      __syncwarp();
-      if (lane == 0) barrier_arrive(taken + 8 * v);
-      if (!(ok = barrier_wait(empty + 8 * s, sparity ^ 1))) break;
-#pragma unroll
-      for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j)
           asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
-                       :: "r"(to + s * kStage + h * 32 * 128 + ((u0 + j) ^ x) * 16), "r"(w[h][4 * j]), "r"(w[h][4 * j + 1]), "r"(w[h][4 * j + 2]),
-                          "r"(w[h][4 * j + 3]) : "memory");
+                       :: "r"(to + s * kStage + row + ((u0 + j) ^ x) * 16), "r"(scaled(__byte_perm(q[2 * j], 0, 0x4140), scale)),
+                          "r"(scaled(__byte_perm(q[2 * j], 0, 0x4342), scale)), "r"(scaled(__byte_perm(q[2 * j + 1], 0, 0x4140), scale)),
+                          "r"(scaled(__byte_perm(q[2 * j + 1], 0, 0x4342), scale)) : "memory");
+      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) arrive<PAIR>(first_full + 8 * s);
-      if ((s += 2) >= kStages) s -= kStages, sparity ^= 1;
-      if ((v += 2) >= kSlots) v -= kSlots, vparity ^= 1;
+      if (lane == 0) {
+        arrive<PAIR>(first_full + 8 * s);
+        barrier_arrive(taken + 8 * v);
+      }
+      if ((s += kExpanders) >= kStages) s -= kStages, sparity ^= 1;
+      if ((v += kExpanders) >= kSlots) v -= kSlots, vparity ^= 1;
     }
   }
   if (!ok) g_wait_failed = 1;
@@ -382,7 +406,7 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   const uint32_t together = PAIR ? 2 : p.split;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)sms / together) * together);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Groups<G>::kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute cluster;
