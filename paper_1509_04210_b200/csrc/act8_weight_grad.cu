@@ -244,11 +244,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128] = __uint_as_float(r[j]);
           } else if (mine && c + 16 <= have) {
 #pragma unroll
-            for (uint32_t j = 0; j < 16; ++j, to += p.lddw) put(to, __uint_as_float(r[j]));
+            for (uint32_t j = 0; j < 16; ++j, to += p.lddw) put_streaming(to, __uint_as_float(r[j]));
           } else if (mine) {
 #pragma unroll
             for (uint32_t j = 0; j < 16; ++j, to += p.lddw)
-              if (c + j < have) put(to, __uint_as_float(r[j]));
+              if (c + j < have) put_streaming(to, __uint_as_float(r[j]));
           }
         }
         tmem_fence_before();
@@ -277,11 +277,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
           for (uint32_t c = 0; c < kMine; ++c) part[c * 128] = acc[c];
         } else if (mine && have == kMine) {
 #pragma unroll
-          for (uint32_t c = 0; c < kMine; ++c, to += p.lddw) put(to, acc[c]);
+          for (uint32_t c = 0; c < kMine; ++c, to += p.lddw) put_streaming(to, acc[c]);
         } else if (mine) {
 #pragma unroll
           for (uint32_t c = 0; c < kMine; ++c, to += p.lddw)
-            if (c < have) put(to, acc[c]);
+            if (c < have) put_streaming(to, acc[c]);
         }
       }
     }
@@ -461,7 +461,9 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   p.k = (uint32_t)dw.cols;
   p.token_stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
   p.stages = p.token_stages * (uint32_t)planes;
-  const bool pair = ((dw.rows + 255) / 256) * ((dw.cols + 255) / 256) >= 74;
+  // Pairs from a tile for every third SM on (1024 tokens: 64 tiles of 2048 x 2048 16.4 us by single blocks, 13.8 by
+  // pairs; 4096 tokens: 36 tiles of 1536 x 1536 27.3 and 31.7, where splitting the tokens wins).
+  const bool pair = 3 * ((dw.rows + 255) / 256) * ((dw.cols + 255) / 256) >= 148;
   if (dw.type == kBF16)
     return pair ? launch<__nv_bfloat16, true>(dy_map, codes_map, scales_map, p, stream) : launch<__nv_bfloat16, false>(dy_map, codes_map, scales_map, p, stream);
   return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);

@@ -172,6 +172,11 @@ template <typename G> __device__ __forceinline__ void put(G* to, float v) {
   if constexpr (sizeof(G) == 2) *to = __float2bfloat16_rn(v);
   else *to = v;
 }
+// For results that are larger than L2 more often than not (151 MB of weight gradients: 32.4 us against 34.5).
+template <typename G> __device__ __forceinline__ void put_streaming(G* to, float v) {
+  if constexpr (sizeof(G) == 2) __stcs(to, __float2bfloat16_rn(v));
+  else __stcs(to, v);
+}
 
 // The end of a tile whose sum was split over the blocks of a cluster, each of which holds its part as
 // [column][128 lanes] at `part`: this block adds the parts of every split-th column in rank order and writes
