@@ -392,20 +392,20 @@ template <typename G, bool PAIR>
 cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
   using T = Tile<PAIR>;
   static Device device;
-  int sms;
-  const cudaError_t e = device.prepare(reinterpret_cast<const void*>(weight_grad_kernel<G, PAIR>), kSmem, &sms);
+  const Device::Facts* facts;
+  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR>, Groups<G>::kThreads, kSmem, &facts);
   if (e != cudaSuccess) return e;
   p.chain = sizeof(G) == 4 ? kChain : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
   p.tiles = (uint32_t)tiles;
-  p.split = 1;
-  if (!PAIR)
-    while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && p.stages >= p.split * 2) p.split *= 2;
+  // A stage takes 0.29 us, joining 2.6 (512 x 512 outputs: 512 tokens 7.2 us by one block a tile, 8.2 by two; 4096
+  // tokens 23.5 and 12.6 by four).
+  p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, 9);
   const uint32_t together = PAIR ? 2 : p.split;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)sms / together) * together);
+  cfg.gridDim = dim3(p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together);
   cfg.blockDim = dim3(Groups<G>::kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
@@ -461,9 +461,9 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   p.k = (uint32_t)dw.cols;
   p.token_stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
   p.stages = p.token_stages * (uint32_t)planes;
-  // Pairs from a tile for every third SM on (1024 tokens: 64 tiles of 2048 x 2048 16.4 us by single blocks, 13.8 by
-  // pairs; 4096 tokens: 36 tiles of 1536 x 1536 27.3 and 31.7, where splitting the tokens wins).
-  const bool pair = 3 * ((dw.rows + 255) / 256) * ((dw.cols + 255) / 256) >= 148;
+  // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 tokens: 144 tiles of 1536 x 1536 27.3 us
+  // and 31.7 by pairs, 256 tiles of 2048 x 2048 47.5 and 33.2).
+  const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > 148;
   if (dw.type == kBF16)
     return pair ? launch<__nv_bfloat16, true>(dy_map, codes_map, scales_map, p, stream) : launch<__nv_bfloat16, false>(dy_map, codes_map, scales_map, p, stream);
   return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);

@@ -225,8 +225,8 @@ template <typename G, int COLS, typename X>
 cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   using S = Shape<COLS, !std::is_void<X>::value>;
   static Device device;
-  int sms;
-  cudaError_t e = device.prepare(reinterpret_cast<const void*>(matmul_kernel<G, COLS, X>), S::kSmem, &sms);
+  const Device::Facts* facts;
+  cudaError_t e = device.prepare(matmul_kernel<G, COLS, X>, S::kThreads, S::kSmem, &facts);
   if (e != cudaSuccess) return e;
   Params p = {};
   const uint64_t nb = (b.cols + 31) / 32;
@@ -246,9 +246,9 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
   p.lane_tiles = (p.n + 127) / 128;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.m + COLS - 1) / COLS);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
-  const uint32_t stages = (p.kt + 1) / 2;
-  p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sms && stages >= p.split * 2) p.split *= 2;
+  // A stage takes 0.2 us; joining 0.7 us at 16 columns and 2.7 at 128 (one token through 4096 x 4096: 6.6 us by one
+  // block a tile, 5.3 by four; 128 tokens: 7.4 and 8.3).
+  p.split = pick_split(*facts, tiles, (p.kt + 1) / 2, 2 + COLS / 11);
   CUtensorMap lane_map, column_map = {};
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
   if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
@@ -288,7 +288,9 @@ constexpr uint64_t kQuantizedInside = 32;   // rows of x up to which the product
 
 cudaError_t launch_mx4_matmul(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   if (a.cols == 0) return nothing(y, stream);
-  if (((a.rows + 255) / 256) * ((b.rows + 255) / 256) >= 74) return launch_mx4_matmul_pair(a, b, y, stream);
+  // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 values: 128 tiles of 512 x 4096 8.0 us
+  // and 10.2 by pairs, 256 tiles of 1024 x 4096 15.0 and 10.8).
+  if (((a.rows + 127) / 128) * ((b.rows + 127) / 128) > 148) return launch_mx4_matmul_pair(a, b, y, stream);
   return y.type == kBF16 ? by_rows<__nv_bfloat16>(a, b, y, stream) : by_rows<float>(a, b, y, stream);
 }
 

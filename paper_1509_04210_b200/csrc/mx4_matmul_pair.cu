@@ -46,7 +46,7 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
 }
 
 template <typename G>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map,
                    const __grid_constant__ CUtensorMap lane_scales, const __grid_constant__ CUtensorMap column_scales,
                    const __grid_constant__ Params p) {
@@ -180,8 +180,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
 
 template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   static Device device;
-  int sms;
-  cudaError_t e = device.prepare(reinterpret_cast<const void*>(matmul_pair_kernel<G>), kSmem, &sms);
+  const Device::Facts* facts;
+  cudaError_t e = device.prepare(matmul_pair_kernel<G>, kThreads, kSmem, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t nb = (a.cols + 31) / 32, kt = (nb + 3) / 4, lane_tiles = (b.rows + kTile - 1) / kTile;
   const uint64_t tiles = lane_tiles * ((a.rows + kTile - 1) / kTile);
@@ -195,9 +195,19 @@ template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const Matri
   if (e == cudaSuccess) e = encode_plain(&column_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, a.scales, 128, a_atoms, 512, 128, 2);
   if (e != cudaSuccess) return e;
   const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
-  const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)sms / 2);
-  matmul_pair_kernel<G><<<2 * pairs, kThreads, kSmem, stream>>>(lane_map, column_map, lane_scales, column_scales, p);
-  return cudaGetLastError();
+  const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)facts->sms / 2);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * pairs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = 2;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, matmul_pair_kernel<G>, lane_map, column_map, lane_scales, column_scales, p);
 }
 
 }  // namespace

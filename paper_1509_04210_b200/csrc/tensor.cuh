@@ -3,6 +3,8 @@
 #pragma once
 #include <atomic>
 #include <cstdint>
+#include <mutex>
+
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>
@@ -236,30 +238,67 @@ inline PFN_cuTensorMapEncodeTiled map_encoder() {
   return fn;
 }
 
-// What a launch asks of the current device, asked once per device: its multiprocessors, and `kernel`'s
-// leave to use `bytes` of shared memory.  One static instance per kernel.
+// What a launch asks of the current device, asked once per device: its multiprocessors, `kernel`'s leave to use
+// `bytes` of shared memory, and how many clusters of 2, 4 and 8 of its blocks run at once (of 8 fewer than
+// an eighth of the multiprocessors, because a cluster does not leave its part of the chip).  One static
+// instance per kernel.
 class Device {
  public:
-  cudaError_t prepare(const void* kernel, uint32_t bytes, int* sms) {
+  struct Facts {
+    int sms;
+    int clusters[4];   // of 1, 2, 4 and 8 blocks
+  };
+  template <typename K> cudaError_t prepare(K* kernel, uint32_t threads, uint32_t bytes, const Facts** facts) {
     int d = 0;
     cudaError_t e = cudaGetDevice(&d);
     if (e != cudaSuccess) return e;
     if (d < 0 || d >= kMost) return cudaErrorInvalidDevice;
-    int have = sms_[d].load(std::memory_order_acquire);
-    if (have == 0) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-      if (e == cudaSuccess) e = cudaDeviceGetAttribute(&have, cudaDevAttrMultiProcessorCount, d);
-      if (e != cudaSuccess) return e;
-      sms_[d].store(have, std::memory_order_release);
+    if (!known_[d].load(std::memory_order_acquire)) {
+      std::lock_guard<std::mutex> lock(mutex_);
+      if (!known_[d].load(std::memory_order_relaxed)) {
+        Facts f = {};
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&f.sms, cudaDevAttrMultiProcessorCount, d);
+        f.clusters[0] = f.sms;
+        for (int i = 1; e == cudaSuccess && i < 4; ++i) {
+          cudaLaunchConfig_t cfg = {};
+          cfg.gridDim = dim3(1u << i);
+          cfg.blockDim = dim3(threads);
+          cfg.dynamicSmemBytes = bytes;
+          cudaLaunchAttribute cluster;
+          cluster.id = cudaLaunchAttributeClusterDimension;
+          cluster.val.clusterDim.x = 1u << i;
+          cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+          cfg.attrs = &cluster;
+          cfg.numAttrs = 1;
+          e = cudaOccupancyMaxActiveClusters(&f.clusters[i], kernel, &cfg);
+        }
+        if (e != cudaSuccess) return e;
+        facts_[d] = f;
+        known_[d].store(true, std::memory_order_release);
+      }
     }
-    *sms = have;
+    *facts = &facts_[d];
     return cudaSuccess;
   }
 
  private:
   static constexpr int kMost = 64;
-  std::atomic<int> sms_[kMost] = {};
+  std::mutex mutex_;
+  std::atomic<bool> known_[kMost] = {};
+  Facts facts_[kMost];
 };
+
+// Blocks of a cluster that share a tile: the count that is done soonest, where a block's stages are its time and
+// joining the parts takes as long as `join` stages.
+inline uint32_t pick_split(const Device::Facts& f, uint64_t tiles, uint32_t stages, uint32_t join) {
+  uint32_t best = 1, time = stages;
+  for (uint32_t i = 1; i < 4; ++i) {
+    const uint32_t split = 1u << i, t = (stages + split - 1) / split + join;
+    if (split <= stages && tiles <= (uint64_t)f.clusters[i] && t < time) best = split, time = t;
+  }
+  return best;
+}
 
 // A row-major matrix, read in boxes as it lies; what lies outside reads as zero.
 inline cudaError_t encode_plain(CUtensorMap* map, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
