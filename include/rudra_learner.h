@@ -129,6 +129,12 @@ int rudra_act8_weight_grad(const void* dy_dev, int dy_dtype, uint64_t lddy, uint
                            const void* codes_dev, const void* scales_dev, uint64_t k, void* dw_dev, int dw_dtype,
                            uint64_t lddw, void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
 
+/* Waits for cuda_stream and reports asynchronous CUDA errors, and kernels of this header that gave up, as
+ * RUDRA_E_CUDA.  The kernels of the two products wait on barriers inside a block or cluster; a wait
+ * that lasts about two seconds (which no working GPU needs) ends, and its kernel with it: what such a call
+ * wrote is not to be used.  Clears what it reports. */
+int rudra_learner_sync(void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,6 +107,7 @@ def lib():
         "rudra_act8_scales_bytes": (u64, [u64, u64]),
         "rudra_act8_forward": (C.c_int, [C.c_int, vp, vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, vp, vp, vp]),
         "rudra_act8_backward": (C.c_int, [C.c_int, vp, C.c_int, u64, u64, u64, vp, vp, vp, vp, vp, vp, u64, vp]),
+        "rudra_learner_sync": (C.c_int, [vp]),
         "rudra_act8_weight_grad_workspace": (u64, [vp, C.c_int, u64, u64, u64]),
         "rudra_act8_weight_grad": (C.c_int, [vp, C.c_int, u64, u64, u64, vp, vp, u64, vp, C.c_int, u64, vp, u64, vp]),
     }

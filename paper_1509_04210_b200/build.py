@@ -1,9 +1,11 @@
 """Builds ``librudra_ps.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_PKG, "csrc")
@@ -14,6 +16,9 @@ SOURCES = ["ps.cu", "update.cu", "snapshot.cu", "leaf.cu", "noalloc.cu", "sched.
 # measurement utility of the benchmark, a library of its own: not part of the product interface
 PROBE_LIB_PATH = os.path.join(_PKG, "librudra_probe.so")
 PROBE_SOURCES = ["probe.cu"]
+# the torch binding of the learner-side operators, host code only
+LEARNER_PATH = os.path.join(_PKG, "_learner.so")
+LEARNER_SOURCE = "learner_torch.cpp"
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-cudart", "static", "-shared",
@@ -56,6 +61,41 @@ def build_probe(force: bool = False, verbose: bool = False) -> str:
     return _compile(PROBE_LIB_PATH, PROBE_SOURCES, verbose)
 
 
+def learner_needs_build() -> bool:
+    if not os.path.exists(LEARNER_PATH):
+        return True
+    t = os.path.getmtime(LEARNER_PATH)
+    return any(os.path.getmtime(d) > t for d in [os.path.join(_CSRC, LEARNER_SOURCE), os.path.join(_INCLUDE, "rudra_learner.h")])
+
+
+def build_learner(force: bool = False) -> str:
+    """The torch binding of the learner-side operators, a CPython module next to the library it calls."""
+    if not force and not learner_needs_build():
+        return LEARNER_PATH
+    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    tmp = LEARNER_PATH + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           "-I", sysconfig.get_paths()["include"], "-I", _INCLUDE]
+    for d in (os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
+        cmd += ["-isystem", d]
+    cmd += [os.path.join(_CSRC, LEARNER_SOURCE), "-o", tmp, "-L", _PKG, "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN",
+            "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    subprocess.check_call(cmd)
+    os.replace(tmp, LEARNER_PATH)
+    return LEARNER_PATH
+
+
+def load_learner() -> None:
+    """Builds the binding if it is absent or stale; a build that fails is an error unless an older one is there."""
+    try:
+        build_learner()
+    except Exception as exc:
+        if not os.path.exists(LEARNER_PATH):
+            raise ImportError("_learner.so is missing and could not be built: %r" % (exc,)) from exc
+
+
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
     print(build_probe(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_learner(force="--force" in sys.argv))

@@ -469,4 +469,6 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);
 }
 
+cudaError_t act8_weight_grad_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+
 }  // namespace rudra

@@ -186,4 +186,17 @@ int rudra_act8_weight_grad(const void* dy_dev, int dy_dtype, uint64_t lddy, uint
   });
 }
 
+int rudra_learner_sync(void* cuda_stream) {
+  return guarded([&]() -> int {
+    cudaError_t e = cudaStreamSynchronize(stream_of(cuda_stream));
+    bool raised = false;
+    if (e == cudaSuccess) e = rudra::mx4_matmul_gave_up(&raised);
+    if (e == cudaSuccess) e = rudra::mx4_matmul_pair_gave_up(&raised);
+    if (e == cudaSuccess) e = rudra::act8_weight_grad_gave_up(&raised);
+    if (e != cudaSuccess) return cuda_fail(e, "learner-side operators");
+    if (raised) return fail(RUDRA_E_CUDA, "a product kernel gave up a wait: its result is not valid");
+    return 0;
+  });
+}
+
 }  // extern "C"

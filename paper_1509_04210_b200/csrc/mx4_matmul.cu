@@ -311,4 +311,6 @@ cudaError_t launch_mx4_linear(const MatrixIn& x, const Mx4& b, const MatrixOut& 
   return e != cudaSuccess ? e : launch_mx4_matmul({codes, scales, x.rows, x.cols}, b, y, stream);
 }
 
+cudaError_t mx4_matmul_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+
 }  // namespace rudra

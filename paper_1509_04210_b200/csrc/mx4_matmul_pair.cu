@@ -216,4 +216,6 @@ cudaError_t launch_mx4_matmul_pair(const Mx4& a, const Mx4& b, const MatrixOut& 
   return y.type == kBF16 ? launch<__nv_bfloat16>(a, b, y, stream) : launch<float>(a, b, y, stream);
 }
 
+cudaError_t mx4_matmul_pair_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+
 }  // namespace rudra

@@ -300,6 +300,18 @@ inline uint32_t pick_split(const Device::Facts& f, uint64_t tiles, uint32_t stag
   return best;
 }
 
+// The flag that a kernel raises when it gives up a wait, read and lowered with the stream's work done.
+template <typename F> cudaError_t take_flag(const F& symbol, bool* raised) {
+  uint32_t v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, symbol, sizeof(v));
+  if (e == cudaSuccess && v) {
+    *raised = true;
+    v = 0;
+    e = cudaMemcpyToSymbol(symbol, &v, sizeof(v));
+  }
+  return e;
+}
+
 // A row-major matrix, read in boxes as it lies; what lies outside reads as zero.
 inline cudaError_t encode_plain(CUtensorMap* map, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
                                 uint32_t box_cols, uint32_t box_rows) {

@@ -490,6 +490,7 @@ def test_refusals_on_the_gpu():
         L.act8_forward("silu", x, x)
     with pytest.raises(ValueError):
         L.act8_weight_grad(torch.zeros((5, 64), device="cuda"), L.act8_save(x))
+    assert L.sync() is None
     off = torch.zeros(4096, dtype=torch.uint8, device="cuda")[1:]
     with pytest.raises(rb.RudraError) as e:
         L.mx4_quantize(x, out=L.MX4(off, q.scales, 4, 64))      # codes not on a 32-byte boundary
