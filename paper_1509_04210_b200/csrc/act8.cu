@@ -1,7 +1,7 @@
 // Activation functions with an 8-bit checkpoint of their input: forward (value and checkpoint in one
 // pass) and backward (slope from the checkpoint).  Element-wise but for a block's shared scale, so bound
 // by HBM: per value and input 2G + 33/32 bytes each way (G = 2 bf16, 4 f32).  Sigmoids are formed from the
-// fast exponential and reciprocal, each within about 2 ulp in 32 bits.
+// approximate base-2 exponential and reciprocal, each within about 2 units in the last place of 32 bits.
 #include <algorithm>
 
 #include "blocks.cuh"
@@ -10,35 +10,42 @@
 namespace rudra {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
-__device__ __forceinline__ float sigmoid(float x) {
-  float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));   // exp may reach infinity: the reciprocal is 0
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 1 / (1 + 2^t).  2^t may reach infinity, whose reciprocal is 0; results below 2^-126 count as 0.
+__device__ __forceinline__ float sigmoid2(float t) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
 
 constexpr float kGeluA = 1.5957691216057308f;   // 2 sqrt(2 / pi): gelu(x) = x sigmoid(A (x + B x^3))
 constexpr float kGeluB = 0.044715f;
 
+// The sigmoid that f(x) = x * sigmoid is made with.
+template <Act A> __device__ __forceinline__ float gate(float x) {
+  if (A == kGelu) return sigmoid2(x * fmaf(-kLog2e * kGeluA * kGeluB * x, x, -kLog2e * kGeluA));
+  return sigmoid2(-kLog2e * x);
+}
+
 template <Act A> __device__ __forceinline__ float value(float x) {
   if (A == kRelu) return x > 0.f ? x : x != x ? x : 0.f;
-  if (A == kGelu) return x * sigmoid(kGeluA * fmaf(kGeluB * x, x * x, x));
-  return x * sigmoid(x);
+  return x * gate<A>(x);
 }
 
 // f'(x); `f`: f(x), from the same sigmoid.
 template <Act A> __device__ __forceinline__ float slope(float x, float& f) {
   if (A == kRelu) { f = x; return x > 0.f ? 1.f : x != x ? x : 0.f; }
-  if (A == kGelu) {
-    const float s = sigmoid(kGeluA * fmaf(kGeluB * x, x * x, x));
-    const float t = s * (1.f - s);
-    f = x * s;
-    // where the sigmoid is 0 or 1 its slope is nothing, however far x^3 has run
-    return t == 0.f ? s : fmaf(x * t, kGeluA * fmaf(3.f * kGeluB * x, x, 1.f), s);
-  }
-  const float s = sigmoid(x);
+  const float s = gate<A>(x);
   f = x * s;
+  if (A == kGelu) {
+    const float t = f * (1.f - s);
+    // where the sigmoid is 0 or 1 its slope is nothing, however far x^2 has run
+    return t == 0.f ? s : fmaf(t, fmaf(3.f * kGeluA * kGeluB * x, x, kGeluA), s);
+  }
   return fmaf(f, 1.f - s, s);
 }
 

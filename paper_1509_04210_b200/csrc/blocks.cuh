@@ -29,13 +29,20 @@ template <typename G> struct Values {
   static constexpr int kWords = kValues * sizeof(G) / 4;
   uint32_t w[kWords];
 
-  __device__ __forceinline__ void load(const G* p, Access access, int have) {
+  // FIRST: first to leave L2, for a matrix that is done with once it is read (quantization of 4096 x 9216 floats
+  // 32.4 us without, 28.0 with it).
+  template <bool FIRST = false> __device__ __forceinline__ void load(const G* p, Access access, int have) {
     if (have == kValues && access == kBy32) {
 #pragma unroll
-      for (int i = 0; i < kWords; i += 8)
-        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
-                     : "l"(reinterpret_cast<const uint32_t*>(p) + i));
+      for (int i = 0; i < kWords; i += 8) {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p) + i;
+        if (FIRST)
+          asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                       : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"(q));
+        else
+          asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                       : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"(q));
+      }
     } else if (sizeof(G) == 2 && have == kValues && access == kBy16) {
 #pragma unroll
       for (int i = 0; i < kWords; i += 4)
@@ -170,16 +177,28 @@ __device__ __forceinline__ void e2m1_values(uint2 codes, float scale, float (&x)
 }
 
 // int8 codes of the thread's values: nearest, ties to even, at most 127 in magnitude.  Adding 1.5 * 2^23
-// rounds to a whole number whose two's complement is the sum's low byte.
-template <typename V> __device__ __forceinline__ uint4 int8_codes(const V& v, uint32_t s) {
+// rounds to a whole number whose two's complement is the sum's low byte; values past 127 are cut off before,
+// two bf16 at a time, or after.
+template <typename G> __device__ __forceinline__ uint4 int8_codes(const Values<G>& v, uint32_t s) {
   constexpr float kWhole = 12582912.f;
   const float inv = inverse_scale(s);
+  const uint32_t top = __float_as_uint(127.f * scale_value(s)) >> 16;   // exact in bf16
+  const uint32_t high = top * 0x10001u, low = high | 0x80008000u;
   uint32_t r[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fminf(fmaxf(fmaf(v.get(4 * q + i), inv, kWhole), kWhole - 127.f), kWhole + 127.f));
+    for (int i = 0; i < 4; ++i) {
+      if (sizeof(G) == 4) {
+        b[i] = __float_as_uint(fminf(fmaxf(fmaf(v.get(4 * q + i), inv, kWhole), kWhole - 127.f), kWhole + 127.f));
+      } else {
+        const __nv_bfloat162 w = __hmax2(__hmin2(reinterpret_cast<const __nv_bfloat162&>(v.w[(4 * q + i) / 2]), reinterpret_cast<const __nv_bfloat162&>(high)),
+                                         reinterpret_cast<const __nv_bfloat162&>(low));
+        const uint32_t u = reinterpret_cast<const uint32_t&>(w);
+        b[i] = __float_as_uint(fmaf(__uint_as_float(i % 2 ? u & 0xFFFF0000u : u << 16), inv, kWhole));
+      }
+    }
     r[q] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   }
   return s == 255u ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(r[0], r[1], r[2], r[3]);

@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __rest
     k[u] = item - row[u] * kt.d;
     const uint32_t c = k[u] * 128 + lane * kValues;
     const int have = item < items && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-    x[u].load(src + (have ? row[u] * ld + c : 0), access, have);
+    x[u].template load<true>(src + (have ? row[u] * ld + c : 0), access, have);
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
@@ -67,11 +67,11 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
       const G* p = src + r * ld + c;
       if (pairs && c + 1 < cols) {
         if (sizeof(G) == 4) {
-          const float2 v = *reinterpret_cast<const float2*>(p);
+          const float2 v = __ldcs(reinterpret_cast<const float2*>(p));
           x[0][i] = v.x;
           x[1][i] = v.y;
         } else {
-          const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+          const uint32_t v = __ldcs(reinterpret_cast<const uint32_t*>(p));
           x[0][i] = __uint_as_float(v << 16);
           x[1][i] = __uint_as_float(v & 0xFFFF0000u);
         }
