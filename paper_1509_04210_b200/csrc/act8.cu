@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "blocks.cuh"
+#include "launch.cuh"
 #include "learner.cuh"
 
 namespace rudra {
@@ -79,6 +80,8 @@ template <typename G, Act A>
 __global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__ x, const G* __restrict__ up, uint64_t ldx,
                                                            uint32_t cols, Divisor per_row, uint32_t units, Access access_in, Access access_out,
                                                            G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
+  admit_next_kernel();
+  await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   const bool in = i < units;
   const int have = in && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
@@ -101,6 +104,8 @@ template <typename G, Act A>
 __global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_t lddy, uint32_t cols, Divisor per_row, uint32_t units,
                                                             Access access_in, Access access_out, Saved saved, Saved saved_up, G* dx, G* dup,
                                                             uint64_t lddx) {
+  admit_next_kernel();
+  await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   if (i >= units || c >= cols) return;
   const int have = (int)min((uint32_t)kValues, cols - c);
@@ -145,12 +150,13 @@ cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const
   for (uint64_t r = 0; r < x.rows; r += part.most) {
     const uint64_t units = std::min(part.most, x.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-    forward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
-        static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
+    const cudaError_t e = launch_after(
+        forward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
         Divisor((uint32_t)part.per_row), (uint32_t)units, in, access_of<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
         from_row(saved, x.cols, r), from_row(saved_up, x.cols, r));
+    if (e != cudaSuccess) return e;
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 template <typename G, Act A>
@@ -160,12 +166,13 @@ cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up
   for (uint64_t r = 0; r < dx.rows; r += part.most) {
     const uint64_t units = std::min(part.most, dx.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-    backward_kernel<G, A><<<(unsigned)((units + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
-        static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
+    const cudaError_t e = launch_after(
+        backward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
         access_of<G>(dy.p, dy.ld), out, from_row(saved, dx.cols, r), from_row(saved_up, dx.cols, r),
         static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
+    if (e != cudaSuccess) return e;
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace

@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "blocks.cuh"
+#include "launch.cuh"
 #include "learner.cuh"
 #include "tensor.cuh"
 
@@ -156,6 +157,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   }
   const uint32_t tmem = *slot;
   bool ok = true;
+  admit_next_kernel();
+  await_previous_kernel();
 
   if (warp < 4) {
     give_registers<R::kManage>();
@@ -351,6 +354,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 template <typename G>
 __global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, uint64_t ld, uint32_t tokens, uint32_t n, uint32_t pitch,
                                                      uint64_t rows, Access access, uint4* __restrict__ out) {
+  admit_next_kernel();
+  await_previous_kernel();
   const uint32_t per_row = pitch / kValues;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t row = i / per_row;
@@ -404,18 +409,8 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   // tokens 23.5 and 12.6 by four).
   p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, 9);
   const uint32_t together = PAIR ? 2 : p.split;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together);
-  cfg.blockDim = dim3(Groups<G>::kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  cfg.stream = stream;
-  cudaLaunchAttribute cluster;
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = together;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, weight_grad_kernel<G, PAIR>, dy, codes, scales, p);
+  const uint32_t blocks = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together;
+  return launch_after(weight_grad_kernel<G, PAIR>, blocks, Groups<G>::kThreads, kSmem, together, stream, dy, codes, scales, p);
 }
 
 }  // namespace
@@ -438,14 +433,12 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     rows = plane_rows(dy.rows);
     const uint64_t blocks = (rows * (pitch / kValues) + 255) / 256;
     if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-    if (dy.type == kF32)
-      planes_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows, (uint32_t)dy.cols,
-                                                                 (uint32_t)pitch, rows, access_of<float>(dy.p, dy.ld), static_cast<uint4*>(workspace));
-    else
-      planes_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(dy.p), dy.ld, (uint32_t)dy.rows,
-                                                                         (uint32_t)dy.cols, (uint32_t)pitch, rows,
-                                                                         access_of<__nv_bfloat16>(dy.p, dy.ld), static_cast<uint4*>(workspace));
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e =
+        dy.type == kF32 ? launch_after(planes_kernel<float>, (uint32_t)blocks, 256, 0, 1, stream, static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows,
+                                       (uint32_t)dy.cols, (uint32_t)pitch, rows, access_of<float>(dy.p, dy.ld), static_cast<uint4*>(workspace))
+                        : launch_after(planes_kernel<__nv_bfloat16>, (uint32_t)blocks, 256, 0, 1, stream, static_cast<const __nv_bfloat16*>(dy.p), dy.ld,
+                                       (uint32_t)dy.rows, (uint32_t)dy.cols, (uint32_t)pitch, rows, access_of<__nv_bfloat16>(dy.p, dy.ld),
+                                       static_cast<uint4*>(workspace));
     if (e != cudaSuccess) return e;
   }
   const uint64_t nb = (dw.cols + 31) / 32, scale_pitch = act8_scale_pitch(dw.cols);

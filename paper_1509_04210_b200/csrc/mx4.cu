@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "blocks.cuh"
+#include "launch.cuh"
 #include "learner.cuh"
 
 namespace rudra {
@@ -19,6 +20,8 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __rest
                                                                  uint32_t items, Access access, uint2* __restrict__ codes,
                                                                  uint32_t* __restrict__ scales) {
   constexpr uint32_t U = 2, kItems = kThreads / 8;
+  admit_next_kernel();
+  await_previous_kernel();
   const uint32_t lane = threadIdx.x % 8, nb = (cols + 31) / 32;
   Values<G> x[U];
   uint32_t row[U], k[U];
@@ -51,6 +54,8 @@ template <typename G>
 __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __restrict__ src, uint64_t ld, uint32_t rows,
                                                                   uint32_t cols, uint32_t column_tiles, bool pairs,
                                                                   uint4* __restrict__ codes, uint32_t* __restrict__ scales) {
+  admit_next_kernel();
+  await_previous_kernel();
   __shared__ uint4 tile[64][5];
   __shared__ uint8_t sbytes[64][4];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -107,6 +112,8 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
                                                               uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
                                                               G* __restrict__ dst, uint64_t ld) {
   constexpr uint32_t U = 2;
+  admit_next_kernel();
+  await_previous_kernel();
   const uint32_t nb = (cols + 31) / 32;
   uint2 w[U];
   uint8_t s[U];
@@ -142,19 +149,19 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
     for (uint64_t r = 0; r < m.rows; r += most) {
       const uint64_t rows = std::min(most, m.rows - r);
       if (rows * kt > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-      quantize_rows_kernel<G><<<grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, stream>>>(
-          src + r * m.ld, m.ld, (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), access_of<G>(src, m.ld),
-          static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2, static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
+      const cudaError_t e = launch_after(
+          quantize_rows_kernel<G>, grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, 1, stream, src + r * m.ld, m.ld, (uint32_t)m.cols,
+          Divisor((uint32_t)kt), (uint32_t)(rows * kt), access_of<G>(src, m.ld), static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2,
+          static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
+      if (e != cudaSuccess) return e;
     }
-  } else {
-    const uint64_t tiles = (m.cols + 63) / 64;
-    const uint64_t blocks = tiles * ((m.rows + 127) / 128);
-    if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-    const bool pairs = reinterpret_cast<uintptr_t>(src) % (2 * sizeof(G)) == 0 && m.ld % 2 == 0;
-    quantize_transposed_kernel<G><<<(unsigned)blocks, 128, 0, stream>>>(src, m.ld, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)tiles, pairs,
-                                                              static_cast<uint4*>(codes), static_cast<uint32_t*>(scales));
+    return cudaSuccess;
   }
-  return cudaGetLastError();
+  const uint64_t tiles = (m.cols + 63) / 64, blocks = tiles * ((m.rows + 127) / 128);
+  if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+  const bool pairs = reinterpret_cast<uintptr_t>(src) % (2 * sizeof(G)) == 0 && m.ld % 2 == 0;
+  return launch_after(quantize_transposed_kernel<G>, (uint32_t)blocks, 128, 0, 1, stream, src, m.ld, (uint32_t)m.rows, (uint32_t)m.cols,
+                      (uint32_t)tiles, pairs, static_cast<uint4*>(codes), static_cast<uint32_t*>(scales));
 }
 
 template <typename G>
@@ -164,11 +171,12 @@ cudaError_t dequantize(const Mx4& m, const MatrixOut& d, cudaStream_t stream) {
   for (uint64_t r = 0; r < m.rows; r += most) {
     const uint64_t units = std::min(most, m.rows - r) * per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-    dequantize_kernel<G><<<grid_of(units, 2 * kThreads), kThreads, 0, stream>>>(
-        static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
+    const cudaError_t e = launch_after(
+        dequantize_kernel<G>, grid_of(units, 2 * kThreads), kThreads, 0, 1, stream, static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
         Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, access_of<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
+    if (e != cudaSuccess) return e;
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace

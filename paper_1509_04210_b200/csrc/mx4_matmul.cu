@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "blocks.cuh"
+#include "launch.cuh"
 #include "learner.cuh"
 #include "tensor.cuh"
 
@@ -103,6 +104,8 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
   tmem_fence_after();
   const uint32_t tmem = *slot;
   bool ok = true;
+  admit_next_kernel();
+  await_previous_kernel();
 
   if (warp == 0) {
     const uint32_t elected = elect();
@@ -253,18 +256,7 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
   if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * p.split));
-  cfg.blockDim = dim3(S::kThreads);
-  cfg.dynamicSmemBytes = S::kSmem;
-  cfg.stream = stream;
-  cudaLaunchAttribute cluster;
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = p.split;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_kernel<G, COLS, X>, lane_map, column_map, p);
+  return launch_after(matmul_kernel<G, COLS, X>, (uint32_t)(tiles * p.split), S::kThreads, S::kSmem, p.split, stream, lane_map, column_map, p);
 }
 
 template <typename G> cudaError_t by_rows(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {

@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "blocks.cuh"
+#include "launch.cuh"
 #include "learner.cuh"
 #include "tensor.cuh"
 
@@ -81,6 +82,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
   cluster_wait();
   const uint32_t tmem = *slot;
   bool ok = true;
+  admit_next_kernel();
+  await_previous_kernel();
 
   if (warp == 0) {
     const uint32_t elected = elect(), first_full = peer_address(full, 0);
@@ -196,18 +199,7 @@ template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const Matri
   if (e != cudaSuccess) return e;
   const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)facts->sms / 2);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * pairs);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  cfg.stream = stream;
-  cudaLaunchAttribute cluster;
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = 2;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_pair_kernel<G>, lane_map, column_map, lane_scales, column_scales, p);
+  return launch_after(matmul_pair_kernel<G>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
 }
 
 }  // namespace
