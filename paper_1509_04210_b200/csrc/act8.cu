@@ -77,43 +77,43 @@ struct Restored {
 // Checkpoint rows are whole blocks of two units (of a thread's values), so unit numbers run through the
 // checkpoint without gaps and neighbouring lanes share a block.
 template <typename G, Act A>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const G* __restrict__ x, const G* __restrict__ up, uint64_t ldx,
-                                                           uint32_t cols, Divisor per_row, uint32_t units, Access access_in, Access access_out,
-                                                           G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
+__global__ void __launch_bounds__(kThreads) forward_kernel(Rows<G> x, Rows<G> up, uint32_t cols, Divisor per_row, uint32_t units,
+                                                           Access access_out, G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   const bool in = i < units;
   const int have = in && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-  const uint64_t at = have ? row * ldx + c : 0;
+  const uint64_t at = have ? row * x.ld + c : 0;
   Values<G> a, b;
-  a.load(x + at, access_in, have);
-  if (A == kSwiglu) b.load(up + at, access_in, have);
+  a.load(x, at, have);
+  if (A == kSwiglu) b.load(up, at, have);
   save(saved, i, row, c / 32, a, in);
   if (A == kSwiglu) save(saved_up, i, row, c / 32, b, in);
   if constexpr (A != kNone) {
-    if (!have) return;
+    __shared__ Waiting waiting[kThreads / 32];
     float v[kValues];
 #pragma unroll
     for (int e = 0; e < kValues; ++e) v[e] = A == kSwiglu ? value<A>(a.get(e)) * b.get(e) : value<A>(a.get(e));
-    store_values(y + row * ldy + c, access_out, have, v);
+    store_values(waiting[threadIdx.x / 32], y + (have ? row * ldy + c : 0), access_out, have, v);
   }
 }
 
 template <typename G, Act A>
-__global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_t lddy, uint32_t cols, Divisor per_row, uint32_t units,
-                                                            Access access_in, Access access_out, Saved saved, Saved saved_up, G* dx, G* dup,
-                                                            uint64_t lddx) {
+__global__ void __launch_bounds__(kThreads) backward_kernel(Rows<G> dy, uint32_t cols, Divisor per_row, uint32_t units, Access access_out, Saved saved,
+                                                            Saved saved_up, G* dx, G* dup, uint64_t lddx) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
-  if (i >= units || c >= cols) return;
-  const int have = (int)min((uint32_t)kValues, cols - c);
+  const int have = i < units && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
+  __shared__ Waiting waiting[kThreads / 32];
   Values<G> g;
-  Restored rx, ru;
-  if (A != kNone) g.load(dy + row * lddy + c, access_in, have);
-  rx.load(saved, i, row, c / 32);
-  if (A == kSwiglu) ru.load(saved_up, i, row, c / 32);
+  Restored rx = {}, ru = {};
+  if (have) {
+    if (A != kNone) g.load(dy, row * dy.ld + c, have);
+    rx.load(saved, i, row, c / 32);
+    if (A == kSwiglu) ru.load(saved_up, i, row, c / 32);
+  }
   float x[kValues], u[kValues];
   rx.values(x);
   if (A == kSwiglu) ru.values(u);
@@ -126,8 +126,9 @@ __global__ void __launch_bounds__(kThreads) backward_kernel(const G* dy, uint64_
       if (A == kSwiglu) u[e] = g.get(e) * f;
     }
   }
-  store_values(dx + row * lddx + c, access_out, have, x);
-  if (A == kSwiglu) store_values(dup + row * lddx + c, access_out, have, u);
+  const uint64_t at = have ? row * lddx + c : 0;
+  store_values(waiting[threadIdx.x / 32], dx + at, access_out, have, x);
+  if (A == kSwiglu) store_values(waiting[threadIdx.x / 32], dup + at, access_out, have, u);
 }
 
 // Rows of a launch: as many as keep the number of its units below 2^31.
@@ -146,14 +147,13 @@ Saved from_row(const Act8& a, uint64_t cols, uint64_t r) {
 template <typename G, Act A>
 cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const Act8& saved, const Act8& saved_up, cudaStream_t stream) {
   const Part part(x.cols);
-  const Access in = A == kSwiglu ? both(access_of<G>(x.p, x.ld), access_of<G>(up, x.ld)) : access_of<G>(x.p, x.ld);
   for (uint64_t r = 0; r < x.rows; r += part.most) {
     const uint64_t units = std::min(part.most, x.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        forward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, static_cast<const G*>(x.p) + r * x.ld, static_cast<const G*>(up) + (up ? r * x.ld : 0), x.ld, (uint32_t)x.cols,
-        Divisor((uint32_t)part.per_row), (uint32_t)units, in, access_of<G>(y.p, y.ld), static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld,
-        from_row(saved, x.cols, r), from_row(saved_up, x.cols, r));
+        forward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(x.p, x.rows, x.cols, x.ld, r),
+        Rows<G>::of(up, x.rows, x.cols, x.ld, r), (uint32_t)x.cols, Divisor((uint32_t)part.per_row), (uint32_t)units, access_of<G>(y.p, y.ld),
+        static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld, from_row(saved, x.cols, r), from_row(saved_up, x.cols, r));
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -167,8 +167,8 @@ cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up
     const uint64_t units = std::min(part.most, dx.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        backward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, static_cast<const G*>(dy.p) + (dy.p ? r * dy.ld : 0), dy.ld, (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units,
-        access_of<G>(dy.p, dy.ld), out, from_row(saved, dx.cols, r), from_row(saved_up, dx.cols, r),
+        backward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(dy.p, dx.rows, dx.cols, dy.ld, r),
+        (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units, out, from_row(saved, dx.cols, r), from_row(saved_up, dx.cols, r),
         static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
     if (e != cudaSuccess) return e;
   }

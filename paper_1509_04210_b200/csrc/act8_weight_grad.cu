@@ -352,8 +352,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 // Planes of bf16 with rows of `pitch` values (whole threads) and `rows` of them (whole stages, the last
 // ones zero): dy itself, or the three parts of a float's significand.
 template <typename G>
-__global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, uint64_t ld, uint32_t tokens, uint32_t n, uint32_t pitch,
-                                                     uint64_t rows, Access access, uint4* __restrict__ out) {
+__global__ void __launch_bounds__(256) planes_kernel(Rows<G> dy, uint32_t tokens, uint32_t n, uint32_t pitch, uint64_t rows,
+                                                     uint4* __restrict__ out) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t per_row = pitch / kValues;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(256) planes_kernel(const G* __restrict__ dy, u
   const uint32_t c = (uint32_t)(i - row * per_row) * kValues;
   const int have = row < tokens && c < n ? (int)min((uint32_t)kValues, n - c) : 0;
   Values<G> v;
-  v.load(dy + (have ? row * ld + c : 0), access, have);
+  v.load(dy, have ? row * dy.ld + c : 0, have);
   if constexpr (sizeof(G) == 2) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) out[row * per_row * 2 + c / 8 + h] = make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]);
@@ -434,11 +434,11 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     const uint64_t blocks = (rows * (pitch / kValues) + 255) / 256;
     if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e =
-        dy.type == kF32 ? launch_after(planes_kernel<float>, (uint32_t)blocks, 256, 0, 1, stream, static_cast<const float*>(dy.p), dy.ld, (uint32_t)dy.rows,
-                                       (uint32_t)dy.cols, (uint32_t)pitch, rows, access_of<float>(dy.p, dy.ld), static_cast<uint4*>(workspace))
-                        : launch_after(planes_kernel<__nv_bfloat16>, (uint32_t)blocks, 256, 0, 1, stream, static_cast<const __nv_bfloat16*>(dy.p), dy.ld,
-                                       (uint32_t)dy.rows, (uint32_t)dy.cols, (uint32_t)pitch, rows, access_of<__nv_bfloat16>(dy.p, dy.ld),
-                                       static_cast<uint4*>(workspace));
+        dy.type == kF32 ? launch_after(planes_kernel<float>, (uint32_t)blocks, 256, 0, 1, stream, Rows<float>::of(dy.p, dy.rows, dy.cols, dy.ld, 0),
+                                       (uint32_t)dy.rows, (uint32_t)dy.cols, (uint32_t)pitch, rows, static_cast<uint4*>(workspace))
+                        : launch_after(planes_kernel<__nv_bfloat16>, (uint32_t)blocks, 256, 0, 1, stream,
+                                       Rows<__nv_bfloat16>::of(dy.p, dy.rows, dy.cols, dy.ld, 0), (uint32_t)dy.rows, (uint32_t)dy.cols,
+                                       (uint32_t)pitch, rows, static_cast<uint4*>(workspace));
     if (e != cudaSuccess) return e;
   }
   const uint64_t nb = (dw.cols + 31) / 32, scale_pitch = act8_scale_pitch(dw.cols);

@@ -16,9 +16,8 @@ constexpr int kThreads = 256;
 
 // Rows as they stand.  Eight lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
 template <typename G>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __restrict__ src, uint64_t ld, uint32_t cols, Divisor kt,
-                                                                 uint32_t items, Access access, uint2* __restrict__ codes,
-                                                                 uint32_t* __restrict__ scales) {
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(Rows<G> src, uint32_t cols, Divisor kt, uint32_t items,
+                                                                 uint2* __restrict__ codes, uint32_t* __restrict__ scales) {
   constexpr uint32_t U = 2, kItems = kThreads / 8;
   admit_next_kernel();
   await_previous_kernel();
@@ -32,7 +31,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const G* __rest
     k[u] = item - row[u] * kt.d;
     const uint32_t c = k[u] * 128 + lane * kValues;
     const int have = item < items && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-    x[u].template load<true>(src + (have ? row[u] * ld + c : 0), access, have);
+    x[u].template load<true>(src, have ? row[u] * src.ld + c : 0, have);
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
@@ -115,6 +114,7 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t nb = (cols + 31) / 32;
+  __shared__ Waiting waiting[kThreads / 32];
   uint2 w[U];
   uint8_t s[U];
   uint32_t row[U], c[U];
@@ -130,11 +130,11 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
-    if ((blockIdx.x * U + u) * kThreads + threadIdx.x >= units) continue;
-    const int have = (int)min((uint32_t)kValues, cols - c[u]);
-    float x[kValues];
-    e2m1_values(w[u], scale_value(s[u]), x);
-    store_values(dst + row[u] * ld + c[u], access, have, x);
+    const bool in = (blockIdx.x * U + u) * kThreads + threadIdx.x < units;
+    const int have = in ? (int)min((uint32_t)kValues, cols - c[u]) : 0;
+    float x[kValues] = {};
+    if (in) e2m1_values(w[u], scale_value(s[u]), x);
+    store_values(waiting[threadIdx.x / 32], dst + (in ? row[u] * ld + c[u] : 0), access, have, x);
   }
 }
 
@@ -150,8 +150,8 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
       const uint64_t rows = std::min(most, m.rows - r);
       if (rows * kt > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
       const cudaError_t e = launch_after(
-          quantize_rows_kernel<G>, grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, 1, stream, src + r * m.ld, m.ld, (uint32_t)m.cols,
-          Divisor((uint32_t)kt), (uint32_t)(rows * kt), access_of<G>(src, m.ld), static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2,
+          quantize_rows_kernel<G>, grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, 1, stream,
+          Rows<G>::of(m.p, m.rows, m.cols, m.ld, r), (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2,
           static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
       if (e != cudaSuccess) return e;
     }

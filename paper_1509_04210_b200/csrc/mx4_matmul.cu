@@ -43,9 +43,6 @@ template <int COLS, bool QUANTIZE> struct Shape {
 struct Params {
   const uint8_t* lane_scales;     // of b
   const uint8_t* column_scales;   // of a
-  const void* x;                  // or a as it came
-  uint64_t ldx;
-  Access access;
   void* y;
   uint64_t ldy;
   uint32_t m, n, k;               // rows of a, rows of b, their length
@@ -70,7 +67,8 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
 // X: type of x where it is brought to MX4 here, else void.
 template <typename G, int COLS, typename X>
 __global__ void __launch_bounds__(Shape<COLS, !std::is_void<X>::value>::kThreads)
-matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map, const __grid_constant__ Params p) {
+matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map, const __grid_constant__ Params p,
+              const __grid_constant__ Rows<typename std::conditional<std::is_void<X>::value, float, X>::type> x) {
   constexpr bool kQuantize = !std::is_void<X>::value;
   using S = Shape<COLS, kQuantize>;
   extern __shared__ uint8_t raw[];
@@ -155,7 +153,6 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
   } else if (kQuantize) {
     // a warp brings every eighth stage's values to MX4, where TMA and the bulk copies would have put them
     using T = typename std::conditional<kQuantize, X, float>::type;
-    const T* x = static_cast<const T*>(p.x);
     for (uint32_t i = first + (warp - 2); i < last; i += S::kQuantizers) {
       const uint32_t c = i - first, s = c % S::kStages;
       uint8_t* stage = smem + s * S::kStage + S::kLanes;
@@ -169,7 +166,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
         for (uint32_t h = 0; h < 4; ++h) {
           const uint32_t r = r0 + 2 * h + lane / 16;
           const int some = r < p.m ? have : 0;
-          v[h].load(x + (some ? r * p.ldx + k0 : 0), p.access, some);
+          v[h].load(x, some ? r * x.ld + k0 : 0, some);
         }
         if (!free && !(ok = free = barrier_wait(empty + 8 * s, (c / S::kStages & 1) ^ 1))) break;
 #pragma unroll
@@ -227,6 +224,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
 template <typename G, int COLS, typename X>
 cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   using S = Shape<COLS, !std::is_void<X>::value>;
+  using T = typename std::conditional<std::is_void<X>::value, float, X>::type;
   static Device device;
   const Device::Facts* facts;
   cudaError_t e = device.prepare(matmul_kernel<G, COLS, X>, S::kThreads, S::kSmem, &facts);
@@ -235,11 +233,6 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
   const uint64_t nb = (b.cols + 31) / 32;
   p.lane_scales = static_cast<const uint8_t*>(b.scales);
   p.column_scales = static_cast<const uint8_t*>(a.scales);
-  if (x) {
-    p.x = x->p;
-    p.ldx = x->ld;
-    p.access = sizeof(typename std::conditional<std::is_void<X>::value, float, X>::type) == 2 ? access_of<__nv_bfloat16>(x->p, x->ld) : access_of<float>(x->p, x->ld);
-  }
   p.y = y.p;
   p.ldy = y.ld;
   p.m = (uint32_t)y.rows;
@@ -256,7 +249,8 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * 16, b.rows, nb * 16, 128);
   if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * 16, a.rows, nb * 16, COLS);
   if (e != cudaSuccess) return e;
-  return launch_after(matmul_kernel<G, COLS, X>, (uint32_t)(tiles * p.split), S::kThreads, S::kSmem, p.split, stream, lane_map, column_map, p);
+  return launch_after(matmul_kernel<G, COLS, X>, (uint32_t)(tiles * p.split), S::kThreads, S::kSmem, p.split, stream, lane_map, column_map, p,
+                      x ? Rows<T>::of(x->p, x->rows, x->cols, x->ld, 0) : Rows<T>::of(nullptr, 0, 0, 0, 0));
 }
 
 template <typename G> cudaError_t by_rows(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {

@@ -495,3 +495,19 @@ def test_refusals_on_the_gpu():
     with pytest.raises(rb.RudraError) as e:
         L.mx4_quantize(x, out=L.MX4(off, q.scales, 4, 64))      # codes not on a 32-byte boundary
     assert e.value.code == rb.E_INVAL and "32-byte" in str(e.value)
+
+
+def test_learners_train_through_the_server():
+    # weights pulled in 4 bits, products, checkpoints and gradients of all operators together: the loss of a
+    # 40-class problem starts near ln 40 = 3.7 and has to fall by a quarter at least
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "learner_step.py")
+    spec = importlib.util.spec_from_file_location("learner_step", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.train(updates=150)
+    assert len(losses) >= 300 and np.isfinite(losses).all()
+    first, last = np.mean(losses[:20]), np.mean(losses[-20:])
+    assert 3.0 < first < 4.5 and last < 0.75 * first, (first, last)

@@ -123,3 +123,35 @@ def test_python_refuses_tensors_that_are_not_on_the_gpu():
         learner.act8_forward("none", torch.zeros(4, 32))
     with pytest.raises(ValueError):
         learner.mx4_dequantize(learner.MX4(torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 4, 32))
+
+
+PROGRAM = r"""
+#include <stdio.h>
+#include "rudra_learner.h"
+
+int main(void) {
+  if (rudra_mx4_codes_bytes(3, 33) != 3 * 32 || rudra_act8_scales_bytes(2, 513) != 64) return 1;
+  if (rudra_mx4_quantize(NULL, RUDRA_F32, 4, 64, 64, 0, NULL, NULL, NULL) != RUDRA_E_INVAL) return 2;
+  if (rudra_act8_forward(RUDRA_ACT_SWIGLU + 1, NULL, NULL, RUDRA_BF16, 0, 0, 0, NULL, 0, NULL, NULL, NULL, NULL, NULL) != RUDRA_E_INVAL) return 3;
+  if (rudra_ps_pull_mx4(NULL, 0, 1, 1, 0, NULL, NULL) != RUDRA_E_INVAL) return 4;
+  if (rudra_mx4_quantize(NULL, RUDRA_F32, 0, 64, 64, 0, NULL, NULL, NULL) != 0) return 5;
+  puts(rudra_last_error());
+  return 0;
+}
+"""
+
+
+def test_the_header_is_plain_c():
+    import subprocess
+    import tempfile
+
+    lib = rb.library_path()
+    rb.lib()
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "t.c"), os.path.join(d, "t")
+        with open(src, "w") as f:
+            f.write(PROGRAM)
+        subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-pedantic", "-I", os.path.join(ROOT, "include"), src, lib,
+                               "-Wl,-rpath," + os.path.dirname(lib), "-o", exe])
+        out = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+        assert out.returncode == 0 and "handle" in out.stdout, (out.returncode, out.stdout, out.stderr)
