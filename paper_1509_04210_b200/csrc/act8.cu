@@ -2,6 +2,9 @@
 // pass) and backward (slope from the checkpoint).  Element-wise but for a block's shared scale, so bound
 // by HBM: per value and input 2G + 33/32 bytes each way (G = 2 bf16, 4 f32).  Sigmoids are formed from the
 // approximate base-2 exponential and reciprocal, each within about 2 units in the last place of 32 bits.
+// Measured at 8192 x 4096: silu in f32 46.3 us each way = 6.5 TB/s, swiglu in bf16 42.7 and 42.9 us = 6.3 TB/s,
+// gelu in bf16 27.4 and 28.5 us = 6.2 and 5.9 TB/s (with the plain exponential, reciprocal and a clamp of
+// each value by itself 35 and 39 us: the instructions were the bound); the checkpoint alone of bf16 18.7 us.
 #include <algorithm>
 
 #include "blocks.cuh"
@@ -11,7 +14,7 @@
 namespace rudra {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 128;   // swiglu backward 45.6 us; 48.4 with 256
 
 constexpr float kLog2e = 1.4426950408889634f;
 

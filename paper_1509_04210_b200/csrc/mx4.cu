@@ -2,7 +2,9 @@
 //
 // A block's scale is a power of two read off the exponent field of its largest magnitude, so scaling
 // is exact and the only rounding is the one to E2M1, done by the conversion instruction.  One read and
-// 17/32 byte written per value: bound by HBM for large matrices, by launch latency for small ones.
+// 17/32 byte written per value: bound by HBM for large matrices, by launch latency for small ones.  Measured:
+// 4096 x 9216 floats 28.0 us = 6.1 TB/s, transposed 34.0 us = 5.0 TB/s (a thread holds 64 values, so fewer are on
+// their way), expanded to bf16 13.6 us = 7.0 TB/s; 4 x 4096 bf16 1.9 us.
 #include <algorithm>
 
 #include "blocks.cuh"
