@@ -403,7 +403,7 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   using T = Tile<PAIR>;
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR>, Groups<G>::kThreads, kSmem, &facts);
+  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR>, Groups<G>::kThreads, kSmem, Groups<G>::kLaunch, &facts);
   if (e != cudaSuccess) return e;
   p.chain = sizeof(G) == 4 ? kChain : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;

@@ -231,7 +231,7 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
   using T = typename std::conditional<std::is_void<X>::value, float, X>::type;
   static Device device;
   const Device::Facts* facts;
-  cudaError_t e = device.prepare(matmul_kernel<G, COLS, X>, S::kThreads, S::kSmem, &facts);
+  cudaError_t e = device.prepare(matmul_kernel<G, COLS, X>, S::kThreads, S::kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   Params p = {};
   const uint64_t nb = (b.cols + 31) / 32;

@@ -187,7 +187,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
 template <typename G> cudaError_t launch(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  cudaError_t e = device.prepare(matmul_pair_kernel<G>, kThreads, kSmem, &facts);
+  cudaError_t e = device.prepare(matmul_pair_kernel<G>, kThreads, kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t nb = (a.cols + 31) / 32, kt = (nb + 3) / 4, lane_tiles = (b.rows + kTile - 1) / kTile;
   const uint64_t tiles = lane_tiles * ((a.rows + kTile - 1) / kTile);

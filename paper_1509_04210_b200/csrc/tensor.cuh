@@ -248,7 +248,9 @@ class Device {
     int sms;
     int clusters[4];   // of 1, 2, 4 and 8 blocks
   };
-  template <typename K> cudaError_t prepare(K* kernel, uint32_t threads, uint32_t bytes, const Facts** facts) {
+  // `registers`: those of a thread that the kernel hands around between its warpgroups, 0 if it does not.  A build that gave it
+  // fewer would wait for registers that never come, and is refused.
+  template <typename K> cudaError_t prepare(K* kernel, uint32_t threads, uint32_t bytes, int registers, const Facts** facts) {
     int d = 0;
     cudaError_t e = cudaGetDevice(&d);
     if (e != cudaSuccess) return e;
@@ -259,6 +261,9 @@ class Device {
         Facts f = {};
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&f.sms, cudaDevAttrMultiProcessorCount, d);
+        cudaFuncAttributes attributes = {};
+        if (e == cudaSuccess && registers) e = cudaFuncGetAttributes(&attributes, kernel);
+        if (e == cudaSuccess && registers && attributes.numRegs != registers) e = cudaErrorInvalidKernelImage;
         f.clusters[0] = f.sms;
         for (int i = 1; e == cudaSuccess && i < 4; ++i) {
           cudaLaunchConfig_t cfg = {};

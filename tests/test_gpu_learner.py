@@ -344,12 +344,21 @@ def test_weight_gradient_against_the_definition(t, n, k, dtype, pad, shift, out)
     got = L.act8_weight_grad(dy, saved, kind)
     g, xq = dyh.astype(np.float64), ref.act8_values(xh)
     want, size = _product(np.ascontiguousarray(g.T), np.ascontiguousarray(xq.T))
-    _close(_np(got), want, max(t, 8) * EPS * size + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0.0))
+    _close(_np(got), want, _sum_tol(t, out) * size + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0.0))
     # the same, written into a flat vector that is to be pushed, at an odd place, with canaries around it
     flat = torch.full((n * k + 20,), 7.0, dtype=kind, device="cuda")
     L.act8_weight_grad(dy, saved, out=flat[13:13 + n * k].view(n, k))
     assert torch.equal(flat[13:13 + n * k].view(n, k), got)
     assert bool((flat[:13] == 7.0).all()) and bool((flat[13 + n * k:] == 7.0).all())
+
+
+def _sum_tol(t, out):
+    """Error of a weight gradient's sum over t tokens, of the sum of magnitudes.  A step of 16 products is cut off below the
+    last place of its largest term, 17 terms by half a unit each at most; an f32 result is gathered every 256
+    tokens (16 steps, 9 units each at most) and the parts, three times as many for f32 gradients, are added with
+    half a unit each.  Never more than a unit for every token."""
+    gathered = 144 + 3 * (t // 256 + 1) if out == "f32" else 9 * (t // 16 + 1)
+    return min(max(t, 8), gathered) * EPS
 
 
 def test_weight_gradient_is_the_derivative_of_the_layer():
@@ -495,6 +504,56 @@ def test_refusals_on_the_gpu():
     with pytest.raises(rb.RudraError) as e:
         L.mx4_quantize(x, out=L.MX4(off, q.scales, 4, 64))      # codes not on a 32-byte boundary
     assert e.value.code == rb.E_INVAL and "32-byte" in str(e.value)
+
+
+def test_matrices_of_more_than_2_to_the_32_values():
+    # every offset on the way is 64 bits wide: rows from both ends and from around the boundaries have to come out
+    # as they do by themselves
+    L, torch = _learner(), _torch()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    rows, cols = 67000, 65536                                       # 4.39e9 values
+    pick = torch.tensor([0, 1, 32767, 32768, 65535, 65536, rows - 2, rows - 1], device="cuda")
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, 8000):
+        x[r:r + 8000].normal_()
+    few = x[pick].contiguous()
+    q = L.mx4_quantize(x)
+    assert torch.equal(q.codes[pick], L.mx4_quantize(few).codes)
+    back = L.mx4_dequantize(q)
+    assert torch.equal(back[pick], L.mx4_dequantize(L.mx4_quantize(few)))
+    del back
+    turned = L.mx4_quantize(x[:, :64], transpose=True)               # blocks down columns that lie 128 KB apart
+    assert torch.equal(L.mx4_dequantize(turned), L.mx4_dequantize(L.mx4_quantize(x[:, :64].contiguous(), transpose=True)))
+    del turned
+    y, saved = L.act8_forward("silu", x)
+    y2, saved2 = L.act8_forward("silu", few)
+    assert torch.equal(y[pick], y2) and torch.equal(saved.codes[pick], saved2.codes)
+    used = (cols + 31) // 32
+    assert torch.equal(saved.scales[pick, :used], saved2.scales[:, :used])
+    dx = L.act8_backward("silu", x, saved, out=y)
+    assert torch.equal(dx[pick], L.act8_backward("silu", few, saved2))
+    del dx, y
+    one = torch.full((rows, 8), 1.0, dtype=torch.bfloat16, device="cuda")
+    dw = L.act8_weight_grad(one, saved)                              # the checkpoint's rows pass 2^32 bytes
+    want = L.act8_values(saved)
+    total, size = torch.zeros((2, cols), dtype=torch.float64, device="cuda")
+    for r in range(0, rows, 8000):
+        part = want[r:r + 8000].double()
+        total += part.sum(0)
+        size += part.abs().sum(0)
+    assert bool(((dw[3].double() - total).abs() <= _sum_tol(rows, "f32") * size).all())
+    del want, saved, q, x
+    a = torch.randn((rows, 64), device="cuda")
+    b = torch.randn((cols, 64), device="cuda")
+    w = L.mx4_quantize(b)
+    big = L.mx4_matmul(a, w)                                         # a product of 2^32 values and more
+    assert torch.equal(big[pick], L.mx4_matmul(a[pick].contiguous(), w))
+    del big
+    t, s = torch.randn((1, cols), device="cuda").bfloat16(), L.act8_save(torch.randn((1, rows), device="cuda"))
+    big = L.act8_weight_grad(t, s, torch.bfloat16)                   # cols x rows outputs
+    at = torch.tensor([0, 1, 32768, 65535], device="cuda")
+    assert torch.equal(big[at], L.act8_weight_grad(t[:, at].contiguous(), s, torch.bfloat16))
 
 
 def test_learners_train_through_the_server():
