@@ -18,10 +18,11 @@
  * nothing thrown or aborted, all work enqueued on cuda_stream (NULL: the legacy default stream) of
  * the current device and asynchronous to the host, nothing allocated, no state between calls.
  * Matrices are row-major; ld is the distance between rows in elements (ld >= row length) and a
- * matrix of dtype may start at any multiple of its element size.  Rows that start on 16-byte (bf16)
- * or 32-byte (f32) boundaries are moved by wide accesses; others by element.  Sizes may be zero
- * (a sum over nothing is zero) and are at most RUDRA_MAX_DIM each.  Outputs must not overlap inputs,
- * except that rudra_act8_backward may write a gradient over dy where both have one layout.
+ * matrix of dtype may start at any multiple of its element size; rows on 32-byte boundaries are the
+ * fastest.  What lies between the rows of a matrix that is read may be read too, but is not used;
+ * what lies between the rows of a matrix that is written is left alone.  Sizes may be zero (a sum
+ * over nothing is zero) and are at most RUDRA_MAX_DIM each.  Outputs must not overlap inputs, except
+ * that rudra_act8_backward may write a gradient over dy where both have one layout.
  */
 #ifndef RUDRA_LEARNER_H
 #define RUDRA_LEARNER_H

@@ -305,10 +305,12 @@ def test_activations_far_out():
         assert dx[0, 0] == 1.0 and dx[0, 1] == 0.0 and dx[1, 0] == 1.0 and dx[1, 1] == 0.0
 
 
-def test_gradient_may_overwrite_dy():
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pad,shift", [(9, 300, 0, 0), (700, 1001, 0, 0), (300, 515, 3, 1)])
+def test_gradient_may_overwrite_dy(dtype, rows, cols, pad, shift):
     L, torch = _learner(), _torch()
-    x, _ = _dev(_normal(9, 300, 1.0, 5), "bf16")
-    dy, _ = _dev(_normal(9, 300, 1.0, 6), "bf16")
+    x, _ = _dev(_normal(rows, cols, 1.0, 5), dtype)
+    dy, _ = _dev(_normal(rows, cols, 1.0, 6), dtype, pad, shift)
     _, saved = L.act8_forward("gelu", x)
     want = L.act8_backward("gelu", dy, saved)
     L.act8_backward("gelu", dy, saved, out=dy)
