@@ -18,11 +18,11 @@
 // A block (or pair) walks over its tiles with two accumulators: while one is taken out the other is
 // filled.  The tensor core truncates where it adds to an accumulator, which costs half a unit in the
 // last place every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken
-// out every kChain stages and the parts are added in registers, rounding to nearest (8192 tokens: an error
-// of 1e-7 instead of 1e-5); a bf16 result keeps 16 bits fewer and is taken out once.
+// out every kChain stages and the parts are added in registers, rounding to nearest (509 tokens in three planes: an
+// error of 2e-7 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out once.
 //
 // Measured: 8192 x 4096 x 4096 to bf16 212 us = 1.30 PFLOP/s, 0.78 of the measured bf16 rate (171 us if nothing had to
-// be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 260 us; 128 x 4096 x 9216 to f32 32 us =
+// be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 235 us; 128 x 4096 x 9216 to f32 32 us =
 // 4.8 TB/s, bound by its 151 MB of results.  Repeated for long the first runs into the power cap (1.56 GHz) and
 // takes 250 us.
 //
@@ -45,7 +45,9 @@ constexpr uint32_t kCodes = kBlockK * kTokens, kScales = 16 * kTokens, kSlots = 
 constexpr uint32_t kSmem = 1024 + kStages * kStage + kSlots * (kCodes + kScales) + 256;
 static_assert(kSmem <= 227 * 1024, "does not fit an SM");
 static_assert(kBlockN * 512 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
-constexpr uint32_t kChain = 4;       // stages in one accumulator where the result is f32
+// Stages in one accumulator where the result is f32: 8192 x 4096 x 4096 takes 259, 235 and 225 us with 4, 8 and 16, and is
+// off by 1.4e-7, 2.0e-7 and 4.0e-7.
+constexpr uint32_t kChain = 8;
 
 // Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out, the
 // others expand, each every third or fourth stage; and the registers of a thread by its group, of those
@@ -461,7 +463,7 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   p.stages = p.token_stages * (uint32_t)planes;
   // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 tokens: 144 tiles of 1536 x 1536 27.3 us
   // and 31.7 by pairs, 256 tiles of 2048 x 2048 47.5 and 33.2).
-  const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > 148;
+  const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > kSms;
   if (dw.type == kBF16)
     return pair ? launch<__nv_bfloat16, true>(dy_map, codes_map, scales_map, p, stream) : launch<__nv_bfloat16, false>(dy_map, codes_map, scales_map, p, stream);
   return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);

@@ -280,7 +280,7 @@ cudaError_t launch_mx4_matmul(const Mx4& a, const Mx4& b, const MatrixOut& y, cu
   if (a.cols == 0) return nothing(y, stream);
   // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 values: 128 tiles of 512 x 4096 8.0 us
   // and 10.2 by pairs, 256 tiles of 1024 x 4096 15.0 and 10.8).
-  if (((a.rows + 127) / 128) * ((b.rows + 127) / 128) > 148) return launch_mx4_matmul_pair(a, b, y, stream);
+  if (((a.rows + 127) / 128) * ((b.rows + 127) / 128) > kSms) return launch_mx4_matmul_pair(a, b, y, stream);
   return y.type == kBF16 ? by_rows<__nv_bfloat16>(a, b, y, stream) : by_rows<float>(a, b, y, stream);
 }
 

@@ -227,6 +227,8 @@ __device__ __forceinline__ uint64_t scale_rows(uint32_t at) {
 
 // ---------------------------------------------------------------------------------------- host
 
+constexpr uint64_t kSms = 148;   // of a B200
+
 // cuTensorMapEncodeTiled, looked up in the driver once.
 inline PFN_cuTensorMapEncodeTiled map_encoder() {
   static const PFN_cuTensorMapEncodeTiled fn = []() -> PFN_cuTensorMapEncodeTiled {
