@@ -77,9 +77,18 @@ struct Restored {
   __device__ __forceinline__ void values(float (&x)[kValues]) const { int8_values(w, scale_value(s), x); }
 };
 
+template <bool ANY, typename G> __device__ __forceinline__ void write(G* p, Access access, int have, const float (&x)[kValues]) {
+  if constexpr (ANY) {
+    __shared__ Meeting meeting[kThreads / 32];
+    store_values_anyhow(meeting[threadIdx.x / 32], p, have, x);
+  } else {
+    store_values(p, access, have, x);
+  }
+}
+
 // Checkpoint rows are whole blocks of two units (of a thread's values), so unit numbers run through the
 // checkpoint without gaps and neighbouring lanes share a block.
-template <typename G, Act A>
+template <typename G, Act A, bool ANY>
 __global__ void __launch_bounds__(kThreads) forward_kernel(Rows<G> x, Rows<G> up, uint32_t cols, Divisor per_row, uint32_t units,
                                                            Access access_out, G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
   admit_next_kernel();
@@ -89,31 +98,29 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(Rows<G> x, Rows<G> up
   const int have = in && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
   const uint64_t at = have ? row * x.ld + c : 0;
   Values<G> a, b;
-  a.load(x, at, have);
-  if (A == kSwiglu) b.load(up, at, have);
+  a.template load<ANY>(x, at, have);
+  if (A == kSwiglu) b.template load<ANY>(up, at, have);
   save(saved, i, row, c / 32, a, in);
   if (A == kSwiglu) save(saved_up, i, row, c / 32, b, in);
   if constexpr (A != kNone) {
-    __shared__ Waiting waiting[kThreads / 32];
     float v[kValues];
 #pragma unroll
     for (int e = 0; e < kValues; ++e) v[e] = A == kSwiglu ? value<A>(a.get(e)) * b.get(e) : value<A>(a.get(e));
-    store_values(waiting[threadIdx.x / 32], y + (have ? row * ldy + c : 0), access_out, have, v);
+    write<ANY>(y + (have ? row * ldy + c : 0), access_out, have, v);
   }
 }
 
-template <typename G, Act A>
+template <typename G, Act A, bool ANY>
 __global__ void __launch_bounds__(kThreads) backward_kernel(Rows<G> dy, uint32_t cols, Divisor per_row, uint32_t units, Access access_out, Saved saved,
                                                             Saved saved_up, G* dx, G* dup, uint64_t lddx) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;
   const int have = i < units && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-  __shared__ Waiting waiting[kThreads / 32];
   Values<G> g;
   Restored rx = {}, ru = {};
   if (have) {
-    if (A != kNone) g.load(dy, row * dy.ld + c, have);
+    if (A != kNone) g.template load<ANY>(dy, row * dy.ld + c, have);
     rx.load(saved, i, row, c / 32);
     if (A == kSwiglu) ru.load(saved_up, i, row, c / 32);
   }
@@ -130,8 +137,8 @@ __global__ void __launch_bounds__(kThreads) backward_kernel(Rows<G> dy, uint32_t
     }
   }
   const uint64_t at = have ? row * lddx + c : 0;
-  store_values(waiting[threadIdx.x / 32], dx + at, access_out, have, x);
-  if (A == kSwiglu) store_values(waiting[threadIdx.x / 32], dup + at, access_out, have, u);
+  write<ANY>(dx + at, access_out, have, x);
+  if (A == kSwiglu) write<ANY>(dup + at, access_out, have, u);
 }
 
 // Rows of a launch: as many as keep the number of its units below 2^31.
@@ -150,12 +157,15 @@ Saved from_row(const Act8& a, uint64_t cols, uint64_t r) {
 template <typename G, Act A>
 cudaError_t forward(const MatrixIn& x, const void* up, const MatrixOut& y, const Act8& saved, const Act8& saved_up, cudaStream_t stream) {
   const Part part(x.cols);
+  const Access in = A == kSwiglu ? both(access_of<G>(x.p, x.ld), access_of<G>(up, x.ld)) : access_of<G>(x.p, x.ld);
+  const Access out = access_of<G>(y.p, A == kNone ? 0 : y.ld);
+  const bool anyhow = in == kByElement || out == kByElement;
   for (uint64_t r = 0; r < x.rows; r += part.most) {
     const uint64_t units = std::min(part.most, x.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        forward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(x.p, x.rows, x.cols, x.ld, r),
-        Rows<G>::of(up, x.rows, x.cols, x.ld, r), (uint32_t)x.cols, Divisor((uint32_t)part.per_row), (uint32_t)units, access_of<G>(y.p, y.ld),
+        anyhow ? forward_kernel<G, A, true> : forward_kernel<G, A, false>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(x.p, x.rows, x.cols, x.ld, r),
+        Rows<G>::of(up, x.rows, x.cols, x.ld, r), (uint32_t)x.cols, Divisor((uint32_t)part.per_row), (uint32_t)units, out,
         static_cast<G*>(y.p) + (y.p ? r * y.ld : 0), y.ld, from_row(saved, x.cols, r), from_row(saved_up, x.cols, r));
     if (e != cudaSuccess) return e;
   }
@@ -166,11 +176,12 @@ template <typename G, Act A>
 cudaError_t backward(const MatrixIn& dy, const Act8& saved, const Act8& saved_up, const MatrixOut& dx, void* dup, cudaStream_t stream) {
   const Part part(dx.cols);
   const Access out = A == kSwiglu ? both(access_of<G>(dx.p, dx.ld), access_of<G>(dup, dx.ld)) : access_of<G>(dx.p, dx.ld);
+  const bool anyhow = out == kByElement || (A != kNone && access_of<G>(dy.p, dy.ld) == kByElement);
   for (uint64_t r = 0; r < dx.rows; r += part.most) {
     const uint64_t units = std::min(part.most, dx.rows - r) * part.per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        backward_kernel<G, A>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(dy.p, dx.rows, dx.cols, dy.ld, r),
+        anyhow ? backward_kernel<G, A, true> : backward_kernel<G, A, false>, (uint32_t)((units + kThreads - 1) / kThreads), kThreads, 0, 1, stream, Rows<G>::of(dy.p, dx.rows, dx.cols, dy.ld, r),
         (uint32_t)dx.cols, Divisor((uint32_t)part.per_row), (uint32_t)units, out, from_row(saved, dx.cols, r), from_row(saved_up, dx.cols, r),
         static_cast<G*>(dx.p) + r * dx.ld, static_cast<G*>(dup) + (dup ? r * dx.ld : 0), dx.ld);
     if (e != cudaSuccess) return e;

@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(256) planes_kernel(Rows<G> dy, uint32_t tokens
   const uint32_t c = (uint32_t)(i - row * per_row) * kValues;
   const int have = row < tokens && c < n ? (int)min((uint32_t)kValues, n - c) : 0;
   Values<G> v;
-  v.load(dy, have ? row * dy.ld + c : 0, have);
+  v.template load<true>(dy, have ? row * dy.ld + c : 0, have);
   if constexpr (sizeof(G) == 2) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) out[row * per_row * 2 + c / 8 + h] = make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]);

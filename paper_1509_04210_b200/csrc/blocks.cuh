@@ -54,8 +54,8 @@ template <typename G> struct Values {
                    : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q));
   }
 
-  // `have` values from element `at` of the matrix; the others are zero.
-  template <bool FIRST = false> __device__ __forceinline__ void load(const Rows<G>& m, uint64_t at, int have) {
+  // `have` values from element `at` of the matrix; the others are zero.  ANY: its rows may lie anyhow.
+  template <bool ANY, bool FIRST = false> __device__ __forceinline__ void load(const Rows<G>& m, uint64_t at, int have) {
     const G* p = m.p + at;
     if (have == kValues && m.access == kBy32) {
 #pragma unroll
@@ -74,7 +74,7 @@ template <typename G> struct Values {
     // element, 40.1 this way.)
     const uintptr_t from = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)31;
     const uintptr_t to = (reinterpret_cast<uintptr_t>(p) + kValues * sizeof(G) + 31) & ~(uintptr_t)31;
-    if (have > 0 && from >= reinterpret_cast<uintptr_t>(m.p) && to <= reinterpret_cast<uintptr_t>(m.end)) {
+    if (ANY && have > 0 && from >= reinterpret_cast<uintptr_t>(m.p) && to <= reinterpret_cast<uintptr_t>(m.end)) {
       uint32_t r[kWords + 8];
       const uint32_t* q = reinterpret_cast<const uint32_t*>(from);
 #pragma unroll
@@ -134,57 +134,84 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// Where a warp's values wait to be written element by element: rows that lie anyhow are written with neighbouring
-// lanes on neighbouring elements.  (Expansion of 4096 x 9215 codes to bf16: 225 us with 16 elements a lane, 36
-// this way.)
-struct Waiting {
-  float v[32][kValues + 1];
+// Where the values of a warp meet when their rows lie anyhow.
+struct alignas(16) Meeting {
+  uint32_t words[32 * (kValues + 1)];
   uint64_t to[32];
   int have[32];
 };
 
-// Writes `have` of a thread's values at p.  A whole warp calls it.
-template <typename G>
-__device__ __forceinline__ void store_values(Waiting& wait, G* p, Access access, int have, const float (&x)[kValues]) {
+// Writes `have` of a thread's values at p, rows on boundaries of 16 or 32 bytes.
+template <typename G> __device__ __forceinline__ void store_values(G* p, Access access, int have, const float (&x)[kValues]) {
   constexpr int kWords = kValues * sizeof(G) / 4;
-  if (access != kByElement) {
-    uint32_t w[kWords];
+  uint32_t w[kWords];
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = sizeof(G) == 4 ? __float_as_uint(x[i]) : pack_bf16(x[2 * i % kValues], x[(2 * i + 1) % kValues]);
-    if (have == kValues && access == kBy32) {
+  for (int i = 0; i < kWords; ++i) w[i] = sizeof(G) == 4 ? __float_as_uint(x[i]) : pack_bf16(x[2 * i % kValues], x[(2 * i + 1) % kValues]);
+  if (have == kValues && access == kBy32) {
 #pragma unroll
-      for (int i = 0; i < kWords; i += 8)
-        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                     :: "l"(reinterpret_cast<uint32_t*>(p) + i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]),
-                        "r"(w[i + 6]), "r"(w[i + 7]) : "memory");
-    } else if (have == kValues) {
+    for (int i = 0; i < kWords; i += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                   :: "l"(reinterpret_cast<uint32_t*>(p) + i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]),
+                      "r"(w[i + 6]), "r"(w[i + 7]) : "memory");
+  } else if (sizeof(G) == 2 && have == kValues && access == kBy16) {
 #pragma unroll
-      for (int i = 0; i < kWords; i += 4) reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-    } else {
+    for (int i = 0; i < kWords; i += 4) reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  } else {
 #pragma unroll
-      for (int i = 0; i < kValues; ++i)
-        if (i < have) {
-          if constexpr (sizeof(G) == 4) p[i] = x[i];
-          else p[i] = __float2bfloat16_rn(x[i]);
-        }
+    for (int i = 0; i < kValues; ++i)
+      if (i < have) {
+        if constexpr (sizeof(G) == 4) p[i] = x[i];
+        else p[i] = __float2bfloat16_rn(x[i]);
+      }
+  }
+}
+
+// The same to rows that lie anyhow; a whole warp calls it.  Expansion of 4096 x 9215 codes to bf16: 225 us with every lane writing
+// its own elements, 36 with neighbouring lanes on neighbouring elements, 27 with runs of bf16 moved to 16-byte boundaries (f32
+// gains nothing by that).
+template <typename G> __device__ __forceinline__ void store_values_anyhow(Meeting& m, G* p, int have, const float (&x)[kValues]) {
+  const int lane = threadIdx.x % 32;
+  constexpr int kPitch = sizeof(G) == 4 ? kValues + 1 : kValues;   // of a lane's values
+  const uint64_t to = reinterpret_cast<uint64_t>(p), next = __shfl_down_sync(0xFFFFFFFFu, to, 1);
+  __syncwarp();
+  if constexpr (sizeof(G) == 4) {
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) m.words[lane * kPitch + i] = __float_as_uint(x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kValues; i += 8)
+      *reinterpret_cast<uint4*>(m.words + (lane * kValues + i) / 2) =
+          make_uint4(pack_bf16(x[i], x[i + 1]), pack_bf16(x[i + 2], x[i + 3]), pack_bf16(x[i + 4], x[i + 5]), pack_bf16(x[i + 6], x[i + 7]));
+  }
+  m.to[lane] = to;
+  m.have[lane] = have;
+  __syncwarp();
+  const G* const values = reinterpret_cast<const G*>(m.words);
+  if (sizeof(G) == 2 && __all_sync(0xFFFFFFFFu, lane == 31 || (have == kValues && next == to + kValues * sizeof(G)))) {
+    // one run of elements: 16 bytes at a time on their boundaries, the words moved by the run's distance from one
+    G* const base = reinterpret_cast<G*>(m.to[0]);
+    const int total = 31 * kValues + m.have[31], head = min(total, (int)((16 - m.to[0] % 16) % 16 / 2));
+    const int pieces = (total - head) / 8, tail = head + 8 * pieces;
+    for (int j = lane; j < pieces; j += 32) {
+      uint32_t r[8];
+      *reinterpret_cast<uint4*>(r) = *reinterpret_cast<const uint4*>(m.words + 4 * j);
+      *reinterpret_cast<uint4*>(r + 4) = *reinterpret_cast<const uint4*>(m.words + 4 * j + 4);
+#pragma unroll
+      for (int i = 0; i < 6; ++i) r[i] = head & 4 ? r[i + 2] : r[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) r[i] = head & 2 ? r[i + 1] : r[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __funnelshift_r(r[i], r[i + 1], head % 2 * 16);
+      *reinterpret_cast<uint4*>(base + head + 8 * j) = make_uint4(r[0], r[1], r[2], r[3]);
     }
+    const int e = lane < head ? lane : tail + lane - head;
+    if (lane < head || e < total) base[e] = values[e];
     return;
   }
-  const int lane = threadIdx.x % 32;
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < kValues; ++i) wait.v[lane][i] = x[i];
-  wait.to[lane] = reinterpret_cast<uint64_t>(p);
-  wait.have[lane] = have;
-  __syncwarp();
 #pragma unroll 4
   for (int i = 0; i < kValues; ++i) {
     const int of = i * (32 / kValues) + lane / kValues, e = lane % kValues;
-    if (e < wait.have[of]) {
-      G* q = reinterpret_cast<G*>(wait.to[of]) + e;
-      if constexpr (sizeof(G) == 4) *q = wait.v[of][e];
-      else *q = __float2bfloat16_rn(wait.v[of][e]);
-    }
+    if (e < m.have[of]) reinterpret_cast<G*>(m.to[of])[e] = values[of * kPitch + e];
   }
 }
 

@@ -17,7 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // Rows as they stand.  Eight lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
-template <typename G>
+template <typename G, bool ANY>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(Rows<G> src, uint32_t cols, Divisor kt, uint32_t items,
                                                                  uint2* __restrict__ codes, uint32_t* __restrict__ scales) {
   constexpr uint32_t U = 2, kItems = kThreads / 8;
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(Rows<G> src, ui
     k[u] = item - row[u] * kt.d;
     const uint32_t c = k[u] * 128 + lane * kValues;
     const int have = item < items && c < cols ? (int)min((uint32_t)kValues, cols - c) : 0;
-    x[u].template load<true>(src, have ? row[u] * src.ld + c : 0, have);
+    x[u].template load<ANY, true>(src, have ? row[u] * src.ld + c : 0, have);
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
     scales[mx4_scale_at(row, (uint64_t)k * 4, kt) / 4] = *reinterpret_cast<const uint32_t*>(sbytes[threadIdx.x]);
 }
 
-template <typename G>
+template <typename G, bool ANY>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                               uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
                                                               G* __restrict__ dst, uint64_t ld) {
@@ -116,7 +116,6 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t nb = (cols + 31) / 32;
-  __shared__ Waiting waiting[kThreads / 32];
   uint2 w[U];
   uint8_t s[U];
   uint32_t row[U], c[U];
@@ -136,7 +135,13 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __res
     const int have = in ? (int)min((uint32_t)kValues, cols - c[u]) : 0;
     float x[kValues] = {};
     if (in) e2m1_values(w[u], scale_value(s[u]), x);
-    store_values(waiting[threadIdx.x / 32], dst + (in ? row[u] * ld + c[u] : 0), access, have, x);
+    G* const to = dst + (in ? row[u] * ld + c[u] : 0);
+    if constexpr (ANY) {
+      __shared__ Meeting meeting[kThreads / 32];
+      store_values_anyhow(meeting[threadIdx.x / 32], to, have, x);
+    } else {
+      store_values(to, access, have, x);
+    }
   }
 }
 
@@ -152,7 +157,7 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
       const uint64_t rows = std::min(most, m.rows - r);
       if (rows * kt > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
       const cudaError_t e = launch_after(
-          quantize_rows_kernel<G>, grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, 1, stream,
+          access_of<G>(m.p, m.ld) == kByElement ? quantize_rows_kernel<G, true> : quantize_rows_kernel<G, false>, grid_of(rows * kt, 2 * kThreads / 8), kThreads, 0, 1, stream,
           Rows<G>::of(m.p, m.rows, m.cols, m.ld, r), (uint32_t)m.cols, Divisor((uint32_t)kt), (uint32_t)(rows * kt), static_cast<uint2*>(codes) + r * ((m.cols + 31) / 32) * 2,
           static_cast<uint32_t*>(scales) + mx4_scale_at(r, 0, kt) / 4);
       if (e != cudaSuccess) return e;
@@ -174,7 +179,7 @@ cudaError_t dequantize(const Mx4& m, const MatrixOut& d, cudaStream_t stream) {
     const uint64_t units = std::min(most, m.rows - r) * per_row;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        dequantize_kernel<G>, grid_of(units, 2 * kThreads), kThreads, 0, 1, stream, static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
+        access_of<G>(d.p, d.ld) == kByElement ? dequantize_kernel<G, true> : dequantize_kernel<G, false>, grid_of(units, 2 * kThreads), kThreads, 0, 1, stream, static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
         Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, access_of<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
     if (e != cudaSuccess) return e;
   }

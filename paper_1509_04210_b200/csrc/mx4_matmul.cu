@@ -170,7 +170,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
         for (uint32_t h = 0; h < 4; ++h) {
           const uint32_t r = r0 + 2 * h + lane / 16;
           const int some = r < p.m ? have : 0;
-          v[h].load(x, some ? r * x.ld + k0 : 0, some);
+          v[h].template load<true>(x, some ? r * x.ld + k0 : 0, some);
         }
         if (!free && !(ok = free = barrier_wait(empty + 8 * s, (c / S::kStages & 1) ^ 1))) break;
 #pragma unroll
