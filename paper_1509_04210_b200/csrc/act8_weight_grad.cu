@@ -2,7 +2,7 @@
 // tensor cores.
 //
 // A code times its block's power of two is a bf16 number exactly, so the checkpoint is expanded to
-// bf16 between two places in shared memory (eight warps, integer and bf16 instructions only) and never exists
+// bf16 between two places in shared memory (12 or 16 warps, integer and bf16 instructions only) and never exists
 // wide in memory.  Both operands run along tokens, the reduction, so both sit in shared memory as they
 // sit in global memory, tokens as rows ("transposed" operands for the tensor core).  Inputs of the layer
 // (k) are the 128 lanes of an accumulator, outputs (n) its columns, so a warp writes 32 neighbouring

@@ -7,8 +7,8 @@
 // of a (tokens) its columns, so one shape serves a single token (16 columns) as well as a batch, and
 // neighbouring lanes write neighbouring outputs.
 //
-// Few tiles: the reduction is split over the blocks of a cluster.  Their parts
-// are added in rank order through distributed shared memory, so the sum does not depend on the run.
+// Few tiles: the reduction is split over the blocks of a cluster.  Their parts are added in rank order
+// through distributed shared memory, so the sum does not depend on the run.
 //
 // Up to 32 tokens the kernel can take x itself: every block brings its slice of the few rows to MX4 on
 // the way into shared memory, which costs less than another launch.
