@@ -27,7 +27,8 @@
 // takes 250 us.
 //
 // dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an
-// exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.
+// exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.  The three meet
+// one expansion of xhat (4096 x 2048 x 2048 to bf16 73 us; 86 with an expansion for each).
 #include <algorithm>
 
 #include "blocks.cuh"
@@ -40,14 +41,14 @@ namespace {
 
 constexpr uint32_t kBlockK = 128, kBlockN = 128, kTokens = 64;      // what a block holds of a stage: inputs, outputs, tokens
 constexpr uint32_t kChunk = 64 * 2 * kTokens;                       // 64 values wide, kTokens rows of 128 bytes
-constexpr uint32_t kStageX = 2 * kChunk, kStage = 4 * kChunk, kStages = 5;
+constexpr uint32_t kStage = 2 * kChunk, kStages = 5;                // of either operand: each has its own ring of five
 constexpr uint32_t kCodes = kBlockK * kTokens, kScales = 16 * kTokens, kSlots = 7;   // of the checkpoint; stages of it on their way
-constexpr uint32_t kSmem = 1024 + kStages * kStage + kSlots * (kCodes + kScales) + 256;
+constexpr uint32_t kSmem = 1024 + 2 * kStages * kStage + kSlots * (kCodes + kScales) + 384;
 static_assert(kSmem <= 227 * 1024, "does not fit an SM");
-static_assert(kBlockN * 512 <= kStages * kStage, "the parts of a split sum are kept where the stages were");
+static_assert(kBlockN * 512 <= 2 * kStages * kStage, "the parts of a split sum are kept where the stages were");
 // Stages in one accumulator where the result is f32: 8192 x 4096 x 4096 takes 259, 235 and 225 us with 4, 8 and 16, and is
 // off by 1.4e-7, 2.0e-7 and 4.0e-7.
-constexpr uint32_t kChain = 8;
+constexpr uint32_t kChain = 8;      // a third of it where dy comes in three planes
 
 // Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out, the
 // others expand, each every third or fourth stage; and the registers of a thread by its group, of those
@@ -70,8 +71,8 @@ struct Params {
   void* dw;
   uint64_t lddw;
   uint32_t n, k;
-  uint32_t token_stages;    // ceil(tokens / kTokens)
-  uint32_t stages;          // of the whole reduction: token_stages for each of dy's planes
+  uint32_t stages;          // ceil(tokens / kTokens)
+  uint32_t plane_rows;      // of dy's planes, which lie one under the other
   uint32_t lane_tiles, tiles;
   uint32_t chain;           // stages in one accumulator
   uint32_t split;           // blocks of a cluster that share a tile's tokens
@@ -112,7 +113,9 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
   return h | h << 16;
 }
 
-template <typename G, bool PAIR>
+// PLANES: matrices that dy is the sum of, 1 or 3.  A stage of xhat meets all of them; where there is one, the stages of both
+// operands share their barriers (two sets cost a stage 0.1 us).
+template <typename G, bool PAIR, uint32_t PLANES>
 __global__ void __launch_bounds__(Groups<G>::kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
                    const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
@@ -121,11 +124,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   constexpr uint32_t kExpanders = R::kExpanders;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t stage0 = smem_address(smem), codes0 = stage0 + kStages * kStage, scales0 = codes0 + kSlots * kCodes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage + kSlots * (kCodes + kScales));
-  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
-                 coded = drained + 16, taken = coded + 8 * kSlots;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4 + 2 * kSlots);
+  const uint32_t x0 = smem_address(smem), dy0 = x0 + kStages * kStage, codes0 = dy0 + kStages * kStage, scales0 = codes0 + kSlots * kCodes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kStages * kStage + kSlots * (kCodes + kScales));
+  const uint32_t x_full = smem_address(bars), x_empty = x_full + 8 * kStages, dy_full = PLANES == 1 ? x_full : x_empty + 8 * kStages,
+                 dy_empty = PLANES == 1 ? x_empty : dy_full + 8 * kStages, ready = x_empty + 24 * kStages, drained = ready + 16, coded = drained + 16, taken = coded + 8 * kSlots;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 4 * kStages + 4 + 2 * kSlots);
 
   const uint32_t warp = warp_index(), lane = threadIdx.x % 32;
   const uint32_t rank = PAIR || p.split > 1 ? cluster_rank() : 0;
@@ -138,8 +141,12 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     prefetch_map(&codes_map);
     prefetch_map(&scales_map);
     for (uint32_t s = 0; s < kStages; ++s) {
-      barrier_init(full + 8 * s, 1 + (PAIR ? 8 : 4));      // dy, and the four warps of a group of each block
-      barrier_init(empty + 8 * s, 1);
+      barrier_init(x_full + 8 * s, (PAIR ? 8 : 4) + (PLANES == 1));      // the four warps of a group of each block, and dy
+      barrier_init(x_empty + 8 * s, 1);
+      if (PLANES > 1) {
+        barrier_init(dy_full + 8 * s, 1);
+        barrier_init(dy_empty + 8 * s, 1);
+      }
     }
     for (uint32_t b = 0; b < 2; ++b) {
       barrier_init(ready + 8 * b, 1);
@@ -170,36 +177,37 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   if (warp < 4) {
     give_registers<R::kManage>();
     if (warp == 0) {
-      const uint32_t elected = elect(), first_full = PAIR ? peer_address(full, 0) : full;
+      const uint32_t elected = elect(), first_full = PAIR ? peer_address(dy_full, 0) : dy_full;
       uint32_t s = 0, parity = 1, issued = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         const int n0 = (int)(tile / p.lane_tiles * T::kN + (PAIR ? rank * kBlockN : 0));
-        for (uint32_t i = first; i < last; ++i, ++issued) {
-          const uint32_t at = stage0 + s * kStage + kStageX;
-          if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
-          if (!PAIR || rank == 0) barrier_expect(full + 8 * s, (PAIR ? 2 : 1) * (kStage - kStageX), elected);
+        for (uint32_t i = first; ok && i < last; ++i) {
+          for (uint32_t plane = 0, row = i * kTokens; plane < PLANES; ++plane, row += p.plane_rows, ++issued) {
+            const uint32_t at = dy0 + s * kStage;
+            if (!(ok = all_lanes(barrier_wait(dy_empty + 8 * s, parity)))) break;
+            if (!PAIR || rank == 0) barrier_expect(dy_full + 8 * s, (PAIR ? 2 : 1) * kStage, elected);
 #pragma unroll
-          for (uint32_t q = 0; q < kBlockN / 64; ++q) {
-            if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), first_full + 8 * s, elected);
-            else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)(i * kTokens), full + 8 * s, elected);
+            for (uint32_t q = 0; q < kBlockN / 64; ++q) {
+              if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, first_full + 8 * s, elected);
+              else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, dy_full + 8 * s, elected);
+            }
+            if (++s == kStages) s = 0, parity ^= 1;
           }
-          if (++s == kStages) s = 0, parity ^= 1;
         }
       }
       // given up: what is on its way has landed once every copy issued has had its time
       if (!ok && rank == 0)
-        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
+        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(dy_full + 8 * (j % kStages), j / kStages & 1);
     } else if (warp == 3) {
       const uint32_t elected = elect();
       uint32_t s = 0, parity = 1, issued = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         const int k0 = (int)(tile % p.lane_tiles * T::kK + (PAIR ? rank * kBlockK : 0));
-        for (uint32_t i = first, t = first % p.token_stages; i < last; ++i, ++issued) {
+        for (uint32_t i = first; i < last; ++i, ++issued) {
           if (!(ok = all_lanes(barrier_wait(taken + 8 * s, parity)))) break;
           barrier_expect(coded + 8 * s, kCodes + kScales, elected);
-          copy_box(codes0 + s * kCodes, &codes_map, k0, (int)(t * kTokens), coded + 8 * s, elected);
-          copy_box(scales0 + s * kScales, &scales_map, k0 / 512 * 16, (int)(t * kTokens), coded + 8 * s, elected);
-          if (++t == p.token_stages) t = 0;          // dy's next plane meets the same tokens
+          copy_box(codes0 + s * kCodes, &codes_map, k0, (int)(i * kTokens), coded + 8 * s, elected);
+          copy_box(scales0 + s * kScales, &scales_map, k0 / 512 * 16, (int)(i * kTokens), coded + 8 * s, elected);
           if (++s == kSlots) s = 0, parity ^= 1;
         }
       }
@@ -207,21 +215,29 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         for (uint32_t j = issued > kSlots ? issued - kSlots : 0; j < issued; ++j) barrier_wait(coded + 8 * (j % kSlots), j / kSlots & 1);
     } else if (warp == 1 && (!PAIR || rank == 0)) {
       const uint32_t elected = elect();
-      uint32_t q = 0, s = 0, parity = 0;     // accumulators so far; stage
+      uint32_t q = 0;     // accumulators so far
+      uint32_t sx = 0, px = 0, sdy = 0, pdy = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         for (uint32_t i = first; ok && i < last; ++q) {
           const uint32_t buffer = q & 1, d = tmem + buffer * T::kN, begin = i, end = min(last, i + p.chain);
           if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
           tmem_fence_after();
-          for (; i < end; ++i) {
-            if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
-            tmem_fence_after();
-            const uint32_t at = stage0 + s * kStage;
-            const uint64_t x = swizzled_columns(at, kChunk), dy = swizzled_columns(at + kStageX, kChunk);
+          for (; ok && i < end; ++i) {
+            if (!(ok = all_lanes(barrier_wait(x_full + 8 * sx, px)))) break;
+            const uint64_t x = swizzled_columns(x0 + sx * kStage, kChunk);
 #pragma unroll
-            for (uint32_t j = 0; j < kTokens / 16; ++j) multiply<PAIR>(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || j, elected);
-            commit<PAIR>(empty + 8 * s, elected);
-            if (++s == kStages) s = 0, parity ^= 1;
+            for (uint32_t plane = 0; plane < PLANES; ++plane) {
+              if (PLANES > 1 && !(ok = all_lanes(barrier_wait(dy_full + 8 * sdy, pdy)))) break;
+              tmem_fence_after();
+              const uint64_t dy = swizzled_columns(dy0 + sdy * kStage, kChunk);
+#pragma unroll
+              for (uint32_t j = 0; j < kTokens / 16; ++j)
+                multiply<PAIR>(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || plane || j, elected);
+              commit<PAIR>(dy_empty + 8 * sdy, elected);
+              if (++sdy == kStages) sdy = 0, pdy ^= 1;
+            }
+            if (PLANES > 1 && ok) commit<PAIR>(x_empty + 8 * sx, elected);
+            if (++sx == kStages) sx = 0, px ^= 1;
           }
           if (ok) commit<PAIR>(ready + 8 * buffer, elected);
         }
@@ -300,8 +316,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     // a thread expands two blocks of 32 values: tokens t and t + 32 of a stage, block b of the four
     const uint32_t mine = (warp - 12) / 4, t = warp % 4 * 8 + lane % 8, b = lane / 8, x = t % 8;
     const uint32_t from = codes0 + t * 128 + ((2 * b) ^ x) * 16, other = ((2 * b) ^ x) % 2 ? 0u - 16 : 16;   // a block's two 16-byte pieces
-    const uint32_t to = stage0 + (b / 2) * kChunk + t * 128, u0 = b % 2 * 4;
-    const uint32_t first_full = PAIR ? peer_address(full, 0) : full;
+    const uint32_t to = x0 + (b / 2) * kChunk + t * 128, u0 = b % 2 * 4;
+    const uint32_t first_full = PAIR ? peer_address(x_full, 0) : x_full;
     const uint32_t length = last - first, total = tile0 < p.tiles ? ((p.tiles - tile0 + tile_step - 1) / tile_step) * length : 0;
     uint32_t s = mine, sparity = 0, v = mine, vparity = 0;     // stage and slot, and which turn of theirs
     uint32_t tile = tile0, i = mine;
@@ -309,7 +325,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       for (; i >= length; i -= length) tile += tile_step;
       const uint32_t scale_at = scales0 + t * 16 + (tile % p.lane_tiles * (T::kK / 32) + (PAIR ? rank * 4 : 0) + b) % 16;
       i += kExpanders;
-      if (!(ok = barrier_wait(coded + 8 * v, vparity) && barrier_wait(empty + 8 * s, sparity ^ 1))) break;
+      if (!(ok = barrier_wait(coded + 8 * v, vparity) && barrier_wait(x_empty + 8 * s, sparity ^ 1))) break;
 #pragma unroll
       for (uint32_t h = 0; h < 2; ++h) {
         const uint32_t row = h * 32 * 128;
@@ -339,7 +355,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   __syncwarp();
   if (!PAIR && p.split > 1) {   // one tile to a cluster
     const uint32_t k0 = tile0 % p.lane_tiles * kBlockK, n0 = tile0 / p.lane_tiles * kBlockN;
-    join_parts(stage0, p.split, rank, min(kBlockN, p.n - n0), min(kBlockK, p.k - k0), static_cast<G*>(p.dw) + (uint64_t)n0 * p.lddw + k0, p.lddw);
+    join_parts(x0, p.split, rank, min(kBlockN, p.n - n0), min(kBlockK, p.k - k0), static_cast<G*>(p.dw) + (uint64_t)n0 * p.lddw + k0, p.lddw);
   }
   tmem_fence_before();
   __syncthreads();
@@ -400,24 +416,24 @@ bool readable(const MatrixIn& dy) {
   return dy.type == kBF16 && reinterpret_cast<uintptr_t>(dy.p) % 16 == 0 && (dy.ld % 8 == 0 || dy.rows <= 1) && dy.ld < (1ull << 32);
 }
 
-template <typename G, bool PAIR>
+template <typename G, bool PAIR, uint32_t PLANES>
 cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
   using T = Tile<PAIR>;
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR>, Groups<G>::kThreads, kSmem, Groups<G>::kLaunch, &facts);
+  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR, PLANES>, Groups<G>::kThreads, kSmem, Groups<G>::kLaunch, &facts);
   if (e != cudaSuccess) return e;
-  p.chain = sizeof(G) == 4 ? kChain : p.stages;
+  p.chain = sizeof(G) == 4 ? (kChain + PLANES - 1) / PLANES : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
   p.tiles = (uint32_t)tiles;
   // A stage takes 0.29 us, joining 2.6 (512 x 512 outputs: 512 tokens 7.2 us by one block a tile, 8.2 by two; 4096
   // tokens 23.5 and 12.6 by four).
-  p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, 9);
+  p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, (9 + PLANES - 1) / PLANES);
   const uint32_t together = PAIR ? 2 : p.split;
   const uint32_t blocks = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together;
-  return launch_after(weight_grad_kernel<G, PAIR>, blocks, Groups<G>::kThreads, kSmem, together, stream, dy, codes, scales, p);
+  return launch_after(weight_grad_kernel<G, PAIR, PLANES>, blocks, Groups<G>::kThreads, kSmem, together, stream, dy, codes, scales, p);
 }
 
 }  // namespace
@@ -459,14 +475,17 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   p.lddw = dw.ld;
   p.n = (uint32_t)dw.rows;
   p.k = (uint32_t)dw.cols;
-  p.token_stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
-  p.stages = p.token_stages * (uint32_t)planes;
+  p.stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
+  p.plane_rows = (uint32_t)rows;
   // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 tokens: 144 tiles of 1536 x 1536 27.3 us
   // and 31.7 by pairs, 256 tiles of 2048 x 2048 47.5 and 33.2).
   const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > kSms;
-  if (dw.type == kBF16)
-    return pair ? launch<__nv_bfloat16, true>(dy_map, codes_map, scales_map, p, stream) : launch<__nv_bfloat16, false>(dy_map, codes_map, scales_map, p, stream);
-  return pair ? launch<float, true>(dy_map, codes_map, scales_map, p, stream) : launch<float, false>(dy_map, codes_map, scales_map, p, stream);
+  const auto run = [&](auto type) {
+    using G = decltype(type);
+    if (planes == 1) return pair ? launch<G, true, 1>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 1>(dy_map, codes_map, scales_map, p, stream);
+    return pair ? launch<G, true, 3>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 3>(dy_map, codes_map, scales_map, p, stream);
+  };
+  return dw.type == kBF16 ? run(__nv_bfloat16()) : run(float());
 }
 
 cudaError_t act8_weight_grad_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
