@@ -18,8 +18,8 @@
 // A block (or pair) walks over its tiles with two accumulators: while one is taken out the other is
 // filled.  The tensor core truncates where it adds to an accumulator, which costs half a unit in the
 // last place every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken
-// out every kChain stages and the parts are added in registers, rounding to nearest (509 tokens in three planes: an
-// error of 2e-7 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out once.
+// out every few stages and the parts are added in registers, rounding to nearest (509 tokens in three planes: an
+// error of 8e-8 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out once.
 //
 // Measured: 8192 x 4096 x 4096 to bf16 212 us = 1.30 PFLOP/s, 0.78 of the measured bf16 rate (171 us if nothing had to
 // be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 235 us; 128 x 4096 x 9216 to f32 32 us =
@@ -28,7 +28,7 @@
 //
 // dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an
 // exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.  The three meet
-// one expansion of xhat (4096 x 2048 x 2048 to bf16 73 us; 86 with an expansion for each).
+// one expansion of xhat (4096 x 2048 x 2048 to bf16 76 us; 86 with an expansion for each).
 #include <algorithm>
 
 #include "blocks.cuh"
@@ -48,7 +48,7 @@ static_assert(kSmem <= 227 * 1024, "does not fit an SM");
 static_assert(kBlockN * 512 <= 2 * kStages * kStage, "the parts of a split sum are kept where the stages were");
 // Stages in one accumulator where the result is f32: 8192 x 4096 x 4096 takes 259, 235 and 225 us with 4, 8 and 16, and is
 // off by 1.4e-7, 2.0e-7 and 4.0e-7.
-constexpr uint32_t kChain = 8;      // a third of it where dy comes in three planes
+constexpr uint32_t kChain = 8;      // 2 where dy comes in three planes
 
 // Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out, the
 // others expand, each every third or fourth stage; and the registers of a thread by its group, of those
@@ -113,15 +113,16 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
   return h | h << 16;
 }
 
-// PLANES: matrices that dy is the sum of, 1 or 3.  A stage of xhat meets all of them; where there is one, the stages of both
-// operands share their barriers (two sets cost a stage 0.1 us).
+// PLANES: matrices that dy is the sum of, 1 or 3.  Two stages of xhat meet all three before they are left, the smallest
+// part first: added to an accumulator that already holds the largest it would be cut off (errors of 6e-7).
+// Where there is one, the stages of both operands share their barriers (two sets cost a stage 0.1 us).
 template <typename G, bool PAIR, uint32_t PLANES>
 __global__ void __launch_bounds__(Groups<G>::kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
                    const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
   using T = Tile<PAIR>;
   using R = Groups<G>;
-  constexpr uint32_t kExpanders = R::kExpanders;
+  constexpr uint32_t kExpanders = R::kExpanders, kGroup = PLANES == 1 ? 1 : 2;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t x0 = smem_address(smem), dy0 = x0 + kStages * kStage, codes0 = dy0 + kStages * kStage, scales0 = codes0 + kSlots * kCodes;
@@ -181,17 +182,19 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       uint32_t s = 0, parity = 1, issued = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         const int n0 = (int)(tile / p.lane_tiles * T::kN + (PAIR ? rank * kBlockN : 0));
-        for (uint32_t i = first; ok && i < last; ++i) {
-          for (uint32_t plane = 0, row = i * kTokens; plane < PLANES; ++plane, row += p.plane_rows, ++issued) {
-            const uint32_t at = dy0 + s * kStage;
-            if (!(ok = all_lanes(barrier_wait(dy_empty + 8 * s, parity)))) break;
-            if (!PAIR || rank == 0) barrier_expect(dy_full + 8 * s, (PAIR ? 2 : 1) * kStage, elected);
+        for (uint32_t i = first; ok && i < last; i += kGroup) {
+          for (uint32_t turn = 0; ok && turn < PLANES; ++turn) {      // the smallest part first
+            for (uint32_t t = i; t < min(last, i + kGroup); ++t, ++issued) {
+              const uint32_t at = dy0 + s * kStage, row = t * kTokens + (PLANES - 1 - turn) * p.plane_rows;
+              if (!(ok = all_lanes(barrier_wait(dy_empty + 8 * s, parity)))) break;
+              if (!PAIR || rank == 0) barrier_expect(dy_full + 8 * s, (PAIR ? 2 : 1) * kStage, elected);
 #pragma unroll
-            for (uint32_t q = 0; q < kBlockN / 64; ++q) {
-              if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, first_full + 8 * s, elected);
-              else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, dy_full + 8 * s, elected);
+              for (uint32_t q = 0; q < kBlockN / 64; ++q) {
+                if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, first_full + 8 * s, elected);
+                else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, dy_full + 8 * s, elected);
+              }
+              if (++s == kStages) s = 0, parity ^= 1;
             }
-            if (++s == kStages) s = 0, parity ^= 1;
           }
         }
       }
@@ -222,22 +225,29 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
           const uint32_t buffer = q & 1, d = tmem + buffer * T::kN, begin = i, end = min(last, i + p.chain);
           if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
           tmem_fence_after();
-          for (; ok && i < end; ++i) {
-            if (!(ok = all_lanes(barrier_wait(x_full + 8 * sx, px)))) break;
-            const uint64_t x = swizzled_columns(x0 + sx * kStage, kChunk);
+          for (; ok && i < end; i += kGroup) {
+            uint32_t sg = sx, pg = px;
 #pragma unroll
-            for (uint32_t plane = 0; plane < PLANES; ++plane) {
-              if (PLANES > 1 && !(ok = all_lanes(barrier_wait(dy_full + 8 * sdy, pdy)))) break;
-              tmem_fence_after();
-              const uint64_t dy = swizzled_columns(dy0 + sdy * kStage, kChunk);
+            for (uint32_t turn = 0; turn < PLANES; ++turn) {
+              sg = sx, pg = px;
+              for (uint32_t t = i; t < min(end, i + kGroup); ++t) {
+                if (turn == 0 && !(ok = all_lanes(barrier_wait(x_full + 8 * sg, pg)))) break;
+                if (PLANES > 1 && !(ok = all_lanes(barrier_wait(dy_full + 8 * sdy, pdy)))) break;
+                tmem_fence_after();
+                const uint64_t x = swizzled_columns(x0 + sg * kStage, kChunk), dy = swizzled_columns(dy0 + (PLANES == 1 ? sg : sdy) * kStage, kChunk);
 #pragma unroll
-              for (uint32_t j = 0; j < kTokens / 16; ++j)
-                multiply<PAIR>(d, x + j * (2048 / 16), dy + j * (2048 / 16), i != begin || plane || j, elected);
-              commit<PAIR>(dy_empty + 8 * sdy, elected);
-              if (++sdy == kStages) sdy = 0, pdy ^= 1;
+                for (uint32_t j = 0; j < kTokens / 16; ++j)
+                  multiply<PAIR>(d, x + j * (2048 / 16), dy + j * (2048 / 16), t != begin || turn || j, elected);
+                if (PLANES > 1) {
+                  commit<PAIR>(dy_empty + 8 * sdy, elected);
+                  if (++sdy == kStages) sdy = 0, pdy ^= 1;
+                }
+                if (turn == PLANES - 1) commit<PAIR>(x_empty + 8 * sg, elected);
+                if (++sg == kStages) sg = 0, pg ^= 1;
+              }
+              if (!ok) break;
             }
-            if (PLANES > 1 && ok) commit<PAIR>(x_empty + 8 * sx, elected);
-            if (++sx == kStages) sx = 0, px ^= 1;
+            sx = sg, px = pg;
           }
           if (ok) commit<PAIR>(ready + 8 * buffer, elected);
         }
@@ -423,7 +433,7 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   const Device::Facts* facts;
   const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR, PLANES>, Groups<G>::kThreads, kSmem, Groups<G>::kLaunch, &facts);
   if (e != cudaSuccess) return e;
-  p.chain = sizeof(G) == 4 ? (kChain + PLANES - 1) / PLANES : p.stages;
+  p.chain = sizeof(G) == 4 ? (PLANES == 1 ? kChain : 2) : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;

@@ -357,9 +357,9 @@ def test_weight_gradient_against_the_definition(t, n, k, dtype, pad, shift, out)
 def _sum_tol(t, out):
     """Error of a weight gradient's sum over t tokens, of the sum of magnitudes.  A step of 16 products is cut off below the
     last place of its largest term, 17 terms by half a unit each at most; an f32 result is gathered every 512
-    tokens (32 steps, 9 units each at most) and the parts, three times as many for f32 gradients, are added with
-    half a unit each.  Never more than a unit for every token."""
-    gathered = 288 + 3 * (t // 512 + 1) if out == "f32" else 9 * (t // 16 + 1)
+    tokens (32 steps, 9 units each at most), for f32 gradients every 128 (three times 8 steps), and the parts are
+    added with half a unit each.  Never more than a unit for every token."""
+    gathered = 288 + t // 128 + 1 if out == "f32" else 9 * (t // 16 + 1)
     return min(max(t, 8), gathered) * EPS
 
 
