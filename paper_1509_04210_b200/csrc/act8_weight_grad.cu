@@ -19,7 +19,8 @@
 // filled.  The tensor core truncates where it adds to an accumulator, which costs half a unit in the
 // last place every 16 tokens, always towards zero.  For an f32 result an accumulator is therefore taken
 // out every few stages and the parts are added in registers, rounding to nearest (509 tokens in three planes: an
-// error of 8e-8 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out once.
+// error of 8e-8 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out
+// once, up to 65 536 tokens.
 //
 // Measured: 8192 x 4096 x 4096 to bf16 212 us = 1.30 PFLOP/s, 0.78 of the measured bf16 rate (171 us if nothing had to
 // be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 235 us; 128 x 4096 x 9216 to f32 32 us =
@@ -30,6 +31,7 @@
 // exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.  The three meet
 // one expansion of xhat (4096 x 2048 x 2048 to bf16 76 us; 86 with an expansion for each).
 #include <algorithm>
+#include <type_traits>
 
 #include "blocks.cuh"
 #include "launch.cuh"
@@ -49,13 +51,17 @@ static_assert(kBlockN * 512 <= 2 * kStages * kStage, "the parts of a split sum a
 // Stages in one accumulator where the result is f32: 8192 x 4096 x 4096 takes 259, 235 and 225 us with 4, 8 and 16, and is
 // off by 1.4e-7, 2.0e-7 and 4.0e-7.
 constexpr uint32_t kChain = 8;      // 2 where dy comes in three planes
+// Stages, times planes, from which on a bf16 result is gathered too, at 16 % more time (2048 x 1024 positive terms: 65 536
+// tokens 304 and 354 us, too small by 1.7e-4 if not gathered; 262 144 tokens 1.14 and 1.35 ms, 8.8e-4, half of what bf16 rounds off).
+constexpr uint64_t kLongest = 1024;
 
 // Warpgroups: 0 manages (warp 0 loads dy, 1 issues, 2 allocates, 3 loads codes), 1 and 2 take results out, the
 // others expand, each every third or fourth stage; and the registers of a thread by its group, of those
-// that the block is launched with.  An f32 result is gathered in up to 128 registers of a thread.
-template <typename G> struct Groups {
-  static constexpr uint32_t kExpanders = sizeof(G) == 4 ? 3 : 4, kThreads = 128 * (3 + kExpanders);
-  static constexpr int kLaunch = sizeof(G) == 4 ? 80 : 72, kManage = sizeof(G) == 4 ? 40 : 56, kTake = sizeof(G) == 4 ? 144 : 72, kExpand = sizeof(G) == 4 ? 48 : 72;
+// that the block is launched with.  GATHER: the parts of a sum are
+// added in up to 128 registers of a thread.
+template <bool GATHER> struct Groups {
+  static constexpr uint32_t kExpanders = GATHER ? 3 : 4, kThreads = 128 * (3 + kExpanders);
+  static constexpr int kLaunch = GATHER ? 80 : 72, kManage = GATHER ? 40 : 56, kTake = GATHER ? 144 : 72, kExpand = GATHER ? 48 : 72;
   static_assert(kManage + 2 * kTake + kExpanders * kExpand <= (3 + kExpanders) * kLaunch && kThreads * kLaunch <= 65536,
                 "more registers than the block has");
 };
@@ -116,12 +122,12 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 // PLANES: matrices that dy is the sum of, 1 or 3.  Two stages of xhat meet all three before they are left, the smallest
 // part first: added to an accumulator that already holds the largest it would be cut off (errors of 6e-7).
 // Where there is one, the stages of both operands share their barriers (two sets cost a stage 0.1 us).
-template <typename G, bool PAIR, uint32_t PLANES>
-__global__ void __launch_bounds__(Groups<G>::kThreads, 1)
+template <typename G, bool PAIR, uint32_t PLANES, bool GATHER>
+__global__ void __launch_bounds__(Groups<GATHER>::kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
                    const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
   using T = Tile<PAIR>;
-  using R = Groups<G>;
+  using R = Groups<GATHER>;
   constexpr uint32_t kExpanders = R::kExpanders, kGroup = PLANES == 1 ? 1 : 2;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -290,7 +296,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) arrive<PAIR>(first_drained + 8 * buffer);
-      } else if constexpr (sizeof(G) == 4) {
+      } else if constexpr (GATHER) {
         float acc[kMine];
         for (uint32_t i = first; i < last; i += p.chain, ++q) {
           const uint32_t buffer = q & 1;
@@ -426,14 +432,14 @@ bool readable(const MatrixIn& dy) {
   return dy.type == kBF16 && reinterpret_cast<uintptr_t>(dy.p) % 16 == 0 && (dy.ld % 8 == 0 || dy.rows <= 1) && dy.ld < (1ull << 32);
 }
 
-template <typename G, bool PAIR, uint32_t PLANES>
+template <typename G, bool PAIR, uint32_t PLANES, bool GATHER>
 cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
   using T = Tile<PAIR>;
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR, PLANES>, Groups<G>::kThreads, kSmem, Groups<G>::kLaunch, &facts);
+  const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR, PLANES, GATHER>, Groups<GATHER>::kThreads, kSmem, Groups<GATHER>::kLaunch, &facts);
   if (e != cudaSuccess) return e;
-  p.chain = sizeof(G) == 4 ? (PLANES == 1 ? kChain : 2) : p.stages;
+  p.chain = GATHER ? (PLANES == 1 ? kChain : 2) : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
@@ -443,7 +449,7 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, (9 + PLANES - 1) / PLANES);
   const uint32_t together = PAIR ? 2 : p.split;
   const uint32_t blocks = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together;
-  return launch_after(weight_grad_kernel<G, PAIR, PLANES>, blocks, Groups<G>::kThreads, kSmem, together, stream, dy, codes, scales, p);
+  return launch_after(weight_grad_kernel<G, PAIR, PLANES, GATHER>, blocks, Groups<GATHER>::kThreads, kSmem, together, stream, dy, codes, scales, p);
 }
 
 }  // namespace
@@ -490,12 +496,15 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 tokens: 144 tiles of 1536 x 1536 27.3 us
   // and 31.7 by pairs, 256 tiles of 2048 x 2048 47.5 and 33.2).
   const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > kSms;
-  const auto run = [&](auto type) {
+  const auto run = [&](auto type, auto gather) {
     using G = decltype(type);
-    if (planes == 1) return pair ? launch<G, true, 1>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 1>(dy_map, codes_map, scales_map, p, stream);
-    return pair ? launch<G, true, 3>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 3>(dy_map, codes_map, scales_map, p, stream);
+    constexpr bool GATHER = decltype(gather)::value;
+    if (planes == 1)
+      return pair ? launch<G, true, 1, GATHER>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 1, GATHER>(dy_map, codes_map, scales_map, p, stream);
+    return pair ? launch<G, true, 3, GATHER>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 3, GATHER>(dy_map, codes_map, scales_map, p, stream);
   };
-  return dw.type == kBF16 ? run(__nv_bfloat16()) : run(float());
+  if (dw.type == kF32) return run(float(), std::true_type());
+  return p.stages * planes > kLongest ? run(__nv_bfloat16(), std::true_type()) : run(__nv_bfloat16(), std::false_type());
 }
 
 cudaError_t act8_weight_grad_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }

@@ -363,6 +363,21 @@ def _sum_tol(t, out):
     return min(max(t, 8), gathered) * EPS
 
 
+@pytest.mark.parametrize("t,kind", [(65_600, "bf16"), (1 << 20, "bf16"), (1 << 20, "f32"), (30_001, "f32")])
+def test_bf16_weight_gradient_over_very_many_tokens(t, kind):
+    # positive terms: a sum that is cut off at every step drifts.  Here it is gathered like an f32 result, so the two
+    # differ by the one rounding to bf16.
+    L, torch = _learner(), _torch()
+    x = torch.rand((t, 40), device="cuda", generator=torch.Generator("cuda").manual_seed(1)) + 0.5
+    dy = torch.rand((t, 12), device="cuda", generator=torch.Generator("cuda").manual_seed(2)) + 0.5
+    dy = dy.to(torch.bfloat16 if kind == "bf16" else torch.float32)
+    saved = L.act8_save(x)
+    exact = L.act8_weight_grad(dy, saved)
+    want = dy.double().T @ L.act8_values(saved, torch.float32).double()
+    assert bool(((exact.double() - want).abs() <= _sum_tol(t, "f32") * want).all())
+    assert torch.equal(L.act8_weight_grad(dy, saved, torch.bfloat16), exact.bfloat16())
+
+
 def test_weight_gradient_is_the_derivative_of_the_layer():
     # L(W) = sum dy * (xhat W^T) is linear in W: its differences are exact, entry by entry
     L, torch = _learner(), _torch()
