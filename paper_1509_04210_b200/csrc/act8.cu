@@ -71,8 +71,8 @@ struct Restored {
   uint4 w;
   uint32_t s;
   __device__ __forceinline__ void load(const Saved& from, uint32_t unit, uint32_t row, uint32_t block) {
-    w = __ldcs(from.codes + unit);
-    s = __ldg(from.scales + (uint64_t)row * from.pitch + block);
+    w = read_once(from.codes + unit);
+    s = read_byte(from.scales + (uint64_t)row * from.pitch + block);
   }
   __device__ __forceinline__ void values(float (&x)[kValues]) const { int8_values(w, scale_value(s), x); }
 };
@@ -90,7 +90,7 @@ template <bool ANY, typename G> __device__ __forceinline__ void write(G* p, Acce
 // checkpoint without gaps and neighbouring lanes share a block.
 template <typename G, Act A, bool ANY>
 __global__ void __launch_bounds__(kThreads) forward_kernel(Rows<G> x, Rows<G> up, uint32_t cols, Divisor per_row, uint32_t units,
-                                                           Access access_out, G* __restrict__ y, uint64_t ldy, Saved saved, Saved saved_up) {
+                                                           Access access_out, G* y, uint64_t ldy, Saved saved, Saved saved_up) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = per_row.quotient(i), c = (i - row * per_row.d) * kValues;

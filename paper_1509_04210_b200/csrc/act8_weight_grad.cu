@@ -392,7 +392,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 // ones zero): dy itself, or the three parts of a float's significand.
 template <typename G>
 __global__ void __launch_bounds__(256) planes_kernel(Rows<G> dy, uint32_t tokens, uint32_t n, uint32_t pitch, uint64_t rows,
-                                                     uint4* __restrict__ out) {
+                                                     uint4* out) {
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t per_row = pitch / kValues;

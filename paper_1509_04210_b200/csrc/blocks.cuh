@@ -48,10 +48,10 @@ template <typename G> struct Values {
   template <bool FIRST> static __device__ __forceinline__ void load32(const uint32_t* q, uint32_t* r) {
     if (FIRST)
       asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q));
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q) : "memory");
     else
       asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q));
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q) : "memory");
   }
 
   // `have` values from element `at` of the matrix; the others are zero.  ANY: its rows may lie anyhow.
@@ -66,7 +66,7 @@ template <typename G> struct Values {
 #pragma unroll
       for (int i = 0; i < kWords; i += 4)
         asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(reinterpret_cast<const uint32_t*>(p) + i));
+                     : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(reinterpret_cast<const uint32_t*>(p) + i) : "memory");
       return;
     }
     // Rows that lie anyhow: the 32-byte pieces around the values, as long as they are in the matrix's memory, moved

@@ -11,6 +11,30 @@ namespace {
 // A kernel launched this way is set up while the one before it still runs, and waits here, before it touches
 // global memory, until that one and all it wrote is done.
 __device__ __forceinline__ void await_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Reads, each by one instruction, of what the kernel before may have written.  They are ordered after the wait above; a
+// read-only load (__ldg, or through a const __restrict__ pointer) promises that nobody writes there for as long as the
+// kernel runs, which does not hold here, and may be moved above the wait.
+__device__ __forceinline__ uint32_t read_byte(const uint8_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.u8 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+// The same of what is read once, first to leave the caches.
+__device__ __forceinline__ uint32_t read_once(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.cs.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 read_once(const uint2* p) {
+  uint2 v;
+  asm volatile("ld.global.cs.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 read_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.cs.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
 // From here on the next kernel may be set up.
 __device__ __forceinline__ void admit_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

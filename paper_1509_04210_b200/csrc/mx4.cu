@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 // Rows as they stand.  Eight lanes take 128 values of a row, i.e. four blocks and one word of scale bytes.
 template <typename G, bool ANY>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(Rows<G> src, uint32_t cols, Divisor kt, uint32_t items,
-                                                                 uint2* __restrict__ codes, uint32_t* __restrict__ scales) {
+                                                                 uint2* codes, uint32_t* scales) {
   constexpr uint32_t U = 2, kItems = kThreads / 8;
   admit_next_kernel();
   await_previous_kernel();
@@ -52,9 +52,9 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(Rows<G> src, ui
 // columns of 32 values each, so that a block lies in one thread; four warps take the four blocks that
 // share a word of scale bytes, and the codes go through shared memory to leave as 64-byte rows.
 template <typename G>
-__global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __restrict__ src, uint64_t ld, uint32_t rows,
+__global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* src, uint64_t ld, uint32_t rows,
                                                                   uint32_t cols, uint32_t column_tiles, bool pairs,
-                                                                  uint4* __restrict__ codes, uint32_t* __restrict__ scales) {
+                                                                  uint4* codes, uint32_t* scales) {
   admit_next_kernel();
   await_previous_kernel();
   __shared__ uint4 tile[64][5];
@@ -73,11 +73,11 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
       const G* p = src + r * ld + c;
       if (pairs && c + 1 < cols) {
         if (sizeof(G) == 4) {
-          const float2 v = __ldcs(reinterpret_cast<const float2*>(p));
-          x[0][i] = v.x;
-          x[1][i] = v.y;
+          const uint2 v = read_once(reinterpret_cast<const uint2*>(p));
+          x[0][i] = __uint_as_float(v.x);
+          x[1][i] = __uint_as_float(v.y);
         } else {
-          const uint32_t v = __ldcs(reinterpret_cast<const uint32_t*>(p));
+          const uint32_t v = read_once(reinterpret_cast<const uint32_t*>(p));
           x[0][i] = __uint_as_float(v << 16);
           x[1][i] = __uint_as_float(v & 0xFFFF0000u);
         }
@@ -109,24 +109,23 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* __res
 }
 
 template <typename G, bool ANY>
-__global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales,
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* codes, const uint8_t* scales,
                                                               uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
-                                                              G* __restrict__ dst, uint64_t ld) {
+                                                              G* dst, uint64_t ld) {
   constexpr uint32_t U = 2;
   admit_next_kernel();
   await_previous_kernel();
   const uint32_t nb = (cols + 31) / 32;
   uint2 w[U];
-  uint8_t s[U];
-  uint32_t row[U], c[U];
+  uint32_t s[U], row[U], c[U];
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
     const uint32_t i = (blockIdx.x * U + u) * kThreads + threadIdx.x;
     row[u] = per_row.quotient(i);
     c[u] = (i - row[u] * per_row.d) * kValues;
     if (i < units) {
-      w[u] = __ldcs(codes + (uint64_t)row[u] * nb * 2 + c[u] / kValues);
-      s[u] = __ldg(scales + mx4_scale_at(row[u], c[u] / 32, kt));
+      w[u] = read_once(codes + (uint64_t)row[u] * nb * 2 + c[u] / kValues);
+      s[u] = read_byte(scales + mx4_scale_at(row[u], c[u] / 32, kt));
     }
   }
 #pragma unroll
