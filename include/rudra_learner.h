@@ -67,9 +67,19 @@ int rudra_mx4_dequantize(const void* codes_dev, const void* scales_dev, uint64_t
 
 /* A pull in 4 bits: quantizes the rows x cols matrix (row-major, contiguous) that starts at weight
  * `offset` of the server's vector, as of every update issued so far, on the handle's stream, and
- * returns the weights' timestamp.  0.53 bytes per weight are written instead of a pull's 4. */
+ * returns the weights' timestamp.  0.53 bytes per weight are written instead of a pull's 4.  The arrays are memory of
+ * the handle's device; ordering other streams' use of them with the handle's stream is the caller's part. */
 int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
                           void* scales_dev);
+
+/* The same for a caller that works on cuda_stream (of the handle's device): the arrays are written after all that
+ * cuda_stream holds at the call, and what it is given later runs after they are written.  Both orders are kept on
+ * the device; one stream for both costs nothing. */
+int64_t rudra_ps_pull_mx4_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                             void* scales_dev, void* cuda_stream);
+
+/* The CUDA device a handle lives on (the one current at its creation). */
+int rudra_ps_device(const rudra_ps* ps);
 
 /* y[m][n] = sum over k of a[m][k] * b[n][k], a (m x k) and b (n x k) in MX4: products exact, sums in
  * 32 bits, one rounding to y's dtype. */

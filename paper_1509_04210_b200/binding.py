@@ -100,6 +100,8 @@ def lib():
         "rudra_mx4_quantize": (C.c_int, [vp, C.c_int, u64, u64, u64, C.c_int, vp, vp, vp]),
         "rudra_mx4_dequantize": (C.c_int, [vp, vp, u64, u64, vp, C.c_int, u64, vp]),
         "rudra_ps_pull_mx4": (i64, [vp, u64, u64, u64, C.c_int, vp, vp]),
+        "rudra_ps_pull_mx4_on": (i64, [vp, u64, u64, u64, C.c_int, vp, vp, vp]),
+        "rudra_ps_device": (C.c_int, [vp]),
         "rudra_mx4_matmul": (C.c_int, [vp, vp, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp]),
         "rudra_mx4_linear_workspace": (u64, [u64, u64]),
         "rudra_mx4_linear": (C.c_int, [vp, C.c_int, u64, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp, u64, vp]),
@@ -212,6 +214,7 @@ class ParameterServer:
         self._h = lib().rudra_ps_create(nparams, lam, n, alpha0, momentum, weight_decay)
         if not self._h:
             raise RudraError(E_INVAL, last_error())
+        self.device = _check(lib().rudra_ps_device(self._h))   # index of the GPU
         if stream is not None:
             self.set_stream(stream)
 
@@ -264,6 +267,12 @@ class ParameterServer:
         """The rows x cols matrix at weight ``offset``, quantized to MX4 (``learner.pull_mx4`` allocates)."""
         return _check(lib().rudra_ps_pull_mx4(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
                                               _ptr(scales_dev)))
+
+    def pull_mx4_on(self, offset, rows, cols, transpose, codes_dev, scales_dev, stream):
+        """The same, between what ``stream`` holds now and what it is given later."""
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+        return _check(lib().rudra_ps_pull_mx4_on(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
+                                                 _ptr(scales_dev), handle))
 
     def pull_host(self, dst_host):
         return _check(lib().rudra_ps_pull_host(self._h, _ptr(dst_host)))

@@ -91,6 +91,7 @@ struct rudra_ps {
   int sm_count = 0;
   uint32_t sweep = 0;              // launches so far: successive launches sweep in opposite directions
   cudaStream_t stream = nullptr;
+  cudaEvent_t order = nullptr;     // orders the handle's stream with a caller's, made on first use
   float* theta = nullptr;
   float* state = nullptr;
   uint64_t ts = 0;
@@ -559,10 +560,16 @@ void rudra_ps_destroy(rudra_ps* ps) {
   DeviceScope dev(ps->device);
   free_host_path(ps);
   for (auto& v : ps->versions) cudaFree(v.buf);
+  if (ps->order) cudaEventDestroy(ps->order);
   cudaFree(ps->theta);
   cudaFree(ps->state);
   ps->magic = 0;
   delete ps;
+}
+
+int rudra_ps_device(const rudra_ps* ps) {
+  if (!valid(ps)) return fail(RUDRA_E_INVAL, "bad handle");
+  return ps->device;
 }
 
 int rudra_ps_set_stream(rudra_ps* ps, void* cuda_stream) {
@@ -1021,8 +1028,20 @@ int64_t rudra_ps_pull_many(rudra_ps* ps, float* const* dsts_dev, uint32_t k) {
 
 int64_t rudra_ps_pull(rudra_ps* ps, float* dst_dev) { return rudra_ps_pull_many(ps, &dst_dev, 1); }
 
-int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
-                          void* scales_dev) {
+namespace {
+
+// `then` runs after all that `first` holds now.
+cudaError_t order_streams(rudra_ps* ps, cudaStream_t first, cudaStream_t then) {
+  if (first == then) return cudaSuccess;
+  cudaError_t e = ps->order ? cudaSuccess : cudaEventCreateWithFlags(&ps->order, cudaEventDisableTiming);
+  if (e == cudaSuccess) e = cudaEventRecord(ps->order, first);
+  if (e == cudaSuccess) e = cudaStreamWaitEvent(then, ps->order, 0);
+  return e;
+}
+
+// caller: the stream whose work comes before and after, if that is to be ordered.
+int64_t pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev, void* scales_dev,
+                 const cudaStream_t* caller) {
   return guarded([&]() -> int64_t {
     if (!valid(ps)) return fail(RUDRA_E_INVAL, "bad handle");
     if (rows > RUDRA_MAX_DIM || cols > RUDRA_MAX_DIM) return fail(RUDRA_E_INVAL, "more than RUDRA_MAX_DIM rows or columns");
@@ -1030,13 +1049,30 @@ int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t
     if (rows == 0 || cols == 0) return (int64_t)ps->ts;
     if (!aligned(codes_dev) || !aligned(scales_dev)) return fail(RUDRA_E_INVAL, "codes or scales are null or not 32-byte aligned");
     DeviceScope dev(ps->device);
+    cudaError_t e = caller ? order_streams(ps, *caller, ps->stream) : cudaSuccess;
+    if (e != cudaSuccess) return cuda_fail(e, "ordering the server's stream after the caller's");
     rudra::MatrixIn src = {ps->theta + offset, rudra::kF32, rows, cols, cols};
-    cudaError_t e = rudra::launch_mx4_quantize(src, transpose != 0, codes_dev, scales_dev, ps->stream);
+    e = rudra::launch_mx4_quantize(src, transpose != 0, codes_dev, scales_dev, ps->stream);
     if (e != cudaSuccess) return cuda_fail(e, "quantization kernel launch");
+    e = caller ? order_streams(ps, ps->stream, *caller) : cudaSuccess;
+    if (e != cudaSuccess) return cuda_fail(e, "ordering the caller's stream after the server's");
     ps->counters[2] += 1;
     ps->counters[3] += 1;
     return (int64_t)ps->ts;
   });
+}
+
+}  // namespace
+
+int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                          void* scales_dev) {
+  return pull_mx4(ps, offset, rows, cols, transpose, codes_dev, scales_dev, nullptr);
+}
+
+int64_t rudra_ps_pull_mx4_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                             void* scales_dev, void* cuda_stream) {
+  const cudaStream_t caller = static_cast<cudaStream_t>(cuda_stream);
+  return pull_mx4(ps, offset, rows, cols, transpose, codes_dev, scales_dev, &caller);
 }
 
 int64_t rudra_ps_pull_host(rudra_ps* ps, float* dst_host) {

@@ -51,13 +51,14 @@ def mx4_matmul(a, b, dtype=torch.bfloat16, out=None):
 
 def pull_mx4(ps, offset, rows, cols, transpose=False, out=None):
     """(the ``rows`` x ``cols`` matrix at weight ``offset`` of a parameter server in MX4, the weights'
-    timestamp); the work runs on the server's stream."""
+    timestamp).  The work runs on the server's stream, after what torch's current stream of the server's device holds and
+    before what that is given later, so the matrix is used like one that was made there."""
     shape = (cols, rows) if transpose else (rows, cols)
     if out is None:
-        out = _n.empty(0, shape[0], shape[1], torch.cuda.current_device())
-    elif not isinstance(out, MX4) or (out.rows, out.cols) != shape:
-        raise ValueError("out: MX4 of %d x %d is wanted" % shape)
-    return out, ps.pull_mx4(offset, rows, cols, transpose, out.codes_ptr, out.scales_ptr)
+        out = _n.empty(0, shape[0], shape[1], ps.device)
+    elif not isinstance(out, MX4) or (out.rows, out.cols, out.device) != shape + (ps.device,):
+        raise ValueError("out: MX4 of %d x %d on the server's device is wanted" % shape)
+    return out, ps.pull_mx4_on(offset, rows, cols, transpose, out.codes_ptr, out.scales_ptr, torch.cuda.current_stream(ps.device).cuda_stream)
 
 
 def act8_save(x, out=None):
