@@ -192,7 +192,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
           for (uint32_t turn = 0; ok && turn < PLANES; ++turn) {      // the smallest part first
             for (uint32_t t = i; t < min(last, i + kGroup); ++t, ++issued) {
               const uint32_t at = dy0 + s * kStage, row = t * kTokens + (PLANES - 1 - turn) * p.plane_rows;
-              if (!(ok = all_lanes(barrier_wait(dy_empty + 8 * s, parity)))) break;
+              if (!(ok = barrier_wait(dy_empty + 8 * s, parity))) break;
               if (!PAIR || rank == 0) barrier_expect(dy_full + 8 * s, (PAIR ? 2 : 1) * kStage, elected);
 #pragma unroll
               for (uint32_t q = 0; q < kBlockN / 64; ++q) {
@@ -213,7 +213,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         const int k0 = (int)(tile % p.lane_tiles * T::kK + (PAIR ? rank * kBlockK : 0));
         for (uint32_t i = first; i < last; ++i, ++issued) {
-          if (!(ok = all_lanes(barrier_wait(taken + 8 * s, parity)))) break;
+          if (!(ok = barrier_wait(taken + 8 * s, parity))) break;
           barrier_expect(coded + 8 * s, kCodes + kScales, elected);
           copy_box(codes0 + s * kCodes, &codes_map, k0, (int)(i * kTokens), coded + 8 * s, elected);
           copy_box(scales0 + s * kScales, &scales_map, k0 / 512 * 16, (int)(i * kTokens), coded + 8 * s, elected);
@@ -229,7 +229,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
         for (uint32_t i = first; ok && i < last; ++q) {
           const uint32_t buffer = q & 1, d = tmem + buffer * T::kN, begin = i, end = min(last, i + p.chain);
-          if (!(ok = all_lanes(barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1)))) break;
+          if (!(ok = barrier_wait(drained + 8 * buffer, (q / 2 & 1) ^ 1))) break;
           tmem_fence_after();
           for (; ok && i < end; i += kGroup) {
             uint32_t sg = sx, pg = px;
@@ -237,8 +237,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             for (uint32_t turn = 0; turn < PLANES; ++turn) {
               sg = sx, pg = px;
               for (uint32_t t = i; t < min(end, i + kGroup); ++t) {
-                if (turn == 0 && !(ok = all_lanes(barrier_wait(x_full + 8 * sg, pg)))) break;
-                if (PLANES > 1 && !(ok = all_lanes(barrier_wait(dy_full + 8 * sdy, pdy)))) break;
+                if (turn == 0 && !(ok = barrier_wait(x_full + 8 * sg, pg))) break;
+                if (PLANES > 1 && !(ok = barrier_wait(dy_full + 8 * sdy, pdy))) break;
                 tmem_fence_after();
                 const uint64_t x = swizzled_columns(x0 + sg * kStage, kChunk), dy = swizzled_columns(dy0 + (PLANES == 1 ? sg : sdy) * kStage, kChunk);
 #pragma unroll

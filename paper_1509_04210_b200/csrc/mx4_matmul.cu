@@ -113,7 +113,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
     const uint32_t elected = elect();
     uint32_t s = 0, parity = 1, issued = 0;
     for (uint32_t i = first; i < last; ++i, ++issued) {
-      if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
+      if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
       const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s, scales = at + S::kLanes + S::kColumns;
       const uint32_t atoms = min(2u, p.kt - 2 * i);
       barrier_expect(bar, S::kLanes + atoms * 512 + (kQuantize ? 0 : S::kColumns + atoms * 512), elected);
@@ -133,7 +133,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
     const uint32_t elected = elect();
     uint32_t s = 0, parity = 0;
     for (uint32_t i = first; i < last; ++i) {
-      if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
+      if (!(ok = barrier_wait(full + 8 * s, parity))) break;
       tmem_fence_after();
       const uint32_t at = stage0 + s * S::kStage, ts = tmem + COLS + s * S::kScaleColumns;
       const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + S::kLanes), scales = scale_rows(at + S::kLanes + S::kColumns);

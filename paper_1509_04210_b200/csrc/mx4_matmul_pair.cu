@@ -96,7 +96,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
       const uint32_t lane_atom = n0 / 128 * p.kt, column_atom = m0 / 128 * p.kt;
       for (uint32_t i = 0; i < stages; ++i) {
         const uint32_t at = stage0 + s * kStage, bar = first_full + 8 * s;
-        if (!(ok = all_lanes(barrier_wait(empty + 8 * s, parity)))) break;
+        if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
         if (rank == 0) barrier_expect(full + 8 * s, 2 * kStage, elected);
         copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
         copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
@@ -116,10 +116,10 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
       const uint32_t elected = elect();
       uint32_t q = 0, s = 0, parity = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++q) {
-        if (!(ok = all_lanes(barrier_wait(drained, (q & 1) ^ 1)))) break;
+        if (!(ok = barrier_wait(drained, (q & 1) ^ 1))) break;
         tmem_fence_after();
         for (uint32_t i = 0; i < stages; ++i) {
-          if (!(ok = all_lanes(barrier_wait(full + 8 * s, parity)))) break;
+          if (!(ok = barrier_wait(full + 8 * s, parity))) break;
           tmem_fence_after();
           const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + s * kScaleColumns;
           const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + kMatrix), scales = scale_rows(at + 2 * kMatrix);

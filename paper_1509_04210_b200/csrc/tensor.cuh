@@ -54,14 +54,15 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void barrier_arrive_cluster(uint32_t remote) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(remote) : "memory");
 }
-// A wait that gives up after about two seconds.  The caller then stops issuing work and the block ends
+// A wait of a whole warp that gives up after about two seconds.  All lanes get one answer, whichever of them gives up first:
+// what follows (shuffles, tensor memory) takes whole warps.  The caller then stops issuing work and the block ends
 // through its ordinary exit; the flag it raises is read by rudra_learner_sync.
 constexpr long long kWaitCycles = 4000000000ll;
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
-  if (barrier_try(bar, parity)) return true;
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, long long limit = kWaitCycles) {
+  if (all_lanes(barrier_try(bar, parity))) return true;
   const long long begin = clock64();
-  while (!barrier_try(bar, parity))
-    if (clock64() - begin > kWaitCycles) return false;
+  while (!all_lanes(barrier_try(bar, parity)))
+    if (!all_lanes(clock64() - begin <= limit)) return false;
   return true;
 }
 __device__ __forceinline__ void barrier_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }

@@ -30,3 +30,10 @@ def test_what_the_kernel_before_writes_is_not_read_as_read_only(name):
     assert not re.findall(r"__ldg\b|__ldcs\b|__ldcg\b|__ldca\b|__restrict__|ld\.global\.nc", code)
     for asm in re.findall(r"asm[^;]*?\"[^;]*?ld\.global.*?;\s*(?=\n)", code, flags=re.S):
         assert "volatile" in asm[:20] and '"memory"' in asm, asm
+
+
+def test_waits_are_those_of_whole_warps():
+    # the one wait in use asks all lanes; nothing else tries a barrier
+    assert all("barrier_try(" not in _code(f) for f in _started_early())
+    body = _code("tensor.cuh").split("bool barrier_wait(")[1].split("\n}")[0]
+    assert body.count("barrier_try(") == body.count("all_lanes(barrier_try(") == 2
