@@ -204,9 +204,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
           }
         }
       }
-      // given up: what is on its way has landed once every copy issued has had its time
-      if (!ok && rank == 0)
-        for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(dy_full + 8 * (j % kStages), j / kStages & 1);
+      if (!PAIR || rank == 0) await_copies(dy_full, issued, kStages);      // of a pair for both blocks, which end together
     } else if (warp == 3) {
       const uint32_t elected = elect();
       uint32_t s = 0, parity = 1, issued = 0;
@@ -220,8 +218,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
           if (++s == kSlots) s = 0, parity ^= 1;
         }
       }
-      if (!ok)
-        for (uint32_t j = issued > kSlots ? issued - kSlots : 0; j < issued; ++j) barrier_wait(coded + 8 * (j % kSlots), j / kSlots & 1);
+      await_copies(coded, issued, kSlots);
     } else if (warp == 1 && (!PAIR || rank == 0)) {
       const uint32_t elected = elect();
       uint32_t q = 0;     // accumulators so far

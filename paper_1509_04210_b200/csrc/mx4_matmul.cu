@@ -125,10 +125,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
       }
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
-    // given up: what is on its way lands before the block may end
-    if (!ok)
-      for (uint32_t k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
-        barrier_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1);
+    await_copies(full, issued, S::kStages);
   } else if (warp == 1) {
     const uint32_t elected = elect();
     uint32_t s = 0, parity = 0;

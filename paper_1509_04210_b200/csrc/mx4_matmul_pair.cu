@@ -108,9 +108,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
         if (++s == kStages) s = 0, parity ^= 1;
       }
     }
-    // given up: what is on its way lands before the blocks may end
-    if (!ok && rank == 0)
-      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j) barrier_wait(full + 8 * (j % kStages), j / kStages & 1);
+    if (rank == 0) await_copies(full, issued, kStages);      // for both blocks, which end together
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t elected = elect();

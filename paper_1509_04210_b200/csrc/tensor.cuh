@@ -65,6 +65,14 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, long
     if (!all_lanes(clock64() - begin <= limit)) return false;
   return true;
 }
+// The end of a loading warp that issued `issued` stages of copies over a ring of barriers at `full`: the last ones land while
+// their block still has its shared memory, even if the warps that should have used them gave up and this one did
+// not.  Costs nothing otherwise, for their users wait for the same.  Copies take microseconds; where a barrier waits
+// for more than copies and this wait runs out too, two seconds have passed since the last of them was issued.
+__device__ __forceinline__ void await_copies(uint32_t full, uint32_t issued, uint32_t ring, long long limit = kWaitCycles) {
+  for (uint32_t j = issued > ring ? issued - ring : 0; j < issued; ++j)
+    if (!barrier_wait(full + 8 * (j % ring), j / ring & 1, limit)) break;
+}
 __device__ __forceinline__ void barrier_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
 // A warpgroup's registers per thread, out of those the block was launched with.

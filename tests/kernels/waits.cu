@@ -28,11 +28,66 @@ __global__ void uneven_wait(long long low, long long high, long long after, uint
   __syncthreads();
 }
 
+constexpr uint32_t kRing = 4, kPiece = 1024;
+
+// Warp 0 brings `stages` pieces into a ring of four; warp 1 uses the first `used` of them and then gives up.  `arrivals`: what
+// a stage's barrier counts, one of which is the loading warp's.  Out: bytes of the last pieces that have not landed once
+// the loading warp is at its end, and how many cycles that end took.
+__global__ void load_and_end(const uint8_t* from, uint32_t stages, uint32_t used, uint32_t arrivals, long long limit, uint32_t* missing, long long* took) {
+  __shared__ alignas(128) uint8_t ring[kRing * kPiece];
+  __shared__ uint64_t bars[2 * kRing];
+  const uint32_t full = smem_address(bars), empty = full + 8 * kRing, lane = threadIdx.x % 32;
+  for (uint32_t i = threadIdx.x; i < kRing * kPiece; i += 64) ring[i] = 0;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < kRing; ++s) {
+      barrier_init(full + 8 * s, arrivals);
+      barrier_init(empty + 8 * s, 1);
+    }
+    barrier_init_fence();
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const uint32_t elected = elect();
+    uint32_t issued = 0;
+    for (; issued < stages; ++issued) {
+      const uint32_t s = issued % kRing;
+      if (!barrier_wait(empty + 8 * s, (issued / kRing & 1) ^ 1, limit)) break;
+      barrier_expect(full + 8 * s, kPiece, elected);
+      copy_bulk(smem_address(ring) + s * kPiece, from + issued * kPiece, kPiece, full + 8 * s, elected);
+    }
+    const long long begin = clock64();
+    await_copies(full, issued, kRing, limit);
+    if (lane == 0) *took = clock64() - begin;
+    uint32_t bad = issued == stages ? 0 : 1u << 30;
+    for (uint32_t j = stages > kRing ? stages - kRing : 0; j < stages; ++j)
+      for (uint32_t i = lane; i < kPiece; i += 32)
+        bad += reinterpret_cast<volatile uint8_t*>(ring)[j % kRing * kPiece + i] != from[j * kPiece + i];
+    atomicAdd(missing, bad);
+  } else {
+    for (uint32_t j = 0; j < used; ++j) {
+      if (!barrier_wait(full + 8 * (j % kRing), j / kRing & 1, limit)) break;
+      if (lane == 0) barrier_arrive(empty + 8 * (j % kRing));
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+}
+
 }  // namespace
 }  // namespace rudra
 
 extern "C" int run_uneven_wait(long long low, long long high, long long after, uint32_t* answers) {
   rudra::uneven_wait<<<1, 64>>>(low, high, after, answers);
+  cudaError_t e = cudaGetLastError();
+  return (int)(e == cudaSuccess ? cudaDeviceSynchronize() : e);
+}
+
+// from: at least 1024 * stages bytes; stages <= used + 4.
+extern "C" int run_load_and_end(const uint8_t* from, uint32_t stages, uint32_t used, uint32_t arrivals, long long limit, uint32_t* missing,
+                                long long* took) {
+  if (stages > used + rudra::kRing) return -1;
+  rudra::load_and_end<<<1, 64>>>(from, stages, used, arrivals, limit, missing, took);
   cudaError_t e = cudaGetLastError();
   return (int)(e == cudaSuccess ? cudaDeviceSynchronize() : e);
 }

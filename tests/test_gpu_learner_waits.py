@@ -19,7 +19,7 @@ def kernels(tmp_path_factory):
 
 
 def test_the_kernels_of_this_test_build(kernels):
-    assert kernels.run_uneven_wait
+    assert kernels.run_uneven_wait and kernels.run_load_and_end
 
 
 @pytest.mark.gpu
@@ -36,3 +36,31 @@ def test_the_lanes_of_a_warp_get_one_answer(kernels, low, high, after):
     i64 = C.c_longlong
     assert kernels.run_uneven_wait(i64(low), i64(high), i64(after), C.c_void_p(answers.data_ptr())) == 0
     assert int(answers) == (-1 if low > after > 0 else 0)
+
+
+def _load_and_end(kernels, stages, used, arrivals, limit):
+    import torch
+
+    data = torch.randint(1, 256, (max(stages, 1) * 1024,), dtype=torch.uint8, device="cuda")
+    missing = torch.zeros(1, dtype=torch.int32, device="cuda")
+    took = torch.zeros(1, dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    assert kernels.run_load_and_end(C.c_void_p(data.data_ptr()), stages, used, arrivals, C.c_longlong(limit), C.c_void_p(missing.data_ptr()),
+                                    C.c_void_p(took.data_ptr())) == 0
+    return int(missing), int(took)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("stages,used", [(0, 0), (1, 0), (3, 0), (4, 0), (4, 4), (5, 1), (7, 3), (9, 5), (12, 8), (12, 12)])
+def test_a_loading_warp_ends_with_its_copies_landed(kernels, stages, used):
+    # whoever uses them stops after `used` stages; the loader issues the rest into the free part of the ring
+    missing, _ = _load_and_end(kernels, stages, used, 1, 1_000_000_000)
+    assert missing == 0
+
+
+@pytest.mark.gpu
+def test_its_end_is_bounded(kernels):
+    # barriers that wait for an arrival that never comes: one limit, not one for every stage
+    limit = 2_000_000
+    _, took = _load_and_end(kernels, 4, 0, 2, limit)
+    assert limit < took < 2 * limit

@@ -37,3 +37,14 @@ def test_waits_are_those_of_whole_warps():
     assert all("barrier_try(" not in _code(f) for f in _started_early())
     body = _code("tensor.cuh").split("bool barrier_wait(")[1].split("\n}")[0]
     assert body.count("barrier_try(") == body.count("all_lanes(barrier_try(") == 2
+
+
+@pytest.mark.parametrize("name,loaders", [("mx4_matmul.cu", 1), ("mx4_matmul_pair.cu", 1), ("act8_weight_grad.cu", 2)])
+def test_loading_warps_end_with_their_copies_landed(name, loaders):
+    # whichever warp gives up, and also where the loading warp itself came to its end: its last copies are waited for
+    # before the block may end, under no condition but that of a pair, whose first block waits for both
+    code = _code(name)
+    ends = re.findall(r"[^\n]*\bawait_copies\(", code)
+    assert len(ends) == loaders and code.count("barrier_expect(") == loaders
+    for line in ends:
+        assert re.fullmatch(r"\s*(if \((!PAIR \|\| )?rank == 0\) )?await_copies\(", line), line
