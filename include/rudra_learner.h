@@ -16,7 +16,8 @@
  *
  * Conventions are those of rudra_ps.h: plain C, codes < 0 with the reason in rudra_last_error(),
  * nothing thrown or aborted, all work enqueued on cuda_stream (NULL: the legacy default stream) of
- * the current device and asynchronous to the host, nothing allocated, no state between calls.
+ * the current device and asynchronous to the host, nothing allocated, no state between calls but which
+ * streams rudra_learner_sync has told of what.
  * Matrices are row-major; ld is the distance between rows in elements (ld >= row length) and a
  * matrix of dtype may start at any multiple of its element size; rows on 32-byte boundaries are the
  * fastest.  What lies between the rows of a matrix that is read may be read too, but is not used;
@@ -143,7 +144,9 @@ int rudra_act8_weight_grad(const void* dy_dev, int dy_dtype, uint64_t lddy, uint
 /* Waits for cuda_stream and reports asynchronous CUDA errors, and kernels of this header that gave up, as
  * RUDRA_E_CUDA.  The kernels of the two products wait on barriers inside a block or cluster; a wait
  * that lasts about two seconds (which no working GPU needs) ends, and its kernel with it: what such a call
- * wrote is not to be used.  Clears what it reports. */
+ * wrote is not to be used.  The kernels count this per device, not per stream: one that gave up, on whichever stream, is
+ * reported to every stream of the device that is asked about afterwards, and once told not again, so each learner on a
+ * shared GPU hears of it from its own stream.  Waits for no other stream. */
 int rudra_learner_sync(void* cuda_stream);
 
 #ifdef __cplusplus

@@ -84,7 +84,7 @@ struct Params {
   uint32_t split;           // blocks of a cluster that share a tile's tokens
 };
 
-__device__ uint32_t g_wait_failed;
+__device__ uint32_t g_gave_up;   // counts up
 
 template <bool PAIR> __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t add, uint32_t elected) {
   if (PAIR)
@@ -364,7 +364,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
       if ((v += kExpanders) >= kSlots) v -= kSlots, vparity ^= 1;
     }
   }
-  if (!ok) g_wait_failed = 1;
+  if (!ok) atomicAdd(&g_gave_up, 1u);
   __syncwarp();
   if (!PAIR && p.split > 1) {   // one tile to a cluster
     const uint32_t k0 = tile0 % p.lane_tiles * kBlockK, n0 = tile0 / p.lane_tiles * kBlockN;
@@ -504,6 +504,6 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   return p.stages * planes > kLongest ? run(__nv_bfloat16(), std::true_type()) : run(__nv_bfloat16(), std::false_type());
 }
 
-cudaError_t act8_weight_grad_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
 
 }  // namespace rudra

@@ -4,6 +4,7 @@
 #include "../../include/rudra_learner.h"
 #include "host.h"
 #include "learner.cuh"
+#include "reports.h"
 
 namespace {
 
@@ -42,6 +43,8 @@ int check_blocks(const char* what, const void* codes, const void* scales, uint64
 }
 int done(cudaError_t e, const char* what) { return e == cudaSuccess ? 0 : cuda_fail(e, what); }
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
+
+rudra::Reports g_reports;   // of rudra_learner_sync
 
 }  // namespace
 
@@ -188,13 +191,18 @@ int rudra_act8_weight_grad(const void* dy_dev, int dy_dtype, uint64_t lddy, uint
 
 int rudra_learner_sync(void* cuda_stream) {
   return guarded([&]() -> int {
-    cudaError_t e = cudaStreamSynchronize(stream_of(cuda_stream));
-    bool raised = false;
-    if (e == cudaSuccess) e = rudra::mx4_matmul_gave_up(&raised);
-    if (e == cudaSuccess) e = rudra::mx4_matmul_pair_gave_up(&raised);
-    if (e == cudaSuccess) e = rudra::act8_weight_grad_gave_up(&raised);
+    const cudaStream_t stream = stream_of(cuda_stream);
+    rudra::Reports::Counts counts = {};
+    unsigned long long id = 0;
+    int device = 0;
+    cudaError_t e = rudra::mx4_matmul_gave_up(&counts[0], stream);
+    if (e == cudaSuccess) e = rudra::mx4_matmul_pair_gave_up(&counts[1], stream);
+    if (e == cudaSuccess) e = rudra::act8_weight_grad_gave_up(&counts[2], stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    if (e == cudaSuccess) e = cudaStreamGetId(stream, &id);
+    if (e == cudaSuccess) e = cudaGetDevice(&device);
     if (e != cudaSuccess) return cuda_fail(e, "learner-side operators");
-    if (raised) return fail(RUDRA_E_CUDA, "a product kernel gave up a wait: its result is not valid");
+    if (g_reports.fresh(device, id, counts)) return fail(RUDRA_E_CUDA, "a product kernel on this device gave up a wait: its result is not valid");
     return 0;
   });
 }

@@ -51,9 +51,9 @@ uint64_t act8_weight_grad_workspace(const MatrixIn& dy);
 cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const MatrixOut& dw, void* workspace,
                                     cudaStream_t stream);
 
-// Whether a kernel of the file gave up a wait since the last call; the device's work has to be done.
-cudaError_t mx4_matmul_gave_up(bool* raised);
-cudaError_t mx4_matmul_pair_gave_up(bool* raised);
-cudaError_t act8_weight_grad_gave_up(bool* raised);
+// A count that goes up where a kernel of the file gives up a wait, as the stream's work leaves it; there once the stream is done.
+cudaError_t mx4_matmul_gave_up(uint32_t* count, cudaStream_t stream);
+cudaError_t mx4_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
+cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream);
 
 }  // namespace rudra

@@ -55,7 +55,7 @@ struct Params {
   uint32_t split;                 // blocks of a cluster that share a tile
 };
 
-__device__ uint32_t g_wait_failed;
+__device__ uint32_t g_gave_up;   // counts up
 
 // Instruction descriptor of kind::mxf4: E2M1 x E2M1, E8M0 scales, M = 128.
 template <int COLS> __device__ constexpr uint32_t instruction() {
@@ -210,7 +210,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
       }
     }
   }
-  if (!ok) g_wait_failed = 1;
+  if (!ok) atomicAdd(&g_gave_up, 1u);
   __syncwarp();
   if (p.split > 1)
     join_parts(stage0, p.split, rank, min((uint32_t)COLS, p.m - m0), min(128u, p.n - n0), static_cast<G*>(p.y) + (uint64_t)m0 * p.ldy + n0, p.ldy);
@@ -298,6 +298,6 @@ cudaError_t launch_mx4_linear(const MatrixIn& x, const Mx4& b, const MatrixOut& 
   return e != cudaSuccess ? e : launch_mx4_matmul({codes, scales, x.rows, x.cols}, b, y, stream);
 }
 
-cudaError_t mx4_matmul_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+cudaError_t mx4_matmul_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
 
 }  // namespace rudra

@@ -38,7 +38,7 @@ struct Params {
   uint32_t lane_tiles, tiles;
 };
 
-__device__ uint32_t g_wait_failed;
+__device__ uint32_t g_gave_up;   // counts up
 
 // kind::mxf4: E2M1 x E2M1, E8M0 scales, 256 x 256.
 constexpr uint32_t kInstruction = 1u << 7 | 1u << 10 | (kTile / 8) << 17 | 1u << 23 | (kTile / 128) << 27;
@@ -170,7 +170,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_co
       }
     }
   }
-  if (!ok) g_wait_failed = 1;
+  if (!ok) atomicAdd(&g_gave_up, 1u);
   __syncwarp();
   tmem_fence_before();
   __syncthreads();
@@ -209,6 +209,6 @@ cudaError_t launch_mx4_matmul_pair(const Mx4& a, const Mx4& b, const MatrixOut& 
   return y.type == kBF16 ? launch<__nv_bfloat16>(a, b, y, stream) : launch<float>(a, b, y, stream);
 }
 
-cudaError_t mx4_matmul_pair_gave_up(bool* raised) { return take_flag(g_wait_failed, raised); }
+cudaError_t mx4_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
 
 }  // namespace rudra

@@ -56,7 +56,7 @@ __device__ __forceinline__ void barrier_arrive_cluster(uint32_t remote) {
 }
 // A wait of a whole warp that gives up after about two seconds.  All lanes get one answer, whichever of them gives up first:
 // what follows (shuffles, tensor memory) takes whole warps.  The caller then stops issuing work and the block ends
-// through its ordinary exit; the flag it raises is read by rudra_learner_sync.
+// through its ordinary exit; the count it raises is read by rudra_learner_sync.
 constexpr long long kWaitCycles = 4000000000ll;
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, long long limit = kWaitCycles) {
   if (all_lanes(barrier_try(bar, parity))) return true;
@@ -316,16 +316,9 @@ inline uint32_t pick_split(const Device::Facts& f, uint64_t tiles, uint32_t stag
   return best;
 }
 
-// The flag that a kernel raises when it gives up a wait, read and lowered with the stream's work done.
-template <typename F> cudaError_t take_flag(const F& symbol, bool* raised) {
-  uint32_t v = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&v, symbol, sizeof(v));
-  if (e == cudaSuccess && v) {
-    *raised = true;
-    v = 0;
-    e = cudaMemcpyToSymbol(symbol, &v, sizeof(v));
-  }
-  return e;
+// The count that kernels raise when they give up a wait, on its way to `count` behind the stream's work.
+template <typename F> cudaError_t read_count(const F& symbol, uint32_t* count, cudaStream_t stream) {
+  return cudaMemcpyFromSymbolAsync(count, symbol, sizeof(*count), 0, cudaMemcpyDeviceToHost, stream);
 }
 
 // A row-major matrix, read in boxes as it lies; what lies outside reads as zero.

@@ -88,5 +88,6 @@ def act8_weight_grad(dy, saved, dtype=torch.float32, out=None):
 
 
 def sync(device=None):
-    """Waits for torch's current stream; raises ``RudraError`` if a kernel of these operators gave up a wait."""
+    """Waits for torch's current stream; raises ``RudraError``, once on each stream, if a kernel of these operators gave up a wait
+    on the device."""
     _n.synchronize(torch.cuda.current_device() if device is None else int(device))

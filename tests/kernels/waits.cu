@@ -1,6 +1,7 @@
 // Kernels of a test: the product kernels' waits and copies by themselves, with limits short enough to run out.
 #include <cstdint>
 
+#include "../../paper_1509_04210_b200/csrc/reports.h"
 #include "../../paper_1509_04210_b200/csrc/tensor.cuh"
 
 namespace rudra {
@@ -74,6 +75,18 @@ __global__ void load_and_end(const uint8_t* from, uint32_t stages, uint32_t used
   __syncthreads();
 }
 
+__device__ uint32_t g_count;
+
+// Whether a stream is told of the count, as rudra_learner_sync does it; < 0: a CUDA error.
+int told(Reports& reports, cudaStream_t stream) {
+  Reports::Counts counts = {};
+  unsigned long long id = 0;
+  cudaError_t e = read_count(g_count, &counts[1], stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  if (e == cudaSuccess) e = cudaStreamGetId(stream, &id);
+  return e == cudaSuccess ? (int)reports.fresh(0, id, counts) : -(int)e;
+}
+
 }  // namespace
 }  // namespace rudra
 
@@ -90,4 +103,18 @@ extern "C" int run_load_and_end(const uint8_t* from, uint32_t stages, uint32_t u
   rudra::load_and_end<<<1, 64>>>(from, stages, used, arrivals, limit, missing, took);
   cudaError_t e = cudaGetLastError();
   return (int)(e == cudaSuccess ? cudaDeviceSynchronize() : e);
+}
+
+// Asks for two streams and the legacy one after the host set the count to `count`; a bit for each that is told.
+extern "C" int run_told(uint32_t count, void* a, void* b) {
+  static rudra::Reports reports;
+  if (cudaMemcpyToSymbol(rudra::g_count, &count, sizeof(count)) != cudaSuccess) return -1;
+  int bits = 0;
+  void* const streams[3] = {a, b, nullptr};
+  for (int i = 0; i < 3; ++i) {
+    const int t = rudra::told(reports, static_cast<cudaStream_t>(streams[i]));
+    if (t < 0) return t;
+    bits |= t << i;
+  }
+  return bits;
 }

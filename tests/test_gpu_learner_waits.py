@@ -64,3 +64,36 @@ def test_its_end_is_bounded(kernels):
     limit = 2_000_000
     _, took = _load_and_end(kernels, 4, 0, 2, limit)
     assert limit < took < 2 * limit
+
+
+@pytest.mark.gpu
+def test_every_stream_is_told_once(kernels):
+    import torch
+
+    torch.zeros(1, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    told = [kernels.run_told(count, *[C.c_void_p(s.cuda_stream) for s in streams]) for count in (0, 0, 1, 1, 5, 5)]
+    assert told == [0, 0, 7, 0, 7, 0]
+
+
+@pytest.mark.gpu
+def test_sync_waits_for_its_own_stream_only():
+    import torch
+    from paper_1509_04210_b200 import learner as L
+
+    L.sync()
+    side = torch.cuda.Stream()
+    done = torch.cuda.Event()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(1_000_000_000)            # half a second on the legacy stream
+    done.record()
+    with torch.cuda.stream(side):
+        L.sync()
+        assert not done.query()
+        torch.cuda._sleep(200_000_000)
+        own = torch.cuda.Event()
+        own.record()
+        L.sync()
+        assert own.query()
+    torch.cuda.synchronize()
