@@ -108,9 +108,10 @@ __global__ void __launch_bounds__(128) quantize_transposed_kernel(const G* src, 
     scales[mx4_scale_at(row, (uint64_t)k * 4, kt) / 4] = *reinterpret_cast<const uint32_t*>(sbytes[threadIdx.x]);
 }
 
+// codes and dst from a launch's first row on, scales of the whole matrix.
 template <typename G, bool ANY>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* codes, const uint8_t* scales,
-                                                              uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
+                                                              uint32_t first_row, uint32_t cols, Divisor per_row, uint32_t kt, uint32_t units, Access access,
                                                               G* dst, uint64_t ld) {
   constexpr uint32_t U = 2;
   admit_next_kernel();
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint2* codes
     c[u] = (i - row[u] * per_row.d) * kValues;
     if (i < units) {
       w[u] = read_once(codes + (uint64_t)row[u] * nb * 2 + c[u] / kValues);
-      s[u] = read_byte(scales + mx4_scale_at(row[u], c[u] / 32, kt));
+      s[u] = read_byte(scales + mx4_scale_at(first_row + row[u], c[u] / 32, kt));
     }
   }
 #pragma unroll
@@ -173,13 +174,13 @@ cudaError_t quantize(const MatrixIn& m, bool transpose, void* codes, void* scale
 template <typename G>
 cudaError_t dequantize(const Mx4& m, const MatrixOut& d, cudaStream_t stream) {
   const uint64_t per_row = (m.cols + kValues - 1) / kValues, nb = (m.cols + 31) / 32, kt = (m.cols + 127) / 128;
-  const uint64_t most = std::max<uint64_t>(1, 0x70000000ull / per_row / 128) * 128;
+  const uint64_t most = 0x70000000ull / per_row;   // rows of a launch, 14 or more: the count of its work stays below 2^31
   for (uint64_t r = 0; r < m.rows; r += most) {
     const uint64_t units = std::min(most, m.rows - r) * per_row;
-    if (units > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_after(
-        access_of<G>(d.p, d.ld) == kByElement ? dequantize_kernel<G, true> : dequantize_kernel<G, false>, grid_of(units, 2 * kThreads), kThreads, 0, 1, stream, static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales) + mx4_scale_at(r, 0, kt), (uint32_t)m.cols,
-        Divisor((uint32_t)per_row), (uint32_t)kt, (uint32_t)units, access_of<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
+        access_of<G>(d.p, d.ld) == kByElement ? dequantize_kernel<G, true> : dequantize_kernel<G, false>, grid_of(units, 2 * kThreads), kThreads, 0, 1, stream,
+        static_cast<const uint2*>(m.codes) + r * nb * 2, static_cast<const uint8_t*>(m.scales), (uint32_t)r, (uint32_t)m.cols, Divisor((uint32_t)per_row), (uint32_t)kt,
+        (uint32_t)units, access_of<G>(d.p, d.ld), static_cast<G*>(d.p) + r * d.ld, d.ld);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
