@@ -78,10 +78,14 @@ struct Params {
   uint64_t lddw;
   uint32_t n, k;
   uint32_t stages;          // ceil(tokens / kTokens)
-  uint32_t plane_rows;      // of dy's planes, which lie one under the other
   uint32_t lane_tiles, tiles;
   uint32_t chain;           // stages in one accumulator
   uint32_t split;           // blocks of a cluster that share a tile's tokens
+};
+
+// dy's planes, the largest part first.
+template <uint32_t PLANES> struct Planes {
+  CUtensorMap map[PLANES];
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -124,7 +128,7 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 // Where there is one, the stages of both operands share their barriers (two sets cost a stage 0.1 us).
 template <typename G, bool PAIR, uint32_t PLANES, bool GATHER>
 __global__ void __launch_bounds__(Groups<GATHER>::kThreads, 1)
-weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap codes_map,
+weight_grad_kernel(const __grid_constant__ Planes<PLANES> dy_planes, const __grid_constant__ CUtensorMap codes_map,
                    const __grid_constant__ CUtensorMap scales_map, const __grid_constant__ Params p) {
   using T = Tile<PAIR>;
   using R = Groups<GATHER>;
@@ -144,7 +148,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
   const uint32_t last = PAIR ? p.stages : (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
 
   if (threadIdx.x == 0) {
-    prefetch_map(&dy_map);
+#pragma unroll
+    for (uint32_t q = 0; q < PLANES; ++q) prefetch_map(&dy_planes.map[q]);
     prefetch_map(&codes_map);
     prefetch_map(&scales_map);
     for (uint32_t s = 0; s < kStages; ++s) {
@@ -190,14 +195,15 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         const int n0 = (int)(tile / p.lane_tiles * T::kN + (PAIR ? rank * kBlockN : 0));
         for (uint32_t i = first; ok && i < last; i += kGroup) {
           for (uint32_t turn = 0; ok && turn < PLANES; ++turn) {      // the smallest part first
+            const CUtensorMap* dy_map = &dy_planes.map[PLANES - 1 - turn];
             for (uint32_t t = i; t < min(last, i + kGroup); ++t, ++issued) {
-              const uint32_t at = dy0 + s * kStage, row = t * kTokens + (PLANES - 1 - turn) * p.plane_rows;
+              const uint32_t at = dy0 + s * kStage, row = t * kTokens;
               if (!(ok = barrier_wait(dy_empty + 8 * s, parity))) break;
               if (!PAIR || rank == 0) barrier_expect(dy_full + 8 * s, (PAIR ? 2 : 1) * kStage, elected);
 #pragma unroll
               for (uint32_t q = 0; q < kBlockN / 64; ++q) {
-                if (PAIR) copy_box_pair(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, first_full + 8 * s, elected);
-                else copy_box(at + q * kChunk, &dy_map, n0 + 64 * (int)q, (int)row, dy_full + 8 * s, elected);
+                if (PAIR) copy_box_pair(at + q * kChunk, dy_map, n0 + 64 * (int)q, (int)row, first_full + 8 * s, elected);
+                else copy_box(at + q * kChunk, dy_map, n0 + 64 * (int)q, (int)row, dy_full + 8 * s, elected);
               }
               if (++s == kStages) s = 0, parity ^= 1;
             }
@@ -430,12 +436,14 @@ bool readable(const MatrixIn& dy) {
 }
 
 template <typename G, bool PAIR, uint32_t PLANES, bool GATHER>
-cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
+cudaError_t launch(const CUtensorMap* dy, const CUtensorMap& codes, const CUtensorMap& scales, Params p, cudaStream_t stream) {
   using T = Tile<PAIR>;
   static Device device;
   const Device::Facts* facts;
   const cudaError_t e = device.prepare(weight_grad_kernel<G, PAIR, PLANES, GATHER>, Groups<GATHER>::kThreads, kSmem, Groups<GATHER>::kLaunch, &facts);
   if (e != cudaSuccess) return e;
+  Planes<PLANES> planes;
+  std::copy(dy, dy + PLANES, planes.map);
   p.chain = GATHER ? (PLANES == 1 ? kChain : 2) : p.stages;
   p.lane_tiles = (p.k + T::kK - 1) / T::kK;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.n + T::kN - 1) / T::kN);
@@ -446,7 +454,7 @@ cudaError_t launch(const CUtensorMap& dy, const CUtensorMap& codes, const CUtens
   p.split = PAIR ? 1 : pick_split(*facts, tiles, p.stages, (9 + PLANES - 1) / PLANES);
   const uint32_t together = PAIR ? 2 : p.split;
   const uint32_t blocks = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, (uint32_t)facts->sms / together) * together;
-  return launch_after(weight_grad_kernel<G, PAIR, PLANES, GATHER>, blocks, Groups<GATHER>::kThreads, kSmem, together, stream, dy, codes, scales, p);
+  return launch_after(weight_grad_kernel<G, PAIR, PLANES, GATHER>, blocks, Groups<GATHER>::kThreads, kSmem, together, stream, planes, codes, scales, p);
 }
 
 }  // namespace
@@ -468,7 +476,7 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     pitch = plane_pitch(dy.cols);
     rows = plane_rows(dy.rows);
     const uint64_t blocks = (rows * (pitch / kValues) + 255) / 256;
-    if (blocks > 0x7FFFFFFFull || planes * rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     const cudaError_t e =
         dy.type == kF32 ? launch_after(planes_kernel<float>, (uint32_t)blocks, 256, 0, 1, stream, Rows<float>::of(dy.p, dy.rows, dy.cols, dy.ld, 0),
                                        (uint32_t)dy.rows, (uint32_t)dy.cols, (uint32_t)pitch, rows, static_cast<uint4*>(workspace))
@@ -478,8 +486,10 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     if (e != cudaSuccess) return e;
   }
   const uint64_t nb = (dw.cols + 31) / 32, scale_pitch = act8_scale_pitch(dw.cols);
-  CUtensorMap dy_map, codes_map, scales_map;
-  cudaError_t e = encode_rows(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, from, dy.cols, planes * rows, pitch * 2, kTokens);
+  CUtensorMap dy_maps[3], codes_map, scales_map;
+  cudaError_t e = cudaSuccess;
+  for (uint64_t q = 0; e == cudaSuccess && q < planes; ++q)
+    e = encode_rows(&dy_maps[q], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, static_cast<const uint8_t*>(from) + q * rows * pitch * 2, dy.cols, rows, pitch * 2, kTokens);
   if (e == cudaSuccess) e = encode_rows(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, saved.codes, nb * 32, dy.rows, nb * 32, kTokens);
   if (e == cudaSuccess) e = encode_plain(&scales_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, saved.scales, scale_pitch, dy.rows, scale_pitch, 16, kTokens);
   if (e != cudaSuccess) return e;
@@ -489,7 +499,6 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
   p.n = (uint32_t)dw.rows;
   p.k = (uint32_t)dw.cols;
   p.stages = (uint32_t)((dy.rows + kTokens - 1) / kTokens);
-  p.plane_rows = (uint32_t)rows;
   // Pairs once the tiles of single blocks no longer fit the SMs at once (4096 tokens: 144 tiles of 1536 x 1536 27.3 us
   // and 31.7 by pairs, 256 tiles of 2048 x 2048 47.5 and 33.2).
   const bool pair = ((dw.rows + 127) / 128) * ((dw.cols + 127) / 128) > kSms;
@@ -497,8 +506,8 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
     using G = decltype(type);
     constexpr bool GATHER = decltype(gather)::value;
     if (planes == 1)
-      return pair ? launch<G, true, 1, GATHER>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 1, GATHER>(dy_map, codes_map, scales_map, p, stream);
-    return pair ? launch<G, true, 3, GATHER>(dy_map, codes_map, scales_map, p, stream) : launch<G, false, 3, GATHER>(dy_map, codes_map, scales_map, p, stream);
+      return pair ? launch<G, true, 1, GATHER>(dy_maps, codes_map, scales_map, p, stream) : launch<G, false, 1, GATHER>(dy_maps, codes_map, scales_map, p, stream);
+    return pair ? launch<G, true, 3, GATHER>(dy_maps, codes_map, scales_map, p, stream) : launch<G, false, 3, GATHER>(dy_maps, codes_map, scales_map, p, stream);
   };
   if (dw.type == kF32) return run(float(), std::true_type());
   return p.stages * planes > kLongest ? run(__nv_bfloat16(), std::true_type()) : run(__nv_bfloat16(), std::false_type());
