@@ -8,6 +8,8 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -180,7 +182,16 @@ struct Matrix {
 
 int dtype_of(c10::ScalarType t) { return t == at::kFloat ? RUDRA_F32 : t == at::kBFloat16 ? RUDRA_BF16 : -1; }
 
+// These operators record nothing for torch's differentiation: results would come out detached without a word.
+void check_no_gradient(const char* what, const at::Tensor& t) {
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    refuse("%s requires a gradient, which these operators do not record: detach it, or call them under torch.no_grad()", what);
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
+    refuse("%s has a tangent, which these operators do not carry on", what);
+}
+
 Matrix matrix(const char* what, const at::Tensor& t) {
+  check_no_gradient(what, t);
   const int dtype = dtype_of(t.scalar_type());
   if (dtype < 0 || !t.is_cuda() || t.dim() != 2) refuse("%s: a two-dimensional float32 or bfloat16 tensor on the GPU is wanted", what);
   Matrix m = {t.data_ptr(), dtype, t.size(0), t.size(1), t.stride(0), (int)t.get_device()};

@@ -3,8 +3,10 @@
 Marshalling only, as in ``binding``: outputs are allocated with torch, the work runs in the native
 library on torch's current stream of the inputs' device.  Matrices are two-dimensional float32 or
 bfloat16 tensors whose rows are contiguous; rows may lie any distance apart.  Arguments that do not fit
-raise ``ValueError`` here or ``RudraError`` from the library.  The marshalling itself is native
-(``csrc/learner_torch.cpp``, built on first use if absent or stale); there is no fallback.
+raise ``ValueError`` here or ``RudraError`` from the library.  So does a tensor that requires a gradient
+while torch records gradients, or has a tangent: a layer's backward pass is written out with these operators, which
+record nothing themselves.  The marshalling itself is native (``csrc/learner_torch.cpp``, built on first
+use if absent or stale); there is no fallback.
 """
 from __future__ import annotations
 
