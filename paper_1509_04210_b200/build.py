@@ -1,6 +1,8 @@
 """Builds ``librudra_ps.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import hashlib
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -61,11 +63,29 @@ def build_probe(force: bool = False, verbose: bool = False) -> str:
     return _compile(PROBE_LIB_PATH, PROBE_SOURCES, verbose)
 
 
+def learner_sources() -> list:
+    return [os.path.join(_CSRC, LEARNER_SOURCE), os.path.join(_INCLUDE, "rudra_learner.h"), os.path.join(_INCLUDE, "rudra_ps.h")]
+
+
+def _torch_version() -> str:
+    return importlib.metadata.version("torch")
+
+
+def learner_key() -> str:
+    """What a binding has to be built from: its sources, and the torch and Python it is loaded into.  Compiled into it."""
+    h = hashlib.sha256()
+    for path in learner_sources():
+        with open(path, "rb") as f:
+            h.update(f.read() + b"\0")
+    h.update(("%s %s" % (_torch_version(), sysconfig.get_config_var("SOABI"))).encode())
+    return h.hexdigest()
+
+
 def learner_needs_build() -> bool:
     if not os.path.exists(LEARNER_PATH):
         return True
-    t = os.path.getmtime(LEARNER_PATH)
-    return any(os.path.getmtime(d) > t for d in [os.path.join(_CSRC, LEARNER_SOURCE), os.path.join(_INCLUDE, "rudra_learner.h")])
+    with open(LEARNER_PATH, "rb") as f:
+        return learner_key().encode() not in f.read()
 
 
 def build_learner(force: bool = False) -> str:
@@ -76,6 +96,7 @@ def build_learner(force: bool = False) -> str:
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     tmp = LEARNER_PATH + ".tmp.%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           '-DRUDRA_LEARNER_KEY="%s"' % learner_key(),
            "-I", sysconfig.get_paths()["include"], "-I", _INCLUDE]
     for d in (os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
         cmd += ["-isystem", d]
@@ -87,12 +108,11 @@ def build_learner(force: bool = False) -> str:
 
 
 def load_learner() -> None:
-    """Builds the binding if it is absent or stale; a build that fails is an error unless an older one is there."""
+    """Builds the binding if it is absent or stale; a stale one is never loaded, its arguments may differ from the library's."""
     try:
         build_learner()
     except Exception as exc:
-        if not os.path.exists(LEARNER_PATH):
-            raise ImportError("_learner.so is missing and could not be built: %r" % (exc,)) from exc
+        raise ImportError("_learner.so is missing, or from other sources or another torch, and could not be built: %r" % (exc,)) from exc
 
 
 if __name__ == "__main__":

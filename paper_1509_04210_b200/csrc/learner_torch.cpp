@@ -491,7 +491,8 @@ PyMODINIT_FUNC PyInit__learner() {
   if (!g_error || !g_types[kMx4] || !g_types[kAct8]) return nullptr;
   PyObject* m = PyModule_Create(&module);
   if (!m) return nullptr;
-  if (PyModule_AddObjectRef(m, "MX4", reinterpret_cast<PyObject*>(g_types[kMx4])) < 0 ||
+  if (PyModule_AddStringConstant(m, "build_key", RUDRA_LEARNER_KEY) < 0 ||
+      PyModule_AddObjectRef(m, "MX4", reinterpret_cast<PyObject*>(g_types[kMx4])) < 0 ||
       PyModule_AddObjectRef(m, "Act8", reinterpret_cast<PyObject*>(g_types[kAct8])) < 0) {
     Py_DECREF(m);
     return nullptr;
