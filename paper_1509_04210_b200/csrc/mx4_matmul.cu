@@ -10,8 +10,8 @@
 // Few tiles: the reduction is split over the blocks of a cluster.  Their parts are added in rank order
 // through distributed shared memory, so the sum does not depend on the run.
 //
-// Up to 32 tokens the kernel can take x itself: every block brings its slice of the few rows to MX4 on
-// the way into shared memory, which costs less than another launch.
+// Up to 16 tokens the kernel takes x itself: every block brings its slice of the few rows to MX4 on
+// the way into shared memory, which costs less than another launch (figures at kQuantizedInside).
 //
 // Measured: one token through 4096 x 9216 6.2 us (20 MB of weights, of which 1.9 us are spent before the first
 // and 1.2 us joining), 100 x 1000 x 4096 6.9 us, 256 x 4096 x 4096 7.6 us: latencies, of the copies and of the
@@ -178,7 +178,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constan
           const uint2 w = e2m1_codes(v[h], e);
           if (r >= p.m) continue;
           *reinterpret_cast<uint2*>(stage + r * 128 + ((u / 2) ^ (r % 8)) * 16 + u % 2 * 8) = w;
-          if (u % 2 == 0) stage[S::kColumns + 1024 + u / 8 * 512 + r * 16 + u / 2 % 4] = (uint8_t)e;   // r < 32
+          if (u % 2 == 0) stage[S::kColumns + 1024 + u / 8 * 512 + r * 16 + u / 2 % 4] = (uint8_t)e;   // r < 16
         }
       }
       if (!ok) break;
@@ -254,6 +254,7 @@ cudaError_t launch(const Mx4& a, const MatrixIn* x, const Mx4& b, const MatrixOu
                       x ? Rows<T>::of(x->p, x->rows, x->cols, x->ld, 0) : Rows<T>::of(nullptr, 0, 0, 0, 0));
 }
 
+// The narrowest tile that takes all rows, else 128: scale bytes come in atoms of 128 rows, and a tile begins with one.
 template <typename G> cudaError_t by_rows(const Mx4& a, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
   if (y.rows <= 16) return launch<G, 16, void>(a, nullptr, b, y, stream);
   if (y.rows <= 32) return launch<G, 32, void>(a, nullptr, b, y, stream);
@@ -262,14 +263,18 @@ template <typename G> cudaError_t by_rows(const Mx4& a, const Mx4& b, const Matr
 }
 
 template <typename G, typename X> cudaError_t quantizing(const MatrixIn& x, const Mx4& b, const MatrixOut& y, cudaStream_t stream) {
-  return y.rows <= 16 ? launch<G, 16, X>({}, &x, b, y, stream) : launch<G, 32, X>({}, &x, b, y, stream);
+  return launch<G, 16, X>({}, &x, b, y, stream);
 }
 
 cudaError_t nothing(const MatrixOut& y, cudaStream_t stream) {   // a sum over nothing
   return cudaMemset2DAsync(y.p, y.ld * (y.type == kBF16 ? 2 : 4), 0, y.cols * (y.type == kBF16 ? 2 : 4), y.rows, stream);
 }
 
-constexpr uint64_t kQuantizedInside = 32;   // rows of x up to which the product brings them to MX4 itself
+// Rows of x up to which the product brings them to MX4 itself, and beyond which that is a launch of its own.  Inside and by
+// itself, bf16: 4096 outputs of 9216 inputs, device time of 8, 16 and 32 rows 6.2, 8.8 and 13.8 us and 6.1, 6.4 and 7.3 us, one call
+// among others from the host 6.5, 9.2, 14.1 and 7.2, 7.5, 8.3; 4096 of 4096 device 4.9, 6.4, 8.8 and 5.3, 5.5, 6.1, host 5.2, 6.7,
+// 9.1 and 7.0, 7.0, 7.2 (two calls into the driver, and a workspace).  Sixteen rows fill the narrowest tile.
+constexpr uint64_t kQuantizedInside = 16;
 
 }  // namespace
 

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(1, 130, 320), (2, 40, 33), (7, 200, 1000), (16, 129, 96), (17, 256, 320), (32, 300, 2200), (33, 140, 320), (2305, 2049, 96)])
 @pytest.mark.parametrize("dtype,pad,shift", [("f32", 0, 0), ("bf16", 0, 0), ("f32", 1, 1), ("bf16", 3, 5)])
 def test_blocks_of_nan_infinity_and_zero(m, n, k, dtype, pad, shift):
-    # up to 32 rows x is brought to MX4 inside the product; 2305 x 2049 goes through pairs of blocks
+    # up to 16 rows x is brought to MX4 inside the product; 2305 x 2049 goes through pairs of blocks
     L, torch = _learner(), _torch()
     x, w = _normal(m, k, 1.0, 21), _normal(n, k, 1.0, 22)
     last = m - 1
@@ -33,7 +33,7 @@ def test_blocks_of_nan_infinity_and_zero(m, n, k, dtype, pad, shift):
 
 def test_rows_of_a_product_are_the_same_in_every_batch():
     # Whole numbers under one scale: every partial sum is exact in 32 bits, however the reduction is split, so rows have to
-    # come out alike in batches that take x as it is (up to 32), 16, 32, 64 and 128 wide tiles, and pairs of blocks.
+    # come out alike in batches that take x as it is (up to 16), 16, 32, 64 and 128 wide tiles, and pairs of blocks.
     L, torch = _learner(), _torch()
     n, k, rows = 2100, 2304, 2400
     gen = _rng(23)

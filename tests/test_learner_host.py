@@ -155,3 +155,10 @@ def test_the_header_is_plain_c():
                                "-Wl,-rpath," + os.path.dirname(lib), "-o", exe])
         out = subprocess.run([exe], capture_output=True, text=True, timeout=60)
         assert out.returncode == 0 and "handle" in out.stdout, (out.returncode, out.stdout, out.stderr)
+
+
+def test_only_a_handful_of_rows_is_brought_to_mx4_inside_the_product():
+    # from 17 rows on a launch of its own is the faster way, and needs the workspace for it
+    need = rb.lib().rudra_mx4_linear_workspace
+    assert all(need(m, k) == 0 for m in (0, 1, 8, 16) for k in (1, 4096, 9216))
+    assert all(need(m, k) >= m * 16 * -(-k // 32) for m in (17, 24, 32, 33) for k in (1, 4096, 9216))
