@@ -195,7 +195,8 @@ int rudra_learner_sync(void* cuda_stream) {
     rudra::Reports::Counts counts = {};
     unsigned long long id = 0;
     int device = 0;
-    cudaError_t e = rudra::mx4_matmul_gave_up(&counts[0], stream);
+    cudaError_t e = cudaStreamSynchronize(stream);      // first: a stream that is being captured refuses, and takes no copies to `counts`
+    if (e == cudaSuccess) e = rudra::mx4_matmul_gave_up(&counts[0], stream);
     if (e == cudaSuccess) e = rudra::mx4_matmul_pair_gave_up(&counts[1], stream);
     if (e == cudaSuccess) e = rudra::act8_weight_grad_gave_up(&counts[2], stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(stream);

@@ -42,3 +42,10 @@ def test_counts_are_never_set_back():
     for name in ("mx4_matmul.cu", "mx4_matmul_pair.cu", "act8_weight_grad.cu", "tensor.cuh", "learner.cu"):
         text = open(os.path.join(CSRC, name)).read()
         assert "cudaMemcpyToSymbol" not in text and "g_wait_failed =" not in text, name
+
+
+def test_a_sync_waits_before_it_copies():
+    # on a stream that is being captured the wait is refused, so no copy to this call's memory gets into the graph
+    text = open(os.path.join(CSRC, "learner.cu")).read()
+    body = text[text.index("int rudra_learner_sync("):]
+    assert body.index("cudaStreamSynchronize(") < body.index("mx4_matmul_gave_up(")
