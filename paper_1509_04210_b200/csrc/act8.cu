@@ -1,8 +1,10 @@
 // Activation functions with an 8-bit checkpoint of their input: forward (value and checkpoint in one
 // pass) and backward (slope from the checkpoint).  Element-wise but for a block's shared scale, so bound
 // by HBM: per value and input 2G + 33/32 bytes each way (G = 2 bf16, 4 f32).  Sigmoids are formed from the
-// approximate base-2 exponential and reciprocal, each within about 2 units in the last place of 32 bits.
-// Measured at 8192 x 4096: silu in f32 46.3 us each way = 6.5 TB/s, swiglu in bf16 42.7 and 42.9 us = 6.3 TB/s,
+// approximate base-2 exponential and reciprocal, each within about 2 units in the last place of 32 bits; the exponent is
+// rounded before that (x log2 e to 32 bits), so far out a sigmoid is off by some |x| 2^-24 of itself (gelu in f32: 1.8e-7 over a
+// normal x, 1.6e-7 with the plain exponential).
+// Measured at 8192 x 4096: silu in f32 46.3 us each way = 6.5 TB/s, swiglu in bf16 42.9 and 44.1 us = 6.3 and 6.2 TB/s,
 // gelu in bf16 27.4 and 28.5 us = 6.2 and 5.9 TB/s (with the plain exponential, reciprocal and a clamp of
 // each value by itself 35 and 39 us: the instructions were the bound); the checkpoint alone of bf16 18.7 us.
 #include <algorithm>

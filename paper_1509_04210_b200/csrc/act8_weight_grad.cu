@@ -22,13 +22,17 @@
 // error of 8e-8 instead of 2.6e-6); a bf16 result keeps 16 bits fewer and is taken out
 // once, up to 65 536 tokens.
 //
-// Measured: 8192 x 4096 x 4096 to bf16 212 us = 1.30 PFLOP/s, 0.78 of the measured bf16 rate (171 us if nothing had to
-// be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 235 us; 128 x 4096 x 9216 to f32 32 us =
-// 4.8 TB/s, bound by its 151 MB of results.  Repeated for long the first runs into the power cap (1.56 GHz) and
-// takes 250 us.
+// Measured: 8192 x 4096 x 4096 to bf16 212 us = 1.29 PFLOP/s, 0.78 of the measured bf16 rate (171 us if nothing had to
+// be expanded; 256 tiles are 3.5 rounds of 74 pairs, which cost 4), to f32 234 us; repeated for long both run into the
+// power cap (1.56 GHz) and take 248 and 274 us.  128 x 4096 x 9216 to f32 31.7 us = 4.8 TB/s of its 151 MB of results, which
+// a kernel that only stores them writes in 22.8 us (6.6 TB/s): the bound is here, where loads from tensor memory and stores of
+// a warp take turns, not HBM.
+//
+// The kernels that gather hold 64 or 128 parts of sums in a thread's registers and spill beside them: 24 bytes a thread in
+// single blocks, 88 (f32 results) or 96 (bf16) in pairs.
 //
 // dy in f32 is first cut into three bf16 matrices whose sum it is (8 bits of the significand each, an
-// exact split), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.  The three meet
+// exact split down to 2^-133, the last bit of bf16), and dy whose rows TMA cannot read is copied to rows it can; both go through the workspace.  The three meet
 // one expansion of xhat (4096 x 2048 x 2048 to bf16 76 us; 86 with an expansion for each).
 #include <algorithm>
 #include <type_traits>

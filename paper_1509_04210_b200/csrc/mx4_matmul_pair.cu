@@ -10,8 +10,9 @@
 // scale bytes of six stages take another 144), so results are first taken into registers, which frees
 // it for the next tile, and written out while that one is computed.
 //
-// Measured at 8192 x 4096 x 9216: 93 us = 6.6 PFLOP/s, four times the measured bf16 rate (246 us with one SM to a
-// tile of 128 x 256); the copies alone, with no multiplication, 89 us.
+// Measured at 8192 x 4096 x 9216: 93 to 96 us = 6.5 PFLOP/s, four times the measured bf16 rate (246 us with one SM to a
+// tile of 128 x 256); the copies alone, with no multiplication, 89 us.  Repeated for long it runs into the power cap and
+// takes 116 us = 5.3 PFLOP/s.
 #include <algorithm>
 
 #include "blocks.cuh"
