@@ -270,9 +270,8 @@ class ParameterServer:
 
     def pull_mx4_on(self, offset, rows, cols, transpose, codes_dev, scales_dev, stream):
         """The same, between what ``stream`` holds now and what it is given later."""
-        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
         return _check(lib().rudra_ps_pull_mx4_on(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
-                                                 _ptr(scales_dev), handle))
+                                                 _ptr(scales_dev), stream if isinstance(stream, int) else stream.cuda_stream))
 
     def pull_host(self, dst_host):
         return _check(lib().rudra_ps_pull_host(self._h, _ptr(dst_host)))

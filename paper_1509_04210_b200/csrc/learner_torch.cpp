@@ -297,6 +297,13 @@ PyObject* empty(PyObject*, PyObject* const* a, Py_ssize_t n) {   // kind, rows, 
   });
 }
 
+PyObject* current_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {   // device
+  return returning([&]() -> PyObject* {
+    count(n, 1);
+    return PyLong_FromVoidPtr(c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)number(a[0])).stream());
+  });
+}
+
 PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // x, transpose, out
   return returning([&]() -> PyObject* {
     count(n, 3);
@@ -460,7 +467,7 @@ PyObject* synchronize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // device
 
 PyMethodDef methods[] = {
 #define RUDRA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
-    RUDRA_METHOD(empty), RUDRA_METHOD(mx4_quantize), RUDRA_METHOD(mx4_dequantize), RUDRA_METHOD(mx4_matmul), RUDRA_METHOD(act8_values),
+    RUDRA_METHOD(empty), RUDRA_METHOD(current_stream), RUDRA_METHOD(mx4_quantize), RUDRA_METHOD(mx4_dequantize), RUDRA_METHOD(mx4_matmul), RUDRA_METHOD(act8_values),
     RUDRA_METHOD(act8_forward), RUDRA_METHOD(act8_backward), RUDRA_METHOD(act8_weight_grad), RUDRA_METHOD(synchronize),
 #undef RUDRA_METHOD
     {nullptr, nullptr, 0, nullptr}};

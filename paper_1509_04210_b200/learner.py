@@ -55,12 +55,12 @@ def pull_mx4(ps, offset, rows, cols, transpose=False, out=None):
     """(the ``rows`` x ``cols`` matrix at weight ``offset`` of a parameter server in MX4, the weights'
     timestamp).  The work runs on the server's stream, after what torch's current stream of the server's device holds and
     before what that is given later, so the matrix is used like one that was made there."""
-    shape = (cols, rows) if transpose else (rows, cols)
+    m, n, device = (cols, rows, ps.device) if transpose else (rows, cols, ps.device)
     if out is None:
-        out = _n.empty(0, shape[0], shape[1], ps.device)
-    elif not isinstance(out, MX4) or (out.rows, out.cols, out.device) != shape + (ps.device,):
-        raise ValueError("out: MX4 of %d x %d on the server's device is wanted" % shape)
-    return out, ps.pull_mx4_on(offset, rows, cols, transpose, out.codes_ptr, out.scales_ptr, torch.cuda.current_stream(ps.device).cuda_stream)
+        out = _n.empty(0, m, n, device)
+    elif not isinstance(out, MX4) or (out.rows, out.cols, out.device) != (m, n, device):
+        raise ValueError("out: MX4 of %d x %d on the server's device is wanted" % (m, n))
+    return out, ps.pull_mx4_on(offset, rows, cols, transpose, out.codes_ptr, out.scales_ptr, _n.current_stream(device))
 
 
 def act8_save(x, out=None):

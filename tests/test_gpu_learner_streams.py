@@ -106,3 +106,23 @@ def test_pulls_on_another_stream_can_be_captured():
     torch.cuda.synchronize()
     assert torch.equal(got, L.mx4_dequantize(L.mx4_quantize(theta.view(rows, cols) * 2.0)))
     ps.close()
+
+
+def test_a_pull_may_be_torchs_first_use_of_the_gpu():
+    import os
+    import subprocess
+    import sys
+
+    program = """
+import numpy as np
+from paper_1509_04210_b200 import binding as rb, learner as L
+ps = rb.ParameterServer(64 * 96, 1, 1, 0.1)
+ps.set_weights_host(np.full(64 * 96, 1.5, dtype=np.float32))
+q, ts = L.pull_mx4(ps, 0, 64, 96)
+import torch
+assert ts == 0 and bool((L.mx4_dequantize(q, torch.float32) == 1.5).all()) and q.codes.shape == (64, 48)
+L.sync()
+ps.close()
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", program], cwd=root, check=True, timeout=120)

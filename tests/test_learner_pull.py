@@ -1,6 +1,4 @@
 """What learner.pull_mx4 asks of the server, with a server that only records it: no GPU needed."""
-import types
-
 import pytest
 import torch
 
@@ -38,7 +36,7 @@ def parts(monkeypatch):
     monkeypatch.setattr(learner, "MX4", Codes)
     monkeypatch.setattr(learner._n, "empty", empty)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=1000 + (device or 0)))
+    monkeypatch.setattr(learner._n, "current_stream", lambda device: 1000 + device)
     return made
 
 
