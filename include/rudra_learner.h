@@ -3,6 +3,9 @@
  * compute on the same GPU as the server: weights in 4 bits and the product with them, activation
  * checkpoints in 8 bits and the backward pass that reads them.
  *
+ * Beside them what a residual network's learner needs: weights and activations in 8-bit floating point and
+ * the product with them, the norm in front of a layer with its backward pass, and the clipping of what is pushed.
+ *
  * A learner of Section 2 (Gupta, Zhang, Wang, arXiv 1509.04210) pulls weights, runs a mini-batch
  * forward and backward and pushes a gradient.  With lambda learners to a GPU its memory and its
  * bandwidth are shared lambda ways, so what each learner holds is made small: the weights it
@@ -145,6 +148,100 @@ uint64_t rudra_act8_weight_grad_workspace(const void* dy_dev, int dy_dtype, uint
 int rudra_act8_weight_grad(const void* dy_dev, int dy_dtype, uint64_t lddy, uint64_t tokens, uint64_t n,
                            const void* codes_dev, const void* scales_dev, uint64_t k, void* dw_dev, int dw_dtype,
                            uint64_t lddw, void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * FP8: a matrix in 8-bit floating point with a scale for each block.  128 consecutive values of a row (or, square, 128 rows
+ * of them) form a block (the last of a row may be short).  The block's scale byte s stands for 2^(s - 127),
+ * the smallest power of two (s >= 0) under which its largest magnitude is at most 448; a value is the E4M3
+ * number (largest 448, smallest 2^-9, three bits after the leading one) nearest to x * 2^(127 - s), ties to the even
+ * code.  A block that holds an infinity or a NaN has s = 255, and all of it stands for NaN.  Values are off by at most 1/16 of
+ * themselves or 2^-17 of the block's largest magnitude, whichever is more, and exact in float (magnitudes from 248 * 2^120 on
+ * stand for 2^128, an infinity there); in bf16 too down to 2^-130.
+ *
+ * codes: rows of 128 * ceil(cols / 128) bytes, codes past cols zero.  scales: a byte for each row and block, square or not, in
+ * the order that MX4 has them in, with nb = ceil(cols / 128).  Both arrays start on 32-byte boundaries; scale
+ * bytes of blocks past nb are zero, those of rows past the last are never used.
+ */
+uint64_t rudra_fp8_codes_bytes(uint64_t rows, uint64_t cols);
+uint64_t rudra_fp8_scales_bytes(uint64_t rows, uint64_t cols);
+
+/* src (rows x cols of dtype) to FP8.  transpose != 0: the FP8 matrix is src's transpose (cols x rows).  square == 0: blocks run
+ * along the rows of the result.  square != 0: blocks of 128 x 128, so that a matrix and its transpose have the same
+ * values: for weights, which forward and backward pass both read. */
+int rudra_fp8_quantize(const void* src_dev, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, int transpose, int square,
+                       void* codes_dev, void* scales_dev, void* cuda_stream);
+
+/* The values an FP8 matrix (rows x cols) stands for, as dtype. */
+int rudra_fp8_dequantize(const void* codes_dev, const void* scales_dev, uint64_t rows, uint64_t cols, void* dst_dev,
+                         int dtype, uint64_t ld, void* cuda_stream);
+
+/* rudra_ps_pull_mx4 and rudra_ps_pull_mx4_on with the matrix in FP8, its blocks square: 1.01 bytes per weight. */
+int64_t rudra_ps_pull_fp8(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                          void* scales_dev);
+int64_t rudra_ps_pull_fp8_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                             void* scales_dev, void* cuda_stream);
+
+/* y[m][n] = sum over k of a[m][k] * b[n][k], a (m x k) and b (n x k) in FP8: products exact, sums in 32 bits, one rounding to
+ * y's dtype.  With a transposed quantization of both factors it is a layer's weight gradient. The order of a sum depends
+ * on m, n, k and the device alone. */
+int rudra_fp8_matmul(const void* a_codes_dev, const void* a_scales_dev, uint64_t m, const void* b_codes_dev,
+                     const void* b_scales_dev, uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy,
+                     void* cuda_stream);
+
+/* The same with a = x (m x k of x_dtype) brought to FP8 inside the call, by pieces of rows.  workspace_dev:
+ * rudra_fp8_linear_workspace(m, k) bytes (zero for few rows) on a 32-byte boundary, free for other use once
+ * the call's work has run. */
+uint64_t rudra_fp8_linear_workspace(uint64_t m, uint64_t k);
+int rudra_fp8_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, const void* w_codes_dev,
+                     const void* w_scales_dev, uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy,
+                     void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, a row (token) at a time:
+ *     s = x + residual, rounded to dtype;   y = s * weight / sqrt(mean(s^2) + eps)
+ * computed from the rounded s in 32 bits (rows whose squares add up to 2^128 or more are out of range).  x, residual,
+ * sum and y are tokens x channels of one dtype; weight holds `channels` values.  residual_dev NULL: s = x, and sum_dev is
+ * NULL; otherwise sum_dev receives s, and may be x's or the residual's memory in the same layout.  y leaves as any of
+ * y_dev (dtype; may be x's memory in the same layout where sum_dev is not), FP8 (blocks along the rows) and ACT8 (the
+ * checkpoint that rudra_act8_weight_grad takes), the last two from y before it is rounded to dtype; what is NULL is not
+ * wanted, but one is.  eps >= 0.
+ */
+int rudra_rms_norm(const void* x_dev, uint64_t ldx, const void* residual_dev, uint64_t ldr, int dtype, uint64_t tokens,
+                   uint64_t channels, const void* weight_dev, int weight_dtype, float eps, void* sum_dev, uint64_t ldsum,
+                   void* y_dev, uint64_t ldy, void* fp8_codes_dev, void* fp8_scales_dev, void* act8_codes_dev,
+                   void* act8_scales_dev, void* cuda_stream);
+
+/* The backward pass, from the s that went into the norm: with r = 1 / sqrt(mean(s^2) + eps),
+ *     ds = r * (weight * dy - s * r^2 * mean(weight * dy * s)) + dsum,    dweight = sum over tokens of dy * s * r.
+ * ds is the gradient of x and of the residual alike; dsum (NULL: zero) is what comes down the residual stream.  dy, s, dsum
+ * and ds are tokens x channels of one dtype; ds may be dy's or dsum's memory in the same layout.  dweight is of
+ * dweight_dtype, wherever it lies in the vector that rudra_ps_push takes; its sums are in 32 bits, in an order that
+ * depends on tokens, channels and the device alone.  workspace_dev:
+ * rudra_rms_norm_backward_workspace(tokens, channels) bytes on a 32-byte boundary. */
+uint64_t rudra_rms_norm_backward_workspace(uint64_t tokens, uint64_t channels);
+int rudra_rms_norm_backward(const void* dy_dev, uint64_t lddy, const void* s_dev, uint64_t lds, const void* dsum_dev,
+                            uint64_t lddsum, int dtype, uint64_t tokens, uint64_t channels, const void* weight_dev,
+                            int weight_dtype, float eps, void* ds_dev, uint64_t ldds, void* dweight_dev,
+                            int dweight_dtype, void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The norm of `count` gradients together: the square root of the sum of all their squares, to *norm_dev (a float).  Gradient i
+ * is sizes[i] consecutive values of dtypes[i]; the three lists are host memory, read before the call returns.  Squares of 16 values
+ * are added in 32 bits, all beyond that, and squares a float does not hold, in 64; the order depends on the list alone.
+ * workspace_dev: rudra_grad_norm_workspace(count) bytes on a 32-byte boundary.  A list has at most 2^24 gradients and
+ * 2^43 values.
+ */
+uint64_t rudra_grad_norm_workspace(uint64_t count);
+int rudra_grad_norm(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, float* norm_dev,
+                    void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
+
+/* outs[i] = grads[i] * (norm <= max_norm ? 1 : max_norm / norm), norm = *norm_dev: for instance into the layers' parts of the
+ * vector that rudra_ps_push takes, in its dtype.  outs_dev[i] may be grads_dev[i] with the same dtype; no two outputs and
+ * no output and another gradient may overlap, which is refused.  Where all are scaled in their place and norm <= max_norm
+ * nothing is read or written.  A norm that is NaN makes every value NaN, an infinite one the finite values zero and the
+ * others NaN, unless max_norm is infinite too.  max_norm >= 0. */
+int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, const float* norm_dev,
+                    float max_norm, void* const* outs_dev, const int* out_dtypes, void* cuda_stream);
 
 /* Waits for cuda_stream and reports asynchronous CUDA errors, and kernels of this header that gave up, as
  * RUDRA_E_CUDA.  The kernels of the two products wait on barriers inside a block or cluster; a wait

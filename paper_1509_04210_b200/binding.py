@@ -112,6 +112,21 @@ def lib():
         "rudra_learner_sync": (C.c_int, [vp]),
         "rudra_act8_weight_grad_workspace": (u64, [vp, C.c_int, u64, u64, u64]),
         "rudra_act8_weight_grad": (C.c_int, [vp, C.c_int, u64, u64, u64, vp, vp, u64, vp, C.c_int, u64, vp, u64, vp]),
+        "rudra_fp8_codes_bytes": (u64, [u64, u64]),
+        "rudra_fp8_scales_bytes": (u64, [u64, u64]),
+        "rudra_fp8_quantize": (C.c_int, [vp, C.c_int, u64, u64, u64, C.c_int, C.c_int, vp, vp, vp]),
+        "rudra_fp8_dequantize": (C.c_int, [vp, vp, u64, u64, vp, C.c_int, u64, vp]),
+        "rudra_ps_pull_fp8": (i64, [vp, u64, u64, u64, C.c_int, vp, vp]),
+        "rudra_ps_pull_fp8_on": (i64, [vp, u64, u64, u64, C.c_int, vp, vp, vp]),
+        "rudra_fp8_matmul": (C.c_int, [vp, vp, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp]),
+        "rudra_fp8_linear_workspace": (u64, [u64, u64]),
+        "rudra_fp8_linear": (C.c_int, [vp, C.c_int, u64, u64, vp, vp, u64, u64, vp, C.c_int, u64, vp, u64, vp]),
+        "rudra_rms_norm": (C.c_int, [vp, u64, vp, u64, C.c_int, u64, u64, vp, C.c_int, C.c_float, vp, u64, vp, u64, vp, vp, vp, vp, vp]),
+        "rudra_rms_norm_backward_workspace": (u64, [u64, u64]),
+        "rudra_rms_norm_backward": (C.c_int, [vp, u64, vp, u64, vp, u64, C.c_int, u64, u64, vp, C.c_int, C.c_float, vp, u64, vp, C.c_int, vp, u64, vp]),
+        "rudra_grad_norm_workspace": (u64, [u64]),
+        "rudra_grad_norm": (C.c_int, [vp, vp, vp, u64, vp, vp, u64, vp]),
+        "rudra_grad_clip": (C.c_int, [vp, vp, vp, u64, vp, C.c_float, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -271,6 +286,16 @@ class ParameterServer:
     def pull_mx4_on(self, offset, rows, cols, transpose, codes_dev, scales_dev, stream):
         """The same, between what ``stream`` holds now and what it is given later."""
         return _check(lib().rudra_ps_pull_mx4_on(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
+                                                 _ptr(scales_dev), stream if isinstance(stream, int) else stream.cuda_stream))
+
+    def pull_fp8(self, offset, rows, cols, transpose, codes_dev, scales_dev):
+        """The rows x cols matrix at weight ``offset`` in FP8 with blocks of 128 x 128 (``learner.pull_fp8`` allocates)."""
+        return _check(lib().rudra_ps_pull_fp8(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
+                                              _ptr(scales_dev)))
+
+    def pull_fp8_on(self, offset, rows, cols, transpose, codes_dev, scales_dev, stream):
+        """The same, between what ``stream`` holds now and what it is given later."""
+        return _check(lib().rudra_ps_pull_fp8_on(self._h, int(offset), int(rows), int(cols), int(bool(transpose)), _ptr(codes_dev),
                                                  _ptr(scales_dev), stream if isinstance(stream, int) else stream.cuda_stream))
 
     def pull_host(self, dst_host):

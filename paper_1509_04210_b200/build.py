@@ -14,7 +14,8 @@ _CSRC = os.path.join(_PKG, "csrc")
 _INCLUDE = os.path.join(os.path.dirname(_PKG), "include")
 LIB_PATH = os.path.join(_PKG, "librudra_ps.so")
 SOURCES = ["ps.cu", "update.cu", "snapshot.cu", "leaf.cu", "noalloc.cu", "sched.cpp",
-           "learner.cu", "mx4.cu", "mx4_matmul.cu", "mx4_matmul_pair.cu", "act8.cu", "act8_weight_grad.cu"]
+           "learner.cu", "mx4.cu", "mx4_matmul.cu", "mx4_matmul_pair.cu", "act8.cu", "act8_weight_grad.cu",
+           "fp8.cu", "fp8_matmul.cu", "fp8_matmul_pair.cu", "rms_norm.cu", "grad_clip.cu"]
 # measurement utility of the benchmark, a library of its own: not part of the product interface
 PROBE_LIB_PATH = os.path.join(_PKG, "librudra_probe.so")
 PROBE_SOURCES = ["probe.cu"]
@@ -23,7 +24,7 @@ LEARNER_PATH = os.path.join(_PKG, "_learner.so")
 LEARNER_SOURCE = "learner_torch.cpp"
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-cudart", "static", "-shared",
+    "-Xcompiler", "-fPIC", "-cudart", "static", "-shared", "-t", "0",
 ]
 
 

@@ -26,6 +26,12 @@ struct Mx4 {
   const void* scales;
   uint64_t rows, cols;
 };
+// A matrix in FP8: rows of 128 * ceil(cols / 128) bytes of codes, scale bytes in the tensor cores' order.
+struct Fp8 {
+  const void* codes;
+  const void* scales;
+  uint64_t rows, cols;
+};
 // A checkpoint: rows of 32 * ceil(cols / 32) int8 codes, rows of act8_scale_pitch(cols) scale bytes.
 struct Act8 {
   void* codes;
@@ -50,10 +56,51 @@ cudaError_t launch_act8_backward(Act act, const MatrixIn& dy, const Act8& saved,
 uint64_t act8_weight_grad_workspace(const MatrixIn& dy);
 cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const MatrixOut& dw, void* workspace,
                                     cudaStream_t stream);
+cudaError_t launch_fp8_quantize(const MatrixIn& src, bool transpose, bool square, void* codes, void* scales, cudaStream_t stream);
+cudaError_t launch_fp8_dequantize(const Fp8& src, const MatrixOut& dst, cudaStream_t stream);
+cudaError_t launch_fp8_matmul(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream);
+cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream);   // of launch_fp8_matmul: many tiles
+uint64_t fp8_linear_workspace(uint64_t m, uint64_t k);
+cudaError_t launch_fp8_linear(const MatrixIn& x, const Fp8& b, const MatrixOut& y, void* workspace, cudaStream_t stream);
+
+// Root-mean-square norm.  Matrices without memory (p null) are not given or not wanted; all have x's shape and type.
+struct NormForward {
+  MatrixIn x, residual;
+  const void* weight;          // one for each column
+  GradType weight_type;
+  float eps;
+  MatrixOut sum, y;
+  Act8 fp8, kept;              // y in FP8, and in ACT8
+};
+cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream);
+struct NormBackward {
+  MatrixIn dy, s, dsum;
+  const void* weight;
+  GradType weight_type;
+  float eps;
+  MatrixOut ds;                // may be dy's memory, or dsum's
+  void* dw;
+  GradType dw_type;
+};
+uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols);
+cudaError_t launch_rms_norm_backward(const NormBackward& n, void* workspace, cudaStream_t stream);
+
+// A list of gradients, each `size` values one after another.
+struct Gradient {
+  const void* p;
+  void* out;                   // of grad_clip; may be p
+  uint64_t size;
+  GradType type, out_type;
+};
+uint64_t grad_norm_workspace(uint64_t count);
+cudaError_t launch_grad_norm(const Gradient* grads, uint64_t count, float* norm, void* workspace, cudaStream_t stream);
+cudaError_t launch_grad_clip(const Gradient* grads, uint64_t count, const float* norm, float max_norm, cudaStream_t stream);
 
 // A count that goes up where a kernel of the file gives up a wait, as the stream's work leaves it; there once the stream is done.
 cudaError_t mx4_matmul_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t mx4_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream);
+cudaError_t fp8_matmul_gave_up(uint32_t* count, cudaStream_t stream);
+cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
 
 }  // namespace rudra

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <cstdint>
+#include <vector>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
@@ -41,9 +42,9 @@ void check(int code) {
 
 // ------------------------------------------------------------------------------- codes and scales
 
-enum Kind { kMx4, kAct8 };
+enum Kind { kMx4, kAct8, kFp8 };
 
-// A matrix in blocks of 32: codes and scale bytes in one buffer, or in two tensors that the caller gave.
+// A matrix in blocks of 32 or 128: codes and scale bytes in one buffer, or in two tensors that the caller gave.
 struct Blocks {
   PyObject_HEAD
   at::Tensor* codes;    // or the buffer
@@ -53,14 +54,19 @@ struct Blocks {
   int device;
 };
 
-PyTypeObject* g_types[2] = {nullptr, nullptr};
-const char* const kNames[2] = {"MX4", "Act8"};
+PyTypeObject* g_types[3] = {nullptr, nullptr, nullptr};
+const char* const kNames[3] = {"MX4", "Act8", "FP8"};
 
-int64_t codes_bytes(Kind k, int64_t rows, int64_t cols) { return (int64_t)(k == kMx4 ? rudra_mx4_codes_bytes(rows, cols) : rudra_act8_codes_bytes(rows, cols)); }
-int64_t scales_bytes(Kind k, int64_t rows, int64_t cols) { return (int64_t)(k == kMx4 ? rudra_mx4_scales_bytes(rows, cols) : rudra_act8_scales_bytes(rows, cols)); }
+int64_t codes_bytes(Kind k, int64_t rows, int64_t cols) {
+  return (int64_t)(k == kMx4 ? rudra_mx4_codes_bytes(rows, cols) : k == kAct8 ? rudra_act8_codes_bytes(rows, cols) : rudra_fp8_codes_bytes(rows, cols));
+}
+int64_t scales_bytes(Kind k, int64_t rows, int64_t cols) {
+  return (int64_t)(k == kMx4 ? rudra_mx4_scales_bytes(rows, cols) : k == kAct8 ? rudra_act8_scales_bytes(rows, cols) : rudra_fp8_scales_bytes(rows, cols));
+}
 int64_t codes_room(Kind k, int64_t rows, int64_t cols) { return (codes_bytes(k, rows, cols) + 511) / 512 * 512; }
 
-Kind kind_of(PyObject* o) { return PyObject_TypeCheck(o, g_types[kMx4]) ? kMx4 : kAct8; }
+Kind kind_of(PyTypeObject* t) { return PyType_IsSubtype(t, g_types[kMx4]) ? kMx4 : PyType_IsSubtype(t, g_types[kAct8]) ? kAct8 : kFp8; }
+Kind kind_of(PyObject* o) { return kind_of(Py_TYPE(o)); }
 
 at::Tensor bytes(int64_t n, int device) {
   return at::detail::empty_cuda({n}, at::kByte, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
@@ -107,7 +113,7 @@ PyObject* blocks_new(PyTypeObject* type, PyObject* args, PyObject* kwargs) {
     PyObject *c, *s;
     long long rows, cols;
     if (!PyArg_ParseTupleAndKeywords(args, kwargs, "OOLL", const_cast<char**>(names), &c, &s, &rows, &cols)) return nullptr;
-    const Kind k = PyType_IsSubtype(type, g_types[kMx4]) ? kMx4 : kAct8;
+    const Kind k = kind_of(type);
     check_size(rows, cols);
     const at::Tensor &codes = tensor("codes", c), &scales = tensor("scales", s);
     const at::Tensor* both[2] = {&codes, &scales};
@@ -143,8 +149,9 @@ PyObject* blocks_codes(PyObject* o, void*) {
     const Blocks* b = reinterpret_cast<Blocks*>(o);
     if (b->scales) return THPVariable_Wrap(*b->codes);
     const Kind k = kind_of(o);
-    at::Tensor t = b->codes->narrow(0, 0, codes_bytes(k, b->rows, b->cols)).view({b->rows, (b->cols + 31) / 32 * (k == kMx4 ? 16 : 32)});
-    return THPVariable_Wrap(k == kMx4 ? t : t.view(at::kChar));
+    const int64_t pitch = k == kMx4 ? (b->cols + 31) / 32 * 16 : k == kAct8 ? (b->cols + 31) / 32 * 32 : (b->cols + 127) / 128 * 128;
+    at::Tensor t = b->codes->narrow(0, 0, codes_bytes(k, b->rows, b->cols)).view({b->rows, pitch});
+    return THPVariable_Wrap(k == kAct8 ? t.view(at::kChar) : t);
   });
 }
 PyObject* blocks_scales(PyObject* o, void*) {
@@ -153,7 +160,7 @@ PyObject* blocks_scales(PyObject* o, void*) {
     if (b->scales) return THPVariable_Wrap(*b->scales);
     const Kind k = kind_of(o);
     at::Tensor t = b->codes->narrow(0, codes_room(k, b->rows, b->cols), scales_bytes(k, b->rows, b->cols));
-    return THPVariable_Wrap(k == kMx4 ? t : t.view({b->rows, (b->cols + 511) / 512 * 16}));
+    return THPVariable_Wrap(k == kAct8 ? t.view({b->rows, (b->cols + 511) / 512 * 16}) : t);
   });
 }
 PyObject* blocks_rows(PyObject* o, void*) { return PyLong_FromLongLong(reinterpret_cast<Blocks*>(o)->rows); }
@@ -200,6 +207,16 @@ Matrix matrix(const char* what, const at::Tensor& t) {
   return m;
 }
 Matrix matrix(const char* what, PyObject* o) { return matrix(what, tensor(what, o)); }
+
+// A one-dimensional tensor of consecutive values.
+Matrix vector(const char* what, const at::Tensor& t) {
+  check_no_gradient(what, t);
+  const int dtype = dtype_of(t.scalar_type());
+  if (dtype < 0 || !t.is_cuda() || t.dim() != 1) refuse("%s: a one-dimensional float32 or bfloat16 tensor on the GPU is wanted", what);
+  if (t.size(0) > 1 && t.stride(0) != 1) refuse("%s: its values have to be contiguous", what);
+  return {t.data_ptr(), dtype, 1, t.size(0), t.size(0), (int)t.get_device()};
+}
+Matrix vector(const char* what, PyObject* o) { return vector(what, tensor(what, o)); }
 
 c10::ScalarType scalar_type(PyObject* o) {
   if (!THPDtype_Check(o) || dtype_of(reinterpret_cast<THPDtype*>(o)->scalar_type) < 0) refuse("dtype: float32 or bfloat16 is wanted");
@@ -249,6 +266,7 @@ class Held {
   explicit Held(Blocks* b) : o_(reinterpret_cast<PyObject*>(b)) {}
   Held(const Held&) = delete;
   ~Held() { Py_XDECREF(o_); }
+  PyObject* get() const { return o_; }
   PyObject* give() {
     PyObject* o = o_;
     o_ = nullptr;
@@ -293,7 +311,7 @@ PyObject* empty(PyObject*, PyObject* const* a, Py_ssize_t n) {   // kind, rows, 
   return returning([&]() -> PyObject* {
     count(n, 4);
     const long long k = number(a[0]);
-    return reinterpret_cast<PyObject*>(new_blocks(k ? kAct8 : kMx4, number(a[1]), number(a[2]), (int)number(a[3])));
+    return reinterpret_cast<PyObject*>(new_blocks(k == 2 ? kFp8 : k ? kAct8 : kMx4, number(a[1]), number(a[2]), (int)number(a[3])));
   });
 }
 
@@ -452,6 +470,212 @@ PyObject* act8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {   // d
   });
 }
 
+PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // x, transpose, square, out
+  return returning([&]() -> PyObject* {
+    count(n, 4);
+    const Matrix x = matrix("x", a[0]);
+    const bool t = truth(a[1]), square = truth(a[2]);
+    Blocks* q = blocks("out", kFp8, a[3], t ? x.cols : x.rows, t ? x.rows : x.cols, x.device);
+    Held held(q);
+    const On on(x.device);
+    check(rudra_fp8_quantize(x.p, x.dtype, x.rows, x.cols, x.ld, t, square, q->codes_at, q->scales_at, on.stream()));
+    return held.give();
+  });
+}
+
+PyObject* fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q, dtype, out
+  return returning([&]() -> PyObject* {
+    count(n, 3);
+    const Blocks* q = wanted("q", kFp8, a[0]);
+    const Output y = output("out", a[2], q->rows, q->cols, scalar_type(a[1]), true, q->device);
+    Held held(y.object);
+    const On on(q->device);
+    check(rudra_fp8_dequantize(q->codes_at, q->scales_at, q->rows, q->cols, y.m.p, y.m.dtype, y.m.ld, on.stream()));
+    return held.give();
+  });
+}
+
+PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {   // a, b, dtype, out
+  return returning([&]() -> PyObject* {
+    count(n, 4);
+    const Blocks* b = wanted("b", kFp8, a[1]);
+    const bool coded = PyObject_TypeCheck(a[0], g_types[kFp8]);
+    const Blocks* left = coded ? reinterpret_cast<const Blocks*>(a[0]) : nullptr;
+    const Matrix x = coded ? Matrix{nullptr, 0, left->rows, left->cols, 0, left->device} : matrix("a", a[0]);
+    if (x.cols != b->cols) refuse("a has rows of %lld values, b of %lld", (long long)x.cols, (long long)b->cols);
+    same_device(x.device, b->device);
+    const Output y = output("out", a[3], x.rows, b->rows, scalar_type(a[2]), true, b->device);
+    Held held(y.object);
+    const On on(b->device);
+    if (coded) {
+      check(rudra_fp8_matmul(left->codes_at, left->scales_at, x.rows, b->codes_at, b->scales_at, b->rows, x.cols, y.m.p, y.m.dtype, y.m.ld, on.stream()));
+    } else {
+      const uint64_t need = rudra_fp8_linear_workspace(x.rows, x.cols);
+      at::Tensor work;
+      if (need) work = bytes((int64_t)need, b->device);
+      check(rudra_fp8_linear(x.p, x.dtype, x.ld, x.rows, b->codes_at, b->scales_at, b->rows, x.cols, y.m.p, y.m.dtype, y.m.ld,
+                             need ? work.data_ptr() : nullptr, need, on.stream()));
+    }
+    return held.give();
+  });
+}
+
+// A matrix of the shape, dtype and device of x.
+Matrix alike(const char* what, PyObject* o, const Matrix& x) {
+  const Matrix m = matrix(what, o);
+  if (m.rows != x.rows || m.cols != x.cols || m.dtype != x.dtype || m.device != x.device)
+    refuse("%s: a %lld x %lld matrix of the operator's dtype on the input's device is wanted", what, (long long)x.rows, (long long)x.cols);
+  return m;
+}
+Matrix norm_weight(PyObject* o, const Matrix& x) {
+  const Matrix w = vector("weight", o);
+  if (w.cols != x.cols || w.device != x.device) refuse("weight: %lld values on the input's device are wanted", (long long)x.cols);
+  return w;
+}
+float real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw Raised();
+  return (float)v;
+}
+c10::ScalarType type_of(const Matrix& m) { return m.dtype == RUDRA_F32 ? at::kFloat : at::kBFloat16; }
+
+// x, weight, residual, eps, fp8, keep, out, out_sum, saved -> y, then s if there is a residual, then saved if it is kept
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return returning([&]() -> PyObject* {
+    count(n, 9);
+    const Matrix x = matrix("x", a[0]), w = norm_weight(a[1], x);
+    const bool two = a[2] != Py_None, fp8 = truth(a[4]), keep = truth(a[5]) || a[8] != Py_None;
+    const Matrix r = two ? alike("residual", a[2], x) : Matrix{};
+    const float eps = real(a[3]);
+    if (!two && a[7] != Py_None) refuse("out_sum: there is no residual to add");
+    const Output y = fp8 ? Output{reinterpret_cast<PyObject*>(blocks("out", kFp8, a[6], x.rows, x.cols, x.device)), {}}
+                         : output("out", a[6], x.rows, x.cols, type_of(x), false, x.device);
+    Held held(y.object);
+    const Blocks* q = fp8 ? reinterpret_cast<const Blocks*>(y.object) : nullptr;
+    const Output s = two ? output("out_sum", a[7], x.rows, x.cols, type_of(x), false, x.device) : Output{Py_NewRef(Py_None), {}};
+    Held held_sum(s.object);
+    Blocks* kept = keep ? blocks("saved", kAct8, a[8], x.rows, x.cols, x.device) : nullptr;
+    Held held_kept(kept);
+    const On on(x.device);
+    check(rudra_rms_norm(x.p, x.ld, two ? r.p : nullptr, r.ld, x.dtype, x.rows, x.cols, w.p, w.dtype, eps, s.m.p, s.m.ld, y.m.p, y.m.ld,
+                         q ? q->codes_at : nullptr, q ? q->scales_at : nullptr, kept ? kept->codes_at : nullptr, kept ? kept->scales_at : nullptr, on.stream()));
+    if (two && keep) return Py_BuildValue("NNN", held.give(), held_sum.give(), held_kept.give());
+    if (two) return Py_BuildValue("NN", held.give(), held_sum.give());
+    if (keep) return Py_BuildValue("NN", held.give(), held_kept.give());
+    return held.give();
+  });
+}
+
+// dy, s, weight, eps, dsum, dtype, out, out_weight -> (ds, dweight)
+PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return returning([&]() -> PyObject* {
+    count(n, 8);
+    const Matrix s = matrix("s", a[1]), dy = alike("dy", a[0], s), w = norm_weight(a[2], s);
+    const float eps = real(a[3]);
+    const Matrix more = a[4] != Py_None ? alike("dsum", a[4], s) : Matrix{};
+    const c10::ScalarType type = scalar_type(a[5]);
+    const Output ds = output("out", a[6], s.rows, s.cols, type_of(s), false, s.device);
+    Held held(ds.object);
+    Matrix dw;
+    PyObject* dw_object;
+    if (a[7] == Py_None) {
+      const at::Tensor t = at::detail::empty_cuda({s.cols}, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)s.device), std::nullopt);
+      dw = {t.data_ptr(), dtype_of(type), 1, s.cols, s.cols, s.device};
+      dw_object = THPVariable_Wrap(t);
+    } else {
+      dw = vector("out_weight", a[7]);
+      if (dw.cols != s.cols || dw.device != s.device) refuse("out_weight: %lld values on the input's device are wanted", (long long)s.cols);
+      dw_object = Py_NewRef(a[7]);
+    }
+    Held held_weight(dw_object);
+    const On on(s.device);
+    const uint64_t need = rudra_rms_norm_backward_workspace(s.rows, s.cols);
+    at::Tensor work;
+    if (need) work = bytes((int64_t)need, s.device);
+    check(rudra_rms_norm_backward(dy.p, dy.ld, s.p, s.ld, more.p, more.ld, s.dtype, s.rows, s.cols, w.p, w.dtype, eps, ds.m.p, ds.m.ld, dw.p, dw.dtype,
+                                  need ? work.data_ptr() : nullptr, need, on.stream()));
+    return Py_BuildValue("NN", held.give(), held_weight.give());
+  });
+}
+
+// A list of gradients, or of where they go: any shape, values one after another.
+struct Gradients {
+  std::vector<const void*> p;
+  std::vector<int> dtypes;
+  std::vector<uint64_t> sizes;
+  int device = -1;
+};
+Gradients gradients(const char* what, PyObject* o) {
+  Gradients g;
+  const Held fast(PySequence_Fast(o, "a list of tensors is wanted"));
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.get());
+  PyObject** items = PySequence_Fast_ITEMS(fast.get());
+  if (n == 0) refuse("%s: an empty list", what);
+  g.p.reserve(n);
+  g.dtypes.reserve(n);
+  g.sizes.reserve(n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const at::Tensor& t = tensor(what, items[i]);
+    check_no_gradient(what, t);
+    const int dtype = dtype_of(t.scalar_type());
+    if (dtype < 0 || !t.is_cuda() || !t.is_contiguous()) refuse("%s: contiguous float32 or bfloat16 tensors on the GPU are wanted", what);
+    if (g.device >= 0) same_device(g.device, (int)t.get_device());
+    g.device = (int)t.get_device();
+    g.p.push_back(t.data_ptr());
+    g.dtypes.push_back(dtype);
+    g.sizes.push_back((uint64_t)t.numel());
+  }
+  return g;
+}
+
+// A float on the device: the caller's (a new reference), or a new one of no dimensions.
+Output scalar(const char* what, PyObject* given, int device) {
+  if (given == Py_None) {
+    const at::Tensor t = at::detail::empty_cuda({}, at::kFloat, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
+    return {THPVariable_Wrap(t), {t.data_ptr(), RUDRA_F32, 1, 1, 1, device}};
+  }
+  const at::Tensor& t = tensor(what, given);
+  check_no_gradient(what, t);
+  if (t.scalar_type() != at::kFloat || !t.is_cuda() || t.numel() != 1 || (int)t.get_device() != device) refuse("%s: one float32 value on the gradients' device is wanted", what);
+  return {Py_NewRef(given), {t.data_ptr(), RUDRA_F32, 1, 1, 1, device}};
+}
+
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gradients, out
+  return returning([&]() -> PyObject* {
+    count(n, 2);
+    const Gradients g = gradients("gradients", a[0]);
+    const Output norm = scalar("out", a[1], g.device);
+    Held held(norm.object);
+    const On on(g.device);
+    const uint64_t need = rudra_grad_norm_workspace(g.p.size());
+    const at::Tensor work = bytes((int64_t)need, g.device);
+    check(rudra_grad_norm(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<float*>(norm.m.p), work.data_ptr(), need, on.stream()));
+    return held.give();
+  });
+}
+
+PyObject* clip_gradients(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gradients, max_norm, out, norm -> norm
+  return returning([&]() -> PyObject* {
+    count(n, 4);
+    const Gradients g = gradients("gradients", a[0]);
+    const float most = real(a[1]);
+    const bool in_place = a[2] == Py_None;
+    const Gradients to = in_place ? Gradients() : gradients("out", a[2]);
+    if (!in_place && (to.sizes != g.sizes || to.device != g.device)) refuse("out: as many tensors as gradients, each of its gradient's size and device, are wanted");
+    const Output norm = scalar("norm", a[3], g.device);
+    Held held(norm.object);
+    const On on(g.device);
+    if (a[3] == Py_None) {
+      const uint64_t need = rudra_grad_norm_workspace(g.p.size());
+      const at::Tensor work = bytes((int64_t)need, g.device);
+      check(rudra_grad_norm(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<float*>(norm.m.p), work.data_ptr(), need, on.stream()));
+    }
+    check(rudra_grad_clip(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<const float*>(norm.m.p), most,
+                          const_cast<void* const*>(in_place ? g.p.data() : to.p.data()), in_place ? g.dtypes.data() : to.dtypes.data(), on.stream()));
+    return held.give();
+  });
+}
+
 PyObject* synchronize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // device
   return returning([&]() -> PyObject* {
     count(n, 1);
@@ -468,7 +692,8 @@ PyObject* synchronize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // device
 PyMethodDef methods[] = {
 #define RUDRA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
     RUDRA_METHOD(empty), RUDRA_METHOD(current_stream), RUDRA_METHOD(mx4_quantize), RUDRA_METHOD(mx4_dequantize), RUDRA_METHOD(mx4_matmul), RUDRA_METHOD(act8_values),
-    RUDRA_METHOD(act8_forward), RUDRA_METHOD(act8_backward), RUDRA_METHOD(act8_weight_grad), RUDRA_METHOD(synchronize),
+    RUDRA_METHOD(act8_forward), RUDRA_METHOD(act8_backward), RUDRA_METHOD(act8_weight_grad), RUDRA_METHOD(fp8_quantize), RUDRA_METHOD(fp8_dequantize),
+    RUDRA_METHOD(fp8_matmul), RUDRA_METHOD(rms_norm), RUDRA_METHOD(rms_norm_backward), RUDRA_METHOD(grad_norm), RUDRA_METHOD(clip_gradients), RUDRA_METHOD(synchronize),
 #undef RUDRA_METHOD
     {nullptr, nullptr, 0, nullptr}};
 
@@ -495,12 +720,15 @@ PyMODINIT_FUNC PyInit__learner() {
                            "MX4(codes, scales, rows, cols): a matrix in microscaled 4-bit floating point, uint8 tensors laid out as the header says.");
   g_types[kAct8] = new_type("paper_1509_04210_b200._learner.Act8",
                             "Act8(codes, scales, rows, cols): an 8-bit checkpoint of rows tokens x cols channels, laid out as the header says.");
-  if (!g_error || !g_types[kMx4] || !g_types[kAct8]) return nullptr;
+  g_types[kFp8] = new_type("paper_1509_04210_b200._learner.FP8",
+                           "FP8(codes, scales, rows, cols): a matrix in 8-bit floating point in blocks of 128, one-byte tensors laid out as the header says.");
+  if (!g_error || !g_types[kMx4] || !g_types[kAct8] || !g_types[kFp8]) return nullptr;
   PyObject* m = PyModule_Create(&module);
   if (!m) return nullptr;
   if (PyModule_AddStringConstant(m, "build_key", RUDRA_LEARNER_KEY) < 0 ||
       PyModule_AddObjectRef(m, "MX4", reinterpret_cast<PyObject*>(g_types[kMx4])) < 0 ||
-      PyModule_AddObjectRef(m, "Act8", reinterpret_cast<PyObject*>(g_types[kAct8])) < 0) {
+      PyModule_AddObjectRef(m, "Act8", reinterpret_cast<PyObject*>(g_types[kAct8])) < 0 ||
+      PyModule_AddObjectRef(m, "FP8", reinterpret_cast<PyObject*>(g_types[kFp8])) < 0) {
     Py_DECREF(m);
     return nullptr;
   }

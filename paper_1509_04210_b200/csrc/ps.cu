@@ -1039,9 +1039,12 @@ cudaError_t order_streams(rudra_ps* ps, cudaStream_t first, cudaStream_t then) {
   return e;
 }
 
+// Which form a matrix is pulled in.
+enum class Pulled { kMx4, kFp8 };
+
 // caller: the stream whose work comes before and after, if that is to be ordered.
-int64_t pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev, void* scales_dev,
-                 const cudaStream_t* caller) {
+int64_t pull_blocks(Pulled form, rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev, void* scales_dev,
+                    const cudaStream_t* caller) {
   return guarded([&]() -> int64_t {
     if (!valid(ps)) return fail(RUDRA_E_INVAL, "bad handle");
     if (rows > RUDRA_MAX_DIM || cols > RUDRA_MAX_DIM) return fail(RUDRA_E_INVAL, "more than RUDRA_MAX_DIM rows or columns");
@@ -1052,7 +1055,8 @@ int64_t pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, in
     cudaError_t e = caller ? order_streams(ps, *caller, ps->stream) : cudaSuccess;
     if (e != cudaSuccess) return cuda_fail(e, "ordering the server's stream after the caller's");
     rudra::MatrixIn src = {ps->theta + offset, rudra::kF32, rows, cols, cols};
-    e = rudra::launch_mx4_quantize(src, transpose != 0, codes_dev, scales_dev, ps->stream);
+    e = form == Pulled::kMx4 ? rudra::launch_mx4_quantize(src, transpose != 0, codes_dev, scales_dev, ps->stream)
+                             : rudra::launch_fp8_quantize(src, transpose != 0, true, codes_dev, scales_dev, ps->stream);
     if (e != cudaSuccess) return cuda_fail(e, "quantization kernel launch");
     e = caller ? order_streams(ps, ps->stream, *caller) : cudaSuccess;
     if (e != cudaSuccess) return cuda_fail(e, "ordering the caller's stream after the server's");
@@ -1066,13 +1070,24 @@ int64_t pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, in
 
 int64_t rudra_ps_pull_mx4(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
                           void* scales_dev) {
-  return pull_mx4(ps, offset, rows, cols, transpose, codes_dev, scales_dev, nullptr);
+  return pull_blocks(Pulled::kMx4, ps, offset, rows, cols, transpose, codes_dev, scales_dev, nullptr);
 }
 
 int64_t rudra_ps_pull_mx4_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
                              void* scales_dev, void* cuda_stream) {
   const cudaStream_t caller = static_cast<cudaStream_t>(cuda_stream);
-  return pull_mx4(ps, offset, rows, cols, transpose, codes_dev, scales_dev, &caller);
+  return pull_blocks(Pulled::kMx4, ps, offset, rows, cols, transpose, codes_dev, scales_dev, &caller);
+}
+
+int64_t rudra_ps_pull_fp8(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                          void* scales_dev) {
+  return pull_blocks(Pulled::kFp8, ps, offset, rows, cols, transpose, codes_dev, scales_dev, nullptr);
+}
+
+int64_t rudra_ps_pull_fp8_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint64_t cols, int transpose, void* codes_dev,
+                             void* scales_dev, void* cuda_stream) {
+  const cudaStream_t caller = static_cast<cudaStream_t>(cuda_stream);
+  return pull_blocks(Pulled::kFp8, ps, offset, rows, cols, transpose, codes_dev, scales_dev, &caller);
 }
 
 int64_t rudra_ps_pull_host(rudra_ps* ps, float* dst_host) {
