@@ -11,11 +11,14 @@
 #include "fp8.cuh"
 #include "launch.cuh"
 #include "learner.cuh"
+#include "tensor.cuh"
 
 namespace rudra {
 namespace {
 
 constexpr uint32_t kMostThreads = 512;
+constexpr uint32_t kMostWarps = kMostThreads / 32;
+constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers
 
 // Sum over the threads of a block in a fixed order; every thread gets it.  `room`: 32 floats.
 __device__ __forceinline__ float block_sum(float v, float* room) {
@@ -29,6 +32,45 @@ __device__ __forceinline__ float block_sum(float v, float* room) {
   for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
   return s;
 }
+
+// Where the threads of a row meet: its warps' two sums, for this row and the next.
+using Room = float2[2][kMostWarps];
+
+// Sums over the `warps` warps of a row in a fixed order; every thread gets them.  The next row's go to the other half of the
+// room, so that one barrier a row is enough.
+__device__ __forceinline__ float2 row_sums(float2 v, uint32_t warps, uint32_t group, uint32_t parity, Room& room) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) {
+    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
+    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
+  }
+  if (warps == 1) return v;
+  const uint32_t lane = threadIdx.x % 32;
+  if (lane == 0) room[parity][threadIdx.x / 32] = v;
+  asm volatile("barrier.cta.sync %0, %1;" :: "r"(group + 1), "r"(warps * 32) : "memory");
+  v = lane < warps ? room[parity][group * warps + lane] : make_float2(0.f, 0.f);
+#pragma unroll
+  for (int d = 16; d; d /= 2) {
+    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
+    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
+  }
+  return v;
+}
+
+// 1 / sqrt(m) as a float and what it is off by.
+struct Root {
+  float hi, lo;
+  __device__ __forceinline__ explicit Root(float m) {
+    hi = __frsqrt_rn(m);
+    const float p = hi * hi, off = fmaf(m, p, -1.f) + m * fmaf(hi, hi, -p);     // m hi^2 - 1
+    lo = fabsf(off) < 1e-6f && m < 1e30f ? -0.5f * hi * off : 0.f;               // where nothing in it overflowed or was lost
+  }
+  // s * w / sqrt(m), rounded about once: two products round twice, and turn twice as many codes of an 8-bit output into their neighbours.
+  __device__ __forceinline__ float scaled(float s, float w) const {
+    const float t = s * hi, off = fmaf(s, lo, fmaf(s, hi, -t));
+    return fmaf(t, w, off * w);
+  }
+};
 
 template <typename G> __device__ __forceinline__ float rounded(float v) {
   if constexpr (sizeof(G) == 4) return v;
@@ -82,6 +124,58 @@ __device__ __forceinline__ void put_outputs(const Forward<G, W>& p, Meeting* mee
   }
 }
 
+// Rows that are held in registers, a group of `warps` warps to each: 16 values to a thread, twice 16 where TWICE.  A block's groups
+// walk over the rows, each with the next one on its way while it works on one.
+template <typename G, typename W, bool ANY, bool TWICE>
+__global__ void __launch_bounds__(kMostThreads) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
+  constexpr int kParts = TWICE ? 2 : 1;
+  __shared__ Meeting meeting[ANY ? kMostWarps : 1];
+  __shared__ Room room;
+  admit_next_kernel();
+  const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, t = threadIdx.x - group * warps * 32;
+  uint32_t c[kParts];
+  int have[kParts];
+  Values<W> w[kParts];
+  await_previous_kernel();
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) {
+    c[k] = (k * warps * 32 + t) * kValues;
+    have[k] = c[k] < p.cols ? (int)min((uint32_t)kValues, p.cols - c[k]) : 0;
+    w[k].template load<ANY>(p.w, have[k] ? c[k] : 0, have[k]);
+  }
+  Values<G> x[kParts], r[kParts];
+  uint64_t row = blockIdx.x * groups + group;
+  const uint64_t step = (uint64_t)gridDim.x * groups;
+  const auto load = [&](uint64_t at) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      x[k].template load<ANY>(p.x, have[k] ? at * p.x.ld + c[k] : 0, have[k]);
+      if (p.residual.p) r[k].template load<ANY>(p.residual, have[k] ? at * p.residual.ld + c[k] : 0, have[k]);
+    }
+  };
+  if (row < rows) load(row);
+  for (uint32_t parity = 0; row < rows; row += step, parity ^= 1) {
+    float s[kParts][kValues], part = 0.f;
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) {
+        s[k][i] = p.residual.p ? rounded<G>(x[k].get(i) + r[k].get(i)) : x[k].get(i);
+        part = fmaf(s[k][i], s[k][i], part);
+      }
+      if (p.sum) store_any<G, ANY>(meeting, p.sum + (have[k] ? row * p.ldsum + c[k] : 0), access_of<G>(p.sum, p.ldsum), have[k], s[k]);
+    }
+    if (row + step < rows) load(row + step);
+    const Root root(row_sums(make_float2(part, 0.f), warps, group, parity, room).x / p.columns + p.eps);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) s[k][i] = root.scaled(s[k][i], w[k].get(i));
+      put_outputs<G, W, ANY>(p, meeting, row, c[k], have[k], s[k]);
+    }
+  }
+}
+
 // A block to a row of any length, read twice: the second time s where it was written.
 template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kMostThreads) norm_long_kernel(const __grid_constant__ Forward<G, W> p) {
   __shared__ Meeting meeting[ANY ? kMostThreads / 32 : 1];
@@ -108,7 +202,7 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
     total += part;
     if (p.sum) store_any<G, ANY>(meeting, p.sum + (have ? row * p.ldsum + c : 0), access_of<G>(p.sum, p.ldsum), have, s);
   }
-  const float inv = __frsqrt_rn(block_sum(total, room) / p.columns + p.eps);     // its barriers: s is there for all to read
+  const Root root(block_sum(total, room) / p.columns + p.eps);     // its barriers: s is there for all to read
   const Rows<G> again = p.sum ? Rows<G>{p.sum, p.ldsum, p.sum + (gridDim.x - 1) * p.ldsum + p.cols, access_of<G>(p.sum, p.ldsum)} : p.x;
   for (uint64_t c0 = threadIdx.x / 32 * 32 * kValues; c0 < end; c0 += step) {
     const uint64_t c = c0 + lane * kValues;
@@ -119,7 +213,7 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
     w.template load<ANY>(p.w, have ? c : 0, have);
     float y[kValues];
 #pragma unroll
-    for (int i = 0; i < kValues; ++i) y[i] = s.get(i) * inv * w.get(i);
+    for (int i = 0; i < kValues; ++i) y[i] = root.scaled(s.get(i), w.get(i));
     put_outputs<G, W, ANY>(p, meeting, row, (uint32_t)c, have, y);
   }
 }
@@ -134,6 +228,118 @@ template <typename G, typename W> struct Backward {
   float eps, columns;
   float2* stats;           // of a row: 1 / rms and m / rms^2
 };
+
+// Both gradients from rows that are held in registers, a group of `warps` warps to each, 16 values to a thread or twice 16.  A
+// block's groups walk over the rows and add up what the rows give for the weight; at the end the groups' sums are added in order
+// in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
+// are one cluster, which adds the parts itself.
+template <typename G, typename W, bool ANY, bool TWICE, bool CLUSTER>
+__global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
+  constexpr int kParts = TWICE ? 2 : 1;
+  constexpr bool kAhead = sizeof(G) == 2 && !TWICE;      // where registers do for two rows
+  __shared__ Meeting meeting[ANY ? kMostWarps : 1];
+  __shared__ Room room;
+  extern __shared__ float sums[];
+  admit_next_kernel();
+  const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
+  uint32_t c[kParts];
+  int have[kParts];
+  Values<W> w[kParts];
+  await_previous_kernel();
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) {
+    c[k] = (k * T + t) * kValues;
+    have[k] = c[k] < p.cols ? (int)min((uint32_t)kValues, p.cols - c[k]) : 0;
+    w[k].template load<ANY>(p.w, have[k] ? c[k] : 0, have[k]);
+  }
+  Values<G> s[kParts], dy[kParts], more[kParts];
+  uint64_t row = blockIdx.x * groups + group;
+  const uint64_t step = (uint64_t)gridDim.x * groups;
+  const auto load = [&](uint64_t at, Values<G> (&vs)[kParts], Values<G> (&vd)[kParts], Values<G> (&vm)[kParts]) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      vs[k].template load<ANY>(p.s, have[k] ? at * p.s.ld + c[k] : 0, have[k]);
+      vd[k].template load<ANY>(p.dy, have[k] ? at * p.dy.ld + c[k] : 0, have[k]);
+      if (p.dsum.p) vm[k].template load<ANY>(p.dsum, have[k] ? at * p.dsum.ld + c[k] : 0, have[k]);
+    }
+  };
+  float total[kParts][kValues] = {};
+  if (row < p.rows) load(row, s, dy, more);
+  for (uint32_t parity = 0; row < p.rows; row += step, parity ^= 1) {
+    Values<G> s1[kParts], dy1[kParts], more1[kParts];
+    if (kAhead && row + step < p.rows) load(row + step, s1, dy1, more1);
+    float2 part = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) {
+        part.x = fmaf(s[k].get(i), s[k].get(i), part.x);
+        part.y = fmaf(dy[k].get(i) * w[k].get(i), s[k].get(i), part.y);
+      }
+    part = row_sums(part, warps, group, parity, room);
+    const float inv = __frsqrt_rn(part.x / p.columns + p.eps), m = part.y / p.columns * inv * inv;
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      float d[kValues];
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) {
+        const float a = s[k].get(i), b = dy[k].get(i);
+        total[k][i] = fmaf(b, a * inv, total[k][i]);
+        d[i] = fmaf(b, w[k].get(i), -a * m) * inv;
+        if (p.dsum.p) d[i] += more[k].get(i);
+      }
+      store_any<G, ANY>(meeting, p.ds + (have[k] ? row * p.ldds + c[k] : 0), access_of<G>(p.ds, p.ldds), have[k], d);
+    }
+    if (kAhead) {
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) s[k] = s1[k], dy[k] = dy1[k], more[k] = more1[k];
+    } else if (row + step < p.rows) {
+      load(row + step, s, dy, more);
+    }
+  }
+  const uint32_t all = kParts * kValues * T;
+  for (uint32_t g = 0; (groups > 1 || CLUSTER) && g < groups; ++g) {
+    if (g == group)
+#pragma unroll
+      for (int k = 0; k < kParts; ++k)
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+          float* const to = sums + (k * kValues + i) * T + t;
+          *to = g ? *to + total[k][i] : total[k][i];
+        }
+    __syncthreads();
+  }
+  if (CLUSTER) {
+    const uint32_t blocks = gridDim.x, rank = blocks > 1 ? cluster_rank() : 0;
+    if (blocks > 1) {
+      cluster_arrive();
+      cluster_wait();
+    }
+    const uint32_t at = smem_address(sums);
+    for (uint32_t j = rank * blockDim.x + threadIdx.x; j < all; j += blocks * blockDim.x) {
+      float v = 0.f;
+      for (uint32_t b = 0; b < blocks; ++b) v += blocks > 1 ? peer_value(at + 4 * j, b) : sums[j];
+      const uint32_t i = j / T, column = (i / kValues * T + j % T) * kValues + i % kValues;
+      if (column < p.cols) {
+        if (dw_type == kBF16) static_cast<__nv_bfloat16*>(dw)[column] = __float2bfloat16_rn(v);
+        else static_cast<float*>(dw)[column] = v;
+      }
+    }
+    if (blocks > 1) {      // the sums stay until all have read them
+      cluster_arrive();
+      cluster_wait();
+    }
+    return;
+  }
+  if (groups > 1) {
+    for (uint32_t j = threadIdx.x; j < all; j += blockDim.x) parts[(uint64_t)blockIdx.x * all + j] = sums[j];
+  } else {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) parts[(uint64_t)blockIdx.x * all + (k * kValues + i) * T + t] = total[k][i];
+  }
+}
 
 // A row's statistics, by a block.
 template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kMostThreads) norm_stats_kernel(const __grid_constant__ Backward<G, W> p) {
@@ -210,28 +416,42 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
   }
 }
 
-// dw: the parts of all shares added in order, by eight warps in turn.
-template <typename D> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t shares, uint32_t cols, D* dw) {
+// dw: the parts of all shares added in order, by eight warps in turn.  A part has `length` values, in the columns' order or, T not
+// zero, in that of the threads.
+template <typename D> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t shares, uint32_t length, uint32_t T, uint32_t cols, D* dw) {
   __shared__ float room[8][32];
   admit_next_kernel();
   await_previous_kernel();
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, j = blockIdx.x * 32 + lane;
   float total = 0.f;
-  if (c < cols)
-    for (uint32_t i = warp; i < shares; i += 8) total += parts[(uint64_t)i * cols + c];
+  if (j < length) {
+#pragma unroll 4
+    for (uint32_t i = warp; i < shares; i += 8) total += parts[(uint64_t)i * length + j];
+  }
   room[warp][lane] = total;
   __syncthreads();
-  if (warp == 0 && c < cols) {
-    for (int i = 1; i < 8; ++i) total += room[i][lane];
+  const uint32_t i = T ? j / T : 0, c = T ? (i / kValues * T + j % T) * kValues + i % kValues : j;
+  if (warp == 0 && j < length && c < cols) {
+    for (int k = 1; k < 8; ++k) total += room[k][lane];
     if constexpr (sizeof(D) == 4) dw[c] = total;
     else dw[c] = __float2bfloat16_rn(total);
   }
 }
 
-uint32_t threads_for(uint64_t cols) {   // of a row: 16 values each
-  return (uint32_t)std::min<uint64_t>(kMostThreads, ((cols + kValues - 1) / kValues + 31) / 32 * 32);
-}
+// How rows that are held in registers are given to blocks: as many to a block as fill it, and as many blocks as run at once.
+struct Split {
+  bool twice;
+  uint32_t warps, threads, blocks;
+  Split(uint64_t rows, uint64_t padded) {
+    twice = padded > kMostThreads * kValues;
+    const uint64_t per_warp = 32 * kValues * (twice ? 2 : 1);
+    warps = (uint32_t)((padded + per_warp - 1) / per_warp);
+    const uint32_t groups = (uint32_t)std::min<uint64_t>(kMostWarps / warps, rows);
+    threads = groups * warps * 32;
+    blocks = (uint32_t)std::min<uint64_t>((rows + groups - 1) / groups, kSms * std::max(1u, kMostThreads / threads));
+  }
+  uint32_t length() const { return warps * 32 * kValues * (twice ? 2 : 1); }     // of a part of the weight's gradient
+};
 
 template <typename G, typename W> cudaError_t forward(const NormForward& n, cudaStream_t stream) {
   const uint64_t rows = n.x.rows, cols = n.x.cols;
@@ -258,8 +478,13 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   if (p.residual.p) all = both(all, p.residual.access);
   if (p.sum) all = both(all, access_of<G>(p.sum, p.ldsum));
   if (p.y) all = both(all, access_of<G>(p.y, p.ldy));
-  return launch_overlapped(all == kByElement ? norm_long_kernel<G, W, true> : norm_long_kernel<G, W, false>, (uint32_t)rows,
-                           threads_for(std::max<uint64_t>(cols, (uint64_t)p.nb * kFp8Block)), 0, 1, stream, p);
+  const uint64_t padded = std::max(std::max<uint64_t>(cols, (uint64_t)p.nb * kFp8Block), (uint64_t)p.kept_blocks * 32);
+  const bool any = all == kByElement;
+  if (padded > kMostHeld)
+    return launch_overlapped(any ? norm_long_kernel<G, W, true> : norm_long_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
+  const Split a(rows, padded);
+  return launch_overlapped(a.twice ? any ? norm_kernel<G, W, true, true> : norm_kernel<G, W, false, true> : any ? norm_kernel<G, W, true, false> : norm_kernel<G, W, false, false>,
+                           a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
 }
 
 constexpr uint64_t kMostShares = 296;
@@ -267,6 +492,28 @@ constexpr uint64_t kMostShares = 296;
 uint64_t shares_for(uint64_t rows, uint64_t cols) {
   const uint64_t strips = (cols + 31) / 32;
   return std::max<uint64_t>(1, std::min(kMostShares / std::min(strips, kMostShares), (rows + 7) / 8));
+}
+
+constexpr uint32_t kMostCluster = 8;
+
+template <typename G, typename W, bool ANY, bool TWICE, bool CLUSTER>
+cudaError_t run_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
+  static Device device;
+  const Device::Facts* facts;
+  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, ANY, TWICE, CLUSTER>, kMostThreads, kMostHeld * sizeof(float), 0, &facts);
+  if (e != cudaSuccess) return e;
+  const uint32_t smem = CLUSTER || a.threads > a.warps * 32 ? a.length() * (uint32_t)sizeof(float) : 0;
+  return launch_overlapped(norm_backward_kernel<G, W, ANY, TWICE, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
+}
+template <typename G, typename W, bool ANY, typename... A> cudaError_t pick_backward(const Split& a, A&&... args) {
+  if (a.blocks <= kMostCluster) return a.twice ? run_backward<G, W, ANY, true, true>(args...) : run_backward<G, W, ANY, false, true>(args...);
+  return a.twice ? run_backward<G, W, ANY, true, false>(args...) : run_backward<G, W, ANY, false, false>(args...);
+}
+
+cudaError_t join(const NormBackward& n, const float* parts, uint32_t shares, uint32_t length, uint32_t T, cudaStream_t stream) {
+  const uint32_t strips = (length + 31) / 32, cols = (uint32_t)n.s.cols;
+  if (n.dw_type == kBF16) return launch_overlapped(norm_join_kernel<__nv_bfloat16>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<__nv_bfloat16*>(n.dw));
+  return launch_overlapped(norm_join_kernel<float>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<float*>(n.dw));
 }
 
 template <typename G, typename W> cudaError_t backward(const NormBackward& n, void* workspace, cudaStream_t stream) {
@@ -285,16 +532,20 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
   p.stats = static_cast<float2*>(workspace);
   Access all = both(both(p.dy.access, p.s.access), both(p.w.access, access_of<G>(p.ds, p.ldds)));
   if (p.dsum.p) all = both(all, p.dsum.access);
+  const bool any = all == kByElement;
+  if (cols <= kMostHeld) {
+    const Split a(rows, cols);
+    float* parts = static_cast<float*>(workspace);
+    const cudaError_t e = any ? pick_backward<G, W, true>(a, p, a, parts, n, stream) : pick_backward<G, W, false>(a, p, a, parts, n, stream);
+    return e != cudaSuccess || a.blocks <= kMostCluster ? e : join(n, parts, a.blocks, a.length(), a.warps * 32, stream);
+  }
   const uint64_t strips = (cols + 31) / 32, shares = shares_for(rows, cols);
   float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + (rows * sizeof(float2) + 31) / 32 * 32);
-  const bool any = all == kByElement;
-  cudaError_t e = launch_overlapped(any ? norm_stats_kernel<G, W, true> : norm_stats_kernel<G, W, false>, (uint32_t)rows, threads_for(cols), 0, 1, stream, p);
+  cudaError_t e = launch_overlapped(any ? norm_stats_kernel<G, W, true> : norm_stats_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
   if (e == cudaSuccess) e = launch_overlapped(norm_weight_kernel<G, W>, (uint32_t)(strips * shares), 256, 0, 1, stream, p, (uint32_t)strips, (uint32_t)shares, parts);
   // only now: it may be written over dy
-  if (e == cudaSuccess) e = launch_overlapped(any ? norm_input_kernel<G, W, true> : norm_input_kernel<G, W, false>, (uint32_t)rows, threads_for(cols), 0, 1, stream, p);
-  if (e != cudaSuccess) return e;
-  return n.dw_type == kBF16 ? launch_overlapped(norm_join_kernel<__nv_bfloat16>, (uint32_t)strips, 256, 0, 1, stream, parts, (uint32_t)shares, (uint32_t)cols, static_cast<__nv_bfloat16*>(n.dw))
-                            : launch_overlapped(norm_join_kernel<float>, (uint32_t)strips, 256, 0, 1, stream, parts, (uint32_t)shares, (uint32_t)cols, static_cast<float*>(n.dw));
+  if (e == cudaSuccess) e = launch_overlapped(any ? norm_input_kernel<G, W, true> : norm_input_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
+  return e != cudaSuccess ? e : join(n, parts, (uint32_t)shares, (uint32_t)cols, 0, stream);
 }
 
 }  // namespace
@@ -305,6 +556,10 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 }
 
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
+  if (cols <= kMostHeld) {
+    const Split a(rows, cols);
+    return a.blocks <= kMostCluster ? 0 : (uint64_t)a.blocks * a.length() * sizeof(float);
+  }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
 }
 

@@ -84,7 +84,7 @@ def test_norm_refusals():
         _refused(f(eps=eps), "eps")
     assert f(x=None, t=0, w=None, y=None) == 0
 
-    def b(dy=P, s=P, m=None, dtype=1, t=4, c=64, w=P, wt=0, eps=1e-6, ds=P, ldds=64, dw=P, dwt=0, ws=P, n=1 << 30):
+    def b(dy=P, s=P, m=None, dtype=1, t=400, c=64, w=P, wt=0, eps=1e-6, ds=P, ldds=64, dw=P, dwt=0, ws=P, n=1 << 30):
         return L.rudra_rms_norm_backward(dy, 64, s, 64, m, 64, dtype, t, c, w, wt, eps, ds, ldds, dw, dwt, ws, n, None)
 
     _refused(b(dy=None), "gradient of the output")
@@ -98,7 +98,7 @@ def test_norm_refusals():
     _refused(b(dwt=9), "dtype")
     _refused(b(ws=None), "workspace")
     _refused(b(ws=P + 4), "workspace")
-    _refused(b(n=L.rudra_rms_norm_backward_workspace(4, 64) - 1), "workspace")
+    _refused(b(n=L.rudra_rms_norm_backward_workspace(400, 64) - 1), "workspace")
     _refused(b(eps=float("nan")), "eps")
 
 
