@@ -11,14 +11,14 @@
 #include "fp8.cuh"
 #include "launch.cuh"
 #include "learner.cuh"
+#include "pairs.cuh"
 #include "tensor.cuh"
 
 namespace rudra {
 namespace {
 
 constexpr uint32_t kMostThreads = 512;
-constexpr uint32_t kMostWarps = kMostThreads / 32;
-constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers
+constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers: 32 to a thread
 
 // Sum over the threads of a block in a fixed order; every thread gets it.  `room`: 32 floats.
 __device__ __forceinline__ float block_sum(float v, float* room) {
@@ -33,39 +33,50 @@ __device__ __forceinline__ float block_sum(float v, float* room) {
   return s;
 }
 
-// Where the threads of a row meet: its warps' two sums, for this row and the next.
-using Room = float2[2][kMostWarps];
+// Where the threads of a row meet: its warps' sums, for this row and the next.
+template <typename T> using Room = T[2][32];
+
+__device__ __forceinline__ float exchanged(float v, int d) { return v + __shfl_xor_sync(0xFFFFFFFFu, v, d); }
+__device__ __forceinline__ Pair exchanged(Pair v, int d) {
+  return v + Pair(__shfl_xor_sync(0xFFFFFFFFu, v.lo(), d), __shfl_xor_sync(0xFFFFFFFFu, v.hi(), d));
+}
 
 // Sums over the `warps` warps of a row in a fixed order; every thread gets them.  The next row's go to the other half of the
 // room, so that one barrier a row is enough.
-__device__ __forceinline__ float2 row_sums(float2 v, uint32_t warps, uint32_t group, uint32_t parity, Room& room) {
+template <typename T> __device__ __forceinline__ T row_sum(T v, uint32_t warps, uint32_t group, uint32_t parity, Room<T>& room) {
 #pragma unroll
-  for (int d = 16; d; d /= 2) {
-    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
-    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
-  }
+  for (int d = 16; d; d /= 2) v = exchanged(v, d);
   if (warps == 1) return v;
-  const uint32_t lane = threadIdx.x % 32;
+  const uint32_t lane = threadIdx.x % 32, span = 1u << (32 - __clz(warps - 1)), of = lane & (span - 1);
   if (lane == 0) room[parity][threadIdx.x / 32] = v;
   asm volatile("barrier.cta.sync %0, %1;" :: "r"(group + 1), "r"(warps * 32) : "memory");
-  v = lane < warps ? room[parity][group * warps + lane] : make_float2(0.f, 0.f);
+  v = of < warps ? room[parity][group * warps + of] : T{};
 #pragma unroll
-  for (int d = 16; d; d /= 2) {
-    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
-    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
-  }
+  for (uint32_t d = 16; d; d /= 2)
+    if (d < span) v = exchanged(v, (int)d);
   return v;
 }
 
-// 1 / sqrt(m) as a float and what it is off by.
+// sum / n from 1 / n, rounded about as a division would be, at a fraction of its instructions.
+__device__ __forceinline__ float mean(float sum, float n, float one_nth) {
+  const float q = sum * one_nth, off = fmaf(-q, n, sum);
+  return fabsf(q) < 1e30f ? fmaf(off, one_nth, q) : q;      // beyond that `off` may be no number
+}
+
+// 1 / sqrt(m) as a float and what that is off by.
 struct Root {
   float hi, lo;
   __device__ __forceinline__ explicit Root(float m) {
-    hi = __frsqrt_rn(m);
+    hi = rsqrtf(m);
     const float p = hi * hi, off = fmaf(m, p, -1.f) + m * fmaf(hi, hi, -p);     // m hi^2 - 1
     lo = fabsf(off) < 1e-6f && m < 1e30f ? -0.5f * hi * off : 0.f;               // where nothing in it overflowed or was lost
   }
+  __device__ __forceinline__ float value() const { return hi + lo; }
   // s * w / sqrt(m), rounded about once: two products round twice, and turn twice as many codes of an 8-bit output into their neighbours.
+  __device__ __forceinline__ Pair scaled(Pair s, Pair w) const {
+    const Pair h(hi), t = s * h, off = fma(s, Pair(lo), fma(s, h, Pair(-t.lo(), -t.hi())));
+    return fma(t, w, off * w);
+  }
   __device__ __forceinline__ float scaled(float s, float w) const {
     const float t = s * hi, off = fmaf(s, lo, fmaf(s, hi, -t));
     return fmaf(t, w, off * w);
@@ -92,7 +103,7 @@ template <typename G, typename W> struct Forward {
   uint4* kept;             // ACT8 of y
   uint8_t* kept_scales;
   uint32_t cols, nb, kt, kept_blocks, kept_pitch;
-  float eps, columns;      // cols as a float
+  float eps, columns, one_nth;   // cols as a float, and its inverse
 };
 
 // What leaves of a thread's 16 values of y: column `c` of `row`, `have` of them in the row.  Whole warps.
@@ -124,55 +135,152 @@ __device__ __forceinline__ void put_outputs(const Forward<G, W>& p, Meeting* mee
   }
 }
 
-// Rows that are held in registers, a group of `warps` warps to each: 16 values to a thread, twice 16 where TWICE.  A block's groups
-// walk over the rows, each with the next one on its way while it works on one.
-template <typename G, typename W, bool ANY, bool TWICE>
-__global__ void __launch_bounds__(kMostThreads) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
-  constexpr int kParts = TWICE ? 2 : 1;
-  __shared__ Meeting meeting[ANY ? kMostWarps : 1];
-  __shared__ Room room;
-  admit_next_kernel();
-  const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, t = threadIdx.x - group * warps * 32;
-  uint32_t c[kParts];
-  int have[kParts];
-  Values<W> w[kParts];
-  await_previous_kernel();
+// The same of a row that is held: y as pairs, of the columns that a Piece has from c on.  `bytes`: 512 of the warp's.
+template <Lie LIE, typename G, typename W>
+__device__ __forceinline__ void put_blocks(const Forward<G, W>& p, uint8_t* bytes, uint64_t row, uint32_t c, const Pair (&y)[kPairs]) {
+  const uint32_t lane = threadIdx.x % 32, c0 = LIE == kSpread ? c - lane + lane * kValues : c;     // where the 16 codes that this lane writes begin
+  if (p.codes) {
+    uint4 w;
+    uint32_t s;
+    if constexpr (LIE == kSpread) {
+      // 32 lanes hold four blocks side by side; their codes go through shared memory to leave as 16 bytes a lane
+      s = 0;
+      __syncwarp();
 #pragma unroll
-  for (int k = 0; k < kParts; ++k) {
-    c[k] = (k * warps * 32 + t) * kValues;
-    have[k] = c[k] < p.cols ? (int)min((uint32_t)kValues, p.cols - c[k]) : 0;
-    w[k].template load<ANY>(p.w, have[k] ? c[k] : 0, have[k]);
-  }
-  Values<G> x[kParts], r[kParts];
-  uint64_t row = blockIdx.x * groups + group;
-  const uint64_t step = (uint64_t)gridDim.x * groups;
-  const auto load = [&](uint64_t at) {
+      for (int b = 0; b < 4; ++b) {
+        const Pair u = y[2 * b], v = y[2 * b + 1];
+        const uint32_t e = fp8_scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(larger(larger(u.lo(), u.hi()), larger(v.lo(), v.hi())))));
+        const float inv = inverse_scale(e);
+        const uint32_t four = e == 255u ? 0u : e4m3_codes4(u.lo() * inv, u.hi() * inv, v.lo() * inv, v.hi() * inv);
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      x[k].template load<ANY>(p.x, have[k] ? at * p.x.ld + c[k] : 0, have[k]);
-      if (p.residual.p) r[k].template load<ANY>(p.residual, have[k] ? at * p.residual.ld + c[k] : 0, have[k]);
+        for (int i = 0; i < 4; ++i) bytes[(4 * b + i) * 32 + lane] = (uint8_t)(four >> 8 * i);
+        if (lane / 8 == b) s = e;
+      }
+      __syncwarp();
+      w = *reinterpret_cast<const uint4*>(bytes + lane * kValues);
+    } else {
+      float most = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) most = larger(larger(most, y[i].lo()), y[i].hi());
+      s = fp8_scale_byte(fp8_block_max_bits(__float_as_uint(most)));
+      const Pair inv(inverse_scale(s));
+      uint32_t r[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const Pair u = y[2 * q] * inv, v = y[2 * q + 1] * inv;
+        r[q] = e4m3_codes4(u.lo(), u.hi(), v.lo(), v.hi());
+      }
+      w = s == 255u ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(r[0], r[1], r[2], r[3]);
     }
-  };
-  if (row < rows) load(row);
-  for (uint32_t parity = 0; row < rows; row += step, parity ^= 1) {
-    float s[kParts][kValues], part = 0.f;
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
+    const uint32_t b = c0 / kFp8Block;
+    if (b < p.nb) {
+      p.codes[row * (p.nb * 8) + c0 / kValues] = w;
+      if (c0 % kFp8Block == 0) put_fp8_scale(p.scales, row, b, p.nb, p.kt, s);
+    }
+  }
+  if (p.kept) {
+    uint4 w;
+    uint32_t s;
+    if constexpr (LIE == kSpread) {
+      // the lanes hold a block at a time
+      constexpr float kWhole = 12582912.f;
+      s = 0;
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < kValues; ++i) {
-        s[k][i] = p.residual.p ? rounded<G>(x[k].get(i) + r[k].get(i)) : x[k].get(i);
-        part = fmaf(s[k][i], s[k][i], part);
+        const float v = i % 2 ? y[i / 2].hi() : y[i / 2].lo();
+        const uint32_t e = scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v) & 0x7FFFFFFFu), 6);
+        const float code = fminf(fmaxf(fmaf(v, inverse_scale(e), kWhole), kWhole - 127.f), kWhole + 127.f);
+        bytes[i * 32 + lane] = e == 255u ? 0 : (uint8_t)__float_as_uint(code);
+        if (lane / 2 == i) s = e;
       }
-      if (p.sum) store_any<G, ANY>(meeting, p.sum + (have[k] ? row * p.ldsum + c[k] : 0), access_of<G>(p.sum, p.ldsum), have[k], s[k]);
-    }
-    if (row + step < rows) load(row + step);
-    const Root root(row_sums(make_float2(part, 0.f), warps, group, parity, room).x / p.columns + p.eps);
+      __syncwarp();
+      w = *reinterpret_cast<const uint4*>(bytes + lane * kValues);
+    } else {
+      Values<float> v;
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-#pragma unroll
-      for (int i = 0; i < kValues; ++i) s[k][i] = root.scaled(s[k][i], w[k].get(i));
-      put_outputs<G, W, ANY>(p, meeting, row, c[k], have[k], s[k]);
+      for (int i = 0; i < kPairs; ++i) v.w[2 * i] = __float_as_uint(y[i].lo()), v.w[2 * i + 1] = __float_as_uint(y[i].hi());
+      s = scale_byte(block_max_bits(v.max_bits()), 6);
+      w = int8_codes(v, s);
     }
+    const uint32_t b = c0 / 32;
+    if (b < p.kept_blocks) {
+      p.kept[row * (p.kept_blocks * 2) + c0 / kValues] = w;
+      if (c0 % 32 == 0) p.kept_scales[row * p.kept_pitch + b] = (uint8_t)s;
+    }
+  }
+}
+
+// The columns of a row's piece k that thread t of T has: where they begin, and how many there are.
+template <Lie LIE> __device__ __forceinline__ void place(uint32_t t, uint32_t T, uint32_t k, uint32_t cols, uint32_t& c, int& have) {
+  const uint32_t at = k * T + t;
+  c = LIE == kSpread ? at / 32 * 32 * kValues + at % 32 : at * kValues;
+  have = c >= cols ? 0 : (int)min((uint32_t)kValues, LIE == kSpread ? (cols - c + 31) / 32 : cols - c);
+}
+// The column of value i of thread t.
+template <Lie LIE> __device__ __forceinline__ uint32_t column_of(uint32_t t, uint32_t T, uint32_t i) {
+  const uint32_t at = i / kValues * T + t;
+  return LIE == kSpread ? at / 32 * 32 * kValues + i % kValues * 32 + at % 32 : at * kValues + i % kValues;
+}
+
+// Rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread; a block's groups walk over
+// the rows.
+template <typename G, typename W, Lie LIE, int PARTS>
+__global__ void __launch_bounds__(PARTS == 1 ? 768 : 512) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
+  __shared__ alignas(16) uint8_t bytes[LIE == kSpread ? (PARTS == 1 ? 24 : 16) : 1][512];
+  __shared__ Room<float> room;
+  admit_next_kernel();
+  const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
+  const uint64_t first = blockIdx.x * groups + group, step = (uint64_t)gridDim.x * groups;
+  uint32_t c[PARTS];
+  int have[PARTS];
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) place<LIE>(t, T, k, p.cols, c[k], have[k]);
+  const G *x = p.x.p + first * p.x.ld, *residual = p.residual.p + first * p.residual.ld;
+  G *sum = p.sum + first * p.ldsum, *y = p.y + first * p.ldy;
+  await_previous_kernel();
+  for (uint64_t row = first, parity = 0; row < rows; row += step, parity ^= 1) {
+    Piece<G, LIE> s[PARTS];
+    Pair part(0.f);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      s[k].load(x + c[k], have[k]);
+      if (p.residual.p) {
+        Piece<G, LIE> r;
+        r.load(residual + c[k], have[k]);
+        s[k].add(s[k], r);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      if (p.sum) s[k].store(sum + c[k], have[k]);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) part = fma(s[k].pair(i), s[k].pair(i), part);
+    }
+    const float squares = row_sum(part.sum(), warps, group, (uint32_t)parity, room);
+    const Root root(mean(squares, p.columns, p.one_nth) + p.eps);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      Piece<W, LIE> w;
+      w.load(p.w.p + c[k], have[k]);
+      if (p.y) {
+        Piece<G, LIE> out;
+        const Pair r(root.value());
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) out.set(i, s[k].pair(i) * r * w.pair(i));
+        out.store(y + c[k], have[k]);
+      }
+      if (p.codes || p.kept) {
+        Pair v[kPairs];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = root.scaled(s[k].pair(i), w.pair(i));
+        put_blocks<LIE>(p, bytes[LIE == kSpread ? warp : 0], row, c[k], v);
+      }
+    }
+    x += step * p.x.ld;
+    residual += step * p.residual.ld;
+    sum += step * p.ldsum;
+    y += step * p.ldy;
   }
 }
 
@@ -202,7 +310,7 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
     total += part;
     if (p.sum) store_any<G, ANY>(meeting, p.sum + (have ? row * p.ldsum + c : 0), access_of<G>(p.sum, p.ldsum), have, s);
   }
-  const Root root(block_sum(total, room) / p.columns + p.eps);     // its barriers: s is there for all to read
+  const Root root(mean(block_sum(total, room), p.columns, p.one_nth) + p.eps);     // its barriers: s is there for all to read
   const Rows<G> again = p.sum ? Rows<G>{p.sum, p.ldsum, p.sum + (gridDim.x - 1) * p.ldsum + p.cols, access_of<G>(p.sum, p.ldsum)} : p.x;
   for (uint64_t c0 = threadIdx.x / 32 * 32 * kValues; c0 < end; c0 += step) {
     const uint64_t c = c0 + lane * kValues;
@@ -225,87 +333,96 @@ template <typename G, typename W> struct Backward {
   uint64_t ldds;
   uint64_t rows;
   uint32_t cols;
-  float eps, columns;
+  float eps, columns, one_nth;
   float2* stats;           // of a row: 1 / rms and m / rms^2
 };
 
-// Both gradients from rows that are held in registers, a group of `warps` warps to each, 16 values to a thread or twice 16.  A
+// Both gradients from rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread.  A
 // block's groups walk over the rows and add up what the rows give for the weight; at the end the groups' sums are added in order
 // in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
 // are one cluster, which adds the parts itself.
-template <typename G, typename W, bool ANY, bool TWICE, bool CLUSTER>
+template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
 __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
-  constexpr int kParts = TWICE ? 2 : 1;
-  constexpr bool kAhead = sizeof(G) == 2 && !TWICE;      // where registers do for two rows
-  __shared__ Meeting meeting[ANY ? kMostWarps : 1];
-  __shared__ Room room;
+  constexpr bool kAhead = sizeof(G) == 2 && PARTS == 1;      // where registers do for two rows
+  __shared__ Room<Pair> room;
   extern __shared__ float sums[];
   admit_next_kernel();
   const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
-  uint32_t c[kParts];
-  int have[kParts];
-  Values<W> w[kParts];
-  await_previous_kernel();
-#pragma unroll
-  for (int k = 0; k < kParts; ++k) {
-    c[k] = (k * T + t) * kValues;
-    have[k] = c[k] < p.cols ? (int)min((uint32_t)kValues, p.cols - c[k]) : 0;
-    w[k].template load<ANY>(p.w, have[k] ? c[k] : 0, have[k]);
-  }
-  Values<G> s[kParts], dy[kParts], more[kParts];
+  uint32_t c[PARTS];
+  int have[PARTS];
+  Piece<W, LIE> w[PARTS];
+  Piece<G, LIE> s[PARTS], dy[PARTS], more[PARTS];
   uint64_t row = blockIdx.x * groups + group;
   const uint64_t step = (uint64_t)gridDim.x * groups;
-  const auto load = [&](uint64_t at, Values<G> (&vs)[kParts], Values<G> (&vd)[kParts], Values<G> (&vm)[kParts]) {
+  const G *from_s = p.s.p + row * p.s.ld, *from_dy = p.dy.p + row * p.dy.ld, *from_more = p.dsum.p + row * p.dsum.ld;     // of the row to be loaded next
+  G* ds = p.ds + row * p.ldds;
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      vs[k].template load<ANY>(p.s, have[k] ? at * p.s.ld + c[k] : 0, have[k]);
-      vd[k].template load<ANY>(p.dy, have[k] ? at * p.dy.ld + c[k] : 0, have[k]);
-      if (p.dsum.p) vm[k].template load<ANY>(p.dsum, have[k] ? at * p.dsum.ld + c[k] : 0, have[k]);
+  for (int k = 0; k < PARTS; ++k) place<LIE>(t, T, k, p.cols, c[k], have[k]);
+  const auto load = [&](Piece<G, LIE> (&vs)[PARTS], Piece<G, LIE> (&vd)[PARTS], Piece<G, LIE> (&vm)[PARTS]) {
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      vs[k].load(from_s + c[k], have[k]);
+      vd[k].load(from_dy + c[k], have[k]);
+      if (p.dsum.p) vm[k].load(from_more + c[k], have[k]);
     }
+    from_s += step * p.s.ld;
+    from_dy += step * p.dy.ld;
+    from_more += step * p.dsum.ld;
   };
-  float total[kParts][kValues] = {};
-  if (row < p.rows) load(row, s, dy, more);
+  await_previous_kernel();
+  Pair total[PARTS][kPairs];
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) total[k][i] = Pair(0.f);
+  if (row < p.rows) load(s, dy, more);
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) w[k].load(p.w.p + c[k], have[k]);
   for (uint32_t parity = 0; row < p.rows; row += step, parity ^= 1) {
-    Values<G> s1[kParts], dy1[kParts], more1[kParts];
-    if (kAhead && row + step < p.rows) load(row + step, s1, dy1, more1);
-    float2 part = make_float2(0.f, 0.f);
+    Piece<G, LIE> s1[PARTS], dy1[PARTS], more1[PARTS];
+    if (kAhead && row + step < p.rows) load(s1, dy1, more1);
+    Pair squares(0.f), inner(0.f);
 #pragma unroll
-    for (int k = 0; k < kParts; ++k)
+    for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) {
-        part.x = fmaf(s[k].get(i), s[k].get(i), part.x);
-        part.y = fmaf(dy[k].get(i) * w[k].get(i), s[k].get(i), part.y);
+      for (int i = 0; i < kPairs; ++i) {
+        const Pair a = s[k].pair(i);
+        squares = fma(a, a, squares);
+        inner = fma(dy[k].pair(i) * w[k].pair(i), a, inner);
       }
-    part = row_sums(part, warps, group, parity, room);
-    const float inv = __frsqrt_rn(part.x / p.columns + p.eps), m = part.y / p.columns * inv * inv;
+    const Pair both = row_sum(Pair(squares.sum(), inner.sum()), warps, group, parity, room);
+    const float inv = Root(mean(both.lo(), p.columns, p.one_nth) + p.eps).value();
+    const Pair root(inv), m(-(mean(both.hi(), p.columns, p.one_nth) * inv * inv));
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      float d[kValues];
+    for (int k = 0; k < PARTS; ++k) {
+      Piece<G, LIE> out;
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) {
-        const float a = s[k].get(i), b = dy[k].get(i);
-        total[k][i] = fmaf(b, a * inv, total[k][i]);
-        d[i] = fmaf(b, w[k].get(i), -a * m) * inv;
-        if (p.dsum.p) d[i] += more[k].get(i);
+      for (int i = 0; i < kPairs; ++i) {
+        const Pair a = s[k].pair(i), b = dy[k].pair(i);
+        total[k][i] = fma(b, a * root, total[k][i]);
+        const Pair d = fma(b, w[k].pair(i), a * m) * root;
+        out.set(i, p.dsum.p ? d + more[k].pair(i) : d);
       }
-      store_any<G, ANY>(meeting, p.ds + (have[k] ? row * p.ldds + c[k] : 0), access_of<G>(p.ds, p.ldds), have[k], d);
+      out.store(ds + c[k], have[k]);
     }
+    ds += step * p.ldds;
     if (kAhead) {
 #pragma unroll
-      for (int k = 0; k < kParts; ++k) s[k] = s1[k], dy[k] = dy1[k], more[k] = more1[k];
+      for (int k = 0; k < PARTS; ++k) s[k] = s1[k], dy[k] = dy1[k], more[k] = more1[k];
     } else if (row + step < p.rows) {
-      load(row + step, s, dy, more);
+      load(s, dy, more);
     }
   }
-  const uint32_t all = kParts * kValues * T;
+  const uint32_t all = PARTS * kValues * T;
+  const auto value = [&](int k, int i) { return i % 2 ? total[k][i / 2].hi() : total[k][i / 2].lo(); };
   for (uint32_t g = 0; (groups > 1 || CLUSTER) && g < groups; ++g) {
     if (g == group)
 #pragma unroll
-      for (int k = 0; k < kParts; ++k)
+      for (int k = 0; k < PARTS; ++k)
 #pragma unroll
         for (int i = 0; i < kValues; ++i) {
           float* const to = sums + (k * kValues + i) * T + t;
-          *to = g ? *to + total[k][i] : total[k][i];
+          *to = g ? *to + value(k, i) : value(k, i);
         }
     __syncthreads();
   }
@@ -319,7 +436,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
     for (uint32_t j = rank * blockDim.x + threadIdx.x; j < all; j += blocks * blockDim.x) {
       float v = 0.f;
       for (uint32_t b = 0; b < blocks; ++b) v += blocks > 1 ? peer_value(at + 4 * j, b) : sums[j];
-      const uint32_t i = j / T, column = (i / kValues * T + j % T) * kValues + i % kValues;
+      const uint32_t column = column_of<LIE>(j % T, T, j / T);
       if (column < p.cols) {
         if (dw_type == kBF16) static_cast<__nv_bfloat16*>(dw)[column] = __float2bfloat16_rn(v);
         else static_cast<float*>(dw)[column] = v;
@@ -335,9 +452,9 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
     for (uint32_t j = threadIdx.x; j < all; j += blockDim.x) parts[(uint64_t)blockIdx.x * all + j] = sums[j];
   } else {
 #pragma unroll
-    for (int k = 0; k < kParts; ++k)
+    for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) parts[(uint64_t)blockIdx.x * all + (k * kValues + i) * T + t] = total[k][i];
+      for (int i = 0; i < kValues; ++i) parts[(uint64_t)blockIdx.x * all + (k * kValues + i) * T + t] = value(k, i);
   }
 }
 
@@ -418,7 +535,7 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
 
 // dw: the parts of all shares added in order, by eight warps in turn.  A part has `length` values, in the columns' order or, T not
 // zero, in that of the threads.
-template <typename D> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t shares, uint32_t length, uint32_t T, uint32_t cols, D* dw) {
+template <typename D, Lie LIE> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t shares, uint32_t length, uint32_t T, uint32_t cols, D* dw) {
   __shared__ float room[8][32];
   admit_next_kernel();
   await_previous_kernel();
@@ -430,7 +547,7 @@ template <typename D> __global__ void __launch_bounds__(256) norm_join_kernel(co
   }
   room[warp][lane] = total;
   __syncthreads();
-  const uint32_t i = T ? j / T : 0, c = T ? (i / kValues * T + j % T) * kValues + i % kValues : j;
+  const uint32_t c = T ? column_of<LIE>(j % T, T, j / T) : j;
   if (warp == 0 && j < length && c < cols) {
     for (int k = 1; k < 8; ++k) total += room[k][lane];
     if constexpr (sizeof(D) == 4) dw[c] = total;
@@ -439,18 +556,19 @@ template <typename D> __global__ void __launch_bounds__(256) norm_join_kernel(co
 }
 
 // How rows that are held in registers are given to blocks: as many to a block as fill it, and as many blocks as run at once.
+// `held`: threads that an SM holds of the kernel.
 struct Split {
-  bool twice;
-  uint32_t warps, threads, blocks;
-  Split(uint64_t rows, uint64_t padded) {
-    twice = padded > kMostThreads * kValues;
-    const uint64_t per_warp = 32 * kValues * (twice ? 2 : 1);
+  uint32_t parts, warps, threads, blocks;
+  // most: threads of a block of several rows; held: threads of the kernel that an SM holds; spread: blocks that few rows are given to
+  Split(uint64_t rows, uint64_t padded, uint32_t parts_, uint32_t most, uint32_t held, uint64_t spread) : parts(parts_) {
+    const uint64_t per_warp = 32 * kValues * parts;
     warps = (uint32_t)((padded + per_warp - 1) / per_warp);
-    const uint32_t groups = (uint32_t)std::min<uint64_t>(kMostWarps / warps, rows);
+    // rows that would not fill the SMs otherwise get a block each, or a few to a block
+    const uint32_t groups = (uint32_t)std::min<uint64_t>(std::max(1u, most / 32 / warps), (rows + spread - 1) / spread);
     threads = groups * warps * 32;
-    blocks = (uint32_t)std::min<uint64_t>((rows + groups - 1) / groups, kSms * std::max(1u, kMostThreads / threads));
+    blocks = (uint32_t)std::min<uint64_t>((rows + groups - 1) / groups, kSms * std::max(1u, held / threads));
   }
-  uint32_t length() const { return warps * 32 * kValues * (twice ? 2 : 1); }     // of a part of the weight's gradient
+  uint32_t length() const { return warps * 32 * kValues * parts; }     // of a part of the weight's gradient
 };
 
 template <typename G, typename W> cudaError_t forward(const NormForward& n, cudaStream_t stream) {
@@ -474,6 +592,7 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   p.kept_pitch = (uint32_t)act8_scale_pitch(cols);
   p.eps = n.eps;
   p.columns = (float)cols;
+  p.one_nth = 1.f / p.columns;
   Access all = both(p.x.access, p.w.access);
   if (p.residual.p) all = both(all, p.residual.access);
   if (p.sum) all = both(all, access_of<G>(p.sum, p.ldsum));
@@ -482,9 +601,16 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   const bool any = all == kByElement;
   if (padded > kMostHeld)
     return launch_overlapped(any ? norm_long_kernel<G, W, true> : norm_long_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
-  const Split a(rows, padded);
-  return launch_overlapped(a.twice ? any ? norm_kernel<G, W, true, true> : norm_kernel<G, W, false, true> : any ? norm_kernel<G, W, true, false> : norm_kernel<G, W, false, false>,
-                           a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
+  Lie lie = lie_of(n.x.p, n.x.ld, sizeof(G));
+  lie = std::max(lie, lie_of(n.weight, 0, 1));
+  if (p.residual.p) lie = std::max(lie, lie_of(n.residual.p, n.residual.ld, sizeof(G)));
+  if (p.sum) lie = std::max(lie, lie_of(p.sum, p.ldsum, sizeof(G)));
+  if (p.y) lie = std::max(lie, lie_of(p.y, p.ldy, sizeof(G)));
+  const int parts = padded > 768 * kValues || (lie == kSpread && padded > 2048) ? 2 : 1;
+  const Split a(rows, padded, parts, parts == 1 ? 256 : 512, parts == 1 ? 768 : 512, kSms);
+  const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
+                                 : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 2> : norm_kernel<G, W, kSpread, 2>;
+  return launch_overlapped(kernel, a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
 }
 
 constexpr uint64_t kMostShares = 296;
@@ -496,24 +622,31 @@ uint64_t shares_for(uint64_t rows, uint64_t cols) {
 
 constexpr uint32_t kMostCluster = 8;
 
-template <typename G, typename W, bool ANY, bool TWICE, bool CLUSTER>
+// The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.
+Split backward_split(uint64_t rows, uint64_t cols) {
+  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1;
+  const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
+  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kSms);
+}
+
+template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
 cudaError_t run_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, ANY, TWICE, CLUSTER>, kMostThreads, kMostHeld * sizeof(float), 0, &facts);
+  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, kMostThreads, kMostHeld * sizeof(float), 0, &facts);
   if (e != cudaSuccess) return e;
   const uint32_t smem = CLUSTER || a.threads > a.warps * 32 ? a.length() * (uint32_t)sizeof(float) : 0;
-  return launch_overlapped(norm_backward_kernel<G, W, ANY, TWICE, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
+  return launch_overlapped(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
 }
-template <typename G, typename W, bool ANY, typename... A> cudaError_t pick_backward(const Split& a, A&&... args) {
-  if (a.blocks <= kMostCluster) return a.twice ? run_backward<G, W, ANY, true, true>(args...) : run_backward<G, W, ANY, false, true>(args...);
-  return a.twice ? run_backward<G, W, ANY, true, false>(args...) : run_backward<G, W, ANY, false, false>(args...);
+template <typename G, typename W, Lie LIE> cudaError_t pick_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
+  if (a.blocks <= kMostCluster) return a.parts == 2 ? run_backward<G, W, LIE, 2, true>(p, a, parts, n, stream) : run_backward<G, W, LIE, 1, true>(p, a, parts, n, stream);
+  return a.parts == 2 ? run_backward<G, W, LIE, 2, false>(p, a, parts, n, stream) : run_backward<G, W, LIE, 1, false>(p, a, parts, n, stream);
 }
 
-cudaError_t join(const NormBackward& n, const float* parts, uint32_t shares, uint32_t length, uint32_t T, cudaStream_t stream) {
+template <Lie LIE> cudaError_t join(const NormBackward& n, const float* parts, uint32_t shares, uint32_t length, uint32_t T, cudaStream_t stream) {
   const uint32_t strips = (length + 31) / 32, cols = (uint32_t)n.s.cols;
-  if (n.dw_type == kBF16) return launch_overlapped(norm_join_kernel<__nv_bfloat16>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<__nv_bfloat16*>(n.dw));
-  return launch_overlapped(norm_join_kernel<float>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<float*>(n.dw));
+  if (n.dw_type == kBF16) return launch_overlapped(norm_join_kernel<__nv_bfloat16, LIE>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<__nv_bfloat16*>(n.dw));
+  return launch_overlapped(norm_join_kernel<float, LIE>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<float*>(n.dw));
 }
 
 template <typename G, typename W> cudaError_t backward(const NormBackward& n, void* workspace, cudaStream_t stream) {
@@ -529,15 +662,20 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
   p.cols = (uint32_t)cols;
   p.eps = n.eps;
   p.columns = (float)cols;
+  p.one_nth = 1.f / p.columns;
   p.stats = static_cast<float2*>(workspace);
   Access all = both(both(p.dy.access, p.s.access), both(p.w.access, access_of<G>(p.ds, p.ldds)));
   if (p.dsum.p) all = both(all, p.dsum.access);
   const bool any = all == kByElement;
   if (cols <= kMostHeld) {
-    const Split a(rows, cols);
+    const Split a = backward_split(rows, cols);
     float* parts = static_cast<float*>(workspace);
-    const cudaError_t e = any ? pick_backward<G, W, true>(a, p, a, parts, n, stream) : pick_backward<G, W, false>(a, p, a, parts, n, stream);
-    return e != cudaSuccess || a.blocks <= kMostCluster ? e : join(n, parts, a.blocks, a.length(), a.warps * 32, stream);
+    Lie lie = std::max(std::max(lie_of(n.dy.p, n.dy.ld, sizeof(G)), lie_of(n.s.p, n.s.ld, sizeof(G))), std::max(lie_of(n.ds.p, n.ds.ld, sizeof(G)), lie_of(n.weight, 0, 1)));
+    if (n.dsum.p) lie = std::max(lie, lie_of(n.dsum.p, n.dsum.ld, sizeof(G)));
+    const cudaError_t e = lie == kBy32s ? pick_backward<G, W, kBy32s>(p, a, parts, n, stream)
+                          : lie == kBy16s ? pick_backward<G, W, kBy16s>(p, a, parts, n, stream) : pick_backward<G, W, kSpread>(p, a, parts, n, stream);
+    if (e != cudaSuccess || a.blocks <= kMostCluster) return e;
+    return lie == kSpread ? join<kSpread>(n, parts, a.blocks, a.length(), a.warps * 32, stream) : join<kBy32s>(n, parts, a.blocks, a.length(), a.warps * 32, stream);
   }
   const uint64_t strips = (cols + 31) / 32, shares = shares_for(rows, cols);
   float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + (rows * sizeof(float2) + 31) / 32 * 32);
@@ -545,7 +683,7 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
   if (e == cudaSuccess) e = launch_overlapped(norm_weight_kernel<G, W>, (uint32_t)(strips * shares), 256, 0, 1, stream, p, (uint32_t)strips, (uint32_t)shares, parts);
   // only now: it may be written over dy
   if (e == cudaSuccess) e = launch_overlapped(any ? norm_input_kernel<G, W, true> : norm_input_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
-  return e != cudaSuccess ? e : join(n, parts, (uint32_t)shares, (uint32_t)cols, 0, stream);
+  return e != cudaSuccess ? e : join<kBy32s>(n, parts, (uint32_t)shares, (uint32_t)cols, 0, stream);
 }
 
 }  // namespace
@@ -557,7 +695,7 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
   if (cols <= kMostHeld) {
-    const Split a(rows, cols);
+    const Split a = backward_split(rows, cols);
     return a.blocks <= kMostCluster ? 0 : (uint64_t)a.blocks * a.length() * sizeof(float);
   }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
