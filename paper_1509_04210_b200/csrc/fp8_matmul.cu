@@ -33,10 +33,12 @@ template <int COLS, bool QUANTIZE> struct Shape {
   static constexpr uint32_t kScales = 512 * 2;                           // a scale atom of each operand
   static constexpr uint32_t kStage = kLanes + kColumns + kScales;
   static constexpr uint32_t kStages = COLS == 128 ? 6 : COLS == 64 ? 8 : COLS == 32 ? 9 : 10;
-  static constexpr uint32_t kScaleColumns = 8;                           // tensor memory per stage
+  // Tensor memory of a set of scale atoms.  An atom serves four stages and comes with the first of them; x brought to FP8 here has
+  // one in every stage.  A set is written again once the last stage that read it is done, as the stage whose place it takes is.
+  static constexpr uint32_t kScaleColumns = 8, kSets = QUANTIZE ? kStages : (kStages + 2 + 3) / 4 + 1;
   static constexpr uint32_t kTmem = 256;
   static constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
-  static_assert(kStage % 1024 == 0 && COLS + kStages * kScaleColumns <= kTmem && kSmem <= 227 * 1024, "does not fit an SM");
+  static_assert(kStage % 1024 == 0 && COLS + kSets * kScaleColumns <= kTmem && kSmem <= 227 * 1024, "does not fit an SM");
 };
 
 struct Params {
@@ -108,31 +110,36 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
     for (uint32_t i = first; i < last; ++i, ++issued) {
       if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
       const uint32_t at = stage0 + s * S::kStage, bar = full + 8 * s, scales = at + S::kLanes + S::kColumns;
-      barrier_expect(bar, S::kLanes + 512 + (kQuantize ? 0 : S::kColumns + 512), elected);
+      const bool fresh = kQuantize || i == first || i % 4 == 0;
+      barrier_expect(bar, S::kLanes + (fresh ? 512 : 0) + (kQuantize ? 0 : S::kColumns + (fresh ? 512 : 0)), elected);
       copy_box(at, &lane_map, (int)(i * kFp8Block), (int)n0, bar, elected);
-      copy_bulk(scales, p.lane_scales + ((uint64_t)(n0 / 128) * p.kt + i / 4) * 512, 512, bar, elected);
+      if (fresh) copy_bulk(scales, p.lane_scales + ((uint64_t)(n0 / 128) * p.kt + i / 4) * 512, 512, bar, elected);
       if (!kQuantize) {
         copy_box(at + S::kLanes, &column_map, (int)(i * kFp8Block), (int)m0, bar, elected);
-        copy_bulk(scales + 512, p.column_scales + ((uint64_t)(m0 / 128) * p.kt + i / 4) * 512, 512, bar, elected);
+        if (fresh) copy_bulk(scales + 512, p.column_scales + ((uint64_t)(m0 / 128) * p.kt + i / 4) * 512, 512, bar, elected);
       }
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
     await_copies(full, issued, S::kStages);
   } else if (warp == 1) {
     const uint32_t elected = elect();
-    uint32_t s = 0, parity = 0;
+    uint32_t s = 0, parity = 0, set = 0;
     for (uint32_t i = first; i < last; ++i) {
       if (!(ok = barrier_wait(full + 8 * s, parity))) break;
       tmem_fence_after();
-      const uint32_t at = stage0 + s * S::kStage, ts = tmem + COLS + s * S::kScaleColumns;
+      const uint32_t at = stage0 + s * S::kStage, ts = tmem + COLS + set * S::kScaleColumns;
       const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + S::kLanes), scales = scale_rows(at + S::kLanes + S::kColumns);
       const uint32_t tl = ts, tc = ts + 4, what = instruction<COLS>() | (i % 4) << 29 | (i % 4) << 4;   // the block's byte of the four
+      const uint32_t mine = tc + m0 % 128 / 32;                        // a tile of 64 rows may be the second half of an atom
       // descriptors count in units of 16 bytes
-      scales_to_tmem(tl, scales, elected);
-      scales_to_tmem(tc, scales + 32, elected);
+      if (kQuantize || i == first || i % 4 == 0) {
+        scales_to_tmem(tl, scales, elected);
+        scales_to_tmem(tc, scales + 32, elected);
+      }
 #pragma unroll
       for (uint32_t h = 0; h < 4; ++h)   // 32 values
-        multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, tc, i != first || h, elected);
+        multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, mine, i != first || h, elected);
+      if (kQuantize || i % 4 == 3) set = set + 1 == S::kSets ? 0 : set + 1;
       tensor_commit(empty + 8 * s, elected);
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
@@ -208,6 +215,32 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   }
 }
 
+// How long a product takes, in ns, by its shape.  Measured (warm, one after another, weights out of HBM): a stage of 16, 32, 64 and
+// 128 columns 140, 145, 170 and 210 ns, what comes after a tile's last stage 100 to 1000, joining the parts of a tile 1100 to 2600,
+// 2000 for setting up; a pair's stage 300 (390 on all SMs, where power sets the clock) and 1000 a tile.  For instance 256 x 4096 x 4096:
+// 64 columns 8.2 us, 128 columns 9.7 and split in two 10.9, pairs 13.7; 128 x 1000 x 4096: 64 columns 6.9 us and in four parts 5.5,
+// 128 columns in eight parts 6.4; 1000 x 4096 x 4096: pairs 15.3 us, 128 columns 19.6.
+struct Timed {
+  uint32_t split;
+  uint64_t time;
+};
+Timed best_split(const Device::Facts& f, int columns, uint64_t m, uint64_t n, uint64_t stages) {
+  const int i = columns == 16 ? 0 : columns == 32 ? 1 : columns == 64 ? 2 : 3;
+  constexpr uint64_t kStageTime[4] = {140, 145, 170, 210}, kAfter[4] = {100, 200, 500, 1000}, kJoin[4] = {1100, 1400, 2300, 2600};
+  const uint64_t tiles = ((n + 127) / 128) * ((m + columns - 1) / columns), waves = (tiles + f.sms - 1) / f.sms;
+  Timed best = {1, 2000 + waves * (stages * kStageTime[i] + kAfter[i])};
+  for (uint32_t k = 1; k < 4; ++k) {
+    const uint32_t split = 1u << k;
+    const uint64_t time = 2000 + (stages + split - 1) / split * kStageTime[i] + kAfter[i] + kJoin[i];
+    if (split <= stages && tiles <= (uint64_t)f.clusters[k] && time < best.time) best = {split, time};
+  }
+  return best;
+}
+uint64_t pair_time(const Device::Facts& f, uint64_t m, uint64_t n, uint64_t stages) {
+  const uint64_t tiles = ((n + 255) / 256) * ((m + 255) / 256), waves = (2 * tiles + f.sms - 1) / f.sms;
+  return 2700 + waves * (stages * (waves > 1 ? 390 : 300) + 1000);
+}
+
 template <typename G, int COLS, typename X>
 cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
   using S = Shape<COLS, !std::is_void<X>::value>;
@@ -230,7 +263,7 @@ cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOu
   p.lane_tiles = (p.n + 127) / 128;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.m + COLS - 1) / COLS);
   if (tiles > 0x0FFFFFFFull) return cudaErrorInvalidConfiguration;
-  p.split = pick_split(*facts, tiles, p.stages, 2 + COLS / 11);
+  p.split = best_split(*facts, COLS, p.m, p.n, p.stages).split;
   CUtensorMap lane_map, column_map = {};
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * kFp8Block, b.rows, nb * kFp8Block, 128);
   if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * kFp8Block, a.rows, nb * kFp8Block, COLS);
@@ -239,12 +272,19 @@ cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOu
                            x ? Rows<T>::of(x->p, x->rows, x->cols, x->ld, 0) : Rows<T>::of(nullptr, 0, 0, 0, 0));
 }
 
-// The narrowest tile that takes all rows, else 128: scale bytes come in atoms of 128 rows, and a tile begins with one.
-template <typename G> cudaError_t by_rows(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
-  if (y.rows <= 16) return launch<G, 16, void>(a, nullptr, b, y, stream);
-  if (y.rows <= 32) return launch<G, 32, void>(a, nullptr, b, y, stream);
-  if (y.rows <= 64) return launch<G, 64, void>(a, nullptr, b, y, stream);
-  return launch<G, 128, void>(a, nullptr, b, y, stream);
+// The shape that is done soonest.  Sixteen or 32 columns only where they take all rows: scale bytes come in atoms of 128 rows, of
+// which a tile takes all, the first part or a half.
+template <typename G> cudaError_t by_time(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
+  const uint64_t m = y.rows, n = y.cols, stages = (b.cols + kFp8Block - 1) / kFp8Block;
+  if (m <= 16) return launch<G, 16, void>(a, nullptr, b, y, stream);
+  if (m <= 32) return launch<G, 32, void>(a, nullptr, b, y, stream);
+  static Device device;
+  const Device::Facts* facts;
+  const cudaError_t e = device.prepare(fp8_matmul_kernel<G, 64, void>, Shape<64, false>::kThreads, Shape<64, false>::kSmem, 0, &facts);
+  if (e != cudaSuccess) return e;
+  const uint64_t narrow = best_split(*facts, 64, m, n, stages).time, wide = best_split(*facts, 128, m, n, stages).time;
+  if (pair_time(*facts, m, n, stages) < std::min(narrow, wide)) return launch_fp8_matmul_pair(a, b, y, stream);
+  return narrow <= wide ? launch<G, 64, void>(a, nullptr, b, y, stream) : launch<G, 128, void>(a, nullptr, b, y, stream);
 }
 
 template <typename G, typename X> cudaError_t quantizing(const MatrixIn& x, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
@@ -263,9 +303,7 @@ constexpr uint64_t kQuantizedInside = 16;
 
 cudaError_t launch_fp8_matmul(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
   if (a.cols == 0) return nothing(y, stream);
-  // Pairs once the tiles of single blocks no longer fit the SMs at once.
-  if (((a.rows + 127) / 128) * ((b.rows + 127) / 128) > kSms) return launch_fp8_matmul_pair(a, b, y, stream);
-  return y.type == kBF16 ? by_rows<__nv_bfloat16>(a, b, y, stream) : by_rows<float>(a, b, y, stream);
+  return y.type == kBF16 ? by_time<__nv_bfloat16>(a, b, y, stream) : by_time<float>(a, b, y, stream);
 }
 
 uint64_t fp8_linear_workspace(uint64_t m, uint64_t k) {

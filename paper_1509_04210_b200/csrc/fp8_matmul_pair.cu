@@ -9,7 +9,7 @@
 // first of the two issues for both.
 //
 // One pair per two SMs walks over its tiles.  Tensor memory holds one accumulator (256 columns; the
-// scale bytes of six stages take another 72), so results are first taken into registers, which frees
+// scale bytes another 36), so results are first taken into registers, which frees
 // it for the next tile, and written out while that one is computed.
 #include <algorithm>
 
@@ -25,10 +25,13 @@ constexpr uint32_t kThreads = 384;        // warp 0 loads, warp 1 issues, warp 2
 constexpr uint32_t kRows = 128, kTile = 256, kStageBytes = 128;      // rows of either matrix in a block; a tile's; of a row per stage
 constexpr uint32_t kMatrix = kRows * kStageBytes, kScales = 512, kBytes = 2 * kMatrix + 3 * kScales, kStages = 6;
 constexpr uint32_t kStage = (kBytes + 1023) / 1024 * 1024;   // the swizzle repeats every 1024 bytes
-constexpr uint32_t kScaleColumns = 12;    // tensor memory per stage: a scale atom of the lanes and of each half of the columns
+// An atom of scale bytes serves four stages, and is copied to tensor memory with the first of them: next to every stage the copies,
+// which the tensor core makes itself, took a fifth of its time.  A third set of atoms is begun with when the stage six before it,
+// and so the last that read the first set, is done.
+constexpr uint32_t kScaleColumns = 12, kScaleSets = 3;    // tensor memory of a set: an atom of the lanes and of each half of the columns
 constexpr uint32_t kTmem = 512;
 constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
-static_assert(kTile + kStages * kScaleColumns <= kTmem && kSmem <= 227 * 1024, "does not fit an SM");
+static_assert(4 * kScaleSets - 4 >= kStages + 2 && kTile + kScaleSets * kScaleColumns <= kTmem && kSmem <= 227 * 1024, "does not fit an SM");
 
 struct Params {
   void* y;
@@ -98,12 +101,14 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
       for (uint32_t i = 0; i < stages; ++i) {
         const uint32_t at = stage0 + s * kStage, bar = first_full + 8 * s;
         if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
-        if (rank == 0) barrier_expect(full + 8 * s, 2 * kBytes, elected);
+        if (rank == 0) barrier_expect(full + 8 * s, 2 * (i % 4 ? 2 * kMatrix : kBytes), elected);
         copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
         copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
-        copy_box_pair(at + 2 * kMatrix, &lane_scales, 0, (int)(lane_atom + i / 4), bar, elected);
-        copy_box_pair(at + 2 * kMatrix + kScales, &column_scales, 0, (int)(column_atom + i / 4), bar, elected);
-        copy_box_pair(at + 2 * kMatrix + 2 * kScales, &column_scales, 0, (int)(column_atom + p.kt + i / 4), bar, elected);   // past the last: zero
+        if (i % 4 == 0) {
+          copy_box_pair(at + 2 * kMatrix, &lane_scales, 0, (int)(lane_atom + i / 4), bar, elected);
+          copy_box_pair(at + 2 * kMatrix + kScales, &column_scales, 0, (int)(column_atom + i / 4), bar, elected);
+          copy_box_pair(at + 2 * kMatrix + 2 * kScales, &column_scales, 0, (int)(column_atom + p.kt + i / 4), bar, elected);   // past the last: zero
+        }
         ++issued;
         if (++s == kStages) s = 0, parity ^= 1;
       }
@@ -112,23 +117,26 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t elected = elect();
-      uint32_t q = 0, s = 0, parity = 0;
+      uint32_t q = 0, s = 0, parity = 0, set = 0;
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++q) {
         if (!(ok = barrier_wait(drained, (q & 1) ^ 1))) break;
         tmem_fence_after();
         for (uint32_t i = 0; i < stages; ++i) {
           if (!(ok = barrier_wait(full + 8 * s, parity))) break;
           tmem_fence_after();
-          const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + s * kScaleColumns;
+          const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + set * kScaleColumns;
           const uint64_t lanes = swizzled_rows(at), columns = swizzled_rows(at + kMatrix), scales = scale_rows(at + 2 * kMatrix);
           const uint32_t tl = ts, tc = ts + 4, what = kInstruction | (i % 4) << 29 | (i % 4) << 4;   // the block's byte of the four
-          scales_to_tmem_pair(tl, scales, elected);
-          scales_to_tmem_pair(tc, scales + kScales / 16, elected);
-          scales_to_tmem_pair(tc + 4, scales + 2 * kScales / 16, elected);
+          if (i % 4 == 0) {
+            scales_to_tmem_pair(tl, scales, elected);
+            scales_to_tmem_pair(tc, scales + kScales / 16, elected);
+            scales_to_tmem_pair(tc + 4, scales + 2 * kScales / 16, elected);
+          }
           // descriptors count in units of 16 bytes
 #pragma unroll
           for (uint32_t h = 0; h < 4; ++h)   // 32 values
             multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, tc, i || h, elected);
+          if (i % 4 == 3 || i + 1 == stages) set = set + 1 == kScaleSets ? 0 : set + 1;
           tensor_commit_pair(empty + 8 * s, elected);
           if (++s == kStages) s = 0, parity ^= 1;
         }
