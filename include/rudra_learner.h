@@ -235,13 +235,16 @@ uint64_t rudra_grad_norm_workspace(uint64_t count);
 int rudra_grad_norm(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, float* norm_dev,
                     void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream);
 
-/* outs[i] = grads[i] * (norm <= max_norm ? 1 : max_norm / norm), norm = *norm_dev: for instance into the layers' parts of the
- * vector that rudra_ps_push takes, in its dtype.  outs_dev[i] may be grads_dev[i] with the same dtype; no two outputs and
- * no output and another gradient may overlap, which is refused.  Where all are scaled in their place and norm <= max_norm
- * nothing is read or written.  A norm that is NaN makes every value NaN, an infinite one the finite values zero and the
- * others NaN, unless max_norm is infinite too.  max_norm >= 0. */
-int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, const float* norm_dev,
-                    float max_norm, void* const* outs_dev, const int* out_dtypes, void* cuda_stream);
+/* outs[i] = grads[i] * (norm <= max_norm ? 1 : max_norm / norm): for instance into the layers' parts of the vector that
+ * rudra_ps_push takes, in its dtype.  norm_known != 0: norm = *norm_dev (of the shards of several ranks together, say);
+ * otherwise it is that of rudra_grad_norm, computed here and left in *norm_dev, and workspace_dev its workspace.
+ * outs_dev[i] may be grads_dev[i] with the same dtype; no two outputs and no output and another gradient may overlap,
+ * which is refused.  Where all are scaled in their place and norm <= max_norm nothing is written.  A norm that is
+ * NaN makes every value NaN, an infinite one the finite values zero and the others NaN, unless max_norm is infinite
+ * too.  max_norm >= 0. */
+int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, float* norm_dev,
+                    int norm_known, float max_norm, void* const* outs_dev, const int* out_dtypes, void* workspace_dev,
+                    uint64_t workspace_bytes, void* cuda_stream);
 
 /* Waits for cuda_stream and reports asynchronous CUDA errors, and kernels of this header that gave up, as
  * RUDRA_E_CUDA.  The kernels of the two products wait on barriers inside a block or cluster; a wait

@@ -126,7 +126,7 @@ def lib():
         "rudra_rms_norm_backward": (C.c_int, [vp, u64, vp, u64, vp, u64, C.c_int, u64, u64, vp, C.c_int, C.c_float, vp, u64, vp, C.c_int, vp, u64, vp]),
         "rudra_grad_norm_workspace": (u64, [u64]),
         "rudra_grad_norm": (C.c_int, [vp, vp, vp, u64, vp, vp, u64, vp]),
-        "rudra_grad_clip": (C.c_int, [vp, vp, vp, u64, vp, C.c_float, vp, vp, vp]),
+        "rudra_grad_clip": (C.c_int, [vp, vp, vp, u64, vp, C.c_int, C.c_float, vp, vp, vp, u64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

@@ -1,209 +1,362 @@
 // The norm of many gradients taken together, and their scaling to a largest norm.
 //
-// The gradients are cut into chunks of kChunk values, each within one gradient; a block takes every gridDim-th chunk.  Where they
-// lie comes as a kernel parameter, so a list costs no copy.  Squares are added in 32 bits over 16 values, everything beyond
-// that in 64, in an order that depends on the list alone; 16 values whose squares leave the range of a float are
-// squared in 64 bits.  One read for the norm, one read and one write for the scaling: bound by HBM.
+// The gradients are cut into units of consecutive values, each within one gradient, which blocks (of a small list: warps) take in
+// turn.  Where the gradients lie comes as a kernel parameter, so a list costs no copy.  Squares are added in 32 bits over 16
+// values, everything beyond that in 64, in an order that depends on the list alone; 16 values whose squares leave the range of a
+// float are squared in 64 bits.  One read for the norm, one read and one write for the scaling: bound by HBM, less what the
+// second read finds in L2; small lists by launches, and have one for both.
 #include <algorithm>
 
-#include "blocks.cuh"
 #include "launch.cuh"
 #include "learner.cuh"
+#include "pairs.cuh"
+#include "tensor.cuh"
 
 namespace rudra {
 namespace {
 
-constexpr uint32_t kThreads = 256, kPieces = 2, kChunk = kThreads * kPieces * kValues;
-constexpr uint32_t kBlocks = 148 * 8;    // at most; a partial sum each
+// Two blocks of 512 threads to an SM, 32 values to a thread: 61 million f32 117 us, 20 million bf16 to f32 in 301 gradients 30 us; six of 256
+// threads 120 and 36, eight of 256 with 16 values 124 and 33.
+constexpr uint32_t kThreads = 512, kPieces = 2, kBlocksPerSm = 2, kLargeUnit = kThreads * kPieces * kValues;
+constexpr uint32_t kBlocks = 148 * kBlocksPerSm;    // at most; a partial sum each
+// Units that are read to stay in L2: 48 MB of f32 (61 million: 123.9 us without, 120.3 with 48 to 80 MB, 121.2 with 100).
+constexpr uint32_t kHotUnits = 732;
+constexpr uint32_t kFusedBlocks = 8, kFusedThreads = 512, kSmallUnit = 32 * kValues;   // one cluster
 
 // Part of a list, as a kernel takes it.
 template <uint32_t MOST> struct List {
   const void* p[MOST];
   void* out[MOST];
   uint64_t size[MOST];
-  uint32_t end[MOST];        // chunks up to and with this gradient's last
+  uint32_t end[MOST];        // units up to and with this gradient's last
   uint8_t wide[MOST];        // bit 0: f32, bit 1: its output is
   uint32_t count;
+  uint32_t hot;              // units from here on are to stay in L2 between the norm and the scaling
 };
 
-// The gradient that chunk c is of: the first whose chunks end behind it.
-template <uint32_t MOST> __device__ __forceinline__ uint32_t gradient_of(const List<MOST>& list, uint32_t c) {
-  uint32_t lo = 0, hi = list.count - 1;
-  while (lo < hi) {
-    const uint32_t mid = (lo + hi) / 2;
-    if (list.end[mid] > c) hi = mid;
-    else lo = mid + 1;
+// Where the gradients' units end, in shared memory: a warp finds a unit's gradient by two votes.
+template <uint32_t MOST> struct Ends {
+  uint32_t end[MOST];
+  __device__ __forceinline__ void fill(const List<MOST>& list) {
+    for (uint32_t i = threadIdx.x; i < list.count; i += blockDim.x) end[i] = list.end[i];
+    __syncthreads();
   }
-  return lo;
-}
+  // Whole warps; c is the same to them and below the last end.
+  __device__ __forceinline__ uint32_t of(uint32_t count, uint32_t c, uint32_t& begin) const {
+    static_assert(MOST <= 1024, "two votes of 32");
+    const uint32_t lane = threadIdx.x % 32;
+    const uint32_t of32 = MOST <= 32 ? 0 : __ffs(__ballot_sync(0xFFFFFFFFu, end[min(lane * 32 + 31, count - 1)] > c)) - 1;
+    const uint32_t g = of32 * 32 + __ffs(__ballot_sync(0xFFFFFFFFu, end[min(of32 * 32 + lane, count - 1)] > c)) - 1;
+    begin = g ? end[g - 1] : 0;
+    return g;
+  }
+};
 
-template <typename G> __device__ __forceinline__ Rows<G> rows_of(const void* p, uint64_t size) {
-  const G* g = static_cast<const G*>(p);
-  return Rows<G>{g, 0, g + size, access_of<G>(p, 0)};
-}
+// Elements by which p lies past a boundary of 32 bytes.  Units begin at the boundary before a gradient, and every thread's 16 values
+// at one; values before the gradient's first do not exist.
+template <typename G> __device__ __host__ __forceinline__ uint32_t past_boundary(const void* p) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) % 32 / sizeof(G)); }
+
+// What of 16 values from `at` (which may be negative) on exists.
+struct Span {
+  int lo, hi;
+  __device__ __forceinline__ Span(int64_t at, uint64_t size) {
+    lo = at < 0 ? (int)-at : 0;
+    hi = (int)max((int64_t)0, min((int64_t)kValues, (int64_t)size - at));
+  }
+  __device__ __forceinline__ bool whole() const { return lo == 0 && hi == kValues; }
+};
 
 // Sum of a thread's squares.
-template <typename G> __device__ __forceinline__ double squares(const Values<G>& v) {
-  float a = 0.f, b = 0.f;
+template <typename G> __device__ __forceinline__ double squares(const Values<G>& x) {
+  Pair s(0.f);
 #pragma unroll
-  for (int i = 0; i < kValues; i += 2) {
-    a = fmaf(v.get(i), v.get(i), a);
-    b = fmaf(v.get(i + 1), v.get(i + 1), b);
+  for (int i = 0; i < kPairs; ++i) {
+    const Pair v(x.get(2 * i), x.get(2 * i + 1));
+    s = fma(v, v, s);
   }
-  const float s = a + b;
-  if (s > 1e-24f && s < 1e38f) return (double)s;      // what squares below 2^-126 lost is nothing next to it
+  const float f = s.sum();
+  if (f > 1e-24f && f < 1e38f) return (double)f;      // what squares below 2^-126 lost is nothing next to it
   double d = 0.0;
 #pragma unroll
-  for (int i = 0; i < kValues; ++i) d = fma((double)v.get(i), (double)v.get(i), d);
+  for (int i = 0; i < kValues; ++i) d = ::fma((double)x.get(i), (double)x.get(i), d);
   return d;
 }
 
-__device__ __forceinline__ double block_sum(double v) {
-  __shared__ double room[kThreads / 32];
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+template <uint32_t THREADS> __device__ __forceinline__ double block_sum(double v) {
+  __shared__ double room[THREADS / 32];
+  v = warp_sum(v);
   if (threadIdx.x % 32 == 0) room[threadIdx.x / 32] = v;
   __syncthreads();
   v = room[0];
-  for (uint32_t i = 1; i < kThreads / 32; ++i) v += room[i];
+#pragma unroll
+  for (uint32_t i = 1; i < THREADS / 32; ++i) v += room[i];
   return v;
 }
 
-template <typename G> __device__ __forceinline__ double chunk_squares(const void* p, uint64_t size, uint64_t at) {
-  const Rows<G> m = rows_of<G>(p, size);
-  Values<G> v[kPieces];
-#pragma unroll
-  for (uint32_t u = 0; u < kPieces; ++u) {
-    const uint64_t c = at + (u * kThreads + threadIdx.x) * kValues;
-    v[u].template load<true>(m, c < size ? c : 0, c < size ? (int)min((uint64_t)kValues, size - c) : 0);
-  }
-  double s = 0.0;
-#pragma unroll
-  for (uint32_t u = 0; u < kPieces; ++u) s += squares(v[u]);
-  return s;
+__device__ __forceinline__ void load_to_stay(const uint32_t* q, uint32_t* r) {
+  asm volatile("ld.global.L2::evict_last.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(q) : "memory");
 }
-
-template <uint32_t MOST> __global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ List<MOST> list, double* parts) {
-  admit_next_kernel();
-  await_previous_kernel();
-  const uint32_t chunks = list.end[list.count - 1];
-  double s = 0.0;
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const uint32_t g = gradient_of(list, c);
-    const uint64_t at = (uint64_t)(c - (g ? list.end[g - 1] : 0)) * kChunk;
-    s += list.wide[g] & 1 ? chunk_squares<float>(list.p[g], list.size[g], at) : chunk_squares<__nv_bfloat16>(list.p[g], list.size[g], at);
-  }
-  s = block_sum(s);
-  if (threadIdx.x == 0) parts[blockIdx.x] = s;
+__device__ __forceinline__ void store_first_out(uint32_t* q, const uint32_t* r) {
+  asm volatile("st.global.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               :: "l"(q), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-
-__global__ void __launch_bounds__(kThreads) norm_kernel(const double* parts, uint64_t count, float* norm) {
-  admit_next_kernel();
-  await_previous_kernel();
-  double s = 0.0;
-  for (uint64_t i = threadIdx.x; i < count; i += kThreads) s += parts[i];
-  s = block_sum(s);
-  if (threadIdx.x == 0) *norm = (float)sqrt(s);
-}
-
-template <typename G, typename D> __device__ __forceinline__ void scale_chunk(Meeting* meeting, const void* p, void* out, uint64_t size, uint64_t at, float by) {
-  const Rows<G> m = rows_of<G>(p, size);
-  D* const to = static_cast<D*>(out);
-  const Access access = access_of<D>(out, 0);
-  Values<G> v[kPieces];
+// Values on a boundary of 32 bytes that are read to stay in L2, to leave it first, or by themselves at a gradient's ends.
+template <typename G> __device__ __forceinline__ void load_aligned(Values<G>& v, const G* p, Span span, bool hot) {
+  if (span.whole()) {
+    const uint32_t* const q = reinterpret_cast<const uint32_t*>(p);
 #pragma unroll
-  for (uint32_t u = 0; u < kPieces; ++u) {
-    const uint64_t c = at + (u * kThreads + threadIdx.x) * kValues;
-    v[u].template load<true>(m, c < size ? c : 0, c < size ? (int)min((uint64_t)kValues, size - c) : 0);
+    for (int i = 0; i < Values<G>::kWords; i += 8) {
+      if (hot) load_to_stay(q + i, v.w + i);
+      else Values<G>::template load32<true>(q + i, v.w + i);
+    }
+    return;
   }
 #pragma unroll
-  for (uint32_t u = 0; u < kPieces; ++u) {
-    const uint64_t c = at + (u * kThreads + threadIdx.x) * kValues;
-    const int have = c < size ? (int)min((uint64_t)kValues, size - c) : 0;
-    float x[kValues];
-#pragma unroll
-    for (int i = 0; i < kValues; ++i) x[i] = v[u].get(i) * by;
-    if (access == kByElement) store_values_anyhow(meeting[threadIdx.x / 32], to + (have ? c : 0), have, x);
-    else store_values(to + (have ? c : 0), access, have, x);
-  }
-}
-
-template <uint32_t MOST, bool IN_PLACE> __global__ void __launch_bounds__(kThreads) scale_kernel(const __grid_constant__ List<MOST> list, const float* norm, float max_norm) {
-  __shared__ Meeting meeting[kThreads / 32];
-  admit_next_kernel();
-  await_previous_kernel();
-  const float n = *const_cast<const volatile float*>(norm), by = n <= max_norm ? 1.f : max_norm / n;
-  if (IN_PLACE && by == 1.f) return;
-  const uint32_t chunks = list.end[list.count - 1];
-  for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
-    const uint32_t c = chunks - 1 - i, g = gradient_of(list, c);      // what the norm read last is still in L2
-    const uint64_t at = (uint64_t)(c - (g ? list.end[g - 1] : 0)) * kChunk;
-    const void* p = list.p[g];
-    void* out = list.out[g];
-    switch (list.wide[g]) {
-      case 0: scale_chunk<__nv_bfloat16, __nv_bfloat16>(meeting, p, out, list.size[g], at, by); break;
-      case 1: scale_chunk<float, __nv_bfloat16>(meeting, p, out, list.size[g], at, by); break;
-      case 2: scale_chunk<__nv_bfloat16, float>(meeting, p, out, list.size[g], at, by); break;
-      default: scale_chunk<float, float>(meeting, p, out, list.size[g], at, by);
+  for (int i = 0; i < Values<G>::kWords; ++i) {
+    if constexpr (sizeof(G) == 4) {
+      v.w[i] = i >= span.lo && i < span.hi ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+    } else {
+      const uint32_t lo = 2 * i >= span.lo && 2 * i < span.hi ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u;
+      const uint32_t hi = 2 * i + 1 >= span.lo && 2 * i + 1 < span.hi ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0u;
+      v.w[i] = lo | hi << 16;
     }
   }
 }
 
-// The list in parts that a kernel takes, empty gradients left out: body(part, blocks).  At most 2^43 values in all, so that
-// chunks count in 32 bits.
-template <uint32_t MOST, typename F> cudaError_t in_parts(const Gradient* grads, uint64_t count, F&& body) {
-  List<MOST> list;
-  list.count = 0;
-  uint32_t chunks = 0;
-  for (uint64_t i = 0; i < count; ++i) {
-    if (!grads[i].size) continue;
-    const uint32_t k = list.count++;
-    list.p[k] = grads[i].p;
-    list.out[k] = grads[i].out;
-    list.size[k] = grads[i].size;
-    list.wide[k] = (uint8_t)((grads[i].type == kF32) | (grads[i].out_type == kF32) << 1);
-    chunks += (uint32_t)((grads[i].size + kChunk - 1) / kChunk);
-    list.end[k] = chunks;
-    if (list.count < MOST) continue;
-    const cudaError_t e = body(list, std::min(chunks, kBlocks));
-    if (e != cudaSuccess) return e;
-    list.count = chunks = 0;
-  }
-  return list.count ? body(list, std::min(chunks, kBlocks)) : cudaSuccess;
+// Squares of PIECES times 16 values of a thread, `step` apart.
+template <typename G, uint32_t PIECES> __device__ __forceinline__ double unit_squares(const void* p, uint64_t size, int64_t at, uint32_t step, bool hot) {
+  at -= past_boundary<G>(p);
+  Values<G> x[PIECES];
+#pragma unroll
+  for (uint32_t u = 0; u < PIECES; ++u) load_aligned(x[u], static_cast<const G*>(p) + (at + u * step), Span(at + u * step, size), hot);
+  double s = 0.0;
+#pragma unroll
+  for (uint32_t u = 0; u < PIECES; ++u) s += squares(x[u]);
+  return s;
+}
+template <uint32_t PIECES, uint32_t MOST> __device__ __forceinline__ double squares_of(const List<MOST>& list, uint32_t g, int64_t at, uint32_t step, bool hot) {
+  return list.wide[g] & 1 ? unit_squares<float, PIECES>(list.p[g], list.size[g], at, step, hot) : unit_squares<__nv_bfloat16, PIECES>(list.p[g], list.size[g], at, step, hot);
 }
 
-constexpr uint32_t kFew = 64, kMany = 960;    // gradients that one launch takes: 2 KB of parameters, and what 32 KB hold
+// Outputs lie on boundaries, gradients anyhow.
+template <typename G, typename D, uint32_t PIECES>
+__device__ __forceinline__ void scale_unit(const void* p, void* out, uint64_t size, int64_t at, uint32_t step, float by) {
+  at -= past_boundary<D>(out);
+  const G* const from = static_cast<const G*>(p);
+  const bool aligned = reinterpret_cast<uintptr_t>(from + at) % 32 == 0;
+  Values<G> x[PIECES];
+#pragma unroll
+  for (uint32_t u = 0; u < PIECES; ++u) {
+    const Span span(at + u * step, size);
+    if (aligned || !span.whole()) load_aligned(x[u], from + (at + u * step), span, false);
+    else x[u].template load<true>(Rows<G>{from, 0, from + size, kByElement}, at + u * step, kValues);
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < PIECES; ++u) {
+    const Span span(at + u * step, size);
+    D* const to = static_cast<D*>(out) + (at + u * step);
+    Piece<D, kBy32s> y;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) y.set(i, Pair(x[u].get(2 * i), x[u].get(2 * i + 1)) * Pair(by));
+    if (span.whole()) {
+#pragma unroll
+      for (int i = 0; i < Values<D>::kWords; i += 8) store_first_out(reinterpret_cast<uint32_t*>(to) + i, y.v.w + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kValues; ++i)
+        if (i >= span.lo && i < span.hi) {
+          if constexpr (sizeof(D) == 4) reinterpret_cast<uint32_t*>(to)[i] = y.v.w[i];
+          else reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)(y.v.w[i / 2] >> i % 2 * 16);
+        }
+    }
+  }
+}
+template <uint32_t PIECES, uint32_t MOST> __device__ __forceinline__ void scale_of(const List<MOST>& list, uint32_t g, int64_t at, uint32_t step, float by) {
+  const void* const p = list.p[g];
+  void* const out = list.out[g];
+  const uint64_t size = list.size[g];
+  switch (list.wide[g]) {
+    case 0: scale_unit<__nv_bfloat16, __nv_bfloat16, PIECES>(p, out, size, at, step, by); break;
+    case 1: scale_unit<float, __nv_bfloat16, PIECES>(p, out, size, at, step, by); break;
+    case 2: scale_unit<__nv_bfloat16, float, PIECES>(p, out, size, at, step, by); break;
+    default: scale_unit<float, float, PIECES>(p, out, size, at, step, by);
+  }
+}
+
+__device__ __forceinline__ float factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : max_norm / norm; }
+
+template <uint32_t MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) squares_kernel(const __grid_constant__ List<MOST> list, double* parts) {
+  __shared__ Ends<MOST> ends;
+  admit_next_kernel();
+  ends.fill(list);
+  const uint32_t units = list.end[list.count - 1];
+  await_previous_kernel();
+  double s = 0.0;
+  for (uint32_t c = blockIdx.x; c < units; c += gridDim.x) {
+    uint32_t begin;
+    const uint32_t g = ends.of(list.count, c, begin);
+    s += squares_of<kPieces>(list, g, (int64_t)(c - begin) * kLargeUnit + threadIdx.x * kValues, kThreads * kValues, c >= list.hot);
+  }
+  s = block_sum<kThreads>(s);
+  if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+// The norm from the parts; every thread gets it.
+__device__ __forceinline__ float norm_of_parts(const double* parts, uint32_t count) {
+  double s = 0.0;
+  for (uint32_t i = threadIdx.x; i < count; i += kThreads) s += parts[i];
+  return (float)sqrt(block_sum<kThreads>(s));
+}
+
+__global__ void __launch_bounds__(kThreads) norm_kernel(const double* parts, uint32_t count, float* norm) {
+  admit_next_kernel();
+  await_previous_kernel();
+  const float n = norm_of_parts(parts, count);
+  if (threadIdx.x == 0) *norm = n;
+}
+
+// parts: the norm is their sum's and is left in *norm; null: it is there already.
+template <uint32_t MOST, bool IN_PLACE>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) scale_kernel(const __grid_constant__ List<MOST> list, const double* parts, uint32_t count, float* norm, float max_norm) {
+  __shared__ Ends<MOST> ends;
+  admit_next_kernel();
+  ends.fill(list);
+  const uint32_t units = list.end[list.count - 1];
+  await_previous_kernel();
+  const float n = parts ? norm_of_parts(parts, count) : *const_cast<volatile float*>(norm), by = factor(n, max_norm);
+  if (parts && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+  if (IN_PLACE && by == 1.f) return;
+  for (uint32_t i = blockIdx.x; i < units; i += gridDim.x) {
+    const uint32_t c = units - 1 - i;      // backwards: what the norm read last is still in L2
+    uint32_t begin;
+    const uint32_t g = ends.of(list.count, c, begin);
+    scale_of<kPieces>(list, g, (int64_t)(c - begin) * kLargeUnit + threadIdx.x * kValues, kThreads * kValues, by);
+  }
+}
+
+// Both by one cluster, a warp to a unit of 512 values.
+template <uint32_t MOST, bool IN_PLACE>
+__global__ void __launch_bounds__(kFusedThreads) clip_kernel(const __grid_constant__ List<MOST> list, float* norm, float max_norm) {
+  __shared__ Ends<MOST> ends;
+  __shared__ double part;
+  admit_next_kernel();
+  ends.fill(list);
+  const uint32_t units = list.end[list.count - 1], first = blockIdx.x * (kFusedThreads / 32) + threadIdx.x / 32, step = kFusedBlocks * (kFusedThreads / 32);
+  await_previous_kernel();
+  double s = 0.0;
+  uint32_t begin;
+  for (uint32_t c = first; c < units; c += step) {
+    const uint32_t g = ends.of(list.count, c, begin);
+    s += squares_of<1>(list, g, (int64_t)(c - begin) * kSmallUnit + threadIdx.x % 32 * kValues, 0, true);
+  }
+  s = block_sum<kFusedThreads>(s);
+  if (threadIdx.x == 0) part = s;
+  cluster_arrive();
+  cluster_wait();
+  s = 0.0;
+#pragma unroll
+  for (uint32_t r = 0; r < kFusedBlocks; ++r) s += peer_double(smem_address(&part), r);
+  const float n = (float)sqrt(s), by = factor(n, max_norm);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+  if (!IN_PLACE || by != 1.f)
+    for (uint32_t c = first; c < units; c += step) {
+      const uint32_t g = ends.of(list.count, c, begin);
+      scale_of<1>(list, g, (int64_t)(c - begin) * kSmallUnit + threadIdx.x % 32 * kValues, 0, by);
+    }
+  cluster_arrive();      // the parts stay until all have read them
+  cluster_wait();
+}
+
+// The list in parts that a kernel takes, empty gradients left out: body(part, units).  At most 2^43 values in all, so that
+// units count in 32 bits.
+template <uint32_t MOST, typename F> cudaError_t in_parts(const Gradient* grads, uint64_t count, uint32_t unit, F&& body) {
+  List<MOST> list;
+  list.count = 0;
+  uint32_t units = 0;
+  for (uint64_t i = 0; i < count; ++i) {
+    const Gradient& g = grads[i];
+    if (!g.size) continue;
+    const uint32_t k = list.count++;
+    list.p[k] = g.p;
+    list.out[k] = g.out;
+    list.size[k] = g.size;
+    list.wide[k] = (uint8_t)((g.type == kF32) | (g.out_type == kF32) << 1);
+    // up to 15 values more, for where units begin before it
+    units += (uint32_t)((g.size + 15 + unit - 1) / unit);
+    list.end[k] = units;
+    if (list.count < MOST) continue;
+    const cudaError_t e = body(list, units);
+    if (e != cudaSuccess) return e;
+    list.count = units = 0;
+  }
+  return list.count ? body(list, units) : cudaSuccess;
+}
+
+// Gradients that one launch takes: 2, 11 and 32 KB of parameters.
+constexpr uint32_t kFew = 64, kSome = 320, kMany = 960;
 static_assert(sizeof(List<kMany>) + 64 <= 32764, "more than kernel parameters may be");
 
-template <uint32_t MOST> cudaError_t norm_of(const Gradient* grads, uint64_t count, float* norm, double* parts, cudaStream_t stream) {
-  uint64_t used = 0;
-  const cudaError_t e = in_parts<MOST>(grads, count, [&](const List<MOST>& list, uint32_t blocks) {
-    double* const to = parts + used;
-    used += blocks;
+template <uint32_t MOST> cudaError_t squares_to(const Gradient* grads, uint64_t count, double* parts, uint32_t* used, cudaStream_t stream) {
+  *used = 0;
+  return in_parts<MOST>(grads, count, kLargeUnit, [&](List<MOST>& list, uint32_t units) {
+    const uint32_t blocks = std::min(units, kBlocks);
+    double* const to = parts + *used;
+    *used += blocks;
+    list.hot = units > kHotUnits ? units - kHotUnits : 0;
     return launch_overlapped(squares_kernel<MOST>, blocks, kThreads, 0, 1, stream, list, to);
   });
+}
+template <uint32_t MOST> cudaError_t norm_of(const Gradient* grads, uint64_t count, float* norm, double* parts, cudaStream_t stream) {
+  uint32_t used;
+  const cudaError_t e = squares_to<MOST>(grads, count, parts, &used, stream);
   return e != cudaSuccess ? e : launch_overlapped(norm_kernel, 1, kThreads, 0, 1, stream, (const double*)parts, used, norm);
 }
 
-template <uint32_t MOST> cudaError_t scale(const Gradient* grads, uint64_t count, const float* norm, float max_norm, bool in_place, cudaStream_t stream) {
-  return in_parts<MOST>(grads, count, [&](const List<MOST>& list, uint32_t blocks) {
-    return launch_overlapped(in_place ? scale_kernel<MOST, true> : scale_kernel<MOST, false>, blocks, kThreads, 0, 1, stream, list, norm, max_norm);
+// Units of 512 values up to which one cluster takes norm and norm's use in one launch.
+constexpr uint64_t kFusedMost = 1024;
+
+template <uint32_t MOST, bool IN_PLACE> cudaError_t clip(const Gradient* grads, uint64_t count, float* norm, float max_norm, bool known, double* parts, cudaStream_t stream) {
+  uint32_t used = 0;
+  if (!known) {
+    uint64_t units = 0;
+    for (uint64_t i = 0; i < count; ++i) units += grads[i].size ? (grads[i].size + 15 + kSmallUnit - 1) / kSmallUnit : 0;
+    if (units && units <= kFusedMost && count <= MOST)
+      return in_parts<MOST>(grads, count, kSmallUnit, [&](const List<MOST>& list, uint32_t) {
+        return launch_overlapped(clip_kernel<MOST, IN_PLACE>, kFusedBlocks, kFusedThreads, 0, kFusedBlocks, stream, list, norm, max_norm);
+      });
+    if (!units) return launch_overlapped(norm_kernel, 1, kThreads, 0, 1, stream, (const double*)parts, 0u, norm);
+    const cudaError_t e = squares_to<MOST>(grads, count, parts, &used, stream);
+    if (e != cudaSuccess) return e;
+  }
+  return in_parts<MOST>(grads, count, kLargeUnit, [&](const List<MOST>& list, uint32_t units) {
+    return launch_overlapped(scale_kernel<MOST, IN_PLACE>, std::min(units, kBlocks), kThreads, 0, 1, stream, list, known ? (const double*)nullptr : (const double*)parts, used, norm,
+                             max_norm);
   });
 }
 
 }  // namespace
 
-uint64_t grad_norm_workspace(uint64_t count) { return (count / kMany + 1) * kBlocks * sizeof(double); }
+uint64_t grad_norm_workspace(uint64_t count) { return (count / kSome + 1) * kBlocks * sizeof(double); }
 
 cudaError_t launch_grad_norm(const Gradient* grads, uint64_t count, float* norm, void* workspace, cudaStream_t stream) {
   double* parts = static_cast<double*>(workspace);
-  return count <= kFew ? norm_of<kFew>(grads, count, norm, parts, stream) : norm_of<kMany>(grads, count, norm, parts, stream);
+  return count <= kFew ? norm_of<kFew>(grads, count, norm, parts, stream)
+         : count <= kSome ? norm_of<kSome>(grads, count, norm, parts, stream) : norm_of<kMany>(grads, count, norm, parts, stream);
 }
 
-cudaError_t launch_grad_clip(const Gradient* grads, uint64_t count, const float* norm, float max_norm, cudaStream_t stream) {
+cudaError_t launch_grad_clip(const Gradient* grads, uint64_t count, float* norm, float max_norm, bool known, void* workspace, cudaStream_t stream) {
   bool in_place = true;
   for (uint64_t i = 0; i < count; ++i) in_place = in_place && grads[i].p == grads[i].out;
-  return count <= kFew ? scale<kFew>(grads, count, norm, max_norm, in_place, stream) : scale<kMany>(grads, count, norm, max_norm, in_place, stream);
+  double* parts = static_cast<double*>(workspace);
+  const auto run = count <= kFew ? in_place ? clip<kFew, true> : clip<kFew, false>
+                   : count <= kSome ? in_place ? clip<kSome, true> : clip<kSome, false> : in_place ? clip<kMany, true> : clip<kMany, false>;
+  return run(grads, count, norm, max_norm, known, parts, stream);
 }
 
 }  // namespace rudra

@@ -70,23 +70,30 @@ int gradients(const void* const* grads, const int* dtypes, const uint64_t* sizes
 bool overlapping(const std::vector<Gradient>& list) {
   struct Span {
     uintptr_t from, to;
-    bool written;
     bool operator<(const Span& o) const { return from < o.from; }
   };
-  std::vector<Span> spans;
-  spans.reserve(2 * list.size());
+  std::vector<Span> written;
+  written.reserve(list.size());
+  uintptr_t low = UINTPTR_MAX, high = 0;
+  bool sorted = true;
   for (const Gradient& g : list) {
     if (!g.size) continue;
-    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p), out = reinterpret_cast<uintptr_t>(g.out);
-    if (p != out || g.type != g.out_type) spans.push_back({p, p + g.size * (g.type == rudra::kBF16 ? 2 : 4), false});
-    spans.push_back({out, out + g.size * (g.out_type == rudra::kBF16 ? 2 : 4), true});
+    const uintptr_t out = reinterpret_cast<uintptr_t>(g.out), end = out + g.size * (g.out_type == rudra::kBF16 ? 2 : 4);
+    sorted = sorted && (written.empty() || written.back().from <= out);
+    written.push_back({out, end});
+    low = std::min(low, out);
+    high = std::max(high, end);
   }
-  if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
-  uintptr_t end = 0, written_end = 0;      // of all before, and of what is written of them
-  for (const Span& s : spans) {
-    if (s.from < (s.written ? end : written_end)) return true;
-    end = std::max(end, s.to);
-    if (s.written) written_end = std::max(written_end, s.to);
+  if (!sorted) std::sort(written.begin(), written.end());
+  for (size_t i = 1; i < written.size(); ++i)
+    if (written[i].from < written[i - 1].to) return true;
+  for (const Gradient& g : list) {
+    if (!g.size || (g.p == g.out && g.type == g.out_type)) continue;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p), end = p + g.size * (g.type == rudra::kBF16 ? 2 : 4);
+    if (p >= high || end <= low) continue;
+    // the first output that begins behind the gradient's first byte, and the one before it
+    const auto at = std::upper_bound(written.begin(), written.end(), Span{p, 0});
+    if ((at != written.end() && at->from < end) || (at != written.begin() && (at - 1)->to > p)) return true;
   }
   return false;
 }
@@ -369,16 +376,20 @@ int rudra_grad_norm(const void* const* grads_dev, const int* dtypes, const uint6
   });
 }
 
-int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, const float* norm_dev, float max_norm,
-                    void* const* outs_dev, const int* out_dtypes, void* cuda_stream) {
+int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, float* norm_dev, int norm_known,
+                    float max_norm, void* const* outs_dev, const int* out_dtypes, void* workspace_dev, uint64_t workspace_bytes, void* cuda_stream) {
   return guarded([&]() -> int {
     std::vector<Gradient> list;
     if (count && !outs_dev) return fail(RUDRA_E_INVAL, "a list of outputs is null");
     if (const int e = gradients(grads_dev, dtypes, sizes, count, outs_dev, out_dtypes, &list)) return e;
     if (const int e = check_vector("norm", norm_dev, RUDRA_F32, 1)) return e;
     if (!(max_norm >= 0.f)) return fail(RUDRA_E_INVAL, "max_norm is negative or not a number");
+    const uint64_t need = norm_known ? 0 : rudra_grad_norm_workspace(count);
+    if (need && (!aligned(workspace_dev) || workspace_bytes < need))
+      return fail(RUDRA_E_INVAL, "workspace is null, not 32-byte aligned or smaller than %llu bytes", (unsigned long long)need);
     if (overlapping(list)) return fail(RUDRA_E_INVAL, "outputs overlap each other or other gradients");
-    return done(rudra::launch_grad_clip(list.data(), list.size(), norm_dev, max_norm, stream_of(cuda_stream)), "gradient clipping kernel launch");
+    return done(rudra::launch_grad_clip(list.data(), list.size(), norm_dev, max_norm, norm_known != 0, workspace_dev, stream_of(cuda_stream)),
+                "gradient clipping kernel launch");
   });
 }
 

@@ -94,7 +94,8 @@ struct Gradient {
 };
 uint64_t grad_norm_workspace(uint64_t count);
 cudaError_t launch_grad_norm(const Gradient* grads, uint64_t count, float* norm, void* workspace, cudaStream_t stream);
-cudaError_t launch_grad_clip(const Gradient* grads, uint64_t count, const float* norm, float max_norm, cudaStream_t stream);
+// known: *norm is the norm; otherwise it is computed, left there, and the workspace needed.
+cudaError_t launch_grad_clip(const Gradient* grads, uint64_t count, float* norm, float max_norm, bool known, void* workspace, cudaStream_t stream);
 
 // A count that goes up where a kernel of the file gives up a wait, as the stream's work leaves it; there once the stream is done.
 cudaError_t mx4_matmul_gave_up(uint32_t* count, cudaStream_t stream);

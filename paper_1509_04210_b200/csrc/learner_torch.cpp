@@ -15,6 +15,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/rudra_learner.h"
@@ -611,19 +612,24 @@ Gradients gradients(const char* what, PyObject* o) {
   const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.get());
   PyObject** items = PySequence_Fast_ITEMS(fast.get());
   if (n == 0) refuse("%s: an empty list", what);
-  g.p.reserve(n);
-  g.dtypes.reserve(n);
-  g.sizes.reserve(n);
+  g.p.resize(n);
+  g.dtypes.resize(n);
+  g.sizes.resize(n);
+  // asked once: only inside a level of forward differentiation has a tensor a tangent
+  const bool recording = c10::GradMode::is_enabled();
+  const bool tangents = c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr;
   for (Py_ssize_t i = 0; i < n; ++i) {
     const at::Tensor& t = tensor(what, items[i]);
-    check_no_gradient(what, t);
-    const int dtype = dtype_of(t.scalar_type());
-    if (dtype < 0 || !t.is_cuda() || !t.is_contiguous()) refuse("%s: contiguous float32 or bfloat16 tensors on the GPU are wanted", what);
-    if (g.device >= 0) same_device(g.device, (int)t.get_device());
-    g.device = (int)t.get_device();
-    g.p.push_back(t.data_ptr());
-    g.dtypes.push_back(dtype);
-    g.sizes.push_back((uint64_t)t.numel());
+    const c10::TensorImpl& impl = *t.unsafeGetTensorImpl();
+    if (tangents || (recording && t.requires_grad())) check_no_gradient(what, t);
+    const int dtype = dtype_of(c10::typeMetaToScalarType(impl.dtype()));
+    if (dtype < 0 || !t.is_cuda() || !impl.is_contiguous()) refuse("%s: contiguous float32 or bfloat16 tensors on the GPU are wanted", what);
+    const int device = (int)impl.device().index();
+    if (g.device >= 0) same_device(g.device, device);
+    g.device = device;
+    g.p[i] = impl.data();
+    g.dtypes[i] = dtype;
+    g.sizes[i] = (uint64_t)impl.numel();
   }
   return g;
 }
@@ -665,13 +671,13 @@ PyObject* clip_gradients(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gra
     const Output norm = scalar("norm", a[3], g.device);
     Held held(norm.object);
     const On on(g.device);
-    if (a[3] == Py_None) {
-      const uint64_t need = rudra_grad_norm_workspace(g.p.size());
-      const at::Tensor work = bytes((int64_t)need, g.device);
-      check(rudra_grad_norm(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<float*>(norm.m.p), work.data_ptr(), need, on.stream()));
-    }
-    check(rudra_grad_clip(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<const float*>(norm.m.p), most,
-                          const_cast<void* const*>(in_place ? g.p.data() : to.p.data()), in_place ? g.dtypes.data() : to.dtypes.data(), on.stream()));
+    const bool known = a[3] != Py_None;
+    const uint64_t need = known ? 0 : rudra_grad_norm_workspace(g.p.size());
+    at::Tensor work;
+    if (need) work = bytes((int64_t)need, g.device);
+    check(rudra_grad_clip(g.p.data(), g.dtypes.data(), g.sizes.data(), g.p.size(), static_cast<float*>(norm.m.p), known, most,
+                          const_cast<void* const*>(in_place ? g.p.data() : to.p.data()), in_place ? g.dtypes.data() : to.dtypes.data(),
+                          need ? work.data_ptr() : nullptr, need, on.stream()));
     return held.give();
   });
 }

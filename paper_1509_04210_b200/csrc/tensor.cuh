@@ -101,6 +101,11 @@ __device__ __forceinline__ float4 peer_load(uint32_t at, uint32_t rank) {
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(peer_address(at, rank)) : "memory");
   return v;
 }
+__device__ __forceinline__ double peer_double(uint32_t at, uint32_t rank) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(peer_address(at, rank)) : "memory");
+  return v;
+}
 __device__ __forceinline__ float peer_value(uint32_t at, uint32_t rank) {      // one of them
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_address(at, rank)) : "memory");

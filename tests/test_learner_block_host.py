@@ -126,9 +126,13 @@ def test_clipping_refusals():
     def clip(grads, outs, max_norm=1.0):
         g, t, n, count = _list(*grads)
         o = (C.c_void_p * count)(*[v[0] for v in outs])
-        return L.rudra_grad_clip(g, t, n, count, P, max_norm, o, (C.c_int * count)(*[v[1] for v in outs]), None)
+        return L.rudra_grad_clip(g, t, n, count, P, 0, max_norm, o, (C.c_int * count)(*[v[1] for v in outs]), P, 1 << 30, None)
 
-    _refused(L.rudra_grad_clip(*one, P, 1.0, None, None, None), "null")
+    _refused(L.rudra_grad_clip(*one, P, 1, 1.0, None, None, None, 0, None), "null")
+    o, d = (C.c_void_p * 1)(P), (C.c_int * 1)(0)
+    for known, at, n in ((0, None, need), (0, P, need - 1), (0, P + 4, need)):
+        _refused(L.rudra_grad_clip(*one, P, known, 1.0, o, d, at, n, None), "workspace")
+    _refused(L.rudra_grad_clip(*one, None, 1, 1.0, o, d, None, 0, None), "norm")
     _refused(clip([(P, 0, 10)], [(P, 0)], -1.0), "max_norm")
     _refused(clip([(P, 0, 10)], [(P, 0)], float("nan")), "max_norm")
     _refused(clip([(P, 0, 10)], [(P + 1, 1)]), "gradient 0")
@@ -271,7 +275,7 @@ int main(void) {
   if (rudra_fp8_codes_bytes(3, 129) != 3 * 256 || rudra_fp8_scales_bytes(129, 513) != 2 * 2 * 512) return 1;
   if (rudra_fp8_quantize(NULL, RUDRA_F32, 4, 64, 64, 0, 1, NULL, NULL, NULL) != RUDRA_E_INVAL) return 2;
   if (rudra_rms_norm(NULL, 0, NULL, 0, RUDRA_BF16, 0, 0, NULL, RUDRA_F32, 1e-6f, NULL, 0, NULL, 0, NULL, NULL, NULL, NULL, NULL) != 0) return 3;
-  if (rudra_grad_clip(NULL, NULL, NULL, 1, NULL, 1.0f, NULL, NULL, NULL) != RUDRA_E_INVAL) return 4;
+  if (rudra_grad_clip(NULL, NULL, NULL, 1, NULL, 0, 1.0f, NULL, NULL, NULL, 0, NULL) != RUDRA_E_INVAL) return 4;
   if (rudra_ps_pull_fp8(NULL, 0, 1, 1, 0, NULL, NULL) != RUDRA_E_INVAL) return 5;
   return 0;
 }
