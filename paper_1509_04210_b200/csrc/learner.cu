@@ -405,11 +405,12 @@ int rudra_learner_sync(void* cuda_stream) {
     if (e == cudaSuccess) e = rudra::act8_weight_grad_gave_up(&counts[2], stream);
     if (e == cudaSuccess) e = rudra::fp8_matmul_gave_up(&counts[3], stream);
     if (e == cudaSuccess) e = rudra::fp8_matmul_pair_gave_up(&counts[4], stream);
+    if (e == cudaSuccess) e = rudra::rms_norm_gave_up(&counts[5], stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
     if (e == cudaSuccess) e = cudaStreamGetId(stream, &id);
     if (e == cudaSuccess) e = cudaGetDevice(&device);
     if (e != cudaSuccess) return cuda_fail(e, "learner-side operators");
-    if (g_reports.fresh(device, id, counts)) return fail(RUDRA_E_CUDA, "a product kernel on this device gave up a wait: its result is not valid");
+    if (g_reports.fresh(device, id, counts)) return fail(RUDRA_E_CUDA, "a kernel on this device gave up a wait: its result is not valid");
     return 0;
   });
 }

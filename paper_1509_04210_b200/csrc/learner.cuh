@@ -103,5 +103,6 @@ cudaError_t mx4_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t fp8_matmul_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
+cudaError_t rms_norm_gave_up(uint32_t* count, cudaStream_t stream);
 
 }  // namespace rudra

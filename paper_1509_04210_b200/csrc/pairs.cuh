@@ -70,6 +70,22 @@ template <typename G, Lie LIE> struct Piece {
       }
     }
   }
+  // The same out of shared memory, where a row begins on a boundary.
+  __device__ __forceinline__ void fetch(const G* p, int have) {
+    if (have == kValues) {
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const uint4 r = reinterpret_cast<const uint4*>(p)[i / 4];
+        v.w[i] = r.x, v.w[i + 1] = r.y, v.w[i + 2] = r.z, v.w[i + 3] = r.w;
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(G) == 4) v.w[i] = i < have ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+      else v.w[i] = (2 * i < have ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u) | (2 * i + 1 < have ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i + 1] << 16 : 0u);
+    }
+  }
   __device__ __forceinline__ Pair pair(int i) const { return Pair(v.get(2 * i), v.get(2 * i + 1)); }
   __device__ __forceinline__ void set(int i, Pair x) {
     if constexpr (sizeof(G) == 4) {

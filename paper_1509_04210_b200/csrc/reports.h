@@ -11,7 +11,7 @@ namespace rudra {
 
 class Reports {
  public:
-  static constexpr int kKernels = 5;   // files that count
+  static constexpr int kKernels = 6;   // files that count
   using Counts = std::array<uint32_t, kKernels>;
 
   // Whether a stream (by its number, which is not given out twice) has not been told of `counts` yet; it now is.

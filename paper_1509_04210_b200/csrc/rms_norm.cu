@@ -223,6 +223,37 @@ template <Lie LIE> __device__ __forceinline__ uint32_t column_of(uint32_t t, uin
   return LIE == kSpread ? at / 32 * 32 * kValues + i % kValues * 32 + at % 32 : at * kValues + i % kValues;
 }
 
+// What a group of warps does with a row that it has in registers; weight(k) gives its k-th piece of the weight.
+template <Lie LIE, int PARTS, typename G, typename W, typename F>
+__device__ __forceinline__ void norm_row(const Forward<G, W>& p, const Piece<G, LIE> (&s)[PARTS], F&& weight, uint64_t row, const uint32_t (&c)[PARTS], const int (&have)[PARTS],
+                                         uint32_t warps, uint32_t group, uint32_t parity, Room<float>& room, uint8_t* bytes) {
+  Pair part(0.f);
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    if (p.sum) s[k].store(p.sum + row * p.ldsum + c[k], have[k]);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) part = fma(s[k].pair(i), s[k].pair(i), part);
+  }
+  const Root root(mean(row_sum(part.sum(), warps, group, parity, room), p.columns, p.one_nth) + p.eps);
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    const Piece<W, LIE> w = weight(k);
+    if (p.y) {
+      Piece<G, LIE> out;
+      const Pair r(root.value());
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) out.set(i, s[k].pair(i) * r * w.pair(i));
+      out.store(p.y + row * p.ldy + c[k], have[k]);
+    }
+    if (p.codes || p.kept) {
+      Pair v[kPairs];
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = root.scaled(s[k].pair(i), w.pair(i));
+      put_blocks<LIE>(p, bytes, row, c[k], v);
+    }
+  }
+}
+
 // Rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread; a block's groups walk over
 // the rows.
 template <typename G, typename W, Lie LIE, int PARTS>
@@ -231,57 +262,136 @@ __global__ void __launch_bounds__(PARTS == 1 ? 768 : 512) norm_kernel(const __gr
   __shared__ Room<float> room;
   admit_next_kernel();
   const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
-  const uint64_t first = blockIdx.x * groups + group, step = (uint64_t)gridDim.x * groups;
   uint32_t c[PARTS];
   int have[PARTS];
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) place<LIE>(t, T, k, p.cols, c[k], have[k]);
-  const G *x = p.x.p + first * p.x.ld, *residual = p.residual.p + first * p.residual.ld;
-  G *sum = p.sum + first * p.ldsum, *y = p.y + first * p.ldy;
   await_previous_kernel();
-  for (uint64_t row = first, parity = 0; row < rows; row += step, parity ^= 1) {
+  uint32_t parity = 0;
+  for (uint64_t row = blockIdx.x * groups + group; row < rows; row += (uint64_t)gridDim.x * groups, parity ^= 1) {
     Piece<G, LIE> s[PARTS];
-    Pair part(0.f);
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
-      s[k].load(x + c[k], have[k]);
+      s[k].load(p.x.p + row * p.x.ld + c[k], have[k]);
       if (p.residual.p) {
         Piece<G, LIE> r;
-        r.load(residual + c[k], have[k]);
+        r.load(p.residual.p + row * p.residual.ld + c[k], have[k]);
         s[k].add(s[k], r);
       }
     }
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
-      if (p.sum) s[k].store(sum + c[k], have[k]);
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) part = fma(s[k].pair(i), s[k].pair(i), part);
-    }
-    const float squares = row_sum(part.sum(), warps, group, (uint32_t)parity, room);
-    const Root root(mean(squares, p.columns, p.one_nth) + p.eps);
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
+    const auto weight = [&](int k) {
       Piece<W, LIE> w;
       w.load(p.w.p + c[k], have[k]);
-      if (p.y) {
-        Piece<G, LIE> out;
-        const Pair r(root.value());
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) out.set(i, s[k].pair(i) * r * w.pair(i));
-        out.store(y + c[k], have[k]);
-      }
-      if (p.codes || p.kept) {
-        Pair v[kPairs];
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = root.scaled(s[k].pair(i), w.pair(i));
-        put_blocks<LIE>(p, bytes[LIE == kSpread ? warp : 0], row, c[k], v);
-      }
-    }
-    x += step * p.x.ld;
-    residual += step * p.residual.ld;
-    sum += step * p.ldsum;
-    y += step * p.ldy;
+      return w;
+    };
+    norm_row<LIE, PARTS>(p, s, weight, row, c, have, warps, group, parity, room, bytes[LIE == kSpread ? warp : 0]);
   }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Many rows whose memory bulk copies can read: a warp keeps a ring of slots filled, each with a row for every group, and the
+// groups never wait for memory.  (8192 x 4096 bf16 to FP8 41 us = 5.7 TB/s; 50 with loads by the groups themselves, which take
+// turns with their arithmetic.)
+
+constexpr uint32_t kMostCluster = 8;      // blocks that add their parts of the weight's gradient themselves
+constexpr uint32_t kRing = 216 * 1024, kMostSlots = 8;
+// Warps that work, and one that copies: forward with 32 values to a thread, backward with 16.
+constexpr uint32_t kForwardWarps = 16, kBackwardWarps = 24;
+
+__device__ uint32_t g_gave_up;   // counts up
+
+// How rows lie in the ring; host and device.
+struct Ring {
+  uint32_t matrices, row, pitch, groups, slots;      // bytes of a row, and of its place in a slot
+  __host__ __device__ uint32_t slot() const { return groups * matrices * pitch; }
+};
+
+// The copying warp: slot by slot a row of each matrix for every group.  `bars`: full barriers, then empty ones.
+template <typename... P> __device__ __forceinline__ bool fill_ring(const Ring& ring, uint32_t ring0, uint32_t bars, uint64_t rows, const P&... matrices) {
+  const uint32_t elected = elect(), full = bars, empty = bars + 8 * ring.slots;
+  uint32_t s = 0, parity = 1, issued = 0;
+  bool ok = true;
+  for (uint64_t first = (uint64_t)blockIdx.x * ring.groups; first < rows; first += (uint64_t)gridDim.x * ring.groups, ++issued) {
+    if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
+    const uint32_t n = (uint32_t)min((uint64_t)ring.groups, rows - first), bar = full + 8 * s;
+    barrier_expect(bar, n * ring.matrices * ring.row, elected);
+    uint32_t to = ring0 + s * ring.slot();
+    for (uint32_t g = 0; g < n; ++g) {
+      const auto copy = [&](const auto& m) {
+        if (!m.p) return;
+        copy_bulk(to, m.p + (first + g) * m.ld, ring.row, bar, elected);
+        to += ring.pitch;
+      };
+      (copy(matrices), ...);
+    }
+    if (++s == ring.slots) s = 0, parity ^= 1;
+  }
+  await_copies(full, issued, ring.slots);
+  return ok;
+}
+__device__ __forceinline__ void prepare_ring(const Ring& ring, uint32_t bars, uint32_t users) {
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < ring.slots; ++s) {
+      barrier_init(bars + 8 * s, 1);
+      barrier_init(bars + 8 * (ring.slots + s), users);
+    }
+    barrier_init_fence();
+  }
+  __syncthreads();
+}
+// The warp has what it wanted of the slot.
+__device__ __forceinline__ void leave_slot(const Ring& ring, uint32_t bars, uint32_t s) {
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) barrier_arrive(bars + 8 * (ring.slots + s));
+}
+
+// A wait that was given up leaves a group working on what the slot holds, so that its barriers are complete; the count tells.
+template <typename G, typename W, Lie LIE, int PARTS>
+__global__ void __launch_bounds__(kForwardWarps * 32 + 32) norm_staged_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps, const __grid_constant__ Ring ring) {
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ Room<float> room;
+  __shared__ alignas(8) uint64_t barriers[2 * kMostSlots];
+  const uint32_t bars = smem_address(barriers), warp = warp_index(), group = warp / warps, T = warps * 32, t = threadIdx.x - group * T;
+  admit_next_kernel();
+  prepare_ring(ring, bars, ring.groups * warps);
+  await_previous_kernel();
+  bool ok = true;
+  if (warp == ring.groups * warps) {
+    ok = fill_ring(ring, smem_address(slots), bars, rows, p.x, p.residual);
+  } else {
+    uint32_t c[PARTS];
+    int have[PARTS];
+    Piece<W, LIE> w[PARTS];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      place<LIE>(t, T, k, p.cols, c[k], have[k]);
+      w[k].load(p.w.p + c[k], have[k]);
+    }
+    uint32_t slot = 0, phase = 0, parity = 0;
+    for (uint64_t first = (uint64_t)blockIdx.x * ring.groups; first < rows; first += (uint64_t)gridDim.x * ring.groups, parity ^= 1) {
+      if (ok) ok = barrier_wait(bars + 8 * slot, phase);
+      const uint64_t row = first + group;
+      if (row < rows) {
+        const G* x = reinterpret_cast<const G*>(slots + slot * ring.slot() + group * ring.matrices * ring.pitch);
+        Piece<G, LIE> s[PARTS];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          s[k].fetch(x + c[k], have[k]);
+          if (p.residual.p) {
+            Piece<G, LIE> r;
+            r.fetch(x + ring.pitch / sizeof(G) + c[k], have[k]);
+            s[k].add(s[k], r);
+          }
+        }
+        leave_slot(ring, bars, slot);
+        norm_row<LIE, PARTS>(p, s, [&](int k) { return w[k]; }, row, c, have, warps, group, parity, room, nullptr);
+      } else {
+        leave_slot(ring, bars, slot);
+      }
+      if (++slot == ring.slots) slot = 0, phase ^= 1;
+    }
+  }
+  if (!ok) atomicAdd(&g_gave_up, 1u);
 }
 
 // A block to a row of any length, read twice: the second time s where it was written.
@@ -336,6 +446,43 @@ template <typename G, typename W> struct Backward {
   float eps, columns, one_nth;
   float2* stats;           // of a row: 1 / rms and m / rms^2
 };
+
+template <int PARTS> __device__ __forceinline__ float total_of(const Pair (&total)[PARTS][kPairs], int k, int i) {
+  return i % 2 ? total[k][i / 2].hi() : total[k][i / 2].lo();
+}
+// The groups' sums for the weight added in order, to the first group's place in `sums`: value i of thread t at i * T + t.  All
+// threads of the block; those of no group come with group = groups.
+template <int PARTS>
+__device__ __forceinline__ void join_groups(float* sums, const Pair (&total)[PARTS][kPairs], uint32_t group, uint32_t groups, uint32_t T, uint32_t t) {
+  const uint32_t all = PARTS * kValues * T;
+  if (group < groups)
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) sums[group * all + (k * kValues + i) * T + t] = total_of(total, k, i);
+  __syncthreads();
+  for (uint32_t j = threadIdx.x; j < all; j += blockDim.x) {
+    float v = sums[j];
+#pragma unroll 4
+    for (uint32_t g = 1; g < groups; ++g) v += sums[g * all + j];
+    sums[j] = v;
+  }
+  __syncthreads();
+}
+// A block's part to where the next kernel adds them.
+template <int PARTS>
+__device__ __forceinline__ void put_part(float* parts, const float* sums, const Pair (&total)[PARTS][kPairs], uint32_t groups, uint32_t T, uint32_t t, bool mine) {
+  const uint32_t all = PARTS * kValues * T;
+  float* const to = parts + (uint64_t)blockIdx.x * all;
+  if (groups > 1) {
+    for (uint32_t j = threadIdx.x; j < all; j += blockDim.x) to[j] = sums[j];
+  } else if (mine) {
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) to[(k * kValues + i) * T + t] = total_of(total, k, i);
+  }
+}
 
 // Both gradients from rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread.  A
 // block's groups walk over the rows and add up what the rows give for the weight; at the end the groups' sums are added in order
@@ -392,16 +539,15 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
       }
     const Pair both = row_sum(Pair(squares.sum(), inner.sum()), warps, group, parity, room);
     const float inv = Root(mean(both.lo(), p.columns, p.one_nth) + p.eps).value();
-    const Pair root(inv), m(-(mean(both.hi(), p.columns, p.one_nth) * inv * inv));
+    const Pair root(inv), m(-(mean(both.hi(), p.columns, p.one_nth) * inv * inv * inv));
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
       Piece<G, LIE> out;
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        const Pair a = s[k].pair(i), b = dy[k].pair(i);
-        total[k][i] = fma(b, a * root, total[k][i]);
-        const Pair d = fma(b, w[k].pair(i), a * m) * root;
-        out.set(i, p.dsum.p ? d + more[k].pair(i) : d);
+        const Pair a = s[k].pair(i), b = dy[k].pair(i) * root;
+        total[k][i] = fma(a, b, total[k][i]);
+        out.set(i, fma(b, w[k].pair(i), p.dsum.p ? fma(a, m, more[k].pair(i)) : a * m));
       }
       out.store(ds + c[k], have[k]);
     }
@@ -414,18 +560,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
     }
   }
   const uint32_t all = PARTS * kValues * T;
-  const auto value = [&](int k, int i) { return i % 2 ? total[k][i / 2].hi() : total[k][i / 2].lo(); };
-  for (uint32_t g = 0; (groups > 1 || CLUSTER) && g < groups; ++g) {
-    if (g == group)
-#pragma unroll
-      for (int k = 0; k < PARTS; ++k)
-#pragma unroll
-        for (int i = 0; i < kValues; ++i) {
-          float* const to = sums + (k * kValues + i) * T + t;
-          *to = g ? *to + value(k, i) : value(k, i);
-        }
-    __syncthreads();
-  }
+  if (groups > 1 || CLUSTER) join_groups<PARTS>(sums, total, group, groups, T, t);
   if (CLUSTER) {
     const uint32_t blocks = gridDim.x, rank = blocks > 1 ? cluster_rank() : 0;
     if (blocks > 1) {
@@ -434,8 +569,11 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
     }
     const uint32_t at = smem_address(sums);
     for (uint32_t j = rank * blockDim.x + threadIdx.x; j < all; j += blocks * blockDim.x) {
-      float v = 0.f;
-      for (uint32_t b = 0; b < blocks; ++b) v += blocks > 1 ? peer_value(at + 4 * j, b) : sums[j];
+      float part[kMostCluster], v = 0.f;
+#pragma unroll
+      for (uint32_t b = 0; b < kMostCluster; ++b) part[b] = b >= blocks ? 0.f : blocks > 1 ? peer_value(at + 4 * j, b) : sums[j];
+#pragma unroll
+      for (uint32_t b = 0; b < kMostCluster; ++b) v += part[b];
       const uint32_t column = column_of<LIE>(j % T, T, j / T);
       if (column < p.cols) {
         if (dw_type == kBF16) static_cast<__nv_bfloat16*>(dw)[column] = __float2bfloat16_rn(v);
@@ -448,14 +586,85 @@ __global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __gri
     }
     return;
   }
-  if (groups > 1) {
-    for (uint32_t j = threadIdx.x; j < all; j += blockDim.x) parts[(uint64_t)blockIdx.x * all + j] = sums[j];
+  put_part<PARTS>(parts, sums, total, groups, T, t, true);
+}
+
+template <typename G, typename W, Lie LIE, int PARTS>
+__global__ void __launch_bounds__((PARTS == 1 ? kBackwardWarps : 16) * 32 + 32) norm_backward_staged_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, const __grid_constant__ Ring ring) {
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ Room<Pair> room;
+  __shared__ alignas(8) uint64_t barriers[2 * kMostSlots];
+  const uint32_t bars = smem_address(barriers), warp = warp_index(), group = warp / warps, T = warps * 32, t = threadIdx.x - group * T;
+  admit_next_kernel();
+  prepare_ring(ring, bars, ring.groups * warps);
+  await_previous_kernel();
+  bool ok = true;
+  Pair total[PARTS][kPairs];
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) total[k][i] = Pair(0.f);
+  if (warp == ring.groups * warps) {
+    ok = fill_ring(ring, smem_address(slots), bars, p.rows, p.s, p.dy, p.dsum);
   } else {
+    uint32_t c[PARTS];
+    int have[PARTS];
+    Piece<W, LIE> w[PARTS];
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k)
+    for (int k = 0; k < PARTS; ++k) {
+      place<LIE>(t, T, k, p.cols, c[k], have[k]);
+      w[k].load(p.w.p + c[k], have[k]);
+    }
+    uint32_t slot = 0, phase = 0, parity = 0;
+    for (uint64_t first = (uint64_t)blockIdx.x * ring.groups; first < p.rows; first += (uint64_t)gridDim.x * ring.groups, parity ^= 1) {
+      if (ok) ok = barrier_wait(bars + 8 * slot, phase);
+      const uint64_t row = first + group;
+      if (row < p.rows) {
+        const G* from = reinterpret_cast<const G*>(slots + slot * ring.slot() + group * ring.matrices * ring.pitch);
+        const uint32_t next = ring.pitch / sizeof(G);
+        Pair squares(0.f), inner(0.f);
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) parts[(uint64_t)blockIdx.x * all + (k * kValues + i) * T + t] = value(k, i);
+        for (int k = 0; k < PARTS; ++k) {
+          Piece<G, LIE> s, dy;
+          s.fetch(from + c[k], have[k]);
+          dy.fetch(from + next + c[k], have[k]);
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            const Pair a = s.pair(i);
+            squares = fma(a, a, squares);
+            inner = fma(dy.pair(i) * w[k].pair(i), a, inner);
+          }
+        }
+        const Pair both = row_sum(Pair(squares.sum(), inner.sum()), warps, group, parity, room);
+        const float inv = Root(mean(both.lo(), p.columns, p.one_nth) + p.eps).value();
+        const Pair root(inv), m(-(mean(both.hi(), p.columns, p.one_nth) * inv * inv * inv));
+        asm volatile("" ::: "memory");      // both are read again: registers for them would cost 24 warps to an SM (63 us instead of 50)
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          Piece<G, LIE> s, dy, more, out;
+          s.fetch(from + c[k], have[k]);
+          dy.fetch(from + next + c[k], have[k]);
+          if (p.dsum.p) more.fetch(from + 2 * next + c[k], have[k]);
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            const Pair a = s.pair(i), b = dy.pair(i) * root;
+            total[k][i] = fma(a, b, total[k][i]);
+            out.set(i, fma(b, w[k].pair(i), p.dsum.p ? fma(a, m, more.pair(i)) : a * m));
+          }
+          out.store(p.ds + row * p.ldds + c[k], have[k]);
+        }
+      }
+      leave_slot(ring, bars, slot);
+      if (++slot == ring.slots) slot = 0, phase ^= 1;
+    }
   }
+  if (!ok) atomicAdd(&g_gave_up, 1u);
+  // The ring is done with: its copies have landed and been used, or the copying warp waited for them.
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(slots);
+  const bool mine = warp < ring.groups * warps;
+  if (ring.groups > 1) join_groups<PARTS>(sums, total, mine ? group : ring.groups, ring.groups, T, t);
+  put_part<PARTS>(parts, sums, total, ring.groups, T, t, mine);
 }
 
 // A row's statistics, by a block.
@@ -571,6 +780,42 @@ struct Split {
   uint32_t length() const { return warps * 32 * kValues * parts; }     // of a part of the weight's gradient
 };
 
+// How many rows of bf16 go through rings, if they do: as many groups as leave three slots, and forward 32 values to a thread where
+// that still makes twelve warps (backward a thread's sums for the weight take the registers for that).  (f32 rows stay with loads
+// by the groups: a warp's 64-byte pieces of shared memory meet in its banks, 8192 x 4096 backward 113 us and 90.)
+struct Staged {
+  Ring ring = {};
+  uint32_t parts = 0, warps = 0, blocks = 0;      // parts 0: not this way
+  Staged(uint64_t rows, uint64_t cols, uint32_t element, uint32_t matrices, uint64_t padded, bool backward) {
+    if (element != 2 || cols * element % 16) return;
+    ring.matrices = matrices;
+    ring.row = (uint32_t)(cols * element);
+    ring.pitch = (ring.row + 127) / 128 * 128;
+    if (ring.pitch * (uint64_t)matrices > kRing / 2) return;
+    const uint32_t all = backward ? kBackwardWarps : kForwardWarps, one = (uint32_t)((padded + 511) / 512), two = (uint32_t)((padded + 1023) / 1024);
+    const uint32_t most = std::max(1u, kRing / 3 / (ring.pitch * matrices));
+    const uint32_t groups1 = one <= all ? std::min(most, all / one) : 0, groups2 = two <= 16 ? std::min(most, 16 / two) : 0;
+    const bool wide = !groups1 || (!backward && one != two && groups2 * two >= 12);
+    const uint32_t groups = std::min(15u, wide ? groups2 : groups1);      // a barrier each
+    if (!groups || rows < 3 * kSms * groups) return;       // too few to keep a ring going
+    parts = wide ? 2 : 1;
+    warps = wide ? two : one;
+    ring.groups = groups;
+    ring.slots = std::min(kMostSlots, kRing / ring.slot());
+    blocks = (uint32_t)kSms;
+  }
+  uint32_t threads() const { return ring.groups * warps * 32 + 32; }
+  uint32_t length() const { return warps * 32 * kValues * parts; }
+};
+
+template <typename G, typename W, Lie LIE, int PARTS> cudaError_t run_staged(const Forward<G, W>& p, uint64_t rows, const Staged& a, cudaStream_t stream) {
+  static Device device;
+  const Device::Facts* facts;
+  const cudaError_t e = device.prepare(norm_staged_kernel<G, W, LIE, PARTS>, a.threads(), kRing, 0, &facts);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped(norm_staged_kernel<G, W, LIE, PARTS>, a.blocks, a.threads(), a.ring.slots * a.ring.slot(), 1, stream, p, (uint32_t)rows, a.warps, a.ring);
+}
+
 template <typename G, typename W> cudaError_t forward(const NormForward& n, cudaStream_t stream) {
   const uint64_t rows = n.x.rows, cols = n.x.cols;
   Forward<G, W> p = {};
@@ -606,6 +851,11 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   if (p.residual.p) lie = std::max(lie, lie_of(n.residual.p, n.residual.ld, sizeof(G)));
   if (p.sum) lie = std::max(lie, lie_of(p.sum, p.ldsum, sizeof(G)));
   if (p.y) lie = std::max(lie, lie_of(p.y, p.ldy, sizeof(G)));
+  if constexpr (sizeof(G) == 2) if (lie != kSpread) {
+    const Staged st(rows, cols, sizeof(G), p.residual.p ? 2 : 1, padded, false);
+    if (st.parts == 1) return lie == kBy32s ? run_staged<G, W, kBy32s, 1>(p, rows, st, stream) : run_staged<G, W, kBy16s, 1>(p, rows, st, stream);
+    if (st.parts == 2) return lie == kBy32s ? run_staged<G, W, kBy32s, 2>(p, rows, st, stream) : run_staged<G, W, kBy16s, 2>(p, rows, st, stream);
+  }
   const int parts = padded > 768 * kValues || (lie == kSpread && padded > 2048) ? 2 : 1;
   const Split a(rows, padded, parts, parts == 1 ? 256 : 512, parts == 1 ? 768 : 512, kSms);
   const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
@@ -620,13 +870,21 @@ uint64_t shares_for(uint64_t rows, uint64_t cols) {
   return std::max<uint64_t>(1, std::min(kMostShares / std::min(strips, kMostShares), (rows + 7) / 8));
 }
 
-constexpr uint32_t kMostCluster = 8;
-
 // The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.
 Split backward_split(uint64_t rows, uint64_t cols) {
   const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1;
   const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
   return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kSms);
+}
+
+template <typename G, typename W, Lie LIE, int PARTS>
+cudaError_t run_staged_backward(const Backward<G, W>& p, const Staged& a, float* parts, cudaStream_t stream) {
+  static Device device;
+  const Device::Facts* facts;
+  const cudaError_t e = device.prepare(norm_backward_staged_kernel<G, W, LIE, PARTS>, a.threads(), kRing, 0, &facts);
+  if (e != cudaSuccess) return e;
+  const uint32_t smem = std::max(a.ring.slots * a.ring.slot(), a.ring.groups > 1 ? a.ring.groups * a.length() * (uint32_t)sizeof(float) : 0u);
+  return launch_overlapped(norm_backward_staged_kernel<G, W, LIE, PARTS>, a.blocks, a.threads(), smem, 1, stream, p, a.warps, parts, a.ring);
 }
 
 template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
@@ -635,7 +893,7 @@ cudaError_t run_backward(const Backward<G, W>& p, const Split& a, float* parts, 
   const Device::Facts* facts;
   const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, kMostThreads, kMostHeld * sizeof(float), 0, &facts);
   if (e != cudaSuccess) return e;
-  const uint32_t smem = CLUSTER || a.threads > a.warps * 32 ? a.length() * (uint32_t)sizeof(float) : 0;
+  const uint32_t groups = a.threads / 32 / a.warps, smem = CLUSTER || groups > 1 ? groups * a.length() * (uint32_t)sizeof(float) : 0;
   return launch_overlapped(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
 }
 template <typename G, typename W, Lie LIE> cudaError_t pick_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
@@ -672,6 +930,14 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
     float* parts = static_cast<float*>(workspace);
     Lie lie = std::max(std::max(lie_of(n.dy.p, n.dy.ld, sizeof(G)), lie_of(n.s.p, n.s.ld, sizeof(G))), std::max(lie_of(n.ds.p, n.ds.ld, sizeof(G)), lie_of(n.weight, 0, 1)));
     if (n.dsum.p) lie = std::max(lie, lie_of(n.dsum.p, n.dsum.ld, sizeof(G)));
+    if constexpr (sizeof(G) == 2) if (lie != kSpread) {
+      const Staged st(rows, cols, sizeof(G), p.dsum.p ? 3 : 2, cols, true);
+      if (st.parts) {
+        const cudaError_t e = st.parts == 1 ? lie == kBy32s ? run_staged_backward<G, W, kBy32s, 1>(p, st, parts, stream) : run_staged_backward<G, W, kBy16s, 1>(p, st, parts, stream)
+                              : lie == kBy32s ? run_staged_backward<G, W, kBy32s, 2>(p, st, parts, stream) : run_staged_backward<G, W, kBy16s, 2>(p, st, parts, stream);
+        return e != cudaSuccess ? e : join<kBy32s>(n, parts, st.blocks, st.length(), st.warps * 32, stream);
+      }
+    }
     const cudaError_t e = lie == kBy32s ? pick_backward<G, W, kBy32s>(p, a, parts, n, stream)
                           : lie == kBy16s ? pick_backward<G, W, kBy16s>(p, a, parts, n, stream) : pick_backward<G, W, kSpread>(p, a, parts, n, stream);
     if (e != cudaSuccess || a.blocks <= kMostCluster) return e;
@@ -688,6 +954,8 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
 
 }  // namespace
 
+cudaError_t rms_norm_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+
 cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
   if (n.x.type == kBF16) return n.weight_type == kBF16 ? forward<__nv_bfloat16, __nv_bfloat16>(n, stream) : forward<__nv_bfloat16, float>(n, stream);
   return n.weight_type == kBF16 ? forward<float, __nv_bfloat16>(n, stream) : forward<float, float>(n, stream);
@@ -696,7 +964,8 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
   if (cols <= kMostHeld) {
     const Split a = backward_split(rows, cols);
-    return a.blocks <= kMostCluster ? 0 : (uint64_t)a.blocks * a.length() * sizeof(float);
+    // enough for either way: rows through rings have whole warps of 1024 columns at most, a part to an SM
+    return a.blocks <= kMostCluster ? 0 : std::max((uint64_t)a.blocks * a.length(), kSms * ((cols + 1023) / 1024 * 1024)) * sizeof(float);
   }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
 }

@@ -136,6 +136,41 @@ def test_backward(t, c, dtype, weight, pad, shift, through):
     assert all(torch.equal(a, b) for a, b in zip(L.rms_norm_backward(again, s, w, eps=EPS), L.rms_norm_backward(again, s, w, eps=EPS, out=again)))
 
 
+#: enough rows to go through rings, at widths that fill a warp, a part of one, several, and more than a block's
+LONG = [(7200, 504), (8000, 40), (3000, 1000), (2000, 4096), (1400, 4112), (1000, 8200), (700, 9216)]
+
+
+@pytest.mark.parametrize("t,c", LONG)
+@pytest.mark.parametrize("pad", [0, 8])
+def test_many_rows(t, c, pad):
+    torch, L = _torch(), _learner()
+    x, r, w, s, hw = _inputs(t, c, "bf16", "f32", pad, 0)
+    tol = (32 + c / 8192) * U
+    want = ref.norm(s, hw, EPS)
+    for residual in (True, False):
+        got = L.rms_norm(x, w, r, eps=EPS) if residual else (L.rms_norm(torch.from_numpy(s).cuda().bfloat16(), w, eps=EPS), None)
+        _close(_np(got[0]), want, tol * np.abs(want) * (1 + 2.0 ** -8) + _half("bf16", want))
+        assert not residual or np.array_equal(_np(got[1]), s.astype(np.float64))
+    y8, total, kept = L.rms_norm(x, w, r, eps=EPS, fp8=True, keep=True)
+    _fp8_near(y8, want, tol)
+    # (few rows by themselves need not give the same codes: their squares are added in another order, within the same bound, and a
+    # value of y that is nearly half way between two codes may fall to either)
+    v = _np(L.act8_values(kept, torch.float32))
+    top = np.repeat(np.abs(np.pad(want, ((0, 0), (0, -c % 32)))).reshape(t, -1, 32).max(axis=2), 32, axis=1)[:, :c]
+    _close(v, want, top / 127 * (1 + tol) + tol * top + 2.0 ** -149)
+    dy, hdy = _dev(_normal(t, c, 1e-3, 5), "bf16", pad)
+    more, hmore = _dev(_normal(t, c, 1e-3, 6), "bf16", 0)
+    sums, hs = _dev(s, "bf16", pad)
+    for m, hm in ((more, hmore), (None, None)):
+        ds, dw = L.rms_norm_backward(dy, sums, w, eps=EPS, dsum=m)
+        want_d, want_w, size, size_w = ref.norm_backward(hdy, hs, hw, EPS, hm)
+        _close(_np(ds), want_d, (96 + c / 1024) * U * size + _half("bf16", want_d))
+        _close(_np(dw), want_w, (t + 64 + c / 8192) * U * size_w)
+        again = L.rms_norm_backward(dy, sums, w, eps=EPS, dsum=m, out=m)
+        assert torch.equal(again[0], ds) and torch.equal(again[1], dw)
+    L.sync()
+
+
 def test_backward_against_differences():
     """The change of sum(g * y) along a direction, from the forward kernel, against the backward kernel's.  With steps of h = 2^-6 of values
     near 1 the central difference is off by h^2 / 6 of third derivatives (a few units each for x, none for w), and by rounding, (32 U) / h of

@@ -251,8 +251,8 @@ def test_every_kernel_waits_for_the_one_before(name):
     assert kernels and kernels == code.count("await_previous_kernel();") == code.count("admit_next_kernel();")
 
 
-@pytest.mark.parametrize("name", ["fp8_matmul.cu", "fp8_matmul_pair.cu"])
-def test_products_wait_as_whole_warps_and_end_with_their_copies_landed(name):
+@pytest.mark.parametrize("name", ["fp8_matmul.cu", "fp8_matmul_pair.cu", "rms_norm.cu"])
+def test_products_and_rings_wait_as_whole_warps_and_end_with_their_copies_landed(name):
     code = _code(name)
     assert "barrier_try(" not in code and "multicast" not in code
     ends = re.findall(r"[^\n]*\bawait_copies\(", code)
