@@ -58,15 +58,20 @@ template <typename G, Lie LIE> struct Piece {
       }
       return;
     }
+    if (LIE == kSpread && have == kValues) gather<true>(p, have);
+    else gather<false>(p, have);
+  }
+  // One by one; ALL: without asking for each whether it is there.
+  template <bool ALL> __device__ __forceinline__ void gather(const G* p, int have) {
     constexpr int kStep = LIE == kSpread ? 32 : 1;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       if constexpr (sizeof(G) == 4) {
-        v.w[i] = i < have ? reinterpret_cast<const uint32_t*>(p)[kStep * i] : 0u;
+        v.w[i] = ALL || i < have ? reinterpret_cast<const uint32_t*>(p)[kStep * i] : 0u;
       } else {
-        const uint32_t lo = 2 * i < have ? reinterpret_cast<const uint16_t*>(p)[2 * kStep * i] : 0u;
-        const uint32_t hi = 2 * i + 1 < have ? reinterpret_cast<const uint16_t*>(p)[2 * kStep * i + kStep] : 0u;
-        v.w[i] = lo | hi << 16;
+        const uint32_t lo = ALL || 2 * i < have ? reinterpret_cast<const uint16_t*>(p)[2 * kStep * i] : 0u;
+        const uint32_t hi = ALL || 2 * i + 1 < have ? reinterpret_cast<const uint16_t*>(p)[2 * kStep * i + kStep] : 0u;
+        v.w[i] = __byte_perm(lo, hi, 0x5410);
       }
     }
   }
@@ -118,10 +123,14 @@ template <typename G, Lie LIE> struct Piece {
       }
       return;
     }
+    if (LIE == kSpread && have == kValues) scatter<true>(p, have);
+    else scatter<false>(p, have);
+  }
+  template <bool ALL> __device__ __forceinline__ void scatter(G* p, int have) const {
     constexpr int kStep = LIE == kSpread ? 32 : 1;
 #pragma unroll
     for (int i = 0; i < kValues; ++i)
-      if (i < have) {
+      if (ALL || i < have) {
         if constexpr (sizeof(G) == 4) reinterpret_cast<uint32_t*>(p)[kStep * i] = v.w[i];
         else reinterpret_cast<uint16_t*>(p)[kStep * i] = (uint16_t)(v.w[i / 2] >> i % 2 * 16);
       }

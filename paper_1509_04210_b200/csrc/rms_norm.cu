@@ -18,6 +18,8 @@ namespace rudra {
 namespace {
 
 constexpr uint32_t kMostThreads = 512;
+constexpr uint32_t kSpreadThreads = 640;      // of a block whose rows lie anyhow
+constexpr uint32_t kMostSums = 2 * kMostThreads * kValues;    // floats of shared memory for the groups' sums
 constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers: 32 to a thread
 
 // Sum over the threads of a block in a fixed order; every thread gets it.  `room`: 32 floats.
@@ -489,8 +491,8 @@ __device__ __forceinline__ void put_part(float* parts, const float* sums, const 
 // in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
 // are one cluster, which adds the parts itself.
 template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
-__global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
-  constexpr bool kAhead = sizeof(G) == 2 && PARTS == 1;      // where registers do for two rows
+__global__ void __launch_bounds__(LIE == kSpread && PARTS == 1 ? kSpreadThreads : kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
+  constexpr bool kAhead = sizeof(G) == 2 && PARTS == 1 && LIE != kSpread;      // where registers do for two rows
   __shared__ Room<Pair> room;
   extern __shared__ float sums[];
   admit_next_kernel();
@@ -856,8 +858,10 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
     if (st.parts == 1) return lie == kBy32s ? run_staged<G, W, kBy32s, 1>(p, rows, st, stream) : run_staged<G, W, kBy16s, 1>(p, rows, st, stream);
     if (st.parts == 2) return lie == kBy32s ? run_staged<G, W, kBy32s, 2>(p, rows, st, stream) : run_staged<G, W, kBy16s, 2>(p, rows, st, stream);
   }
-  const int parts = padded > 768 * kValues || (lie == kSpread && padded > 2048) ? 2 : 1;
-  const Split a(rows, padded, parts, parts == 1 ? 256 : 512, parts == 1 ? 768 : 512, kSms);
+  // Blocks of 256 threads, three to an SM, while a row fits one; 32 values to a thread where a block could not hold a row otherwise, and from
+  // some length on where it lies anyhow (bf16 7001 columns 55 us, and 65 with 16; 4111 columns 45 and 44).
+  const int parts = padded > 768 * kValues || (lie == kSpread && padded > 4608) ? 2 : 1;
+  const Split a(rows, padded, parts, parts == 2 ? 512 : padded > 256 * kValues ? 768 : 256, parts == 2 ? 512 : 768, kSms);
   const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
                                  : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 2> : norm_kernel<G, W, kSpread, 2>;
   return launch_overlapped(kernel, a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
@@ -870,11 +874,12 @@ uint64_t shares_for(uint64_t rows, uint64_t cols) {
   return std::max<uint64_t>(1, std::min(kMostShares / std::min(strips, kMostShares), (rows + 7) / 8));
 }
 
-// The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.
-Split backward_split(uint64_t rows, uint64_t cols) {
-  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1;
+// The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.  Few rows are a
+// cluster's, however they lie.
+Split backward_split(uint64_t rows, uint64_t cols, Lie lie) {
+  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1, most = lie == kSpread && parts == 1 ? kSpreadThreads : kMostThreads;
   const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
-  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kSms);
+  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, most, most, kSms);
 }
 
 template <typename G, typename W, Lie LIE, int PARTS>
@@ -891,7 +896,7 @@ template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
 cudaError_t run_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, kMostThreads, kMostHeld * sizeof(float), 0, &facts);
+  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.threads, kMostSums * sizeof(float), 0, &facts);
   if (e != cudaSuccess) return e;
   const uint32_t groups = a.threads / 32 / a.warps, smem = CLUSTER || groups > 1 ? groups * a.length() * (uint32_t)sizeof(float) : 0;
   return launch_overlapped(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
@@ -926,10 +931,10 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
   if (p.dsum.p) all = both(all, p.dsum.access);
   const bool any = all == kByElement;
   if (cols <= kMostHeld) {
-    const Split a = backward_split(rows, cols);
     float* parts = static_cast<float*>(workspace);
     Lie lie = std::max(std::max(lie_of(n.dy.p, n.dy.ld, sizeof(G)), lie_of(n.s.p, n.s.ld, sizeof(G))), std::max(lie_of(n.ds.p, n.ds.ld, sizeof(G)), lie_of(n.weight, 0, 1)));
     if (n.dsum.p) lie = std::max(lie, lie_of(n.dsum.p, n.dsum.ld, sizeof(G)));
+    const Split a = backward_split(rows, cols, lie);
     if constexpr (sizeof(G) == 2) if (lie != kSpread) {
       const Staged st(rows, cols, sizeof(G), p.dsum.p ? 3 : 2, cols, true);
       if (st.parts) {
@@ -963,9 +968,8 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
   if (cols <= kMostHeld) {
-    const Split a = backward_split(rows, cols);
-    // enough for either way: rows through rings have whole warps of 1024 columns at most, a part to an SM
-    return a.blocks <= kMostCluster ? 0 : std::max((uint64_t)a.blocks * a.length(), kSms * ((cols + 1023) / 1024 * 1024)) * sizeof(float);
+    // enough however they lie: a part to an SM, of whole warps
+    return backward_split(rows, cols, kBy32s).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
   }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
 }
