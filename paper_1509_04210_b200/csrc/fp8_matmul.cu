@@ -47,10 +47,11 @@ struct Params {
   void* y;
   uint64_t ldy;
   uint32_t m, n, k;               // rows of a, rows of b, their length
-  uint32_t stages;                // 128-value blocks along a row
+  uint32_t begin, stages;         // 128-value blocks along a row: the first, and how many
   uint32_t kt;                    // scale atoms, of four of them
   uint32_t lane_tiles;
   uint32_t split;                 // blocks of a cluster that share a tile
+  uint32_t add;                   // to what y holds
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -83,7 +84,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
   const uint32_t tile = blockIdx.x / p.split;
   const uint32_t n0 = (tile % p.lane_tiles) * 128, m0 = (tile / p.lane_tiles) * COLS;
-  const uint32_t first = (uint32_t)((uint64_t)p.stages * rank / p.split), last = (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
+  const uint32_t first = p.begin + (uint32_t)((uint64_t)p.stages * rank / p.split), last = p.begin + (uint32_t)((uint64_t)p.stages * (rank + 1) / p.split);
 
   if (threadIdx.x == 0) {
     prefetch_map(&lane_map);
@@ -199,14 +200,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
         G* y = static_cast<G*>(p.y) + (uint64_t)(m0 + c) * p.ldy + n;
 #pragma unroll
         for (uint32_t j = 0; j < 16; ++j, y += p.ldy)
-          if (m0 + c + j < p.m) put(y, __uint_as_float(r[j]));
+          if (m0 + c + j < p.m) put(y, __uint_as_float(r[j]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
       }
     }
   }
   if (!ok) atomicAdd(&g_gave_up, 1u);
   __syncwarp();
   if (p.split > 1)
-    join_parts(stage0, p.split, rank, min((uint32_t)COLS, p.m - m0), min(128u, p.n - n0), static_cast<G*>(p.y) + (uint64_t)m0 * p.ldy + n0, p.ldy);
+    join_parts(stage0, p.split, rank, min((uint32_t)COLS, p.m - m0), min(128u, p.n - n0), static_cast<G*>(p.y) + (uint64_t)m0 * p.ldy + n0, p.ldy, sizeof(G) == 4 && p.add);
   tmem_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -241,8 +242,13 @@ uint64_t pair_time(const Device::Facts& f, uint64_t m, uint64_t n, uint64_t stag
   return 2700 + waves * (stages * (waves > 1 ? 390 : 300) + 1000);
 }
 
+// Blocks along the rows that one sum takes.
+struct Blocks {
+  uint32_t begin, count;
+};
+
 template <typename G, int COLS, typename X>
-cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
+cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOut& y, Blocks part, cudaStream_t stream) {
   using S = Shape<COLS, !std::is_void<X>::value>;
   using T = typename std::conditional<std::is_void<X>::value, float, X>::type;
   static Device device;
@@ -258,7 +264,9 @@ cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOu
   p.m = (uint32_t)y.rows;
   p.n = (uint32_t)y.cols;
   p.k = (uint32_t)b.cols;
-  p.stages = (uint32_t)nb;
+  p.begin = part.begin;
+  p.stages = part.count;
+  p.add = part.begin != 0;
   p.kt = (uint32_t)((nb + 3) / 4);
   p.lane_tiles = (p.n + 127) / 128;
   const uint64_t tiles = (uint64_t)p.lane_tiles * ((p.m + COLS - 1) / COLS);
@@ -274,21 +282,38 @@ cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOu
 
 // The shape that is done soonest.  Sixteen or 32 columns only where they take all rows: scale bytes come in atoms of 128 rows, of
 // which a tile takes all, the first part or a half.
-template <typename G> cudaError_t by_time(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
-  const uint64_t m = y.rows, n = y.cols, stages = (b.cols + kFp8Block - 1) / kFp8Block;
-  if (m <= 16) return launch<G, 16, void>(a, nullptr, b, y, stream);
-  if (m <= 32) return launch<G, 32, void>(a, nullptr, b, y, stream);
+template <typename G> cudaError_t by_time(const Fp8& a, const Fp8& b, const MatrixOut& y, Blocks part, cudaStream_t stream) {
+  const uint64_t m = y.rows, n = y.cols, stages = part.count;
+  if (m <= 16) return launch<G, 16, void>(a, nullptr, b, y, part, stream);
+  if (m <= 32) return launch<G, 32, void>(a, nullptr, b, y, part, stream);
   static Device device;
   const Device::Facts* facts;
   const cudaError_t e = device.prepare(fp8_matmul_kernel<G, 64, void>, Shape<64, false>::kThreads, Shape<64, false>::kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t narrow = best_split(*facts, 64, m, n, stages).time, wide = best_split(*facts, 128, m, n, stages).time;
-  if (pair_time(*facts, m, n, stages) < std::min(narrow, wide)) return launch_fp8_matmul_pair(a, b, y, stream);
-  return narrow <= wide ? launch<G, 64, void>(a, nullptr, b, y, stream) : launch<G, 128, void>(a, nullptr, b, y, stream);
+  if (pair_time(*facts, m, n, stages) < std::min(narrow, wide)) return launch_fp8_matmul_pair(a, b, y, part.begin, part.count, stream);
+  return narrow <= wide ? launch<G, 64, void>(a, nullptr, b, y, part, stream) : launch<G, 128, void>(a, nullptr, b, y, part, stream);
+}
+
+// f32 results of long rows are gathered in memory: the tensor core cuts a sum off where it adds to it, every 32 values, by more the more
+// there is of it.  (Rows of 2^20 positive values: 1.6e-4 too little in one sum.)  So many blocks to a sum, about; a multiple of the four
+// whose scale bytes share an atom.
+constexpr uint32_t kGathered = 64;
+template <typename G, typename F> cudaError_t in_sums(uint64_t cols, F&& body) {
+  const uint32_t blocks = (uint32_t)((cols + kFp8Block - 1) / kFp8Block), sums = sizeof(G) == 4 ? std::max(1u, (blocks + kGathered / 2) / kGathered) : 1;
+  const uint32_t each = (blocks + sums - 1) / sums + 3 & ~3u;
+  for (uint32_t at = 0; at < blocks; at += each) {
+    const cudaError_t e = body(Blocks{at, std::min(each, blocks - at)});
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+template <typename G> cudaError_t product(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
+  return in_sums<G>(b.cols, [&](Blocks part) { return by_time<G>(a, b, y, part, stream); });
 }
 
 template <typename G, typename X> cudaError_t quantizing(const MatrixIn& x, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
-  return launch<G, 16, X>({}, &x, b, y, stream);
+  return in_sums<G>(b.cols, [&](Blocks part) { return launch<G, 16, X>({}, &x, b, y, part, stream); });
 }
 
 cudaError_t nothing(const MatrixOut& y, cudaStream_t stream) {   // a sum over nothing
@@ -303,7 +328,7 @@ constexpr uint64_t kQuantizedInside = 16;
 
 cudaError_t launch_fp8_matmul(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
   if (a.cols == 0) return nothing(y, stream);
-  return y.type == kBF16 ? by_time<__nv_bfloat16>(a, b, y, stream) : by_time<float>(a, b, y, stream);
+  return y.type == kBF16 ? product<__nv_bfloat16>(a, b, y, stream) : product<float>(a, b, y, stream);
 }
 
 uint64_t fp8_linear_workspace(uint64_t m, uint64_t k) {

@@ -37,9 +37,10 @@ struct Params {
   void* y;
   uint64_t ldy;
   uint32_t m, n;
-  uint32_t stages;               // 128-value blocks along a row
+  uint32_t begin, stages;        // 128-value blocks along a row: the first, a multiple of four, and how many
   uint32_t kt;                   // scale atoms, of four of them
   uint32_t lane_tiles, tiles;
+  uint32_t add;                  // to what y holds
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -97,13 +98,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
     uint32_t s = 0, parity = 1, issued = 0;
     for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step) {
       const uint32_t n0 = tile % p.lane_tiles * kTile + rank * kRows, m0 = tile / p.lane_tiles * kTile;
-      const uint32_t lane_atom = n0 / 128 * p.kt, column_atom = m0 / 128 * p.kt;
+      const uint32_t lane_atom = n0 / 128 * p.kt + p.begin / 4, column_atom = m0 / 128 * p.kt + p.begin / 4;
       for (uint32_t i = 0; i < stages; ++i) {
         const uint32_t at = stage0 + s * kStage, bar = first_full + 8 * s;
         if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
         if (rank == 0) barrier_expect(full + 8 * s, 2 * (i % 4 ? 2 * kMatrix : kBytes), elected);
-        copy_box_pair(at, &lane_map, (int)(i * kStageBytes), (int)n0, bar, elected);
-        copy_box_pair(at + kMatrix, &column_map, (int)(i * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
+        copy_box_pair(at, &lane_map, (int)((p.begin + i) * kStageBytes), (int)n0, bar, elected);
+        copy_box_pair(at + kMatrix, &column_map, (int)((p.begin + i) * kStageBytes), (int)(m0 + rank * kRows), bar, elected);
         if (i % 4 == 0) {
           copy_box_pair(at + 2 * kMatrix, &lane_scales, 0, (int)(lane_atom + i / 4), bar, elected);
           copy_box_pair(at + 2 * kMatrix + kScales, &column_scales, 0, (int)(column_atom + i / 4), bar, elected);
@@ -163,11 +164,11 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
         G* y = static_cast<G*>(p.y) + (uint64_t)m * p.ldy + n;
         if (have == 128) {
 #pragma unroll
-          for (uint32_t c = 0; c < 128; ++c, y += p.ldy) put(y, __uint_as_float(r[c / 16][c % 16]));
+          for (uint32_t c = 0; c < 128; ++c, y += p.ldy) put(y, __uint_as_float(r[c / 16][c % 16]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
         } else {
 #pragma unroll
           for (uint32_t c = 0; c < 128; ++c, y += p.ldy)
-            if (c < have) put(y, __uint_as_float(r[c / 16][c % 16]));
+            if (c < have) put(y, __uint_as_float(r[c / 16][c % 16]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
         }
       }
     }
@@ -184,7 +185,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
   }
 }
 
-template <typename G> cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
+template <typename G> cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
   cudaError_t e = device.prepare(fp8_pair_kernel<G>, kThreads, kSmem, 0, &facts);
@@ -200,15 +201,15 @@ template <typename G> cudaError_t launch(const Fp8& a, const Fp8& b, const Matri
   if (e == cudaSuccess) e = encode_plain(&lane_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, b.scales, 128, b_atoms, 512, 128, 1);
   if (e == cudaSuccess) e = encode_plain(&column_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, a.scales, 128, a_atoms, 512, 128, 1);
   if (e != cudaSuccess) return e;
-  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, (uint32_t)nb, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
+  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, begin, count, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles, begin != 0};
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)facts->sms / 2);
   return launch_overlapped(fp8_pair_kernel<G>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
 }
 
 }  // namespace
 
-cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream) {
-  return y.type == kBF16 ? launch<__nv_bfloat16>(a, b, y, stream) : launch<float>(a, b, y, stream);
+cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
+  return y.type == kBF16 ? launch<__nv_bfloat16>(a, b, y, begin, count, stream) : launch<float>(a, b, y, begin, count, stream);
 }
 
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }

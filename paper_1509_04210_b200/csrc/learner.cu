@@ -66,8 +66,9 @@ int gradients(const void* const* grads, const int* dtypes, const uint64_t* sizes
   return 0;
 }
 
-// Whether what is written overlaps: an output another output or another gradient, or its own gradient other than in its place.
-bool overlapping(const std::vector<Gradient>& list) {
+// Whether what is written overlaps: an output another output, the norm or another gradient, or its own gradient other than in its
+// place.
+bool overlapping(const std::vector<Gradient>& list, const float* norm) {
   struct Span {
     uintptr_t from, to;
     bool operator<(const Span& o) const { return from < o.from; }
@@ -87,15 +88,18 @@ bool overlapping(const std::vector<Gradient>& list) {
   if (!sorted) std::sort(written.begin(), written.end());
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].from < written[i - 1].to) return true;
+  const auto meets = [&](uintptr_t p, uintptr_t end) {
+    if (p >= high || end <= low) return false;
+    // the first output that begins behind the first byte, and the one before it
+    const auto at = std::upper_bound(written.begin(), written.end(), Span{p, 0});
+    return (at != written.end() && at->from < end) || (at != written.begin() && (at - 1)->to > p);
+  };
   for (const Gradient& g : list) {
     if (!g.size || (g.p == g.out && g.type == g.out_type)) continue;
-    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p), end = p + g.size * (g.type == rudra::kBF16 ? 2 : 4);
-    if (p >= high || end <= low) continue;
-    // the first output that begins behind the gradient's first byte, and the one before it
-    const auto at = std::upper_bound(written.begin(), written.end(), Span{p, 0});
-    if ((at != written.end() && at->from < end) || (at != written.begin() && (at - 1)->to > p)) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p);
+    if (meets(p, p + g.size * (g.type == rudra::kBF16 ? 2 : 4))) return true;
   }
-  return false;
+  return meets(reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm + 1));
 }
 
 int done(cudaError_t e, const char* what) { return e == cudaSuccess ? 0 : cuda_fail(e, what); }
@@ -318,6 +322,7 @@ int rudra_rms_norm(const void* x_dev, uint64_t ldx, const void* residual_dev, ui
     }
     if (y_dev)
       if (const int e = check_matrix("output", y_dev, dtype, tokens, channels, ldy)) return e;
+    if (y_dev && y_dev == sum_dev) return fail(RUDRA_E_INVAL, "output and sum are one matrix");
     if (fp8_codes_dev || fp8_scales_dev)
       if (const int e = check_blocks("FP8 output", fp8_codes_dev, fp8_scales_dev, tokens, channels)) return e;
     if (act8_codes_dev || act8_scales_dev)
@@ -387,7 +392,7 @@ int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint6
     const uint64_t need = norm_known ? 0 : rudra_grad_norm_workspace(count);
     if (need && (!aligned(workspace_dev) || workspace_bytes < need))
       return fail(RUDRA_E_INVAL, "workspace is null, not 32-byte aligned or smaller than %llu bytes", (unsigned long long)need);
-    if (overlapping(list)) return fail(RUDRA_E_INVAL, "outputs overlap each other or other gradients");
+    if (overlapping(list, norm_dev)) return fail(RUDRA_E_INVAL, "outputs overlap each other, other gradients or the norm");
     return done(rudra::launch_grad_clip(list.data(), list.size(), norm_dev, max_norm, norm_known != 0, workspace_dev, stream_of(cuda_stream)),
                 "gradient clipping kernel launch");
   });

@@ -203,7 +203,7 @@ template <typename G> __device__ __forceinline__ void put_streaming(G* to, float
 // [column][128 lanes] at `part`: this block adds the parts of every split-th column in rank order and writes
 // them as rows of `out`.  `rows` columns and `lanes` lanes exist.  Every thread of every block calls it.
 template <typename G>
-__device__ __forceinline__ void join_parts(uint32_t part, uint32_t split, uint32_t rank, uint32_t rows, uint32_t lanes, G* out, uint64_t ld) {
+__device__ __forceinline__ void join_parts(uint32_t part, uint32_t split, uint32_t rank, uint32_t rows, uint32_t lanes, G* out, uint64_t ld, bool add = false) {
   cluster_arrive();
   cluster_wait();
   const uint32_t lane = threadIdx.x % 32 * 4, step = blockDim.x / 32 * split;
@@ -218,6 +218,12 @@ __device__ __forceinline__ void join_parts(uint32_t part, uint32_t split, uint32
     for (uint32_t r = 1; r < kMost; ++r)
       if (r < split) s = make_float4(s.x + v[r].x, s.y + v[r].y, s.z + v[r].z, s.w + v[r].w);
     G* to = out + c * ld + lane;
+    if (add) {      // to what is there
+      if (lane < lanes) s.x += (float)to[0];
+      if (lane + 1 < lanes) s.y += (float)to[1];
+      if (lane + 2 < lanes) s.z += (float)to[2];
+      if (lane + 3 < lanes) s.w += (float)to[3];
+    }
     if (lane < lanes) put(to, s.x);
     if (lane + 1 < lanes) put(to + 1, s.y);
     if (lane + 2 < lanes) put(to + 2, s.z);

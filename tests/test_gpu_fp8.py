@@ -163,6 +163,22 @@ def test_blocks_that_differ_by_far_and_non_finite_ones(m):
     assert np.isnan(y[1]).all() and np.isnan(y[3]).all() and np.isnan(y[:, 7]).all() and (np.delete(y[4], 7) == 0).all()
 
 
+@pytest.mark.parametrize("m,n", [(1, 200), (40, 100), (300, 200), (1500, 1600)])
+def test_long_sums_of_positive_values(m, n):
+    """Every addition to a sum cuts it off, by 2^-23 of itself at most: a sum of s blocks of 128 values has 4 s of them, on average half
+    way up, so s * 2^-22 too little at most; f32 results are gathered every 96 blocks at most, with a rounding each: under 3e-5 however long."""
+    torch, L = _torch(), _learner()
+    k = 60000
+    a, b = torch.rand(m, k, device="cuda") + 0.5, torch.rand(n, k, device="cuda") + 0.5
+    qa, qb = L.fp8_quantize(a), L.fp8_quantize(b)
+    want = L.fp8_dequantize(qa, torch.float32).double() @ L.fp8_dequantize(qb, torch.float32).double().t()
+    for x in (qa, a) if m <= 16 else (qa,):
+        off = (L.fp8_matmul(x, qb, torch.float32).double() - want) / want
+        assert off.abs().max().item() < 96 * 2.0 ** -22 + 8 * 2.0 ** -24
+    off = (L.fp8_matmul(qa, qb).double() - want) / want
+    assert off.abs().max().item() < 469 * 2.0 ** -22 + 2.0 ** -8
+
+
 def test_empty_sizes():
     torch, L = _torch(), _learner()
     e = lambda r, c: torch.empty(r, c, device="cuda")  # noqa: E731

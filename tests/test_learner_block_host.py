@@ -76,6 +76,7 @@ def test_norm_refusals():
     _refused(f(r=P, s=P, ldr=5), "residual")
     _refused(f(r=P, s=P, lds=5), "sum")
     _refused(f(y=P + 2), "output")
+    _refused(f(r=P, s=2 * P, y=2 * P), "one matrix")
     _refused(f(y=None), "no output")
     _refused(f(q=P), "FP8")
     _refused(f(q=P, qs=P + 8), "FP8")
@@ -140,6 +141,7 @@ def test_clipping_refusals():
     for grads, outs in (([(P, 0, 10)], [(P, 1)]), ([(P, 0, 10)], [(P + 4, 0)]), ([(P, 0, 10), (P + 36, 0, 5)], [(Q, 0), (Q + 36, 0)]), ([(P, 0, 10), (Q, 0, 10)], [(Q, 0), (P, 0)]),
                         ([(P, 0, 10), (P, 0, 10)], [(P, 0), (P, 0)]), ([(P, 0, 10), (P + 36, 0, 10)], [(P, 0), (P + 36, 0)]), ([(P, 0, 10), (P + 60, 1, 10)], [(Q, 0), (P + 20, 1)])):
         _refused(clip(grads, outs), "overlap")
+    _refused(clip([(Q, 0, 4096)], [(P - 64, 0)]), "overlap")      # the norm is at P
 
 
 def test_tensors_that_are_refused_without_a_gpu():
