@@ -40,7 +40,6 @@ struct Params {
   uint32_t begin, stages;        // 128-value blocks along a row: the first, a multiple of four, and how many
   uint32_t kt;                   // scale atoms, of four of them
   uint32_t lane_tiles, tiles;
-  uint32_t add;                  // to what y holds
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -54,7 +53,8 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
                :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add), "r"(elected) : "memory");
 }
 
-template <typename G>
+// ADD: to what y holds.
+template <typename G, bool ADD>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map,
                 const __grid_constant__ CUtensorMap lane_scales, const __grid_constant__ CUtensorMap column_scales,
@@ -162,13 +162,14 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
       if (lane == 0) barrier_arrive_cluster(first_drained);
       if (n < p.n) {
         G* y = static_cast<G*>(p.y) + (uint64_t)m * p.ldy + n;
+        const auto value = [](uint32_t bits, const G* to) { return ADD ? __uint_as_float(bits) + (float)*to : __uint_as_float(bits); };
         if (have == 128) {
 #pragma unroll
-          for (uint32_t c = 0; c < 128; ++c, y += p.ldy) put(y, __uint_as_float(r[c / 16][c % 16]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
+          for (uint32_t c = 0; c < 128; ++c, y += p.ldy) put(y, value(r[c / 16][c % 16], y));
         } else {
 #pragma unroll
           for (uint32_t c = 0; c < 128; ++c, y += p.ldy)
-            if (c < have) put(y, __uint_as_float(r[c / 16][c % 16]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
+            if (c < have) put(y, value(r[c / 16][c % 16], y));
         }
       }
     }
@@ -185,10 +186,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
   }
 }
 
-template <typename G> cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
+template <typename G, bool ADD> cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  cudaError_t e = device.prepare(fp8_pair_kernel<G>, kThreads, kSmem, 0, &facts);
+  cudaError_t e = device.prepare(fp8_pair_kernel<G, ADD>, kThreads, kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t nb = (a.cols + kFp8Block - 1) / kFp8Block, kt = (nb + 3) / 4, lane_tiles = (b.rows + kTile - 1) / kTile;
   const uint64_t tiles = lane_tiles * ((a.rows + kTile - 1) / kTile);
@@ -201,15 +202,16 @@ template <typename G> cudaError_t launch(const Fp8& a, const Fp8& b, const Matri
   if (e == cudaSuccess) e = encode_plain(&lane_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, b.scales, 128, b_atoms, 512, 128, 1);
   if (e == cudaSuccess) e = encode_plain(&column_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, a.scales, 128, a_atoms, 512, 128, 1);
   if (e != cudaSuccess) return e;
-  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, begin, count, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles, begin != 0};
+  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, begin, count, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)facts->sms / 2);
-  return launch_overlapped(fp8_pair_kernel<G>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
+  return launch_overlapped(fp8_pair_kernel<G, ADD>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
 }
 
 }  // namespace
 
 cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
-  return y.type == kBF16 ? launch<__nv_bfloat16>(a, b, y, begin, count, stream) : launch<float>(a, b, y, begin, count, stream);
+  if (y.type == kBF16) return begin ? cudaErrorInvalidValue : launch<__nv_bfloat16, false>(a, b, y, 0, count, stream);
+  return begin ? launch<float, true>(a, b, y, begin, count, stream) : launch<float, false>(a, b, y, 0, count, stream);
 }
 
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
