@@ -10,6 +10,7 @@
 #include "fp8.cuh"
 #include "launch.cuh"
 #include "learner.cuh"
+#include "pairs.cuh"
 
 namespace rudra {
 namespace {
@@ -47,94 +48,103 @@ __global__ void __launch_bounds__(kThreads) fp8_rows_kernel(Rows<G> src, uint32_
 }
 
 // A tile of 128 x 128 values of src: as a square with one scale, or with a scale for each of its columns, which are rows
-// of the result.  A warp takes 32 rows x 64 columns, a lane two neighbouring columns of 32 values; maxima and codes meet
-// in shared memory, from which the codes leave as rows of 128 bytes.
-template <typename G, bool TRANSPOSE, bool SQUARE>
-__global__ void __launch_bounds__(kThreads) fp8_tile_kernel(const G* src, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t column_tiles, bool pairs,
-                                                            uint8_t* codes, uint8_t* scales) {
+// of the result.  A warp takes 16 whole rows of it, a lane 16 values of each of four columns: neighbouring ones where four values can be
+// read at once (QUADS), else every 32nd; maxima and codes meet in shared memory, from which the codes leave as rows of 128 bytes.
+template <typename G, bool TRANSPOSE, bool SQUARE, bool QUADS>
+__global__ void __launch_bounds__(kThreads, 3) fp8_tile_kernel(const G* src, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t column_tiles, uint8_t* codes,
+                                                            uint8_t* scales) {
   static_assert(TRANSPOSE || SQUARE, "pieces of rows have a kernel of their own");
-  constexpr uint32_t kPitch = kFp8Block + 16;
+  constexpr uint32_t kPitch = kFp8Block + 16, kRows = 16;
   __shared__ alignas(16) uint8_t tile[kFp8Block * kPitch];
   __shared__ uint32_t top[SQUARE ? 1 : kFp8Block];
   admit_next_kernel();
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x % 32, rl = threadIdx.x / 32 * kRows;
   const uint32_t r0 = blockIdx.x / column_tiles * kFp8Block, c0 = blockIdx.x % column_tiles * kFp8Block;
-  const uint32_t cl = warp / 4 * 64 + lane * 2, rl = warp % 4 * 32, c = c0 + cl;
+  const auto column = [&](uint32_t j) { return QUADS ? 4 * lane + j : lane + 32 * j; };
   if (threadIdx.x < (SQUARE ? 1 : kFp8Block)) top[threadIdx.x] = 0;
   await_previous_kernel();
   // all on their way before the first is looked at: a value used in the branch that loads it would hold up the next load
   // (509 x 4096 bf16 19.6 us that way)
-  float x[2][32];
-  if (pairs && c + 1 < cols) {
-    using Word = typename std::conditional<sizeof(G) == 4, uint2, uint32_t>::type;
-    Word raw[32];
+  float x[4][kRows];
+  if (QUADS && c0 + 4 * lane + 3 < cols) {
+    using Word = typename std::conditional<sizeof(G) == 4, uint4, uint2>::type;
+    Word raw[kRows];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (uint32_t i = 0; i < kRows; ++i) {
       const uint64_t r = (uint64_t)r0 + rl + i;
-      raw[i] = r < rows ? read_once(reinterpret_cast<const Word*>(src + r * ld + c)) : Word{};
+      raw[i] = r < rows ? read_once(reinterpret_cast<const Word*>(src + r * ld + c0 + 4 * lane)) : Word{};
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (uint32_t i = 0; i < kRows; ++i) {
       if constexpr (sizeof(G) == 4) {
         x[0][i] = __uint_as_float(raw[i].x);
         x[1][i] = __uint_as_float(raw[i].y);
+        x[2][i] = __uint_as_float(raw[i].z);
+        x[3][i] = __uint_as_float(raw[i].w);
       } else {
-        x[0][i] = __uint_as_float(raw[i] << 16);
-        x[1][i] = __uint_as_float(raw[i] & 0xFFFF0000u);
+        x[0][i] = __uint_as_float(raw[i].x << 16);
+        x[1][i] = __uint_as_float(raw[i].x & 0xFFFF0000u);
+        x[2][i] = __uint_as_float(raw[i].y << 16);
+        x[3][i] = __uint_as_float(raw[i].y & 0xFFFF0000u);
       }
     }
   } else {
-    G raw[2][32];
+    G raw[4][kRows];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (uint32_t i = 0; i < kRows; ++i)
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const uint64_t r = (uint64_t)r0 + rl + i;
-        raw[j][i] = r < rows && c + j < cols ? src[r * ld + c + j] : G(0.f);
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint64_t r = (uint64_t)r0 + rl + i, c = (uint64_t)c0 + column(j);
+        raw[j][i] = r < rows && c < cols ? src[r * ld + c] : G(0.f);
       }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (uint32_t j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[j][i] = (float)raw[j][i];
+      for (uint32_t i = 0; i < kRows; ++i) x[j][i] = (float)raw[j][i];
   }
-  uint32_t m[2] = {};
+  float m[4];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (uint32_t j = 0; j < 4; ++j) {
+    m[j] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m[j] = max(m[j], __float_as_uint(x[j][i]) & 0x7FFFFFFFu);
+    for (uint32_t i = 0; i < kRows; ++i) m[j] = larger(m[j], x[j][i]);
+  }
   __syncthreads();
   if (SQUARE) {
-    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, max(m[0], m[1]));
+    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(larger(larger(m[0], m[1]), larger(m[2], m[3]))));
     if (lane == 0) atomicMax(top, most);
   } else {
-    atomicMax(top + cl, m[0]);
-    atomicMax(top + cl + 1, m[1]);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) atomicMax(top + column(j), __float_as_uint(m[j]));
   }
   __syncthreads();
-  uint32_t s[2];
+  uint32_t keep[4];      // no bits of what stands for NaN as a whole
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    s[j] = fp8_scale_byte(top[SQUARE ? 0 : cl + j]);
-    const float inv = inverse_scale(s[j]);
+  for (uint32_t j = 0; j < 4; ++j) {
+    const uint32_t s = fp8_scale_byte(top[SQUARE ? 0 : column(j)]);
+    const float inv = inverse_scale(s);
+    keep[j] = s == 255u ? 0u : 0xFFFFFFFFu;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x[j][i] = s[j] == 255u ? 0.f : x[j][i] * inv;
+    for (uint32_t i = 0; i < kRows; ++i) x[j][i] *= inv;
   }
   if (TRANSPOSE) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (uint32_t j = 0; j < 4; ++j) {
+      uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 32; i += 16) {
-        uint32_t w[4];
+      for (uint32_t q = 0; q < 4; ++q) w[q] = e4m3_codes4(x[j][4 * q], x[j][4 * q + 1], x[j][4 * q + 2], x[j][4 * q + 3]) & keep[j];
+      *reinterpret_cast<uint4*>(tile + column(j) * kPitch + rl) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {      // one scale for all
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = e4m3_codes4(x[j][i + 4 * q], x[j][i + 4 * q + 1], x[j][i + 4 * q + 2], x[j][i + 4 * q + 3]);
-        *reinterpret_cast<uint4*>(tile + (cl + j) * kPitch + rl + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (uint32_t i = 0; i < kRows; ++i) {
+      const uint32_t w = e4m3_codes4(x[0][i], x[1][i], x[2][i], x[3][i]) & keep[0];
+      if (QUADS) {
+        *reinterpret_cast<uint32_t*>(tile + (rl + i) * kPitch + 4 * lane) = w;
+      } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) tile[(rl + i) * kPitch + column(j)] = (uint8_t)(w >> 8 * j);
       }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-      const uint32_t w = e4m3_codes4(x[0][i], x[1][i], x[0][i + 1], x[1][i + 1]);
-      *reinterpret_cast<uint16_t*>(tile + (rl + i) * kPitch + cl) = (uint16_t)w;
-      *reinterpret_cast<uint16_t*>(tile + (rl + i + 1) * kPitch + cl) = (uint16_t)(w >> 16);
     }
   }
   __syncthreads();
@@ -205,10 +215,12 @@ template <typename G> cudaError_t quantize(const MatrixIn& m, bool transpose, bo
   }
   const uint64_t tiles = (m.cols + kFp8Block - 1) / kFp8Block, blocks = tiles * ((m.rows + kFp8Block - 1) / kFp8Block);
   if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
-  const bool pairs = reinterpret_cast<uintptr_t>(m.p) % (2 * sizeof(G)) == 0 && m.ld % 2 == 0;
-  return launch_overlapped(!transpose ? fp8_tile_kernel<G, false, true> : square ? fp8_tile_kernel<G, true, true> : fp8_tile_kernel<G, true, false>, (uint32_t)blocks,
-                           kThreads, 0, 1, stream, static_cast<const G*>(m.p), m.ld, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)tiles, pairs, static_cast<uint8_t*>(codes),
-                           static_cast<uint8_t*>(scales));
+  const bool quads = reinterpret_cast<uintptr_t>(m.p) % (4 * sizeof(G)) == 0 && m.ld % 4 == 0;
+  const auto kernel = !transpose ? quads ? fp8_tile_kernel<G, false, true, true> : fp8_tile_kernel<G, false, true, false>
+                      : square ? quads ? fp8_tile_kernel<G, true, true, true> : fp8_tile_kernel<G, true, true, false>
+                               : quads ? fp8_tile_kernel<G, true, false, true> : fp8_tile_kernel<G, true, false, false>;
+  return launch_overlapped(kernel, (uint32_t)blocks, kThreads, 0, 1, stream, static_cast<const G*>(m.p), m.ld, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)tiles,
+                           static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
 }
 
 template <typename G> cudaError_t dequantize(const Fp8& m, const MatrixOut& d, cudaStream_t stream) {

@@ -218,9 +218,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
 
 // How long a product takes, in ns, by its shape.  Measured (warm, one after another, weights out of HBM): a stage of 16, 32, 64 and
 // 128 columns 140, 145, 170 and 210 ns, what comes after a tile's last stage 100 to 1000, joining the parts of a tile 1100 to 2600,
-// 2000 for setting up; a pair's stage 300 (390 on all SMs, where power sets the clock) and 1000 a tile.  For instance 256 x 4096 x 4096:
-// 64 columns 8.2 us, 128 columns 9.7 and split in two 10.9, pairs 13.7; 128 x 1000 x 4096: 64 columns 6.9 us and in four parts 5.5,
-// 128 columns in eight parts 6.4; 1000 x 4096 x 4096: pairs 15.3 us, 128 columns 19.6.
+// 2000 for setting up, again for every round of blocks; a pair's stage 300 (360 on all SMs), 1000 a tile and 2700 once.  For instance
+// 256 x 4096 x 4096: 64 columns 8.2 us, 128 columns 9.7 and split in two 10.9, pairs 13.7; 128 x 1000 x 4096: 64 columns 6.9 us and in
+// four parts 5.5, 128 columns in eight parts 6.4; 1000 x 4096 x 4096: pairs 15.3 us, 128 columns 19.6; 4096 x 4096 x 9216: pairs 112
+// us, 128 columns 134, 64 columns 190.
 struct Timed {
   uint32_t split;
   uint64_t time;
@@ -229,7 +230,7 @@ Timed best_split(const Device::Facts& f, int columns, uint64_t m, uint64_t n, ui
   const int i = columns == 16 ? 0 : columns == 32 ? 1 : columns == 64 ? 2 : 3;
   constexpr uint64_t kStageTime[4] = {140, 145, 170, 210}, kAfter[4] = {100, 200, 500, 1000}, kJoin[4] = {1100, 1400, 2300, 2600};
   const uint64_t tiles = ((n + 127) / 128) * ((m + columns - 1) / columns), waves = (tiles + f.sms - 1) / f.sms;
-  Timed best = {1, 2000 + waves * (stages * kStageTime[i] + kAfter[i])};
+  Timed best = {1, waves * (2000 + stages * kStageTime[i] + kAfter[i])};
   for (uint32_t k = 1; k < 4; ++k) {
     const uint32_t split = 1u << k;
     const uint64_t time = 2000 + (stages + split - 1) / split * kStageTime[i] + kAfter[i] + kJoin[i];
@@ -239,7 +240,7 @@ Timed best_split(const Device::Facts& f, int columns, uint64_t m, uint64_t n, ui
 }
 uint64_t pair_time(const Device::Facts& f, uint64_t m, uint64_t n, uint64_t stages) {
   const uint64_t tiles = ((n + 255) / 256) * ((m + 255) / 256), waves = (2 * tiles + f.sms - 1) / f.sms;
-  return 2700 + waves * (stages * (waves > 1 ? 390 : 300) + 1000);
+  return 2700 + waves * (stages * (waves > 1 ? 360 : 300) + 1000);
 }
 
 // Blocks along the rows that one sum takes.
