@@ -3,7 +3,9 @@
 //
 // A block's scale is a power of two read off its largest magnitude, so scaling is exact and the only rounding is the one
 // to E4M3, done by the conversion instruction.  One read and 129/128 bytes written per value: bound by HBM for large
-// matrices, by launch latency for small ones.
+// matrices, by launch latency for small ones.  Measured: rows of 8192 x 9216 bf16 35.7 us and of 4096 x 9216 f32 29.6 us = 6.4 TB/s,
+// expanded 35.1 and 29.5 us; 8192 x 4096 bf16 transposed 19.6 us = 5.1 TB/s (256-byte pieces of rows), 4096 x 9216 f32 by squares
+// 25.5 and transposed 26.6 us (partly out of L2); 4 x 4096 bf16 2.6 us.
 #include <algorithm>
 #include <type_traits>
 

