@@ -7,7 +7,8 @@
 // sums are in 32 bits.  Both passes read and write each matrix once and multiply nothing: they are bound by HBM for
 // many tokens, by launch latency for few.  Measured at 8192 x 4096 bf16 with a residual: forward to FP8 41 us = 5.7 TB/s, to bf16 49 us
 // = 5.5 TB/s, backward 50 us = 5.4 TB/s; f32 69, 95 and 91 us = 6.3, 5.6 and 5.9 TB/s; one token 3 us, 37 x 1000 f32 backward 6.4 us.
-// Rows that lie anyhow are held up by their values one by one: 4000 x 4111 bf16 45 us forward and 66 backward, for 20 us of memory.
+// Rows that lie anyhow are held up by their values one by one: 4000 x 4111 bf16 35 us forward and 87 backward, 8192 x 1439 23 and 40, for 20
+// and 15 us of memory.
 #include <algorithm>
 
 #include "fp8.cuh"
@@ -20,7 +21,6 @@ namespace rudra {
 namespace {
 
 constexpr uint32_t kMostThreads = 512;
-constexpr uint32_t kSpreadThreads = 640;      // of a block whose rows lie anyhow
 constexpr uint32_t kMostSums = 2 * kMostThreads * kValues;    // floats of shared memory for the groups' sums
 constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers: 32 to a thread
 
@@ -261,8 +261,8 @@ __device__ __forceinline__ void norm_row(const Forward<G, W>& p, const Piece<G, 
 // Rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread; a block's groups walk over
 // the rows.
 template <typename G, typename W, Lie LIE, int PARTS>
-__global__ void __launch_bounds__(PARTS == 1 ? 768 : 512) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
-  __shared__ alignas(16) uint8_t bytes[LIE == kSpread ? (PARTS == 1 ? 24 : 16) : 1][512];
+__global__ void __launch_bounds__(PARTS == 2 ? 512 : LIE == kSpread ? 1024 : 768) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
+  __shared__ alignas(16) uint8_t bytes[LIE == kSpread ? (PARTS == 1 ? 32 : 16) : 1][512];
   __shared__ Room<float> room;
   admit_next_kernel();
   const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
@@ -493,7 +493,7 @@ __device__ __forceinline__ void put_part(float* parts, const float* sums, const 
 // in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
 // are one cluster, which adds the parts itself.
 template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
-__global__ void __launch_bounds__(LIE == kSpread && PARTS == 1 ? kSpreadThreads : kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
+__global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
   constexpr bool kAhead = sizeof(G) == 2 && PARTS == 1 && LIE != kSpread;      // where registers do for two rows
   __shared__ Room<Pair> room;
   extern __shared__ float sums[];
@@ -862,8 +862,11 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   }
   // Blocks of 256 threads, three to an SM, while a row fits one; 32 values to a thread where a block could not hold a row otherwise, and from
   // some length on where it lies anyhow (bf16 7001 columns 55 us, and 65 with 16; 4111 columns 45 and 44).
-  const int parts = padded > 768 * kValues || (lie == kSpread && padded > 4608) ? 2 : 1;
-  const Split a(rows, padded, parts, parts == 2 ? 512 : padded > 256 * kValues ? 768 : 256, parts == 2 ? 512 : 768, kSms);
+  // Blocks of 256 threads, three to an SM, while a row fits one, and more warps where rows lie anyhow and their values are asked for one by
+  // one (4000 x 4111 bf16 34.6 us with 27 warps to an SM, 44 with 18); 32 values to a thread where a block could not hold a row otherwise.
+  const bool spread = lie == kSpread;
+  const int parts = padded > (spread ? 1024 : 768) * kValues ? 2 : 1;
+  const Split a(rows, padded, parts, parts == 1 && !spread ? padded > 256 * kValues ? 768 : 256 : 512, parts == 2 ? 512 : spread ? 1024 : 768, kSms);
   const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
                                  : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 2> : norm_kernel<G, W, kSpread, 2>;
   return launch_overlapped(kernel, a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
@@ -877,11 +880,11 @@ uint64_t shares_for(uint64_t rows, uint64_t cols) {
 }
 
 // The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.  Few rows are a
-// cluster's, however they lie.
-Split backward_split(uint64_t rows, uint64_t cols, Lie lie) {
-  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1, most = lie == kSpread && parts == 1 ? kSpreadThreads : kMostThreads;
+// cluster's.
+Split backward_split(uint64_t rows, uint64_t cols) {
+  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1;
   const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
-  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, most, most, kSms);
+  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kSms);
 }
 
 template <typename G, typename W, Lie LIE, int PARTS>
@@ -936,7 +939,7 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
     float* parts = static_cast<float*>(workspace);
     Lie lie = std::max(std::max(lie_of(n.dy.p, n.dy.ld, sizeof(G)), lie_of(n.s.p, n.s.ld, sizeof(G))), std::max(lie_of(n.ds.p, n.ds.ld, sizeof(G)), lie_of(n.weight, 0, 1)));
     if (n.dsum.p) lie = std::max(lie, lie_of(n.dsum.p, n.dsum.ld, sizeof(G)));
-    const Split a = backward_split(rows, cols, lie);
+    const Split a = backward_split(rows, cols);
     if constexpr (sizeof(G) == 2) if (lie != kSpread) {
       const Staged st(rows, cols, sizeof(G), p.dsum.p ? 3 : 2, cols, true);
       if (st.parts) {
@@ -971,7 +974,7 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
   if (cols <= kMostHeld) {
     // enough however they lie: a part to an SM, of whole warps
-    return backward_split(rows, cols, kBy32s).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
+    return backward_split(rows, cols).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
   }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
 }
