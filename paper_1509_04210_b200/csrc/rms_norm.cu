@@ -310,23 +310,36 @@ struct Ring {
   __host__ __device__ uint32_t slot() const { return groups * matrices * pitch; }
 };
 
-// The copying warp: slot by slot a row of each matrix for every group.  `bars`: full barriers, then empty ones.
-template <typename... P> __device__ __forceinline__ bool fill_ring(const Ring& ring, uint32_t ring0, uint32_t bars, uint64_t rows, const P&... matrices) {
-  const uint32_t elected = elect(), full = bars, empty = bars + 8 * ring.slots;
+// The copying warp: slot by slot a row of each matrix for every group.  LANES: by a lane for each group (16384 x 512 without residual 7.7 us, and
+// 8.8 by one lane); else by one for all, with addresses that are the same to the warp (8192 x 4096 to FP8 41.0 us, and 42.3 in a
+// kernel that could do either).  `bars`: full barriers, then empty ones.
+template <bool LANES, typename... P> __device__ __forceinline__ bool fill_ring(const Ring& ring, uint32_t ring0, uint32_t bars, uint64_t rows, const P&... matrices) {
+  const uint32_t elected = elect(), lane = threadIdx.x % 32, full = bars, empty = bars + 8 * ring.slots;
   uint32_t s = 0, parity = 1, issued = 0;
   bool ok = true;
   for (uint64_t first = (uint64_t)blockIdx.x * ring.groups; first < rows; first += (uint64_t)gridDim.x * ring.groups, ++issued) {
     if (!(ok = barrier_wait(empty + 8 * s, parity))) break;
-    const uint32_t n = (uint32_t)min((uint64_t)ring.groups, rows - first), bar = full + 8 * s;
+    const uint32_t n = (uint32_t)min((uint64_t)ring.groups, rows - first), bar = full + 8 * s, slot = ring0 + s * ring.slot();
     barrier_expect(bar, n * ring.matrices * ring.row, elected);
-    uint32_t to = ring0 + s * ring.slot();
-    for (uint32_t g = 0; g < n; ++g) {
+    uint32_t to = slot;
+    if constexpr (LANES) {
+      __syncwarp();
+      to += lane * ring.matrices * ring.pitch;
       const auto copy = [&](const auto& m) {
         if (!m.p) return;
-        copy_bulk(to, m.p + (first + g) * m.ld, ring.row, bar, elected);
+        copy_bulk(to, m.p + (first + (lane < n ? lane : 0)) * m.ld, ring.row, bar, lane < n);
         to += ring.pitch;
       };
       (copy(matrices), ...);
+    } else {
+      for (uint32_t g = 0; g < n; ++g) {
+        const auto copy = [&](const auto& m) {
+          if (!m.p) return;
+          copy_bulk(to, m.p + (first + g) * m.ld, ring.row, bar, elected);
+          to += ring.pitch;
+        };
+        (copy(matrices), ...);
+      }
     }
     if (++s == ring.slots) s = 0, parity ^= 1;
   }
@@ -361,7 +374,7 @@ __global__ void __launch_bounds__(kForwardWarps * 32 + 32) norm_staged_kernel(co
   await_previous_kernel();
   bool ok = true;
   if (warp == ring.groups * warps) {
-    ok = fill_ring(ring, smem_address(slots), bars, rows, p.x, p.residual);
+    ok = fill_ring<PARTS == 1>(ring, smem_address(slots), bars, rows, p.x, p.residual);      // 16 values to a thread: short rows, many groups
   } else {
     uint32_t c[PARTS];
     int have[PARTS];
@@ -609,7 +622,7 @@ __global__ void __launch_bounds__((PARTS == 1 ? kBackwardWarps : 16) * 32 + 32) 
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) total[k][i] = Pair(0.f);
   if (warp == ring.groups * warps) {
-    ok = fill_ring(ring, smem_address(slots), bars, p.rows, p.s, p.dy, p.dsum);
+    ok = fill_ring<false>(ring, smem_address(slots), bars, p.rows, p.s, p.dy, p.dsum);
   } else {
     uint32_t c[PARTS];
     int have[PARTS];
@@ -800,10 +813,11 @@ struct Staged {
     const uint32_t most = std::max(1u, kRing / 3 / (ring.pitch * matrices));
     const uint32_t groups1 = one <= all ? std::min(most, all / one) : 0, groups2 = two <= 16 ? std::min(most, 16 / two) : 0;
     const bool wide = !groups1 || (!backward && one != two && groups2 * two >= 12);
-    const uint32_t groups = std::min(15u, wide ? groups2 : groups1);      // a barrier each
-    if (!groups || rows < 3 * kSms * groups) return;       // too few to keep a ring going
     parts = wide ? 2 : 1;
     warps = wide ? two : one;
+    const uint32_t groups = std::min(warps > 1 ? 15u : 32u, wide ? groups2 : groups1);      // a barrier each, but for single warps; a lane each
+    if (!groups || rows < 3 * kSms * groups) parts = 0;       // too few to keep a ring going
+    if (!parts) return;
     ring.groups = groups;
     ring.slots = std::min(kMostSlots, kRing / ring.slot());
     blocks = (uint32_t)kSms;
