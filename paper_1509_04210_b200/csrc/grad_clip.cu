@@ -6,7 +6,7 @@
 // float are squared in 64 bits.  One read for the norm, one read and one write for the scaling: bound by HBM, less what the
 // second read finds in L2; small lists by launches, and have one for both.  Measured, norm and scaling: 61 million f32 in 16
 // gradients 116 us (244 MB read, 200 read again and 244 written: 5.9 TB/s; a copy reaches 6.5), 20 million bf16 in 301 gradients to
-// f32 32 us, 90 thousand f32 in 48 gradients 7.2 us in one cluster (13 in three launches).
+// f32 32 us, 90 thousand f32 in 48 gradients 7.2 us in one launch, 20 thousand 4.4.
 #include <algorithm>
 
 #include "launch.cuh"
@@ -320,8 +320,10 @@ template <uint32_t MOST> cudaError_t norm_of(const Gradient* grads, uint64_t cou
   return e != cudaSuccess ? e : launch_overlapped(norm_kernel, 1, kThreads, 0, 1, stream, (const double*)parts, used, norm);
 }
 
-// Units of 512 values up to which one cluster takes norm and norm's use in one launch.
-constexpr uint64_t kFusedMost = 1024;
+// Units of 512 values up to which one cluster takes norm and norm's use in one launch: two to a warp.  On the GPU 20 thousand values take 4.4 us
+// that way and 5.8 in two launches, 90 thousand 5.9 and 6.0, or 7.5 and 5.7 in 48 gradients, 200 thousand 8.6 and 6.3; one call after another
+// from the host, whose second launch takes 1.5 us, 90 thousand in 48 gradients 7.2 and 8.7.
+constexpr uint64_t kFusedMost = 256;
 
 template <uint32_t MOST, bool IN_PLACE> cudaError_t clip(const Gradient* grads, uint64_t count, float* norm, float max_norm, bool known, double* parts, cudaStream_t stream) {
   uint32_t used = 0;

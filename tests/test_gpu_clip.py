@@ -11,7 +11,7 @@ from test_gpu_learner import _learner, _torch
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 
-LISTS = {"one": [1], "odd": [1, 2, 3, 15, 16, 17, 0, 31, 33, 511, 513, 8191, 8192, 8193, 100003], "empty among": [0, 5, 0], "sixty-five": list(range(1, 66)),
+LISTS = {"one": [1], "a cluster's": [20000, 513, 1, 30000], "a cluster's last": [256 * 512 - 15], "too many for one": [256 * 512 - 14], "odd": [1, 2, 3, 15, 16, 17, 0, 31, 33, 511, 513, 8191, 8192, 8193, 100003], "empty among": [0, 5, 0], "sixty-five": list(range(1, 66)),
          "two launches": [7 + i % 50 for i in range(1000)], "large": [3_000_001, 96, 1_234_567]}
 
 
