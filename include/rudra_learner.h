@@ -201,7 +201,8 @@ int rudra_fp8_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, c
 /*
  * Root-mean-square norm with the residual's addition, a row (token) at a time:
  *     s = x + residual, rounded to dtype;   y = s * weight / sqrt(mean(s^2) + eps)
- * computed from the rounded s in 32 bits (rows whose squares add up to 2^128 or more are out of range).  x, residual,
+ * computed from the rounded s in 32 bits (rows whose squares add up to 2^128 or more are out of range; squares below 2^-126 are
+ * lost, which shows where eps is that small).  x, residual,
  * sum and y are tokens x channels of one dtype; weight holds `channels` values.  residual_dev NULL: s = x, and sum_dev is
  * NULL; otherwise sum_dev receives s, and may be x's or the residual's memory in the same layout.  y leaves as any of
  * y_dev (dtype; may be x's memory in the same layout where sum_dev is not), FP8 (blocks along the rows) and ACT8 (the
@@ -249,7 +250,7 @@ int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint6
                     uint64_t workspace_bytes, void* cuda_stream);
 
 /* Waits for cuda_stream and reports asynchronous CUDA errors, and kernels of this header that gave up, as
- * RUDRA_E_CUDA.  The kernels of the two products wait on barriers inside a block or cluster; a wait
+ * RUDRA_E_CUDA.  The kernels of the products, and of the norm of many rows, wait on barriers inside a block or cluster; a wait
  * that lasts about two seconds (which no working GPU needs) ends, and its kernel with it: what such a call
  * wrote is not to be used.  The kernels count this per device, not per stream: one that gave up, on whichever stream, is
  * reported to every stream of the device that is asked about afterwards, and once told not again, so each learner on a
