@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <cstdint>
+#include <memory>
 #include <vector>
 
 #include <ATen/core/Tensor.h>
@@ -599,8 +600,10 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// A list of gradients, or of where they go: any shape, values one after another.
+// A list of gradients, or of where they go: any shape, values one after another.  It holds the tensors until the launches are made:
+// those of a generator have no other owner.
 struct Gradients {
+  std::unique_ptr<Held> list;
   std::vector<const void*> p;
   std::vector<int> dtypes;
   std::vector<uint64_t> sizes;
@@ -608,9 +611,9 @@ struct Gradients {
 };
 Gradients gradients(const char* what, PyObject* o) {
   Gradients g;
-  const Held fast(PySequence_Fast(o, "a list of tensors is wanted"));
-  const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.get());
-  PyObject** items = PySequence_Fast_ITEMS(fast.get());
+  g.list = std::make_unique<Held>(PySequence_Fast(o, "a list of tensors is wanted"));
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(g.list->get());
+  PyObject** items = PySequence_Fast_ITEMS(g.list->get());
   if (n == 0) refuse("%s: an empty list", what);
   g.p.resize(n);
   g.dtypes.resize(n);

@@ -142,3 +142,24 @@ def test_shapes_orders_and_refusals():
     two = torch.zeros(200, device="cuda")
     L.clip_gradients([pool, pool], 1e-3, out=[two[:100], two[100:]])       # the same gradient twice, read only
     assert torch.equal(two[:100], two[100:]) and abs(two.double().norm().item() - 1e-3) < 1e-8
+
+
+def test_a_generators_tensors_live_until_the_launch():
+    torch, L = _torch(), _learner()
+
+    class Last(torch.Tensor):
+        def __del__(self):
+            self.plain.fill_(float("nan"))      # on the stream: before the launch it would be the norm's
+
+    def last(g):
+        plain = g.float()
+        t = plain.as_subclass(Last)
+        t.plain = plain
+        return t
+    grads, held = _grads([700, 3, 40000], ["bf16"], 0)
+    n, _ = ref.clip(held, 1.0)
+    assert abs(L.grad_norm(last(g) for g in grads).item() - n) <= 6 * U * n
+    out = [torch.empty(g.numel(), device="cuda") for g in grads]
+    most = float(np.float32(n / 3))
+    assert abs(L.clip_gradients((last(g) for g in grads), most, out=(o for o in out)).item() - n) <= 6 * U * n
+    _check(out, held, ref.clip(held, most)[1], "f32")
