@@ -242,7 +242,7 @@ int rudra_grad_norm(const void* const* grads_dev, const int* dtypes, const uint6
  * rudra_ps_push takes, in its dtype.  norm_known != 0: norm = *norm_dev (of the shards of several ranks together, say);
  * otherwise it is that of rudra_grad_norm, computed here and left in *norm_dev, and workspace_dev its workspace.
  * outs_dev[i] may be grads_dev[i] with the same dtype; no two outputs, no output and another gradient, nor the norm and an
- * output may overlap, which is refused.  Where all are scaled in their place and norm <= max_norm nothing is written.  A norm that is
+ * output (or, where it is computed, a gradient) may overlap, which is refused.  Where all are scaled in their place and norm <= max_norm nothing is written.  A norm that is
  * NaN makes every value NaN, an infinite one the finite values zero and the others NaN, unless max_norm is infinite
  * too.  max_norm >= 0. */
 int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint64_t* sizes, uint64_t count, float* norm_dev,

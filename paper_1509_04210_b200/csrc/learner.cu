@@ -67,8 +67,8 @@ int gradients(const void* const* grads, const int* dtypes, const uint64_t* sizes
 }
 
 // Whether what is written overlaps: an output another output, the norm or another gradient, or its own gradient other than in its
-// place.
-bool overlapping(const std::vector<Gradient>& list, const float* norm) {
+// place; the norm, where it is `computed`, a gradient.
+bool overlapping(const std::vector<Gradient>& list, const float* norm, bool computed) {
   struct Span {
     uintptr_t from, to;
     bool operator<(const Span& o) const { return from < o.from; }
@@ -94,12 +94,13 @@ bool overlapping(const std::vector<Gradient>& list, const float* norm) {
     const auto at = std::upper_bound(written.begin(), written.end(), Span{p, 0});
     return (at != written.end() && at->from < end) || (at != written.begin() && (at - 1)->to > p);
   };
+  const uintptr_t n = reinterpret_cast<uintptr_t>(norm), n_end = reinterpret_cast<uintptr_t>(norm + 1);
   for (const Gradient& g : list) {
     if (!g.size || (g.p == g.out && g.type == g.out_type)) continue;
-    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p);
-    if (meets(p, p + g.size * (g.type == rudra::kBF16 ? 2 : 4))) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(g.p), end = p + g.size * (g.type == rudra::kBF16 ? 2 : 4);
+    if (meets(p, end) || (computed && p < n_end && n < end)) return true;
   }
-  return meets(reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm + 1));
+  return meets(n, n_end);
 }
 
 int done(cudaError_t e, const char* what) { return e == cudaSuccess ? 0 : cuda_fail(e, what); }
@@ -392,7 +393,7 @@ int rudra_grad_clip(const void* const* grads_dev, const int* dtypes, const uint6
     const uint64_t need = norm_known ? 0 : rudra_grad_norm_workspace(count);
     if (need && (!aligned(workspace_dev) || workspace_bytes < need))
       return fail(RUDRA_E_INVAL, "workspace is null, not 32-byte aligned or smaller than %llu bytes", (unsigned long long)need);
-    if (overlapping(list, norm_dev)) return fail(RUDRA_E_INVAL, "outputs overlap each other, other gradients or the norm");
+    if (overlapping(list, norm_dev, norm_known == 0)) return fail(RUDRA_E_INVAL, "outputs overlap each other, other gradients or the norm, or it a gradient");
     return done(rudra::launch_grad_clip(list.data(), list.size(), norm_dev, max_norm, norm_known != 0, workspace_dev, stream_of(cuda_stream)),
                 "gradient clipping kernel launch");
   });

@@ -874,8 +874,6 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
     if (st.parts == 1) return lie == kBy32s ? run_staged<G, W, kBy32s, 1>(p, rows, st, stream) : run_staged<G, W, kBy16s, 1>(p, rows, st, stream);
     if (st.parts == 2) return lie == kBy32s ? run_staged<G, W, kBy32s, 2>(p, rows, st, stream) : run_staged<G, W, kBy16s, 2>(p, rows, st, stream);
   }
-  // Blocks of 256 threads, three to an SM, while a row fits one; 32 values to a thread where a block could not hold a row otherwise, and from
-  // some length on where it lies anyhow (bf16 7001 columns 55 us, and 65 with 16; 4111 columns 45 and 44).
   // Blocks of 256 threads, three to an SM, while a row fits one, and more warps where rows lie anyhow and their values are asked for one by
   // one (4000 x 4111 bf16 34.6 us with 27 warps to an SM, 44 with 18); 32 values to a thread where a block could not hold a row otherwise.
   const bool spread = lie == kSpread;

@@ -142,6 +142,8 @@ def test_clipping_refusals():
                         ([(P, 0, 10), (P, 0, 10)], [(P, 0), (P, 0)]), ([(P, 0, 10), (P + 36, 0, 10)], [(P, 0), (P + 36, 0)]), ([(P, 0, 10), (P + 60, 1, 10)], [(Q, 0), (P + 20, 1)])):
         _refused(clip(grads, outs), "overlap")
     _refused(clip([(Q, 0, 4096)], [(P - 64, 0)]), "overlap")      # the norm is at P
+    _refused(clip([(P - 36, 0, 10)], [(Q, 0)]), "overlap")        # in a gradient's last value, and in its first
+    _refused(clip([(Q, 0, 10), (P, 1, 10)], [(2 * Q, 0), (3 * Q, 1)]), "overlap")
 
 
 def test_tensors_that_are_refused_without_a_gpu():
