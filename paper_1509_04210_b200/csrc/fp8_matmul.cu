@@ -15,7 +15,7 @@
 // the way into shared memory.
 //
 // Measured: one token through 4096 x 9216 9.1 us (37.7 MB of weights at 4.1 TB/s; 2 us of it before the first and 1 joining; a kernel that
-// multiplies on the ordinary cores as the weights pass took 13), 256 x 4096 x 4096 8.2 us, 128 x 1000 x 4096 5.7 us, 512 x 512 x 512
+// multiplies on the ordinary cores as the weights pass took 13), 256 x 4096 x 4096 8.1 us, 128 x 1000 x 4096 5.3 us, 512 x 512 x 512
 // 2.9 us.  A stage of 64 columns brings 24 KB to an SM in 0.16 us, 83 bytes a cycle, which is what an SM takes in.
 #include <algorithm>
 #include <type_traits>
@@ -221,23 +221,23 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
 }
 
 // How long a product takes, in ns, by its shape.  Measured (warm, one after another, weights out of HBM): a stage of 16, 32, 64 and
-// 128 columns 140, 145, 170 and 210 ns, what comes after a tile's last stage 100 to 1000, joining the parts of a tile 1100 to 2600,
-// 2000 for setting up, again for every round of blocks; a pair's stage 300 (360 on all SMs), 1000 a tile and 2700 once.  For instance
-// 256 x 4096 x 4096: 64 columns 8.2 us, 128 columns 9.7 and split in two 10.9, pairs 13.7; 128 x 1000 x 4096: 64 columns 6.9 us and in
-// four parts 5.5, 128 columns in eight parts 6.4; 1000 x 4096 x 4096: pairs 15.3 us, 128 columns 19.6; 4096 x 4096 x 9216: pairs 112
-// us, 128 columns 134, 64 columns 190.
+// 128 columns 140, 145, 170 and 210 ns, what comes after a tile's last stage 100 to 1000, joining the parts of a tile 1100 to 4350 by its
+// rows, 2000 for setting up, again for every round of blocks; a pair's stage 300 (360 on all SMs), 1000 a tile and 2700 once.  For instance
+// 256 x 4096 x 4096: 64 columns 8.1 us, 128 columns 9.7 and split in two 10.5, pairs 13.7; 128 x 4096 x 4096: 64 columns 7.9 us, in two parts
+// 9.0, 128 columns in four parts 8.8; 65 x 4096 x 4096: that 7.4; 512 x 300 x 8192: 64 columns 11.7 us and in four parts 7.0, 128 columns in
+// eight parts 7.8; 1000 x 4096 x 4096: pairs 14.7 us, 128 columns 19.6; 4096 x 4096 x 9216: pairs 109 us, 128 columns 134, 64 columns 190.
 struct Timed {
   uint32_t split;
   uint64_t time;
 };
 Timed best_split(const Device::Facts& f, int columns, uint64_t m, uint64_t n, uint64_t stages) {
   const int i = columns == 16 ? 0 : columns == 32 ? 1 : columns == 64 ? 2 : 3;
-  constexpr uint64_t kStageTime[4] = {140, 145, 170, 210}, kAfter[4] = {100, 200, 500, 1000}, kJoin[4] = {1100, 1400, 2300, 2600};
+  constexpr uint64_t kStageTime[4] = {140, 145, 170, 210}, kAfter[4] = {100, 200, 500, 1000}, kJoin[4] = {1100, 1400, 1000, 1150}, kJoinRow[4] = {0, 0, 30, 25};
   const uint64_t tiles = ((n + 127) / 128) * ((m + columns - 1) / columns), waves = (tiles + f.sms - 1) / f.sms;
   Timed best = {1, waves * (2000 + stages * kStageTime[i] + kAfter[i])};
   for (uint32_t k = 1; k < 4; ++k) {
     const uint32_t split = 1u << k;
-    const uint64_t time = 2000 + (stages + split - 1) / split * kStageTime[i] + kAfter[i] + kJoin[i];
+    const uint64_t time = 2000 + (stages + split - 1) / split * kStageTime[i] + kAfter[i] + kJoin[i] + std::min<uint64_t>(m, columns) * kJoinRow[i];
     if (split <= stages && tiles <= (uint64_t)f.clusters[k] && time < best.time) best = {split, time};
   }
   return best;

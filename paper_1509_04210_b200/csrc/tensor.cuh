@@ -225,7 +225,7 @@ __device__ __forceinline__ void join_parts(uint32_t part, uint32_t split, uint32
       if (lane + 2 < lanes) s.z += (float)to[2];
       if (lane + 3 < lanes) s.w += (float)to[3];
     }
-    if (whole && lane + 3 < lanes) {      // four at once: 128x4096x4096 in 8 bits 9.1 -> 8.7 us
+    if (whole && lane + 3 < lanes) {      // four at once: 128x1000x4096 in 8 bits 5.5 -> 5.3 us
       if constexpr (sizeof(G) == 4) {
         *reinterpret_cast<float4*>(to) = s;
       } else {
