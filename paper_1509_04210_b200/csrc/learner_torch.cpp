@@ -609,7 +609,8 @@ struct Gradients {
   std::vector<uint64_t> sizes;
   int device = -1;
 };
-Gradients gradients(const char* what, PyObject* o) {
+// written: what a tensor shares with lazy copies of it becomes its own first.
+Gradients gradients(const char* what, PyObject* o, bool written) {
   Gradients g;
   g.list = std::make_unique<Held>(PySequence_Fast(o, "a list of tensors is wanted"));
   const Py_ssize_t n = PySequence_Fast_GET_SIZE(g.list->get());
@@ -630,7 +631,7 @@ Gradients gradients(const char* what, PyObject* o) {
     const int device = (int)impl.device().index();
     if (g.device >= 0) same_device(g.device, device);
     g.device = device;
-    g.p[i] = impl.data();
+    g.p[i] = written ? t.mutable_data_ptr() : t.const_data_ptr();
     g.dtypes[i] = dtype;
     g.sizes[i] = (uint64_t)impl.numel();
   }
@@ -652,7 +653,7 @@ Output scalar(const char* what, PyObject* given, int device) {
 PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gradients, out
   return returning([&]() -> PyObject* {
     count(n, 2);
-    const Gradients g = gradients("gradients", a[0]);
+    const Gradients g = gradients("gradients", a[0], false);
     const Output norm = scalar("out", a[1], g.device);
     Held held(norm.object);
     const On on(g.device);
@@ -666,10 +667,10 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gradient
 PyObject* clip_gradients(PyObject*, PyObject* const* a, Py_ssize_t n) {   // gradients, max_norm, out, norm -> norm
   return returning([&]() -> PyObject* {
     count(n, 4);
-    const Gradients g = gradients("gradients", a[0]);
     const float most = real(a[1]);
     const bool in_place = a[2] == Py_None;
-    const Gradients to = in_place ? Gradients() : gradients("out", a[2]);
+    const Gradients to = in_place ? Gradients() : gradients("out", a[2], true);      // first: what is read may be one of them
+    const Gradients g = gradients("gradients", a[0], in_place);
     if (!in_place && (to.sizes != g.sizes || to.device != g.device)) refuse("out: as many tensors as gradients, each of its gradient's size and device, are wanted");
     const Output norm = scalar("norm", a[3], g.device);
     Held held(norm.object);
