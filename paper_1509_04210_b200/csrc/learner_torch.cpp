@@ -51,7 +51,7 @@ struct Blocks {
   PyObject_HEAD
   at::Tensor* codes;    // or the buffer
   at::Tensor* scales;   // or null
-  void *codes_at, *scales_at;
+  void *codes_at, *scales_at;      // as placed() left them
   int64_t rows, cols;
   int device;
 };
@@ -78,20 +78,43 @@ void check_size(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0 || rows > RUDRA_MAX_DIM || cols > RUDRA_MAX_DIM) refuse("a matrix of %lld x %lld", (long long)rows, (long long)cols);
 }
 
+// Whether the caller's codes and scales do for a matrix of this size.
+void check_given(Kind k, const at::Tensor& codes, const at::Tensor& scales, int64_t rows, int64_t cols) {
+  const at::Tensor* both[2] = {&codes, &scales};
+  const int64_t need[2] = {codes_bytes(k, rows, cols), scales_bytes(k, rows, cols)};
+  for (int i = 0; i < 2; ++i)
+    if (!both[i]->is_cuda() || both[i]->element_size() != 1 || !both[i]->is_contiguous() || both[i]->numel() < need[i])
+      refuse("%s of a %lld x %lld %s: %lld contiguous bytes on the GPU are wanted", i ? "scales" : "codes", (long long)rows, (long long)cols, kNames[k], (long long)need[i]);
+  if (codes.get_device() != scales.get_device()) refuse("codes and scales on different devices");
+}
+
+// Codes and scales where they lie now: a tensor may have been given other memory since the last call.  written: what they share
+// with lazy copies becomes their own first.
+Blocks* placed(Kind k, Blocks* b, bool written) {
+  const auto at = [&](const at::Tensor& t) { return written ? t.mutable_data_ptr() : const_cast<void*>(t.const_data_ptr()); };
+  if (b->scales) {
+    check_given(k, *b->codes, *b->scales, b->rows, b->cols);
+    if (b->codes->get_device() != b->device) refuse("%s: its codes are on another device now", kNames[k]);
+    b->codes_at = at(*b->codes);
+    b->scales_at = at(*b->scales);
+  } else {
+    b->codes_at = at(*b->codes);
+    b->scales_at = static_cast<char*>(b->codes_at) + codes_room(k, b->rows, b->cols);
+  }
+  return b;
+}
+
 Blocks* new_blocks(Kind k, int64_t rows, int64_t cols, int device) {
   check_size(rows, cols);
-  const int64_t split = codes_room(k, rows, cols);
-  at::Tensor buffer = bytes(split + scales_bytes(k, rows, cols), device);
+  at::Tensor buffer = bytes(codes_room(k, rows, cols) + scales_bytes(k, rows, cols), device);
   Blocks* b = reinterpret_cast<Blocks*>(g_types[k]->tp_alloc(g_types[k], 0));
   if (!b) throw Raised();
-  b->codes_at = buffer.data_ptr();
-  b->scales_at = static_cast<char*>(b->codes_at) + split;
   b->codes = new at::Tensor(std::move(buffer));
   b->scales = nullptr;
   b->rows = rows;
   b->cols = cols;
   b->device = device;
-  return b;
+  return placed(k, b, true);
 }
 
 template <typename F> PyObject* returning(F&& body) {
@@ -118,18 +141,11 @@ PyObject* blocks_new(PyTypeObject* type, PyObject* args, PyObject* kwargs) {
     const Kind k = kind_of(type);
     check_size(rows, cols);
     const at::Tensor &codes = tensor("codes", c), &scales = tensor("scales", s);
-    const at::Tensor* both[2] = {&codes, &scales};
-    const int64_t need[2] = {codes_bytes(k, rows, cols), scales_bytes(k, rows, cols)};
-    for (int i = 0; i < 2; ++i)
-      if (!both[i]->is_cuda() || both[i]->element_size() != 1 || !both[i]->is_contiguous() || both[i]->numel() < need[i])
-        refuse("%s of a %lld x %lld %s: %lld contiguous bytes on the GPU are wanted", i ? "scales" : "codes", rows, cols, kNames[k], (long long)need[i]);
-    if (codes.get_device() != scales.get_device()) refuse("codes and scales on different devices");
+    check_given(k, codes, scales, rows, cols);
     Blocks* b = reinterpret_cast<Blocks*>(type->tp_alloc(type, 0));
     if (!b) return nullptr;
     b->codes = new at::Tensor(codes);
     b->scales = new at::Tensor(scales);
-    b->codes_at = codes.data_ptr();
-    b->scales_at = scales.data_ptr();
     b->rows = rows;
     b->cols = cols;
     b->device = (int)codes.get_device();
@@ -168,8 +184,13 @@ PyObject* blocks_scales(PyObject* o, void*) {
 PyObject* blocks_rows(PyObject* o, void*) { return PyLong_FromLongLong(reinterpret_cast<Blocks*>(o)->rows); }
 PyObject* blocks_cols(PyObject* o, void*) { return PyLong_FromLongLong(reinterpret_cast<Blocks*>(o)->cols); }
 PyObject* blocks_device(PyObject* o, void*) { return PyLong_FromLong(reinterpret_cast<Blocks*>(o)->device); }
-PyObject* blocks_codes_at(PyObject* o, void*) { return PyLong_FromVoidPtr(reinterpret_cast<Blocks*>(o)->codes_at); }
-PyObject* blocks_scales_at(PyObject* o, void*) { return PyLong_FromVoidPtr(reinterpret_cast<Blocks*>(o)->scales_at); }
+// For callers that write there (a pull).
+PyObject* blocks_codes_at(PyObject* o, void*) {
+  return returning([&]() -> PyObject* { return PyLong_FromVoidPtr(placed(kind_of(o), reinterpret_cast<Blocks*>(o), true)->codes_at); });
+}
+PyObject* blocks_scales_at(PyObject* o, void*) {
+  return returning([&]() -> PyObject* { return PyLong_FromVoidPtr(placed(kind_of(o), reinterpret_cast<Blocks*>(o), true)->scales_at); });
+}
 
 PyGetSetDef blocks_getset[] = {{"codes", blocks_codes, nullptr, "the codes, a tensor", nullptr},
                                {"scales", blocks_scales, nullptr, "the scale bytes, a tensor", nullptr},
@@ -249,12 +270,13 @@ Blocks* blocks(const char* what, Kind k, PyObject* given, int64_t rows, int64_t 
   Blocks* b = reinterpret_cast<Blocks*>(given);
   if (!PyObject_TypeCheck(given, g_types[k]) || b->rows != rows || b->cols != cols || b->device != device)
     refuse("%s: %s of %lld x %lld on the input's device is wanted", what, kNames[k], (long long)rows, (long long)cols);
+  placed(k, b, true);
   Py_INCREF(given);
   return b;
 }
 Blocks* wanted(const char* what, Kind k, PyObject* given) {
   if (!PyObject_TypeCheck(given, g_types[k])) refuse("%s: %s is wanted", what, kNames[k]);
-  return reinterpret_cast<Blocks*>(given);
+  return placed(k, reinterpret_cast<Blocks*>(given), false);
 }
 
 void same_device(int a, int b) {
@@ -354,7 +376,7 @@ PyObject* mx4_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {   // a, b, d
     count(n, 4);
     const Blocks* b = wanted("b", kMx4, a[1]);
     const bool coded = PyObject_TypeCheck(a[0], g_types[kMx4]);
-    const Blocks* left = coded ? reinterpret_cast<const Blocks*>(a[0]) : nullptr;
+    const Blocks* left = coded ? wanted("a", kMx4, a[0]) : nullptr;
     const Matrix x = coded ? Matrix{nullptr, 0, left->rows, left->cols, 0, left->device} : matrix("a", a[0]);
     if (x.cols != b->cols) refuse("a has rows of %lld values, b of %lld", (long long)x.cols, (long long)b->cols);
     same_device(x.device, b->device);
@@ -502,7 +524,7 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {   // a, b, d
     count(n, 4);
     const Blocks* b = wanted("b", kFp8, a[1]);
     const bool coded = PyObject_TypeCheck(a[0], g_types[kFp8]);
-    const Blocks* left = coded ? reinterpret_cast<const Blocks*>(a[0]) : nullptr;
+    const Blocks* left = coded ? wanted("a", kFp8, a[0]) : nullptr;
     const Matrix x = coded ? Matrix{nullptr, 0, left->rows, left->cols, 0, left->device} : matrix("a", a[0]);
     if (x.cols != b->cols) refuse("a has rows of %lld values, b of %lld", (long long)x.cols, (long long)b->cols);
     same_device(x.device, b->device);

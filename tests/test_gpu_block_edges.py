@@ -31,3 +31,34 @@ def test_a_lazy_copy_becomes_a_tensors_own_before_its_gradient_is_scaled():
     L.clip_gradients([x, z], 1.0, out=[x, y])
     norm = np.sqrt(2500.0)
     assert (np.abs(_np(x) - 3 / norm) <= 8 * U * 3 / norm).all() and (np.abs(_np(y) - 4 / norm) <= 8 * U * 4 / norm).all() and (z == 4).all()
+
+
+@pytest.mark.parametrize("kind", ["FP8", "MX4", "Act8"])
+def test_codes_and_scales_are_taken_where_they_lie_at_the_call(kind):
+    torch, L = _torch(), _learner()
+    rows, cols = 37, 300
+    make, back = {"FP8": (L.fp8_quantize, L.fp8_dequantize), "MX4": (L.mx4_quantize, L.mx4_dequantize)}.get(kind, (lambda x, out=None: L.act8_save(x, out=out), L.act8_values))
+    x = torch.randn(rows, cols, device="cuda")
+    new = make(x)
+    want = back(new, torch.float32)
+    # a lazy copy made after the matrix was: written, its tensors become its own
+    codes, scales = torch.zeros(new.codes.numel() + 9, dtype=torch.uint8, device="cuda"), torch.zeros(new.scales.numel() + 9, dtype=torch.uint8, device="cuda")
+    q = getattr(L, kind)(codes, scales, rows, cols)
+    kept = codes._lazy_clone(), scales._lazy_clone()
+    assert make(x, out=q) is q and torch.equal(back(q, torch.float32), want)
+    assert all((k == 0).all() for k in kept) and q.codes_ptr == codes.data_ptr() and q.scales_ptr == scales.data_ptr()
+    # and read, they are what torch has written since
+    view = new.codes
+    kept = view._lazy_clone()
+    view.zero_()
+    assert (back(new, torch.float32) == 0).all() and (kept != 0).any()
+    del kept
+    make(x, out=new)
+    assert torch.equal(back(new, torch.float32), want)
+    # other memory, too little of it
+    codes.set_(torch.zeros(new.codes.numel(), dtype=torch.uint8, device="cuda"))
+    assert (back(q, torch.float32) == 0).all()
+    codes.set_(torch.zeros(new.codes.numel() - 1, dtype=torch.uint8, device="cuda"))
+    for call in (lambda: back(q), lambda: make(x, out=q), lambda: q.codes_ptr):
+        with pytest.raises(ValueError, match="contiguous bytes"):
+            call()
