@@ -231,6 +231,8 @@ template <Lie LIE> __device__ __forceinline__ uint32_t column_of(uint32_t t, uin
 template <Lie LIE, int PARTS, typename G, typename W, typename F>
 __device__ __forceinline__ void norm_row(const Forward<G, W>& p, const Piece<G, LIE> (&s)[PARTS], F&& weight, uint64_t row, const uint32_t (&c)[PARTS], const int (&have)[PARTS],
                                          uint32_t warps, uint32_t group, uint32_t parity, Room<float>& room, uint8_t* bytes) {
+  // f32 results are the very values that the 8-bit forms are made of; of bf16 ones two products in 32 bits leave nothing to see
+  constexpr bool kExact = sizeof(G) == 4;
   Pair part(0.f);
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) {
@@ -246,7 +248,7 @@ __device__ __forceinline__ void norm_row(const Forward<G, W>& p, const Piece<G, 
       Piece<G, LIE> out;
       const Pair r(root.value());
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) out.set(i, s[k].pair(i) * r * w.pair(i));
+      for (int i = 0; i < kPairs; ++i) out.set(i, kExact ? root.scaled(s[k].pair(i), w.pair(i)) : s[k].pair(i) * r * w.pair(i));
       out.store(p.y + row * p.ldy + c[k], have[k]);
     }
     if (p.codes || p.kept) {

@@ -62,3 +62,20 @@ def test_codes_and_scales_are_taken_where_they_lie_at_the_call(kind):
     for call in (lambda: back(q), lambda: make(x, out=q), lambda: q.codes_ptr):
         with pytest.raises(ValueError, match="contiguous bytes"):
             call()
+
+
+@pytest.mark.parametrize("t,c,shift", [(4096, 4096, 0), (4096, 4097, 1), (1024, 16384, 0), (8000, 130, 4)])
+def test_the_8_bit_forms_of_f32_rows_are_those_of_the_written_ones(t, c, shift):
+    torch, L = _torch(), _learner()
+    gen = torch.Generator("cuda").manual_seed(c)
+    x = torch.randn(t * c + shift, device="cuda", generator=gen)[shift:].view(t, c)
+    w = torch.rand(c, device="cuda", generator=gen) + 0.5
+    # one call writes both; y and FP8 together through the C interface, which alone takes both
+    y, kept = L.rms_norm(x, w, keep=True)
+    assert torch.equal(kept.codes, L.act8_save(y).codes)
+    from paper_1509_04210_b200 import binding as rb
+    q, z = L.fp8_quantize(y), torch.empty_like(y)
+    mine = L.FP8(torch.zeros_like(q.codes), torch.zeros_like(q.scales), t, c)
+    assert rb.lib().rudra_rms_norm(x.data_ptr(), c, None, 0, 0, t, c, w.data_ptr(), 0, 1e-6, None, 0, z.data_ptr(), c, mine.codes_ptr, mine.scales_ptr, None, None,
+                                   torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(z, y) and torch.equal(mine.codes, q.codes) and torch.equal(L.fp8_dequantize(mine, torch.float32), L.fp8_dequantize(q, torch.float32))
