@@ -184,8 +184,8 @@ int64_t rudra_ps_pull_fp8_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint6
 /* y[m][n] = sum over k of a[m][k] * b[n][k], a (m x k) and b (n x k) in FP8: products exact, sums in 32 bits, one rounding to
  * y's dtype.  With a transposed quantization of both factors it is a layer's weight gradient.  The tensor core cuts a sum off
  * where it adds to it, every 32 values; f32 results are gathered, with rounding, every 64 blocks or so: rows of 9 216 to 2^20 normal
- * values came out within 6e-7 of their sums' 2-norm, positive ones 5e-6 too little at most; bf16 results keep one sum (2^20 positive
- * values: 1.6e-4 too little).  The order of a sum depends on m, n, k and the device alone. */
+ * values came out within 6e-7 of their sums' 2-norm, positive ones 5e-6 too little at most; bf16 results are gathered every
+ * 512 blocks: positive values add up to at most 2e-4 too little however long the rows, a twentieth of what the rounding to bf16 takes off.  The order of a sum depends on m, n, k and the device alone. */
 int rudra_fp8_matmul(const void* a_codes_dev, const void* a_scales_dev, uint64_t m, const void* b_codes_dev,
                      const void* b_scales_dev, uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy,
                      void* cuda_stream);

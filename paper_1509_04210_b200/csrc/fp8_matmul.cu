@@ -56,6 +56,7 @@ struct Params {
   uint32_t lane_tiles;
   uint32_t split;                 // blocks of a cluster that share a tile
   uint32_t add;                   // to what y holds
+  uint32_t each;                  // GATHER: blocks that a sum in the accumulator has
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -69,8 +70,9 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
                :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add), "r"(elected) : "memory");
 }
 
-// X: type of x where it is brought to FP8 here, else void.
-template <typename G, int COLS, typename X>
+// X: type of x where it is brought to FP8 here, else void.  GATHER: a long sum's parts of p.each blocks leave the accumulator one after
+// another and are added in registers.
+template <typename G, int COLS, typename X, bool GATHER>
 __global__ void __launch_bounds__(Shape<COLS, !std::is_void<X>::value>::kThreads)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map, const __grid_constant__ Params p,
                   const __grid_constant__ Rows<typename std::conditional<std::is_void<X>::value, float, X>::type> x) {
@@ -81,8 +83,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   const uint32_t stage0 = smem_address(smem);
   float* part = reinterpret_cast<float*>(smem);      // [column][lane], once the stages are done with
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
-  const uint32_t full = smem_address(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * S::kStages + 1);
+  const uint32_t full = smem_address(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, drained = done + 8;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(bars + 2 * S::kStages + 2);
 
   const uint32_t warp = warp_index(), lane = threadIdx.x % 32;
   const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
@@ -98,6 +100,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
       barrier_init(empty + 8 * s, 1);
     }
     barrier_init(done, 1);
+    if (GATHER) barrier_init(drained, 4);      // the warps that take results
     barrier_init_fence();
   }
   if (warp == 1) tmem_alloc(smem_address(slot), S::kTmem);
@@ -108,6 +111,30 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   bool ok = true;
   admit_next_kernel();
   await_previous_kernel();
+
+  const uint32_t group = warp % 4;                       // the lanes of tensor memory a warp may read
+  const bool takes = warp >= 2 && warp < 6;
+  float sum[GATHER ? COLS : 1] = {};
+  uint32_t taken = 0;                                    // parts of the sum
+  // The next part of the sum, as soon as it is there; the accumulator is then free for the one after it.
+  const auto take = [&]() -> bool {
+    if (!barrier_wait(done, taken & 1)) return false;
+    tmem_fence_after();
+#pragma unroll
+    for (int c = 0; c < (GATHER ? COLS : 0); c += 16) {
+      if (m0 + c >= p.m) continue;
+      uint32_t r[16];
+      tmem_load16(tmem + (group * 32 << 16) + c, r);
+      tmem_load_wait();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sum[c + j] += __uint_as_float(r[j]);
+    }
+    ++taken;
+    tmem_fence_before();
+    __syncwarp();
+    if (lane == 0) barrier_arrive(drained);
+    return true;
+  };
 
   if (warp == 0) {
     const uint32_t elected = elect();
@@ -128,8 +155,15 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
     await_copies(full, issued, S::kStages);
   } else if (warp == 1) {
     const uint32_t elected = elect();
-    uint32_t s = 0, parity = 0, set = 0;
+    uint32_t s = 0, parity = 0, set = 0, part_end = first + p.each, parts = 0;
     for (uint32_t i = first; i < last; ++i) {
+      bool begin = i == first;
+      if (GATHER && i == part_end) {
+        tensor_commit(done, elected);
+        if (!(ok = barrier_wait(drained, parts++ & 1))) break;
+        part_end += p.each;
+        begin = true;
+      }
       if (!(ok = barrier_wait(full + 8 * s, parity))) break;
       tmem_fence_after();
       const uint32_t at = stage0 + s * S::kStage, ts = tmem + COLS + set * S::kScaleColumns;
@@ -143,7 +177,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
       }
 #pragma unroll
       for (uint32_t h = 0; h < 4; ++h)   // 32 values
-        multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, mine, i != first || h, elected);
+        multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, mine, !begin || h, elected);
       if (kQuantize || i % 4 == 3) set = set + 1 == S::kSets ? 0 : set + 1;
       tensor_commit(empty + 8 * s, elected);
       if (++s == S::kStages) s = 0, parity ^= 1;
@@ -154,6 +188,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
     using T = typename std::conditional<kQuantize, X, float>::type;
     for (uint32_t i = first + (warp - 2); i < last; i += S::kQuantizers) {
       const uint32_t c = i - first, s = c % S::kStages;
+      // a part of the sum has all its stages of this warp
+      if (GATHER && takes && c / p.each > taken && !(ok = take())) break;
       uint8_t* stage = smem + s * S::kStage + S::kLanes;
       bool free = c < S::kStages;
 #pragma unroll 1
@@ -187,24 +223,34 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   }
   __syncwarp();
 
-  const uint32_t group = warp % 4;                       // the lanes of tensor memory a warp may read
   const uint32_t n = n0 + group * 32 + lane;
-  if (warp >= 2 && warp < 6) {
-    if (!barrier_wait(done, 0)) ok = false;
-    tmem_fence_after();
+  if (takes) {
+    if constexpr (GATHER) {
+      const uint32_t parts = (last - first + p.each - 1) / p.each;
+      while (ok && taken < parts) ok = take();
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) {
+        if (m0 + c >= p.m) continue;
+        if (p.split > 1) part[c * 128 + group * 32 + lane] = sum[c];
+        else if (n < p.n) put(static_cast<G*>(p.y) + (uint64_t)(m0 + c) * p.ldy + n, sum[c]);
+      }
+    } else {
+      if (!barrier_wait(done, 0)) ok = false;
+      tmem_fence_after();
 #pragma unroll 1
-    for (uint32_t c = 0; c < COLS && m0 + c < p.m; c += 16) {
-      uint32_t r[16];
-      tmem_load16(tmem + (group * 32 << 16) + c, r);
-      tmem_load_wait();
-      if (p.split > 1) {
+      for (uint32_t c = 0; c < COLS && m0 + c < p.m; c += 16) {
+        uint32_t r[16];
+        tmem_load16(tmem + (group * 32 << 16) + c, r);
+        tmem_load_wait();
+        if (p.split > 1) {
 #pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128 + group * 32 + lane] = __uint_as_float(r[j]);
-      } else if (n < p.n) {
-        G* y = static_cast<G*>(p.y) + (uint64_t)(m0 + c) * p.ldy + n;
+          for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128 + group * 32 + lane] = __uint_as_float(r[j]);
+        } else if (n < p.n) {
+          G* y = static_cast<G*>(p.y) + (uint64_t)(m0 + c) * p.ldy + n;
 #pragma unroll
-        for (uint32_t j = 0; j < 16; ++j, y += p.ldy)
-          if (m0 + c + j < p.m) put(y, __uint_as_float(r[j]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
+          for (uint32_t j = 0; j < 16; ++j, y += p.ldy)
+            if (m0 + c + j < p.m) put(y, __uint_as_float(r[j]) + (sizeof(G) == 4 && p.add ? (float)*y : 0.f));
+        }
       }
     }
   }
@@ -252,13 +298,19 @@ struct Blocks {
   uint32_t begin, count;
 };
 
+// Blocks that an accumulator's sum has at most where results are bf16; longer ones are gathered in registers.  The tensor core cuts a sum off
+// where it adds to it: of 2^24 positive values in a cluster of eight 6e-3 were lost, in parts of 512 blocks under 2e-4 are, a twentieth
+// of what the rounding to bf16 takes off.
+constexpr uint32_t kOneSum = 512;
+static_assert(kOneSum % 8 == 0, "every quantizing warp has a stage in a whole part");
+
 template <typename G, int COLS, typename X>
 cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOut& y, Blocks part, cudaStream_t stream) {
   using S = Shape<COLS, !std::is_void<X>::value>;
   using T = typename std::conditional<std::is_void<X>::value, float, X>::type;
   static Device device;
   const Device::Facts* facts;
-  cudaError_t e = device.prepare(fp8_matmul_kernel<G, COLS, X>, S::kThreads, S::kSmem, 0, &facts);
+  cudaError_t e = device.prepare(fp8_matmul_kernel<G, COLS, X, false>, S::kThreads, S::kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   Params p = {};
   const uint64_t nb = (b.cols + kFp8Block - 1) / kFp8Block;
@@ -281,8 +333,19 @@ cudaError_t launch(const Fp8& a, const MatrixIn* x, const Fp8& b, const MatrixOu
   e = encode_rows(&lane_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b.codes, nb * kFp8Block, b.rows, nb * kFp8Block, 128);
   if (e == cudaSuccess && !x) e = encode_rows(&column_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.codes, nb * kFp8Block, a.rows, nb * kFp8Block, COLS);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(fp8_matmul_kernel<G, COLS, X>, (uint32_t)(tiles * p.split), S::kThreads, S::kSmem, p.split, stream, lane_map, column_map, p,
-                           x ? Rows<T>::of(x->p, x->rows, x->cols, x->ld, 0) : Rows<T>::of(nullptr, 0, 0, 0, 0));
+  const auto run = [&](auto* kernel) {
+    return launch_overlapped(kernel, (uint32_t)(tiles * p.split), S::kThreads, S::kSmem, p.split, stream, lane_map, column_map, p,
+                             x ? Rows<T>::of(x->p, x->rows, x->cols, x->ld, 0) : Rows<T>::of(nullptr, 0, 0, 0, 0));
+  };
+  if constexpr (sizeof(G) == 2) {
+    if ((p.stages + p.split - 1) / p.split > kOneSum) {
+      p.each = kOneSum;
+      static Device gathering;
+      e = gathering.prepare(fp8_matmul_kernel<G, COLS, X, true>, S::kThreads, S::kSmem, 0, &facts);
+      return e != cudaSuccess ? e : run(fp8_matmul_kernel<G, COLS, X, true>);
+    }
+  }
+  return run(fp8_matmul_kernel<G, COLS, X, false>);
 }
 
 // The shape that is done soonest.  Sixteen or 32 columns only where they take all rows: scale bytes come in atoms of 128 rows, of
@@ -293,10 +356,10 @@ template <typename G> cudaError_t by_time(const Fp8& a, const Fp8& b, const Matr
   if (m <= 32) return launch<G, 32, void>(a, nullptr, b, y, part, stream);
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(fp8_matmul_kernel<G, 64, void>, Shape<64, false>::kThreads, Shape<64, false>::kSmem, 0, &facts);
+  const cudaError_t e = device.prepare(fp8_matmul_kernel<G, 64, void, false>, Shape<64, false>::kThreads, Shape<64, false>::kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t narrow = best_split(*facts, 64, m, n, stages).time, wide = best_split(*facts, 128, m, n, stages).time;
-  if (pair_time(*facts, m, n, stages) < std::min(narrow, wide)) return launch_fp8_matmul_pair(a, b, y, part.begin, part.count, stream);
+  if (pair_time(*facts, m, n, stages) < std::min(narrow, wide)) return launch_fp8_matmul_pair(a, b, y, part.begin, part.count, kOneSum, stream);
   return narrow <= wide ? launch<G, 64, void>(a, nullptr, b, y, part, stream) : launch<G, 128, void>(a, nullptr, b, y, part, stream);
 }
 

@@ -44,6 +44,7 @@ struct Params {
   uint32_t begin, stages;        // 128-value blocks along a row: the first, a multiple of four, and how many
   uint32_t kt;                   // scale atoms, of four of them
   uint32_t lane_tiles, tiles;
+  uint32_t each;                 // GATHER: blocks that a sum in the accumulator has, a multiple of four
 };
 
 __device__ uint32_t g_gave_up;   // counts up
@@ -57,8 +58,9 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
                :: "r"(d), "l"(a), "l"(b), "r"(what), "r"(sa), "r"(sb), "r"(add), "r"(elected) : "memory");
 }
 
-// ADD: to what y holds.
-template <typename G, bool ADD>
+// ADD: to what y holds.  GATHER: a long sum's parts of p.each blocks leave the accumulator one after another and are added in
+// registers.
+template <typename G, bool ADD, bool GATHER>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap column_map,
                 const __grid_constant__ CUtensorMap lane_scales, const __grid_constant__ CUtensorMap column_scales,
@@ -126,7 +128,16 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
       for (uint32_t tile = tile0; ok && tile < p.tiles; tile += tile_step, ++q) {
         if (!(ok = barrier_wait(drained, (q & 1) ^ 1))) break;
         tmem_fence_after();
+        uint32_t part_end = p.each;
         for (uint32_t i = 0; i < stages; ++i) {
+          bool begin = i == 0;
+          if (GATHER && i == part_end) {
+            tensor_commit_pair(ready, elected);
+            ++q;
+            if (!(ok = barrier_wait(drained, (q & 1) ^ 1))) break;
+            part_end += p.each;
+            begin = true;
+          }
           if (!(ok = barrier_wait(full + 8 * s, parity))) break;
           tmem_fence_after();
           const uint32_t at = stage0 + s * kStage, ts = tmem + kTile + set * kScaleColumns;
@@ -140,7 +151,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
           // descriptors count in units of 16 bytes
 #pragma unroll
           for (uint32_t h = 0; h < 4; ++h)   // 32 values
-            multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, tc, i || h, elected);
+            multiply(tmem, lanes + h * 2, columns + h * 2, what, tl, tc, !begin || h, elected);
           if (i % 4 == 3 || i + 1 == stages) set = set + 1 == kScaleSets ? 0 : set + 1;
           tensor_commit_pair(empty + 8 * s, elected);
           if (++s == kStages) s = 0, parity ^= 1;
@@ -155,15 +166,41 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
     for (uint32_t tile = tile0; tile < p.tiles; tile += tile_step, ++q) {
       const uint32_t n = tile % p.lane_tiles * kTile + rank * kRows + group * 32 + lane, m = tile / p.lane_tiles * kTile + half;
       const uint32_t have = m < p.m ? min(128u, p.m - m) : 0;
-      if (!(ok = barrier_wait(ready, q & 1))) break;
-      tmem_fence_after();
       uint32_t r[8][16];
+      if constexpr (GATHER) {
+        float sum[8][16] = {};
+        const uint32_t parts = (stages + p.each - 1) / p.each;
+        for (uint32_t part = 0; part < parts; ++part) {
+          if (part) ++q;
+          if (!(ok = barrier_wait(ready, q & 1))) break;
+          tmem_fence_after();
 #pragma unroll
-      for (uint32_t c = 0; c < 8; ++c) tmem_load16(tmem + (group * 32 << 16) + half + 16 * c, r[c]);
-      tmem_load_wait();
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) barrier_arrive_cluster(first_drained);
+          for (uint32_t c = 0; c < 8; ++c) {
+            uint32_t more[16];
+            tmem_load16(tmem + (group * 32 << 16) + half + 16 * c, more);
+            tmem_load_wait();
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(more[j]);
+          }
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) barrier_arrive_cluster(first_drained);
+        }
+        if (!ok) break;
+#pragma unroll
+        for (uint32_t c = 0; c < 8; ++c)
+#pragma unroll
+          for (uint32_t j = 0; j < 16; ++j) r[c][j] = __float_as_uint(sum[c][j]);
+      } else {
+        if (!(ok = barrier_wait(ready, q & 1))) break;
+        tmem_fence_after();
+#pragma unroll
+        for (uint32_t c = 0; c < 8; ++c) tmem_load16(tmem + (group * 32 << 16) + half + 16 * c, r[c]);
+        tmem_load_wait();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) barrier_arrive_cluster(first_drained);
+      }
       if (n < p.n) {
         G* y = static_cast<G*>(p.y) + (uint64_t)m * p.ldy + n;
         const auto value = [](uint32_t bits, const G* to) { return ADD ? __uint_as_float(bits) + (float)*to : __uint_as_float(bits); };
@@ -190,10 +227,11 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_const
   }
 }
 
-template <typename G, bool ADD> cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
+template <typename G, bool ADD, bool GATHER>
+cudaError_t launch(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, uint32_t each, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  cudaError_t e = device.prepare(fp8_pair_kernel<G, ADD>, kThreads, kSmem, 0, &facts);
+  cudaError_t e = device.prepare(fp8_pair_kernel<G, ADD, GATHER>, kThreads, kSmem, 0, &facts);
   if (e != cudaSuccess) return e;
   const uint64_t nb = (a.cols + kFp8Block - 1) / kFp8Block, kt = (nb + 3) / 4, lane_tiles = (b.rows + kTile - 1) / kTile;
   const uint64_t tiles = lane_tiles * ((a.rows + kTile - 1) / kTile);
@@ -206,16 +244,19 @@ template <typename G, bool ADD> cudaError_t launch(const Fp8& a, const Fp8& b, c
   if (e == cudaSuccess) e = encode_plain(&lane_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, b.scales, 128, b_atoms, 512, 128, 1);
   if (e == cudaSuccess) e = encode_plain(&column_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, a.scales, 128, a_atoms, 512, 128, 1);
   if (e != cudaSuccess) return e;
-  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, begin, count, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles};
+  const Params p = {y.p, y.ld, (uint32_t)y.rows, (uint32_t)y.cols, begin, count, (uint32_t)kt, (uint32_t)lane_tiles, (uint32_t)tiles, each};
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)facts->sms / 2);
-  return launch_overlapped(fp8_pair_kernel<G, ADD>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
+  return launch_overlapped(fp8_pair_kernel<G, ADD, GATHER>, 2 * pairs, kThreads, kSmem, 2, stream, lane_map, column_map, lane_scales, column_scales, p);
 }
 
 }  // namespace
 
-cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream) {
-  if (y.type == kBF16) return begin ? cudaErrorInvalidValue : launch<__nv_bfloat16, false>(a, b, y, 0, count, stream);
-  return begin ? launch<float, true>(a, b, y, begin, count, stream) : launch<float, false>(a, b, y, 0, count, stream);
+cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, uint32_t one_sum, cudaStream_t stream) {
+  if (y.type == kBF16) {
+    if (begin) return cudaErrorInvalidValue;
+    return count > one_sum ? launch<__nv_bfloat16, false, true>(a, b, y, 0, count, one_sum, stream) : launch<__nv_bfloat16, false, false>(a, b, y, 0, count, 0, stream);
+  }
+  return begin ? launch<float, true, false>(a, b, y, begin, count, 0, stream) : launch<float, false, false>(a, b, y, 0, count, 0, stream);
 }
 
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }

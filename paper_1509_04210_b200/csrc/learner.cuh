@@ -59,8 +59,9 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
 cudaError_t launch_fp8_quantize(const MatrixIn& src, bool transpose, bool square, void* codes, void* scales, cudaStream_t stream);
 cudaError_t launch_fp8_dequantize(const Fp8& src, const MatrixOut& dst, cudaStream_t stream);
 cudaError_t launch_fp8_matmul(const Fp8& a, const Fp8& b, const MatrixOut& y, cudaStream_t stream);
-// Of launch_fp8_matmul: many tiles; `count` blocks of 128 values from block `begin` on, added to y unless that is the first.
-cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, cudaStream_t stream);
+// Of launch_fp8_matmul: many tiles; `count` blocks of 128 values from block `begin` on, added to y unless that is the first.  bf16 results
+// have all blocks, in sums of `one_sum` (a multiple of four) that are gathered.
+cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& y, uint32_t begin, uint32_t count, uint32_t one_sum, cudaStream_t stream);
 uint64_t fp8_linear_workspace(uint64_t m, uint64_t k);
 cudaError_t launch_fp8_linear(const MatrixIn& x, const Fp8& b, const MatrixOut& y, void* workspace, cudaStream_t stream);
 

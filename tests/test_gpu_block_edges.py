@@ -79,3 +79,50 @@ def test_the_8_bit_forms_of_f32_rows_are_those_of_the_written_ones(t, c, shift):
     assert rb.lib().rudra_rms_norm(x.data_ptr(), c, None, 0, 0, t, c, w.data_ptr(), 0, 1e-6, None, 0, z.data_ptr(), c, mine.codes_ptr, mine.scales_ptr, None, None,
                                    torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(z, y) and torch.equal(mine.codes, q.codes) and torch.equal(L.fp8_dequantize(mine, torch.float32), L.fp8_dequantize(q, torch.float32))
+
+
+def _product_of_positive(torch, L, m, n, k, seed):
+    """(factors in FP8, the bf16-sized values of the first, their products' sums in 64 bits); rows spread over a factor of two."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    made = []
+    for rows in (m, n):
+        v = torch.empty(rows, k, dtype=torch.bfloat16, device="cuda").uniform_(0.5, 1.5, generator=gen)
+        v *= (torch.rand(rows, 1, device="cuda", generator=gen) + 1.0).bfloat16()
+        made.append(v)
+    qa, qb = (L.fp8_quantize(v) for v in made)
+    want = torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    step = 1 << 19
+    for at in range(0, k, step):          # blocks of 128 do not straddle the cuts
+        a, b = (L.fp8_dequantize(L.fp8_quantize(v[:, at:at + step]), torch.float32).double() for v in made)
+        want += a @ b.t()
+    return qa, qb, made[0], want
+
+
+#: every shape of a tile, its sum split over a cluster and not, and tiles one after another; parts of 512 blocks, the last of any length
+LONG_SUMS = [(1, 200, 600_077), (3, 20_000, 70_000), (16, 130, 560_000), (20, 100, 700_001), (30, 19_000, 66_000), (40, 100, 700_001), (40, 20_000, 70_000), (100, 200, 650_000),
+             (100, 20_000, 131_073), (128, 19_000, 66_000), (1500, 1600, 70_000), (300, 520, 200_001), (5000, 4000, 66_049)]
+
+
+@pytest.mark.parametrize("m,n,k", LONG_SUMS)
+def test_long_sums_of_bf16_results(m, n, k):
+    """A sum in the accumulator has 512 blocks at most, each of four additions that cut it off by up to 2^-23 of itself, on average half way
+    up: 512 * 2^-22; parts are added with a rounding each, and the result is rounded to bf16."""
+    torch, L = _torch(), _learner()
+    qa, qb, x, want = _product_of_positive(torch, L, m, n, k, k)
+    bound = 512 * 2.0 ** -22 + (k / 65536 + 9) * U + 2.0 ** -8
+    for a in (qa, x, x.float()) if m <= 16 else (qa,):
+        y = L.fp8_matmul(a, qb)
+        assert y.dtype == torch.bfloat16 and ((y.double() - want).abs() <= bound * want).all()
+        assert torch.equal(y, L.fp8_matmul(a, qb))
+    L.sync()
+
+
+@pytest.mark.parametrize("m,n", [(5, 5), (20, 20), (40, 50), (100, 20)])
+def test_sums_of_sixteen_million_positive_values_are_right_to_bf16(m, n):
+    # in one sum they came out up to 6e-3 too little
+    torch, L = _torch(), _learner()
+    qa, qb, x, want = _product_of_positive(torch, L, m, n, 1 << 24, 7)
+    for a in (qa, x) if m <= 16 else (qa,):
+        off = (L.fp8_matmul(a, qb).double() - want) / want
+        assert off.abs().max().item() <= 512 * 2.0 ** -22 + 300 * U + 2.0 ** -8
+    L.sync()
