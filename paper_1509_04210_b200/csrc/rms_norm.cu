@@ -14,15 +14,14 @@
 #include "fp8.cuh"
 #include "launch.cuh"
 #include "learner.cuh"
+#include "norm_rows.h"
 #include "pairs.cuh"
 #include "tensor.cuh"
 
 namespace rudra {
 namespace {
 
-constexpr uint32_t kMostThreads = 512;
-constexpr uint32_t kMostSums = 2 * kMostThreads * kValues;    // floats of shared memory for the groups' sums
-constexpr uint64_t kMostHeld = 2 * kMostThreads * kValues;   // columns of a row that a block holds in registers: 32 to a thread
+static_assert(kPiece == kValues && kMultiprocessors == kSms, "rows are given to threads and blocks by these");
 
 // Sum over the threads of a block in a fixed order; every thread gets it.  `room`: 32 floats.
 __device__ __forceinline__ float block_sum(float v, float* room) {
@@ -299,18 +298,7 @@ __global__ void __launch_bounds__(PARTS == 2 ? 512 : LIE == kSpread ? 1024 : 768
 // groups never wait for memory.  (8192 x 4096 bf16 to FP8 41 us = 5.7 TB/s; 50 with loads by the groups themselves, which take
 // turns with their arithmetic.)
 
-constexpr uint32_t kMostCluster = 8;      // blocks that add their parts of the weight's gradient themselves
-constexpr uint32_t kRing = 216 * 1024, kMostSlots = 8;
-// Warps that work, and one that copies: forward with 32 values to a thread, backward with 16.
-constexpr uint32_t kForwardWarps = 16, kBackwardWarps = 24;
-
 __device__ uint32_t g_gave_up;   // counts up
-
-// How rows lie in the ring; host and device.
-struct Ring {
-  uint32_t matrices, row, pitch, groups, slots;      // bytes of a row, and of its place in a slot
-  __host__ __device__ uint32_t slot() const { return groups * matrices * pitch; }
-};
 
 // The copying warp: slot by slot a row of each matrix for every group.  LANES: by a lane for each group (16384 x 512 without residual 7.7 us, and
 // 8.8 by one lane); else by one for all, with addresses that are the same to the warp (8192 x 4096 to FP8 41.0 us, and 42.3 in a
@@ -783,51 +771,6 @@ template <typename D, Lie LIE> __global__ void __launch_bounds__(256) norm_join_
   }
 }
 
-// How rows that are held in registers are given to blocks: as many to a block as fill it, and as many blocks as run at once.
-// `held`: threads that an SM holds of the kernel.
-struct Split {
-  uint32_t parts, warps, threads, blocks;
-  // most: threads of a block of several rows; held: threads of the kernel that an SM holds; spread: blocks that few rows are given to
-  Split(uint64_t rows, uint64_t padded, uint32_t parts_, uint32_t most, uint32_t held, uint64_t spread) : parts(parts_) {
-    const uint64_t per_warp = 32 * kValues * parts;
-    warps = (uint32_t)((padded + per_warp - 1) / per_warp);
-    // rows that would not fill the SMs otherwise get a block each, or a few to a block
-    const uint32_t groups = (uint32_t)std::min<uint64_t>(std::max(1u, most / 32 / warps), (rows + spread - 1) / spread);
-    threads = groups * warps * 32;
-    blocks = (uint32_t)std::min<uint64_t>((rows + groups - 1) / groups, kSms * std::max(1u, held / threads));
-  }
-  uint32_t length() const { return warps * 32 * kValues * parts; }     // of a part of the weight's gradient
-};
-
-// How many rows of bf16 go through rings, if they do: as many groups as leave three slots, and forward 32 values to a thread where
-// that still makes twelve warps (backward a thread's sums for the weight take the registers for that).  (f32 rows stay with loads
-// by the groups: a warp's 64-byte pieces of shared memory meet in its banks, 8192 x 4096 backward 113 us and 90.)
-struct Staged {
-  Ring ring = {};
-  uint32_t parts = 0, warps = 0, blocks = 0;      // parts 0: not this way
-  Staged(uint64_t rows, uint64_t cols, uint32_t element, uint32_t matrices, uint64_t padded, bool backward) {
-    if (element != 2 || cols * element % 16) return;
-    ring.matrices = matrices;
-    ring.row = (uint32_t)(cols * element);
-    ring.pitch = (ring.row + 127) / 128 * 128;
-    if (ring.pitch * (uint64_t)matrices > kRing / 2) return;
-    const uint32_t all = backward ? kBackwardWarps : kForwardWarps, one = (uint32_t)((padded + 511) / 512), two = (uint32_t)((padded + 1023) / 1024);
-    const uint32_t most = std::max(1u, kRing / 3 / (ring.pitch * matrices));
-    const uint32_t groups1 = one <= all ? std::min(most, all / one) : 0, groups2 = two <= 16 ? std::min(most, 16 / two) : 0;
-    const bool wide = !groups1 || (!backward && one != two && groups2 * two >= 12);
-    parts = wide ? 2 : 1;
-    warps = wide ? two : one;
-    const uint32_t groups = std::min(warps > 1 ? 15u : 32u, wide ? groups2 : groups1);      // a barrier each, but for single warps; a lane each
-    if (!groups || rows < 3 * kSms * groups) parts = 0;       // too few to keep a ring going
-    if (!parts) return;
-    ring.groups = groups;
-    ring.slots = std::min(kMostSlots, kRing / ring.slot());
-    blocks = (uint32_t)kSms;
-  }
-  uint32_t threads() const { return ring.groups * warps * 32 + 32; }
-  uint32_t length() const { return warps * 32 * kValues * parts; }
-};
-
 template <typename G, typename W, Lie LIE, int PARTS> cudaError_t run_staged(const Forward<G, W>& p, uint64_t rows, const Staged& a, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
@@ -876,11 +819,8 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
     if (st.parts == 1) return lie == kBy32s ? run_staged<G, W, kBy32s, 1>(p, rows, st, stream) : run_staged<G, W, kBy16s, 1>(p, rows, st, stream);
     if (st.parts == 2) return lie == kBy32s ? run_staged<G, W, kBy32s, 2>(p, rows, st, stream) : run_staged<G, W, kBy16s, 2>(p, rows, st, stream);
   }
-  // Blocks of 256 threads, three to an SM, while a row fits one, and more warps where rows lie anyhow and their values are asked for one by
-  // one (4000 x 4111 bf16 34.6 us with 27 warps to an SM, 44 with 18); 32 values to a thread where a block could not hold a row otherwise.
-  const bool spread = lie == kSpread;
-  const int parts = padded > (spread ? 1024 : 768) * kValues ? 2 : 1;
-  const Split a(rows, padded, parts, parts == 1 && !spread ? padded > 256 * kValues ? 768 : 256 : 512, parts == 2 ? 512 : spread ? 1024 : 768, kSms);
+  const Split a = forward_split(rows, padded, lie == kSpread);
+  const uint32_t parts = a.parts;
   const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
                                  : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 2> : norm_kernel<G, W, kSpread, 2>;
   return launch_overlapped(kernel, a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
@@ -891,14 +831,6 @@ constexpr uint64_t kMostShares = 296;
 uint64_t shares_for(uint64_t rows, uint64_t cols) {
   const uint64_t strips = (cols + 31) / 32;
   return std::max<uint64_t>(1, std::min(kMostShares / std::min(strips, kMostShares), (rows + 7) / 8));
-}
-
-// The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.  Few rows are a
-// cluster's.
-Split backward_split(uint64_t rows, uint64_t cols) {
-  const uint32_t parts = cols > kMostThreads * kValues ? 2 : 1;
-  const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
-  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kSms);
 }
 
 template <typename G, typename W, Lie LIE, int PARTS>

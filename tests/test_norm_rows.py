@@ -1,0 +1,71 @@
+"""How the norm's kernels give rows to blocks: the rules themselves, on the host, no GPU needed."""
+import os
+import subprocess
+
+import pytest
+
+from test_gpu_norm_rings import RINGS
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1509_04210_b200", "csrc")
+
+# backward, matrices, rows, columns -> parts, warps, groups, slots, bytes of a slot, threads
+PROGRAM = r"""
+#include <cinttypes>
+#include <cstdio>
+#include "norm_rows.h"
+
+int main() {
+  int back;
+  unsigned matrices;
+  uint64_t rows, cols, padded;
+  while (std::scanf("%d %u %" SCNu64 " %" SCNu64 " %" SCNu64, &back, &matrices, &rows, &cols, &padded) == 5) {
+    const rudra::Staged s(rows, cols, 2, matrices, padded, back != 0);
+    if (!s.parts) std::printf("0 0 0 0 0 0\n");
+    else std::printf("%u %u %u %u %u %u\n", s.parts, s.warps, s.ring.groups, s.ring.slots, s.ring.slot(), s.threads());
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rings(tmp_path_factory):
+    """Of (backward, matrices, rows, columns, padded columns): (parts, warps, groups, slots, bytes of a slot, threads)."""
+    at = tmp_path_factory.mktemp("rows")
+    (at / "t.cpp").write_text(PROGRAM)
+    exe = str(at / "t")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-I", CSRC, "-isystem", os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"), str(at / "t.cpp"), "-o", exe])
+
+    def ask(queries):
+        out = subprocess.run([exe], input="\n".join(" ".join(map(str, map(int, q))) for q in queries), capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+
+    return ask
+
+
+WAYS = [(False, 1), (False, 2), (True, 2), (True, 3)]       # pass, and the matrices it reads
+
+
+def test_the_rings_that_are_run_on_the_gpu_are_all_that_there_are(rings):
+    for back, matrices in WAYS:
+        all_ = {s[:3] for s in rings([(back, matrices, 1 << 20, c, c) for c in range(8, 16_385, 8)])}
+        run = {s[:3] for s in rings([(back, matrices, t, c, c) for t, c in RINGS])}
+        assert all_ == run, (back, matrices, sorted(all_ ^ run))
+
+
+def test_rings_fit_their_block(rings):
+    for back, matrices in WAYS:
+        queries = [(back, matrices, t, c, p) for t in (444, 1_000, 10_656, 1 << 30) for c in range(8, 16_385, 8) for p in {c, -(-c // 128) * 128}]
+        for (_, _, t, c, padded), (parts, warps, groups, slots, slot, threads) in zip(queries, rings(queries)):
+            if not parts:
+                continue
+            assert parts * warps * 512 >= padded and groups * matrices * -(-2 * c // 128) * 128 == slot
+            assert 2 <= slots <= 8 and slots * slot <= 216 * 1024 and t >= 444 * groups
+            assert groups <= (15 if warps > 1 else 32) and threads == 32 * (groups * warps + 1)      # named barriers; a lane each
+            # what the kernels are built for: 16 warps that work with 32 values to a thread, backward 24 with 16
+            assert groups * warps <= (24 if back and parts == 1 else 16)
+            assert groups * matrices * 2 * c < 1 << 20                # bytes that a barrier counts
+
+
+def test_few_rows_and_rows_that_bulk_copies_do_not_read_go_without(rings):
+    assert all(s[0] == 0 for s in rings([(back, m, t, c, c) for back, m in WAYS for t, c in ((443, 16_384), (2_000, 500), (1 << 20, 12), (1 << 20, 4_111), (1 << 20, 4_100), (100, 4_096))]))
+    assert all(s[0] == 0 for s in rings([(False, 2, 1 << 20, 40_000, 40_000), (True, 3, 1 << 20, 20_000, 20_000)]))
