@@ -39,12 +39,18 @@ inline Split forward_split(uint64_t rows, uint64_t padded, bool anyhow) {
 }
 
 constexpr uint32_t kMostCluster = 8;      // blocks that add their parts of the weight's gradient themselves
+constexpr uint32_t kWideThreads = 640;    // of a block that holds two rows of nine or ten warps
 // The gradients of a row in registers: 32 values to a thread where a block could not hold the row otherwise.  Few rows are a
-// cluster's.
-inline Split backward_split(uint64_t rows, uint64_t cols) {
+// cluster's.  bf16 rows that lie anyhow (`halves`) are held up by their values one by one: where 16 warps hold one and 20 hold two, 20 are
+// faster for all that their threads have fewer registers (4000 x 4111 97 us with 16 and 75 with 20, 3289 x 4999 85 and 69; but 2348 x 7001 69 and 83,
+// 4696 x 3501 67 and 79; f32 4000 x 4111 75 and 73, 3651 x 4503 73 and 75).
+inline Split backward_split(uint64_t rows, uint64_t cols, bool halves) {
   const uint32_t parts = cols > kMostThreads * kPiece ? 2 : 1;
   const Split few(rows, cols, parts, kMostThreads, kMostThreads, 1);
-  return few.blocks <= kMostCluster ? few : Split(rows, cols, parts, kMostThreads, kMostThreads, kMultiprocessors);
+  if (few.blocks <= kMostCluster) return few;
+  const bool wide = halves && parts == 1 && kMostThreads / 32 / few.warps == 1 && kWideThreads / 32 / few.warps == 2;
+  const uint32_t most = wide ? kWideThreads : kMostThreads;
+  return Split(rows, cols, parts, most, most, kMultiprocessors);
 }
 
 constexpr uint32_t kRing = 216 * 1024, kMostSlots = 8;

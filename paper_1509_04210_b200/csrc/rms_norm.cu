@@ -495,8 +495,8 @@ __device__ __forceinline__ void put_part(float* parts, const float* sums, const 
 // block's groups walk over the rows and add up what the rows give for the weight; at the end the groups' sums are added in order
 // in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
 // are one cluster, which adds the parts itself.
-template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
-__global__ void __launch_bounds__(kMostThreads) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
+template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER, uint32_t THREADS>
+__global__ void __launch_bounds__(THREADS) norm_backward_kernel(const __grid_constant__ Backward<G, W> p, uint32_t warps, float* parts, void* dw, GradType dw_type) {
   constexpr bool kAhead = sizeof(G) == 2 && PARTS == 1 && LIE != kSpread;      // where registers do for two rows
   __shared__ Room<Pair> room;
   extern __shared__ float sums[];
@@ -843,17 +843,19 @@ cudaError_t run_staged_backward(const Backward<G, W>& p, const Staged& a, float*
   return launch_overlapped(norm_backward_staged_kernel<G, W, LIE, PARTS>, a.blocks, a.threads(), smem, 1, stream, p, a.warps, parts, a.ring);
 }
 
-template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER>
+template <typename G, typename W, Lie LIE, int PARTS, bool CLUSTER, uint32_t THREADS = kMostThreads>
 cudaError_t run_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
   static Device device;
   const Device::Facts* facts;
-  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.threads, kMostSums * sizeof(float), 0, &facts);
+  const cudaError_t e = device.prepare(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER, THREADS>, a.threads, kMostSums * sizeof(float), 0, &facts);
   if (e != cudaSuccess) return e;
   const uint32_t groups = a.threads / 32 / a.warps, smem = CLUSTER || groups > 1 ? groups * a.length() * (uint32_t)sizeof(float) : 0;
-  return launch_overlapped(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
+  return launch_overlapped(norm_backward_kernel<G, W, LIE, PARTS, CLUSTER, THREADS>, a.blocks, a.threads, smem, CLUSTER ? a.blocks : 1, stream, p, a.warps, parts, n.dw, n.dw_type);
 }
 template <typename G, typename W, Lie LIE> cudaError_t pick_backward(const Backward<G, W>& p, const Split& a, float* parts, const NormBackward& n, cudaStream_t stream) {
   if (a.blocks <= kMostCluster) return a.parts == 2 ? run_backward<G, W, LIE, 2, true>(p, a, parts, n, stream) : run_backward<G, W, LIE, 1, true>(p, a, parts, n, stream);
+  if constexpr (sizeof(G) == 2 && LIE == kSpread)
+    if (a.threads > kMostThreads) return run_backward<G, W, LIE, 1, false, kWideThreads>(p, a, parts, n, stream);
   return a.parts == 2 ? run_backward<G, W, LIE, 2, false>(p, a, parts, n, stream) : run_backward<G, W, LIE, 1, false>(p, a, parts, n, stream);
 }
 
@@ -885,7 +887,7 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
     float* parts = static_cast<float*>(workspace);
     Lie lie = std::max(std::max(lie_of(n.dy.p, n.dy.ld, sizeof(G)), lie_of(n.s.p, n.s.ld, sizeof(G))), std::max(lie_of(n.ds.p, n.ds.ld, sizeof(G)), lie_of(n.weight, 0, 1)));
     if (n.dsum.p) lie = std::max(lie, lie_of(n.dsum.p, n.dsum.ld, sizeof(G)));
-    const Split a = backward_split(rows, cols);
+    const Split a = backward_split(rows, cols, sizeof(G) == 2 && lie == kSpread);
     if constexpr (sizeof(G) == 2) if (lie != kSpread) {
       const Staged st(rows, cols, sizeof(G), p.dsum.p ? 3 : 2, cols, true);
       if (st.parts) {
@@ -920,7 +922,7 @@ cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
 uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
   if (cols <= kMostHeld) {
     // enough however they lie: a part to an SM, of whole warps
-    return backward_split(rows, cols).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
+    return backward_split(rows, cols, false).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
   }
   return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
 }

@@ -126,3 +126,23 @@ def test_sums_of_sixteen_million_positive_values_are_right_to_bf16(m, n):
         off = (L.fp8_matmul(a, qb).double() - want) / want
         assert off.abs().max().item() <= 512 * 2.0 ** -22 + 300 * U + 2.0 ** -8
     L.sync()
+
+
+@pytest.mark.parametrize("t,c", [(297, 4111), (700, 4097), (1001, 5001), (350, 5120), (149, 4999)])
+@pytest.mark.parametrize("weight", ["f32", "bf16"])
+def test_backward_of_two_long_rows_that_lie_anyhow_to_a_block(t, c, weight):
+    # bounds as in test_gpu_norm.py
+    torch, L = _torch(), _learner()
+    gen = torch.Generator("cuda").manual_seed(c)
+    mk = lambda std: (torch.randn(t, c + 3, device="cuda", generator=gen) * std).bfloat16()[:, 1:c + 1]  # noqa: E731
+    s, dy, more = mk(1.0), mk(1e-3), mk(1e-3)
+    w = 1.0 + 0.2 * torch.randn(c, device="cuda", generator=gen)
+    w = w.bfloat16() if weight == "bf16" else w
+    for m in (None, more):
+        ds, dw = L.rms_norm_backward(dy, s, w, dsum=m)
+        want, want_w, size, size_w = ref.norm_backward(_np(dy), _np(s), _np(w), 1e-6, None if m is None else _np(m))
+        assert (np.abs(_np(ds) - want) <= (96 + c / 1024) * U * size + 2.0 ** -8 * np.abs(want)).all()
+        assert (np.abs(_np(dw) - want_w) <= (t + 64 + c / 8192) * U * size_w).all()
+        over = dy.clone() if m is None else m
+        again = L.rms_norm_backward(dy if m is not None else over, s, w, dsum=m, out=over)
+        assert torch.equal(again[0], ds) and torch.equal(again[1], dw)

@@ -8,7 +8,8 @@ from test_gpu_norm_rings import RINGS
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1509_04210_b200", "csrc")
 
-# backward, matrices, rows, columns -> parts, warps, groups, slots, bytes of a slot, threads
+# backward, matrices, rows, columns, padded columns -> parts, warps, groups, slots, bytes of a slot, threads; backward 2: of blocks that
+# load rows themselves, matrices != 0: bf16 rows that lie anyhow -> parts, warps, groups, blocks, floats of a part, threads
 PROGRAM = r"""
 #include <cinttypes>
 #include <cstdio>
@@ -19,6 +20,11 @@ int main() {
   unsigned matrices;
   uint64_t rows, cols, padded;
   while (std::scanf("%d %u %" SCNu64 " %" SCNu64 " %" SCNu64, &back, &matrices, &rows, &cols, &padded) == 5) {
+    if (back == 2) {
+      const rudra::Split s = rudra::backward_split(rows, cols, matrices != 0);
+      std::printf("%u %u %u %u %u %u\n", s.parts, s.warps, s.threads / 32 / s.warps, s.blocks, s.length(), s.threads);
+      continue;
+    }
     const rudra::Staged s(rows, cols, 2, matrices, padded, back != 0);
     if (!s.parts) std::printf("0 0 0 0 0 0\n");
     else std::printf("%u %u %u %u %u %u\n", s.parts, s.warps, s.ring.groups, s.ring.slots, s.ring.slot(), s.threads());
@@ -69,3 +75,16 @@ def test_rings_fit_their_block(rings):
 def test_few_rows_and_rows_that_bulk_copies_do_not_read_go_without(rings):
     assert all(s[0] == 0 for s in rings([(back, m, t, c, c) for back, m in WAYS for t, c in ((443, 16_384), (2_000, 500), (1 << 20, 12), (1 << 20, 4_111), (1 << 20, 4_100), (100, 4_096))]))
     assert all(s[0] == 0 for s in rings([(False, 2, 1 << 20, 40_000, 40_000), (True, 3, 1 << 20, 20_000, 20_000)]))
+
+
+def test_blocks_of_the_backward_pass(rings):
+    for halves in (0, 1):
+        queries = [(2, halves, t, c, 0) for t in (1, 7, 40, 149, 1_000, 4_000, 1 << 30) for c in list(range(1, 16_385, 13)) + [512, 4096, 4097, 5120, 5121, 8192, 8193, 16_384]]
+        for (_, _, t, c, _), (parts, warps, groups, blocks, part, threads) in zip(queries, rings(queries)):
+            assert parts * warps * 512 == part >= c and threads == groups * warps * 32
+            assert threads <= (640 if halves and parts == 1 and 4096 < c <= 5120 else 512)
+            # a part of the weight's gradient to every block, in a workspace that does not know how rows lie
+            assert blocks <= 148 and part <= -(-c // 1024) * 1024
+            assert groups <= (15 if warps > 1 else 32)
+    # bf16 rows of nine or ten warps that lie anyhow: two to a block, as 20 warps hold them
+    assert [s[2] for s in rings([(2, 1, 4_000, c, 0) for c in (4_111, 4_999, 5_120)] + [(2, 0, 4_000, 4_111, 0), (2, 1, 4_000, 4_001, 0), (2, 1, 4_000, 5_121, 0)])] == [2, 2, 2, 1, 2, 1]
