@@ -185,7 +185,8 @@ int64_t rudra_ps_pull_fp8_on(rudra_ps* ps, uint64_t offset, uint64_t rows, uint6
  * y's dtype.  With a transposed quantization of both factors it is a layer's weight gradient.  The tensor core cuts a sum off
  * where it adds to it, every 32 values; f32 results are gathered, with rounding, every 64 blocks or so: rows of 9 216 to 2^20 normal
  * values came out within 6e-7 of their sums' 2-norm, positive ones 5e-6 too little at most; bf16 results are gathered every
- * 512 blocks: positive values add up to at most 2e-4 too little however long the rows, a twentieth of what the rounding to bf16 takes off.  The order of a sum depends on m, n, k and the device alone. */
+ * 512 blocks: positive values add up to at most 2e-4 too little however long the rows, a twentieth of what the rounding to bf16 takes off.
+ * The order of a sum depends on m, n, k, y's dtype and the device alone. */
 int rudra_fp8_matmul(const void* a_codes_dev, const void* a_scales_dev, uint64_t m, const void* b_codes_dev,
                      const void* b_scales_dev, uint64_t n, uint64_t k, void* y_dev, int y_dtype, uint64_t ldy,
                      void* cuda_stream);
@@ -207,7 +208,8 @@ int rudra_fp8_linear(const void* x_dev, int x_dtype, uint64_t ldx, uint64_t m, c
  * NULL; otherwise sum_dev receives s, and may be x's or the residual's memory in the same layout.  y leaves as any of
  * y_dev (dtype; may be x's memory in the same layout where sum_dev is not), FP8 (blocks along the rows) and ACT8 (the
  * checkpoint that rudra_act8_weight_grad takes), the last two from y before it is rounded to dtype; what is NULL is not
- * wanted, but one is.  Outputs do not overlap each other.  eps >= 0.
+ * wanted, but one is.  Outputs do not overlap each other.  eps >= 0.  The order of a row's sum depends on tokens, channels, dtype, the
+ * outputs that are wanted, whether rows and weight all begin on 16-byte boundaries, and the device alone.
  */
 int rudra_rms_norm(const void* x_dev, uint64_t ldx, const void* residual_dev, uint64_t ldr, int dtype, uint64_t tokens,
                    uint64_t channels, const void* weight_dev, int weight_dtype, float eps, void* sum_dev, uint64_t ldsum,
@@ -219,7 +221,8 @@ int rudra_rms_norm(const void* x_dev, uint64_t ldx, const void* residual_dev, ui
  * ds is the gradient of x and of the residual alike; dsum (NULL: zero) is what comes down the residual stream.  dy, s, dsum
  * and ds are tokens x channels of one dtype; ds may be dy's or dsum's memory in the same layout.  dweight is of
  * dweight_dtype, wherever it lies in the vector that rudra_ps_push takes; its sums are in 32 bits, in an order that
- * depends on tokens, channels and the device alone.  workspace_dev:
+ * depends on tokens, channels, dtype, whether there is a dsum, whether rows and weight all begin on 16-byte boundaries, and the device
+ * alone; so do those of a row.  workspace_dev:
  * rudra_rms_norm_backward_workspace(tokens, channels) bytes on a 32-byte boundary. */
 uint64_t rudra_rms_norm_backward_workspace(uint64_t tokens, uint64_t channels);
 int rudra_rms_norm_backward(const void* dy_dev, uint64_t lddy, const void* s_dev, uint64_t lds, const void* dsum_dev,
@@ -230,7 +233,8 @@ int rudra_rms_norm_backward(const void* dy_dev, uint64_t lddy, const void* s_dev
 /*
  * The norm of `count` gradients together: the square root of the sum of all their squares, to *norm_dev (a float).  Gradient i
  * is sizes[i] consecutive values of dtypes[i]; the three lists are host memory, read before the call returns.  Squares of 16 values
- * are added in 32 bits, all beyond that, and squares a float does not hold, in 64; the order depends on the list alone.
+ * are added in 32 bits, all beyond that, and squares a float does not hold, in 64; the order depends on the list alone: its
+ * sizes, dtypes and how far past 32-byte boundaries the gradients begin.
  * workspace_dev: rudra_grad_norm_workspace(count) bytes on a 32-byte boundary.  A list has at most 2^24 gradients and
  * 2^43 values.
  */
@@ -240,7 +244,8 @@ int rudra_grad_norm(const void* const* grads_dev, const int* dtypes, const uint6
 
 /* outs[i] = grads[i] * (norm <= max_norm ? 1 : max_norm / norm): for instance into the layers' parts of the vector that
  * rudra_ps_push takes, in its dtype.  norm_known != 0: norm = *norm_dev (of the shards of several ranks together, say);
- * otherwise it is that of rudra_grad_norm, computed here and left in *norm_dev, and workspace_dev its workspace.
+ * otherwise it is computed here and left in *norm_dev, as rudra_grad_norm does it and with its workspace; the sums of a
+ * small list are added in another order, in 64 bits as well, so that the two floats may be one step apart.
  * outs_dev[i] may be grads_dev[i] with the same dtype; no two outputs, no output and another gradient, nor the norm and an
  * output (or, where it is computed, a gradient) may overlap, which is refused.  Where all are scaled in their place and norm <= max_norm nothing is written.  A norm that is
  * NaN makes every value NaN, an infinite one the finite values zero and the others NaN, unless max_norm is infinite

@@ -146,3 +146,63 @@ def test_backward_of_two_long_rows_that_lie_anyhow_to_a_block(t, c, weight):
         over = dy.clone() if m is None else m
         again = L.rms_norm_backward(dy if m is not None else over, s, w, dsum=m, out=over)
         assert torch.equal(again[0], ds) and torch.equal(again[1], dw)
+
+
+def _at(t, shift):
+    """A copy whose rows begin `shift` elements past a 32-byte boundary, all of them."""
+    torch = _torch()
+    per = 32 // t.element_size()
+    pitch = -(-(t.shape[-1] + shift) // per) * per
+    buf = torch.zeros(t.shape[:-1] + (pitch,), dtype=t.dtype, device="cuda")
+    view = buf[..., shift:shift + t.shape[-1]]
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("t,c", [(3, 4096), (300, 1000), (3_600, 1032), (1_400, 4096), (5, 20_000)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_norms_agree_bit_for_bit_where_sums_have_one_order(t, c, dtype):
+    """Memory, run and neighbours do not matter, nor whether rows begin on 32-byte boundaries or 16 bytes past them.  Where one begins
+    anyhow, sums may be added in another order, and are within the bounds of the other tests."""
+    torch, L = _torch(), _learner()
+    gen = torch.Generator("cuda").manual_seed(t)
+    s, dy, more = ((torch.randn(t, c, device="cuda", generator=gen)).to(getattr(torch, dtype)) for _ in range(3))
+    w = torch.rand(c, device="cuda", generator=gen) + 0.5
+    step = 16 // s.element_size()
+    for m in (None, more):
+        want = L.rms_norm_backward(dy, s, w, dsum=m)
+        for a, b, d, v in ((0, 0, 0, 0), (step, 0, 0, 0), (0, step, 0, 4), (step, step, step, 4)):
+            got = L.rms_norm_backward(_at(dy, a), _at(s, b), _at(w, v), dsum=None if m is None else _at(m, d))
+            assert all(torch.equal(x, y) for x, y in zip(got, want)), (a, b, d, v)
+        y = L.rms_norm(dy, w, m)
+        for a, d, v in ((0, 0, 4), (step, 0, 0), (step, step, 4)):
+            got = L.rms_norm(_at(dy, a), _at(w, v), None if m is None else _at(m, d))
+            assert all(torch.equal(x, z) for x, z in (zip(got, y) if m is not None else ((got, y),)))
+
+
+@pytest.mark.parametrize("sizes", [[700, 3, 40_000], [90, 5_000_001, 17], [5 + i % 40 for i in range(1100)]])
+def test_norms_of_a_list_agree(sizes):
+    torch, L = _torch(), _learner()
+    gen = torch.Generator("cuda").manual_seed(len(sizes))
+    grads = [torch.randn(n, device="cuda", generator=gen) for n in sizes]
+    norm = L.grad_norm(grads)
+    for shift in (0, 0, 8):            # of 32 bytes: nothing changes
+        assert torch.equal(L.grad_norm([_at(g, shift) for g in grads]), norm)
+    # clipping may add the same 64-bit sums in another order: one step of a float at most
+    mine = L.clip_gradients(grads, 1e-3, out=[torch.empty_like(g) for g in grads])
+    assert abs(mine.item() - norm.item()) <= 2.0 ** -23 * norm.item()
+    assert torch.equal(L.clip_gradients(grads, 1e-3, out=[torch.empty_like(g) for g in grads]), mine)
+    assert abs(L.grad_norm([_at(g, 3) for g in grads]).item() - norm.item()) <= 12 * U * norm.item()
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (5, 5000, 20_000), (40, 129, 513), (300, 1000, 14_000), (1500, 1600, 900)])
+@pytest.mark.parametrize("out", ["float32", "bfloat16"])
+def test_products_agree_bit_for_bit_wherever_their_operands_lie(m, n, k, out):
+    torch, L = _torch(), _learner()
+    gen = torch.Generator("cuda").manual_seed(k)
+    x, w = torch.randn(m, k, device="cuda", generator=gen), torch.randn(n, k, device="cuda", generator=gen)
+    dtype = getattr(torch, out)
+    want = L.fp8_matmul(L.fp8_quantize(x), L.fp8_quantize(w), dtype)
+    buf = torch.empty(m, n + 7, dtype=dtype, device="cuda")
+    assert torch.equal(L.fp8_matmul(x, L.fp8_quantize(w.clone()), dtype), want)
+    assert torch.equal(L.fp8_matmul(_at(x, 3), L.fp8_quantize(_at(w, 1)), out=buf[:, 3:n + 3]), want)
