@@ -34,7 +34,8 @@ struct Split {
 // Blocks of 256 threads, three to an SM, while a row fits one, and more warps where rows lie anyhow and their values are asked for one by
 // one (4000 x 4111 bf16 34.6 us with 27 warps to an SM, 44 with 18); 32 values to a thread where a block could not hold a row otherwise.
 inline Split forward_split(uint64_t rows, uint64_t padded, bool anyhow) {
-  const uint32_t parts = padded > (anyhow ? 1024 : 768) * kPiece ? 2 : 1;
+  static_assert(kMostHeld <= 1024 * kPiece, "a block holds rows that lie anyhow with 16 values to a thread");
+  const uint32_t parts = !anyhow && padded > 768 * kPiece ? 2 : 1;
   return Split(rows, padded, parts, parts == 1 && !anyhow ? padded > 256 * kPiece ? 768 : 256 : 512, parts == 2 ? 512 : anyhow ? 1024 : 768, kMultiprocessors);
 }
 

@@ -263,7 +263,8 @@ __device__ __forceinline__ void norm_row(const Forward<G, W>& p, const Piece<G, 
 // the rows.
 template <typename G, typename W, Lie LIE, int PARTS>
 __global__ void __launch_bounds__(PARTS == 2 ? 512 : LIE == kSpread ? 1024 : 768) norm_kernel(const __grid_constant__ Forward<G, W> p, uint32_t rows, uint32_t warps) {
-  __shared__ alignas(16) uint8_t bytes[LIE == kSpread ? (PARTS == 1 ? 32 : 16) : 1][512];
+  static_assert(LIE != kSpread || PARTS == 1, "rows that lie anyhow are held with 16 values to a thread");
+  __shared__ alignas(16) uint8_t bytes[LIE == kSpread ? 32 : 1][512];
   __shared__ Room<float> room;
   admit_next_kernel();
   const uint32_t warp = threadIdx.x / 32, group = warp / warps, groups = blockDim.x / 32 / warps, T = warps * 32, t = threadIdx.x - group * T;
@@ -491,6 +492,11 @@ __device__ __forceinline__ void put_part(float* parts, const float* sums, const 
   }
 }
 
+__device__ __forceinline__ void put_weight(void* dw, GradType type, uint64_t column, float v) {
+  if (type == kBF16) static_cast<__nv_bfloat16*>(dw)[column] = __float2bfloat16_rn(v);
+  else static_cast<float*>(dw)[column] = v;
+}
+
 // Both gradients from rows that are held in registers, a group of `warps` warps to each, 16 * PARTS values to a thread.  A
 // block's groups walk over the rows and add up what the rows give for the weight; at the end the groups' sums are added in order
 // in shared memory and leave as one part, value i of thread t at i * T + t (T threads to a row).  CLUSTER: the blocks
@@ -582,10 +588,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const __grid_con
 #pragma unroll
       for (uint32_t b = 0; b < kMostCluster; ++b) v += part[b];
       const uint32_t column = column_of<LIE>(j % T, T, j / T);
-      if (column < p.cols) {
-        if (dw_type == kBF16) static_cast<__nv_bfloat16*>(dw)[column] = __float2bfloat16_rn(v);
-        else static_cast<float*>(dw)[column] = v;
-      }
+      if (column < p.cols) put_weight(dw, dw_type, column, v);
     }
     if (blocks > 1) {      // the sums stay until all have read them
       cluster_arrive();
@@ -703,23 +706,21 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
   if (threadIdx.x == 0) p.stats[row] = make_float2(inv, m / p.columns * inv * inv);
 }
 
-// Sums over the tokens of a strip of 32 columns: eight warps take rows in turn; strip blockIdx.x % strips, share
-// blockIdx.x / strips of the rows.
-template <typename G, typename W> __global__ void __launch_bounds__(256) norm_weight_kernel(const __grid_constant__ Backward<G, W> p, uint32_t strips, uint32_t shares, float* parts) {
+// The weight's gradient of a strip of 32 columns: eight warps take the tokens in turn.
+template <typename G, typename W> __global__ void __launch_bounds__(256) norm_weight_kernel(const __grid_constant__ Backward<G, W> p, void* dw, GradType dw_type) {
   __shared__ float room[8][32];
   admit_next_kernel();
   await_previous_kernel();
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, share = blockIdx.x / strips;
-  const uint64_t c = (uint64_t)(blockIdx.x % strips) * 32 + lane;
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
   float total = 0.f;
   if (c < p.cols)
-    for (uint64_t r = share * 8 + warp; r < p.rows; r += shares * 8)
-      total = fmaf((float)p.dy.p[r * p.dy.ld + c], (float)p.s.p[r * p.s.ld + c] * p.stats[r].x, total);
+    for (uint64_t r = warp; r < p.rows; r += 8) total = fmaf((float)p.dy.p[r * p.dy.ld + c], (float)p.s.p[r * p.s.ld + c] * p.stats[r].x, total);
   room[warp][lane] = total;
   __syncthreads();
   if (warp == 0 && c < p.cols) {
     for (int i = 1; i < 8; ++i) total += room[i][lane];
-    parts[(uint64_t)share * p.cols + c] = total;
+    put_weight(dw, dw_type, c, total);
   }
 }
 
@@ -749,9 +750,8 @@ template <typename G, typename W, bool ANY> __global__ void __launch_bounds__(kM
   }
 }
 
-// dw: the parts of all shares added in order, by eight warps in turn.  A part has `length` values, in the columns' order or, T not
-// zero, in that of the threads.
-template <typename D, Lie LIE> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t shares, uint32_t length, uint32_t T, uint32_t cols, D* dw) {
+// dw: the blocks' parts added in order, by eight warps in turn.  A part has `length` values in the order of the T threads of a row.
+template <typename D, Lie LIE> __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, uint32_t count, uint32_t length, uint32_t T, uint32_t cols, D* dw) {
   __shared__ float room[8][32];
   admit_next_kernel();
   await_previous_kernel();
@@ -759,11 +759,11 @@ template <typename D, Lie LIE> __global__ void __launch_bounds__(256) norm_join_
   float total = 0.f;
   if (j < length) {
 #pragma unroll 4
-    for (uint32_t i = warp; i < shares; i += 8) total += parts[(uint64_t)i * length + j];
+    for (uint32_t i = warp; i < count; i += 8) total += parts[(uint64_t)i * length + j];
   }
   room[warp][lane] = total;
   __syncthreads();
-  const uint32_t c = T ? column_of<LIE>(j % T, T, j / T) : j;
+  const uint32_t c = column_of<LIE>(j % T, T, j / T);
   if (warp == 0 && j < length && c < cols) {
     for (int k = 1; k < 8; ++k) total += room[k][lane];
     if constexpr (sizeof(D) == 4) dw[c] = total;
@@ -822,15 +822,8 @@ template <typename G, typename W> cudaError_t forward(const NormForward& n, cuda
   const Split a = forward_split(rows, padded, lie == kSpread);
   const uint32_t parts = a.parts;
   const auto kernel = parts == 1 ? lie == kBy32s ? norm_kernel<G, W, kBy32s, 1> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 1> : norm_kernel<G, W, kSpread, 1>
-                                 : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : lie == kBy16s ? norm_kernel<G, W, kBy16s, 2> : norm_kernel<G, W, kSpread, 2>;
+                                 : lie == kBy32s ? norm_kernel<G, W, kBy32s, 2> : norm_kernel<G, W, kBy16s, 2>;
   return launch_overlapped(kernel, a.blocks, a.threads, 0, 1, stream, p, (uint32_t)rows, a.warps);
-}
-
-constexpr uint64_t kMostShares = 296;
-// Shares of the rows whose sums for the weight are taken side by side: two blocks to an SM.
-uint64_t shares_for(uint64_t rows, uint64_t cols) {
-  const uint64_t strips = (cols + 31) / 32;
-  return std::max<uint64_t>(1, std::min(kMostShares / std::min(strips, kMostShares), (rows + 7) / 8));
 }
 
 template <typename G, typename W, Lie LIE, int PARTS>
@@ -859,10 +852,10 @@ template <typename G, typename W, Lie LIE> cudaError_t pick_backward(const Backw
   return a.parts == 2 ? run_backward<G, W, LIE, 2, false>(p, a, parts, n, stream) : run_backward<G, W, LIE, 1, false>(p, a, parts, n, stream);
 }
 
-template <Lie LIE> cudaError_t join(const NormBackward& n, const float* parts, uint32_t shares, uint32_t length, uint32_t T, cudaStream_t stream) {
+template <Lie LIE> cudaError_t join(const NormBackward& n, const float* parts, uint32_t count, uint32_t length, uint32_t T, cudaStream_t stream) {
   const uint32_t strips = (length + 31) / 32, cols = (uint32_t)n.s.cols;
-  if (n.dw_type == kBF16) return launch_overlapped(norm_join_kernel<__nv_bfloat16, LIE>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<__nv_bfloat16*>(n.dw));
-  return launch_overlapped(norm_join_kernel<float, LIE>, strips, 256, 0, 1, stream, parts, shares, length, T, cols, static_cast<float*>(n.dw));
+  if (n.dw_type == kBF16) return launch_overlapped(norm_join_kernel<__nv_bfloat16, LIE>, strips, 256, 0, 1, stream, parts, count, length, T, cols, static_cast<__nv_bfloat16*>(n.dw));
+  return launch_overlapped(norm_join_kernel<float, LIE>, strips, 256, 0, 1, stream, parts, count, length, T, cols, static_cast<float*>(n.dw));
 }
 
 template <typename G, typename W> cudaError_t backward(const NormBackward& n, void* workspace, cudaStream_t stream) {
@@ -901,13 +894,11 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
     if (e != cudaSuccess || a.blocks <= kMostCluster) return e;
     return lie == kSpread ? join<kSpread>(n, parts, a.blocks, a.length(), a.warps * 32, stream) : join<kBy32s>(n, parts, a.blocks, a.length(), a.warps * 32, stream);
   }
-  const uint64_t strips = (cols + 31) / 32, shares = shares_for(rows, cols);
-  float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + (rows * sizeof(float2) + 31) / 32 * 32);
   cudaError_t e = launch_overlapped(any ? norm_stats_kernel<G, W, true> : norm_stats_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
-  if (e == cudaSuccess) e = launch_overlapped(norm_weight_kernel<G, W>, (uint32_t)(strips * shares), 256, 0, 1, stream, p, (uint32_t)strips, (uint32_t)shares, parts);
+  if (e == cudaSuccess) e = launch_overlapped(norm_weight_kernel<G, W>, (uint32_t)((cols + 31) / 32), 256, 0, 1, stream, p, n.dw, n.dw_type);
   // only now: it may be written over dy
   if (e == cudaSuccess) e = launch_overlapped(any ? norm_input_kernel<G, W, true> : norm_input_kernel<G, W, false>, (uint32_t)rows, kMostThreads, 0, 1, stream, p);
-  return e != cudaSuccess ? e : join<kBy32s>(n, parts, (uint32_t)shares, (uint32_t)cols, 0, stream);
+  return e;
 }
 
 }  // namespace
@@ -924,7 +915,7 @@ uint64_t rms_norm_backward_workspace(uint64_t rows, uint64_t cols) {
     // enough however they lie: a part to an SM, of whole warps
     return backward_split(rows, cols, false).blocks <= kMostCluster ? 0 : kSms * ((cols + 1023) / 1024 * 1024) * sizeof(float);
   }
-  return (rows * sizeof(float2) + 31) / 32 * 32 + shares_for(rows, cols) * cols * sizeof(float);
+  return rows * sizeof(float2);      // statistics
 }
 
 cudaError_t launch_rms_norm_backward(const NormBackward& n, void* workspace, cudaStream_t stream) {

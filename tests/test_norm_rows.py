@@ -9,7 +9,7 @@ from test_gpu_norm_rings import RINGS
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1509_04210_b200", "csrc")
 
 # backward, matrices, rows, columns, padded columns -> parts, warps, groups, slots, bytes of a slot, threads; backward 2: of blocks that
-# load rows themselves, matrices != 0: bf16 rows that lie anyhow -> parts, warps, groups, blocks, floats of a part, threads
+# load rows themselves, matrices != 0: bf16 rows that lie anyhow, and forward 3, padded columns, matrices != 0: rows that lie anyhow -> parts, warps, groups, blocks, floats of a part, threads
 PROGRAM = r"""
 #include <cinttypes>
 #include <cstdio>
@@ -20,8 +20,8 @@ int main() {
   unsigned matrices;
   uint64_t rows, cols, padded;
   while (std::scanf("%d %u %" SCNu64 " %" SCNu64 " %" SCNu64, &back, &matrices, &rows, &cols, &padded) == 5) {
-    if (back == 2) {
-      const rudra::Split s = rudra::backward_split(rows, cols, matrices != 0);
+    if (back >= 2) {
+      const rudra::Split s = back == 2 ? rudra::backward_split(rows, cols, matrices != 0) : rudra::forward_split(rows, padded, matrices != 0);
       std::printf("%u %u %u %u %u %u\n", s.parts, s.warps, s.threads / 32 / s.warps, s.blocks, s.length(), s.threads);
       continue;
     }
@@ -88,3 +88,19 @@ def test_blocks_of_the_backward_pass(rings):
             assert groups <= (15 if warps > 1 else 32)
     # bf16 rows of nine or ten warps that lie anyhow: two to a block, as 20 warps hold them
     assert [s[2] for s in rings([(2, 1, 4_000, c, 0) for c in (4_111, 4_999, 5_120)] + [(2, 0, 4_000, 4_111, 0), (2, 1, 4_000, 4_001, 0), (2, 1, 4_000, 5_121, 0)])] == [2, 2, 2, 1, 2, 1]
+
+
+def test_blocks_of_the_forward_pass(rings):
+    for anyhow in (0, 1):
+        queries = [(3, anyhow, t, c, p) for t in (1, 149, 4_000, 1 << 30) for c in list(range(1, 16_385, 13)) + [4096, 8192, 12_288, 12_289, 16_384] for p in {c, -(-c // 128) * 128}]
+        for (_, _, t, _, padded), (parts, warps, groups, _, _, threads) in zip(queries, rings(queries)):
+            assert parts * warps * 512 >= padded and threads == groups * warps * 32 and groups <= (15 if warps > 1 else 32)
+            assert threads <= (1024 if anyhow else 512 if parts == 2 else 768) and not (anyhow and parts == 2)
+
+
+def test_no_kernel_is_built_that_no_call_reaches():
+    code = open(os.path.join(CSRC, "rms_norm.cu")).read()
+    assert "norm_kernel<G, W, kSpread, 2>" not in code
+    from paper_1509_04210_b200 import binding as rb
+    # rows of more than 16 384 values: a token's statistics and nothing else, for the weight's gradient is written at once
+    assert rb.lib().rudra_rms_norm_backward_workspace(5, 20_000) == 40 and rb.lib().rudra_rms_norm_backward_workspace(1, 2**31 - 128) == 8
