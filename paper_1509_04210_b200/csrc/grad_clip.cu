@@ -21,7 +21,8 @@ namespace {
 // threads 120 and 36, eight of 256 with 16 values 124 and 33.
 constexpr uint32_t kThreads = 512, kPieces = 2, kBlocksPerSm = 2, kLargeUnit = kThreads * kPieces * kValues;
 constexpr uint32_t kBlocks = 148 * kBlocksPerSm;    // at most; a partial sum each
-// Units that are read to stay in L2: 48 MB of f32 (61 million: 123.9 us without, 120.3 with 48 to 80 MB, 121.2 with 100).
+// Units that are read to stay in L2 until they are scaled: 48 MB of f32, 24 of bf16 (61 million f32 123.9 us without, 120.3 with 48 to 80 MB,
+// 121.2 with 100; 20 million bf16 in their place 32.1 without, 29.3 with 24 MB, more was not measured).
 constexpr uint32_t kHotUnits = 732;
 constexpr uint32_t kFusedBlocks = 8, kFusedThreads = 512, kSmallUnit = 32 * kValues;   // one cluster
 
@@ -191,6 +192,19 @@ template <uint32_t PIECES, uint32_t MOST> __device__ __forceinline__ void scale_
   }
 }
 
+// Lines of a unit that were asked to stay in L2 leave it like any others; they would not otherwise, even once they are read and written first to
+// leave.  (12 M values read and written over and over took 15.2 us after a clipping instead of 12.8.  Releasing costs 0.5 us where 61 million
+// f32 are scaled, 0.8 with 20 million bf16.)  Whole lines: what is left of a gradient's ends is next to nothing.
+template <uint32_t MOST> __device__ __forceinline__ void release(const List<MOST>& list, uint32_t g, uint64_t at) {
+  constexpr uint32_t kLine = 128;
+  const uint32_t element = list.wide[g] & 1 ? 4 : 2;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(list.p[g]), end = p + list.size[g] * element, from = (p & ~(uintptr_t)31) + at * element;
+  for (uint32_t i = threadIdx.x * kLine; i < kLargeUnit * element; i += kThreads * kLine) {
+    const uintptr_t line = (from & ~(uintptr_t)(kLine - 1)) + i;
+    if (line >= p && line + kLine <= end) asm volatile("applypriority.global.L2::evict_normal [%0], 128;" :: "l"(line) : "memory");
+  }
+}
+
 __device__ __forceinline__ float factor(float norm, float max_norm) { return norm <= max_norm ? 1.f : max_norm / norm; }
 
 template <uint32_t MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) squares_kernel(const __grid_constant__ List<MOST> list, double* parts) {
@@ -233,12 +247,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) scale_kernel(const __g
   await_previous_kernel();
   const float n = parts ? norm_of_parts(parts, count) : *const_cast<volatile float*>(norm), by = factor(n, max_norm);
   if (parts && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
-  if (IN_PLACE && by == 1.f) return;
-  for (uint32_t i = blockIdx.x; i < units; i += gridDim.x) {
+  const bool nothing = IN_PLACE && by == 1.f;
+  const uint32_t first = nothing ? parts ? list.hot : units : 0;      // of those that there is something to do for
+  for (uint32_t i = blockIdx.x; i < units - first; i += gridDim.x) {
     const uint32_t c = units - 1 - i;      // backwards: what the norm read last is still in L2
     uint32_t begin;
     const uint32_t g = ends.of(list.count, c, begin);
-    scale_of<kPieces>(list, g, (int64_t)(c - begin) * kLargeUnit + threadIdx.x * kValues, kThreads * kValues, by);
+    if (parts && c >= list.hot) release(list, g, (uint64_t)(c - begin) * kLargeUnit);      // before it is written: results leave first
+    if (!nothing) scale_of<kPieces>(list, g, (int64_t)(c - begin) * kLargeUnit + threadIdx.x * kValues, kThreads * kValues, by);
   }
 }
 
@@ -255,7 +271,7 @@ __global__ void __launch_bounds__(kFusedThreads) clip_kernel(const __grid_consta
   uint32_t begin;
   for (uint32_t c = first; c < units; c += step) {
     const uint32_t g = ends.of(list.count, c, begin);
-    s += squares_of<1>(list, g, (int64_t)(c - begin) * kSmallUnit + threadIdx.x % 32 * kValues, 0, true);
+    s += squares_of<1>(list, g, (int64_t)(c - begin) * kSmallUnit + threadIdx.x % 32 * kValues, 0, true);      // half a megabyte at most
   }
   s = block_sum<kFusedThreads>(s);
   if (threadIdx.x == 0) part = s;
@@ -300,29 +316,33 @@ template <uint32_t MOST, typename F> cudaError_t in_parts(const Gradient* grads,
   return list.count ? body(list, units) : cudaSuccess;
 }
 
-// Gradients that one launch takes: 2, 11 and 32 KB of parameters.
+// Gradients that one launch takes: 1.9, 9.3 and 27.8 KB of parameters.
 constexpr uint32_t kFew = 64, kSome = 320, kMany = 960;
 static_assert(sizeof(List<kMany>) + 64 <= 32764, "more than kernel parameters may be");
 
-template <uint32_t MOST> cudaError_t squares_to(const Gradient* grads, uint64_t count, double* parts, uint32_t* used, cudaStream_t stream) {
+uint32_t hot_from(uint32_t units) { return units > kHotUnits ? units - kHotUnits : 0; }
+
+// again: the values are read once more.  Else nothing is asked to stay in L2.
+template <uint32_t MOST> cudaError_t squares_to(const Gradient* grads, uint64_t count, bool again, double* parts, uint32_t* used, cudaStream_t stream) {
   *used = 0;
   return in_parts<MOST>(grads, count, kLargeUnit, [&](List<MOST>& list, uint32_t units) {
     const uint32_t blocks = std::min(units, kBlocks);
     double* const to = parts + *used;
     *used += blocks;
-    list.hot = units > kHotUnits ? units - kHotUnits : 0;
+    list.hot = again ? hot_from(units) : units;
     return launch_overlapped(squares_kernel<MOST>, blocks, kThreads, 0, 1, stream, list, to);
   });
 }
 template <uint32_t MOST> cudaError_t norm_of(const Gradient* grads, uint64_t count, float* norm, double* parts, cudaStream_t stream) {
   uint32_t used;
-  const cudaError_t e = squares_to<MOST>(grads, count, parts, &used, stream);
+  const cudaError_t e = squares_to<MOST>(grads, count, false, parts, &used, stream);
   return e != cudaSuccess ? e : launch_overlapped(norm_kernel, 1, kThreads, 0, 1, stream, (const double*)parts, used, norm);
 }
 
 // Units of 512 values up to which one cluster takes norm and norm's use in one launch: two to a warp.  On the GPU 20 thousand values take 4.4 us
 // that way and 5.8 in two launches, 90 thousand 5.9 and 6.0, or 7.5 and 5.7 in 48 gradients, 200 thousand 8.6 and 6.3; one call after another
-// from the host, whose second launch takes 1.5 us, 90 thousand in 48 gradients 7.2 and 8.7.
+// from the host, whose second launch takes 1.5 us, 90 thousand in 48 gradients 7.2 and 8.7.  The rule is the host's: a captured graph of a list of 100
+// to 256 units would be faster with two.
 constexpr uint64_t kFusedMost = 256;
 
 template <uint32_t MOST, bool IN_PLACE> cudaError_t clip(const Gradient* grads, uint64_t count, float* norm, float max_norm, bool known, double* parts, cudaStream_t stream) {
@@ -335,10 +355,11 @@ template <uint32_t MOST, bool IN_PLACE> cudaError_t clip(const Gradient* grads, 
         return launch_overlapped(clip_kernel<MOST, IN_PLACE>, kFusedBlocks, kFusedThreads, 0, kFusedBlocks, stream, list, norm, max_norm);
       });
     if (!units) return launch_overlapped(norm_kernel, 1, kThreads, 0, 1, stream, (const double*)parts, 0u, norm);
-    const cudaError_t e = squares_to<MOST>(grads, count, parts, &used, stream);
+    const cudaError_t e = squares_to<MOST>(grads, count, true, parts, &used, stream);
     if (e != cudaSuccess) return e;
   }
-  return in_parts<MOST>(grads, count, kLargeUnit, [&](const List<MOST>& list, uint32_t units) {
+  return in_parts<MOST>(grads, count, kLargeUnit, [&](List<MOST>& list, uint32_t units) {
+    list.hot = hot_from(units);
     return launch_overlapped(scale_kernel<MOST, IN_PLACE>, std::min(units, kBlocks), kThreads, 0, 1, stream, list, known ? (const double*)nullptr : (const double*)parts, used, norm,
                              max_norm);
   });
