@@ -518,5 +518,6 @@ cudaError_t launch_act8_weight_grad(const MatrixIn& dy, const Act8& saved, const
 }
 
 cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t act8_weight_grad_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 }  // namespace rudra

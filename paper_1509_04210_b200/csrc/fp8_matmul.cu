@@ -418,5 +418,6 @@ cudaError_t launch_fp8_linear(const MatrixIn& x, const Fp8& b, const MatrixOut& 
 }
 
 cudaError_t fp8_matmul_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t fp8_matmul_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 }  // namespace rudra

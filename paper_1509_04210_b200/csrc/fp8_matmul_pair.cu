@@ -260,5 +260,6 @@ cudaError_t launch_fp8_matmul_pair(const Fp8& a, const Fp8& b, const MatrixOut& 
 }
 
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t fp8_matmul_pair_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 }  // namespace rudra

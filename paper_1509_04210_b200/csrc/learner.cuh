@@ -106,5 +106,12 @@ cudaError_t act8_weight_grad_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t fp8_matmul_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t fp8_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream);
 cudaError_t rms_norm_gave_up(uint32_t* count, cudaStream_t stream);
+// Where it lies on the current device.
+cudaError_t mx4_matmul_count(const uint32_t** at);
+cudaError_t mx4_matmul_pair_count(const uint32_t** at);
+cudaError_t act8_weight_grad_count(const uint32_t** at);
+cudaError_t fp8_matmul_count(const uint32_t** at);
+cudaError_t fp8_matmul_pair_count(const uint32_t** at);
+cudaError_t rms_norm_count(const uint32_t** at);
 
 }  // namespace rudra

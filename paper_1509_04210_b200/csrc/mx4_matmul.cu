@@ -304,5 +304,6 @@ cudaError_t launch_mx4_linear(const MatrixIn& x, const Mx4& b, const MatrixOut& 
 }
 
 cudaError_t mx4_matmul_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t mx4_matmul_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 }  // namespace rudra

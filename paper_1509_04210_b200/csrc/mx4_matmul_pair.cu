@@ -211,5 +211,6 @@ cudaError_t launch_mx4_matmul_pair(const Mx4& a, const Mx4& b, const MatrixOut& 
 }
 
 cudaError_t mx4_matmul_pair_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t mx4_matmul_pair_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 }  // namespace rudra

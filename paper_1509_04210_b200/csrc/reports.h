@@ -2,6 +2,7 @@
 // a count is not the one it was last told of, so that no stream's asking takes a report away from another.
 #pragma once
 #include <array>
+#include <atomic>
 #include <cstdint>
 #include <map>
 #include <mutex>
@@ -26,6 +27,36 @@ class Reports {
  private:
   std::mutex mutex_;
   std::map<std::pair<int, uint64_t>, Counts> told_;   // streams without an entry: all zero
+};
+
+// Places that calls take while they run, as many as there are.
+class Places {
+ public:
+  static constexpr int kMost = 64;
+  // The number of one that is free, now taken; -1: none is.
+  int take() {
+    uint64_t taken = taken_.load();
+    while (~taken) {
+      const int i = __builtin_ctzll(~taken);
+      if (taken_.compare_exchange_weak(taken, taken | 1ull << i)) return i;
+    }
+    return -1;
+  }
+  void give(int i) {
+    if (i >= 0) taken_.fetch_and(~(1ull << i));
+  }
+
+  // One of them, for as long as it lives.
+  struct Place {
+    explicit Place(Places& of_) : of(of_), number(of_.take()) {}
+    Place(const Place&) = delete;
+    ~Place() { of.give(number); }
+    Places& of;
+    const int number;      // -1: none
+  };
+
+ private:
+  std::atomic<uint64_t> taken_{0};
 };
 
 }  // namespace rudra

@@ -904,6 +904,7 @@ template <typename G, typename W> cudaError_t backward(const NormBackward& n, vo
 }  // namespace
 
 cudaError_t rms_norm_gave_up(uint32_t* count, cudaStream_t stream) { return read_count(g_gave_up, count, stream); }
+cudaError_t rms_norm_count(const uint32_t** at) { return count_address(g_gave_up, at); }
 
 cudaError_t launch_rms_norm(const NormForward& n, cudaStream_t stream) {
   if (n.x.type == kBF16) return n.weight_type == kBF16 ? forward<__nv_bfloat16, __nv_bfloat16>(n, stream) : forward<__nv_bfloat16, float>(n, stream);

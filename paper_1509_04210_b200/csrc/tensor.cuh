@@ -342,9 +342,15 @@ inline uint32_t pick_split(const Device::Facts& f, uint64_t tiles, uint32_t stag
   return best;
 }
 
-// The count that kernels raise when they give up a wait, on its way to `count` behind the stream's work.
+// The count that kernels raise when they give up a wait, on its way to `count` behind the stream's work; and where it lies.
 template <typename F> cudaError_t read_count(const F& symbol, uint32_t* count, cudaStream_t stream) {
   return cudaMemcpyFromSymbolAsync(count, symbol, sizeof(*count), 0, cudaMemcpyDeviceToHost, stream);
+}
+template <typename F> cudaError_t count_address(const F& symbol, const uint32_t** at) {
+  void* p = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&p, symbol);
+  *at = static_cast<const uint32_t*>(p);
+  return e;
 }
 
 // A row-major matrix, read in boxes as it lies; what lies outside reads as zero.
