@@ -365,7 +365,8 @@ template <typename G> cudaError_t by_time(const Fp8& a, const Fp8& b, const Matr
 
 // f32 results of long rows are gathered in memory: the tensor core cuts a sum off where it adds to it, every 32 values, by more the more
 // there is of it.  (Rows of 2^20 positive values: 1.6e-4 too little in one sum.)  So many blocks to a sum, about; a multiple of the four
-// whose scale bytes share an atom.
+// whose scale bytes share an atom.  Every sum is a launch that reads y and writes it again: 2048 x 4096 x 131072 takes 2.04 ms in f32 and 0.80 in
+// bf16, whose parts stay in registers; 128 x 4096 x 131072 217 and 93 us.
 constexpr uint32_t kGathered = 64;
 template <typename G, typename F> cudaError_t in_sums(uint64_t cols, F&& body) {
   const uint32_t blocks = (uint32_t)((cols + kFp8Block - 1) / kFp8Block), sums = sizeof(G) == 4 ? std::max(1u, (blocks + kGathered / 2) / kGathered) : 1;

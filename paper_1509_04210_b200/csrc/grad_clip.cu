@@ -5,7 +5,7 @@
 // values, everything beyond that in 64, in an order that depends on the list alone; 16 values whose squares leave the range of a
 // float are squared in 64 bits.  One read for the norm, one read and one write for the scaling: bound by HBM, less what the
 // second read finds in L2; small lists by launches, and have one for both.  Measured, norm and scaling: 61 million f32 in 16
-// gradients 116 us (244 MB read, 200 read again and 244 written: 5.9 TB/s; a copy reaches 6.5), 20 million bf16 in 301 gradients to
+// gradients 119 us (244 MB read, 200 read again and 244 written: 5.8 TB/s; a copy reaches 6.5), 20 million bf16 in 301 gradients to
 // f32 32 us, 90 thousand f32 in 48 gradients 7.2 us in one launch, 20 thousand 4.4.
 #include <algorithm>
 

@@ -55,7 +55,7 @@ cudaError_t launch_after(void (*kernel)(P...), uint32_t blocks, uint32_t threads
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
-// The same, under the name that the 8-bit, norm and clipping kernels use.
+// The same, under the name that the 8-bit, norm and clipping kernels use; the rules hold for either.
 template <typename... P, typename... A>
 cudaError_t launch_overlapped(void (*kernel)(P...), uint32_t blocks, uint32_t threads, uint32_t smem, uint32_t cluster, cudaStream_t stream, A&&... args) {
   return launch_after(kernel, blocks, threads, smem, cluster, stream, std::forward<A>(args)...);

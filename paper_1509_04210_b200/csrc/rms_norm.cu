@@ -7,8 +7,9 @@
 // sums are in 32 bits.  Both passes read and write each matrix once and multiply nothing: they are bound by HBM for
 // many tokens, by launch latency for few.  Measured at 8192 x 4096 bf16 with a residual: forward to FP8 41 us = 5.7 TB/s, to bf16 49 us
 // = 5.5 TB/s, backward 50 us = 5.4 TB/s; f32 69, 95 and 91 us = 6.3, 5.6 and 5.9 TB/s; one token 3 us, 37 x 1000 f32 backward 6.4 us.
-// Rows that lie anyhow are held up by their values one by one: 4000 x 4111 bf16 35 us forward and 87 backward, 8192 x 1439 23 and 40, for 20
-// and 15 us of memory.
+// Rows that lie anyhow are held up by their values one by one: 4000 x 4111 bf16 35 us forward and 66 backward, 8192 x 1439 25 and 41, for 20
+// and 15 us of memory.  Rows of more than 16 384 values have a block each and are read twice: 1000 x 20000 bf16 37 us forward and 71 backward,
+// f32 59 and 119, for 25 and 50 us of memory; fewer of them than SMs leave the others idle (16 x 1 000 000 bf16 220 and 273 us for 20).
 #include <algorithm>
 
 #include "fp8.cuh"
